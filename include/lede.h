@@ -558,6 +558,127 @@ int lede_op_read_probe(const void* src, size_t bytes, uint32_t* sink, int32_t gr
 int lede_op_read_groups(const void* src, int32_t n_groups, int32_t tiles, uint32_t* sink, void* stream,
                         float* kernel_ms);
 
+/* ---- a batch of requests over one paged 8-bit cache -----------------------
+ * The operators that a decoding or prompt pass of several sequences takes
+ * beside its linear products: page tables and slots from the requests'
+ * lengths, K/V rows into the cache, attention over it, and the scores of
+ * tokens from logits rows.  (The paper decodes one sequence; Section 4.1
+ * names batch 1.)  They need no context: every pointer is caller-owned
+ * device memory on the current device, work is ordered on `stream`, and no
+ * call allocates, synchronises or keeps anything, so each may be captured
+ * into a graph.  Workspaces hold nothing between calls; calls that may
+ * overlap need one each.
+ *
+ * Cache: one layer's keys and values in one region of lede_op_cache_bytes
+ * (16-byte aligned, cleared to zero by the caller before its first use), in
+ * pages of 64 tokens.  Codes are e4m3 (OCP); a block (page, KV head) of keys
+ * and one of values each has a power-of-two scale 2^e, e >= -100, and holds
+ * the values code * 2^e.  Layout: key codes [n_pages][n_kv][64][head_dim],
+ * value codes [n_pages][n_kv][head_dim][64], scale words
+ * [n_pages][n_kv][2] (uint32: keys, values) of e + 127, plus 256 when the
+ * block holds a NaN.  head_dim is 64 or 128, n_kv at most 1024
+ * (LEDE_E_UNSUPPORTED; lede_op_cache_bytes returns 0). */
+size_t lede_op_cache_bytes(int32_t n_pages, int32_t n_kv_heads, int32_t head_dim);
+
+/* Page tables and the slot map of a pass.  Sequence s has seq_lens[s] cached
+ * tokens in the first pages of its table row (tables + s * table_ld, pool
+ * page per logical page), of which held[s] entries are its own already (at
+ * least the pages its tokens need; more after a rollback, which is a smaller
+ * seq_lens[s]), and gets new_lens[s] >= 0 tokens more.  Pages that it lacks
+ * are taken from free_pages[*free_head ..] in sequence order, then in table
+ * order.  Writes, for n_seqs >= 1 sequences:
+ *   tables     the entries of pages taken (others are left as they are)
+ *   kv_lens    seq_lens + new_lens            (may be seq_lens itself)
+ *   held_out   table entries held             (may be held itself)
+ *   row_start  [n_seqs + 1] prefix sums of new_lens: the rows of a pass
+ *   slots      [max_rows] page * 64 + place of each row's token; -1 behind
+ *              the last row
+ *   status     [4]: 0 or an error, the number of rows, the position in
+ *              free_pages after the call, the first sequence that failed or
+ *              -1.  free_head may be status + 2.
+ * Errors of the lengths are found on the device: LEDE_E_ARG (a negative
+ * length, held outside [pages of seq_lens, table_ld], free_head outside [0,
+ * n_free], more rows than max_rows), LEDE_E_CTX_OVERFLOW (table_ld pages do
+ * not hold the sequence), LEDE_E_KV_FULL (no page left).  Then nothing is
+ * taken: kv_lens = seq_lens, held_out = held, status[2] = *free_head, every
+ * row_start is 0 and every slot -1, so that the pass behind it has no rows.
+ * Returns LEDE_E_ARG on null pointers (free_pages may be null with n_free =
+ * 0, slots with max_rows = 0) and sizes below these. */
+int lede_op_cache_plan(const int32_t* seq_lens, const int32_t* new_lens, const int32_t* held, int32_t n_seqs,
+                       const int32_t* free_pages, int32_t n_free, const int32_t* free_head, int32_t* tables,
+                       int32_t table_ld, int32_t max_rows, int32_t* kv_lens, int32_t* held_out, int32_t* row_start,
+                       int64_t* slots, int32_t* status, void* stream);
+
+/* K/V rows into the cache: row r (k + r * ldk and v + r * ldv elements of
+ * `dtype`, n_kv heads of head_dim) goes to slots[r]; a slot outside the pool
+ * skips its row.  Rows of one page stand next to each other, as a plan lays
+ * them out, and no slot is given twice (else what the pages involved hold is
+ * undefined).  A block's scale is the smallest with |x| <= 448 * 2^e for
+ * its finite entries: rows that include a page's first token start it anew,
+ * others keep the larger of the old and their own, and when it grows the
+ * page's codes are rounded to the new one (exact but for the smallest).
+ * Rounding is to nearest, ties to even; an entry that is not finite becomes
+ * a NaN.  Tokens of the page that the call does not write keep their values.
+ * LEDE_E_ARG: null pointers, a bad dtype, n_rows < 0, a row stride below
+ * n_kv * head_dim; k, v, cache or row strides not multiples of 16 bytes. */
+int lede_op_cache_append(int32_t dtype, const void* k, int64_t ldk, const void* v, int64_t ldv, const int64_t* slots,
+                         int32_t n_rows, void* cache, int32_t n_pages, int32_t n_kv_heads, int32_t head_dim,
+                         void* stream);
+
+/* The rows that slots of the cache hold, rounded to `dtype`; any order, any
+ * number of times.  Rows whose slot lies outside the pool are left as they
+ * are.  Errors as lede_op_cache_append. */
+int lede_op_cache_read(int32_t dtype, const void* cache, int32_t n_pages, int32_t n_kv_heads, int32_t head_dim,
+                       const int64_t* slots, int32_t n_rows, void* k, int64_t ldk, void* v, int64_t ldv, void* stream);
+
+/* Causal attention of the rows of a pass over the cache: sequence s has the
+ * query rows row_start[s] .. row_start[s + 1] - 1 of q (row r at q + r * ldq,
+ * n_heads heads of head_dim), which are the last of its kv_lens[s] cached
+ * tokens: row i of n sees the tokens up to position kv_lens[s] - n + i.
+ * Query head h reads KV head h / (n_heads / n_kv_heads); weights are
+ * softmax(scale q.k).  out (row stride ldo) has q's dtype; a row that sees no
+ * token is 0, rows outside every sequence are left as they are.  Any
+ * mix of lengths (none, one, many) is taken; max_new and max_kv, the largest
+ * number of rows and of cached tokens that a sequence is expected to have,
+ * only spread the work: larger lengths are right, too, if slower.  Table
+ * entries outside the pool are never followed: rows that see such a page are
+ * NaN.  kv_lens above 64 * table_ld count as that, row_start is held to [0,
+ * n_rows].  Scores, softmax statistics and sums are fp32; a NaN or infinity
+ * stays with the rows that see it.
+ * workspace: lede_op_cache_attention_bytes of the same sizes (may be 0).
+ * LEDE_E_ARG: null pointers, bad sizes, n_heads not a multiple of n_kv_heads,
+ * a scale that is not finite, a small workspace; q, out, cache, workspace or
+ * row strides not multiples of 16 bytes.  LEDE_E_UNSUPPORTED: more than 65535
+ * sequences, more than 65536 heads, or a grid above 2^31 blocks. */
+size_t lede_op_cache_attention_bytes(int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads,
+                                     int32_t head_dim, int32_t max_new, int32_t max_kv);
+int lede_op_cache_attention(int32_t dtype, const void* q, int64_t ldq, const void* cache, int32_t n_pages,
+                            const int32_t* tables, int32_t table_ld, const int32_t* kv_lens, const int32_t* row_start,
+                            int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                            float scale, int32_t max_new, int32_t max_kv, void* out, int64_t ldo, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Scores of tokens under softmax(logits / temperature), row by row (the
+ * exit policy's features, Section 3.1.1, for given tokens and any number of
+ * rows): logits row r is V entries of `dtype` at logits + r * ld (any element
+ * alignment).  Every output is optional but for the top ones with n_top > 0:
+ *   logprobs      [n_rows] log p of tokens[r]; NaN for a token outside [0, V)
+ *   ranks         [n_rows] entries before it in the order below; -1 likewise
+ *   entropy       [n_rows] -sum p log p in nats
+ *   top_ids, top_logprobs  [n_rows][n_top] the first n_top in that order
+ * The order: larger logits first, a NaN before them all, then lower indices.
+ * Entries of -infinity have p = 0; a row of nothing else, or with a NaN or
+ * +infinity, has NaN scores.  Sums are fp32, log p is formed in fp64 and
+ * rounded.  workspace: lede_op_logprobs_bytes of the same sizes.
+ * LEDE_E_ARG: null pointers, bad sizes, n_top > V, ld < V, a temperature that
+ * is not finite and > 0 (or whose reciprocal overflows), a small or
+ * misaligned (16 bytes) workspace.  LEDE_E_UNSUPPORTED: V above 2^20, n_top
+ * above 32. */
+size_t lede_op_logprobs_bytes(int32_t n_rows, int32_t V, int32_t n_top);
+int lede_op_logprobs(int32_t dtype, const void* logits, int64_t ld, int32_t n_rows, int32_t V, float temperature,
+                     const int32_t* tokens, int32_t n_top, float* logprobs, int32_t* ranks, float* entropy,
+                     int32_t* top_ids, float* top_logprobs, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

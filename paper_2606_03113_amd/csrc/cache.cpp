@@ -1,0 +1,172 @@
+// Entry points of a batch's operators: the paged 8-bit K/V cache and the log
+// probabilities of logits rows.  No call allocates, synchronises or keeps
+// anything between calls.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/lede.h"
+#include "cache.h"
+
+using namespace lede;
+
+namespace {
+
+hipStream_t S_(void* s) { return (hipStream_t)s; }
+int done(hipError_t e) { return e == hipSuccess ? LEDE_OK : LEDE_E_HIP; }
+bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+bool dtype_ok(int32_t dt) { return dt == LEDE_DTYPE_F32 || dt == LEDE_DTYPE_BF16; }
+int es_of(int32_t dt) { return dt == LEDE_DTYPE_BF16 ? 2 : 4; }
+
+// A cache's shape: LEDE_OK, or why it is none.  Page and token counts stay in
+// 32 bits, byte offsets are 64-bit everywhere.
+int check_cache(int32_t n_pages, int32_t n_kv, int32_t hd) {
+  if (n_pages < 1 || n_kv < 1) return LEDE_E_ARG;
+  if ((hd != 64 && hd != 128) || n_kv > 1024) return LEDE_E_UNSUPPORTED;
+  return LEDE_OK;
+}
+
+// Rows that the kernels read or write in 16-byte pieces.
+bool rows_ok(const void* p, int64_t ld, int64_t width, int32_t dt) {
+  return p && aligned(p, 16) && ld >= width && ld * es_of(dt) % 16 == 0;
+}
+
+// Row tiles and splits of an attention's grid.  The kernels are right for any
+// lengths; this decides how the work spreads.
+struct AttnGrid { int n_tiles, n_split, min_chunk; int64_t blocks; };
+AttnGrid attn_grid(int32_t n_seqs, int32_t nq, int32_t nkv, int32_t max_new, int32_t max_kv) {
+  AttnGrid g;
+  const int64_t tiles = std::max<int64_t>(1, ((int64_t)max_new * (nq / nkv) + 15) / 16);
+  g.n_tiles = (int)std::min<int64_t>(tiles, 65536);
+  const int64_t whole = (int64_t)n_seqs * nkv * g.n_tiles;
+  const int64_t pages = ((int64_t)max_kv + CACHE_PAGE - 1) / CACHE_PAGE;
+  g.min_chunk = 4;
+  g.n_split = (int)std::max<int64_t>(1, std::min((2048 + whole - 1) / whole, (pages + g.min_chunk - 1) / g.min_chunk));
+  g.blocks = whole * g.n_split;
+  return g;
+}
+
+constexpr int64_t MOST_BLOCKS = 0x7FFFFFFF;
+constexpr int32_t MOST_SEQS = 65535;
+constexpr int32_t MOST_VOCAB = 1 << 20;
+constexpr int32_t MOST_TOP = 32;
+constexpr int LOGPROBS_SEG = 8192;   // entries of a row that one block holds
+
+int logprobs_segments(int32_t V) { return (V + 7 + LOGPROBS_SEG - 1) / LOGPROBS_SEG; }  // (+ 7: a row may begin inside a 16-byte piece)
+
+}  // namespace
+
+extern "C" {
+
+size_t lede_op_cache_bytes(int32_t n_pages, int32_t n_kv_heads, int32_t head_dim) {
+  return check_cache(n_pages, n_kv_heads, head_dim) ? 0 : cache_bytes(n_pages, n_kv_heads, head_dim);
+}
+
+int lede_op_cache_plan(const int32_t* seq_lens, const int32_t* new_lens, const int32_t* held, int32_t n_seqs,
+                       const int32_t* free_pages, int32_t n_free, const int32_t* free_head, int32_t* tables,
+                       int32_t table_ld, int32_t max_rows, int32_t* kv_lens, int32_t* held_out, int32_t* row_start,
+                       int64_t* slots, int32_t* status, void* stream) {
+  if (!seq_lens || !new_lens || !held || !free_head || !tables || !kv_lens || !held_out || !row_start || !status)
+    return LEDE_E_ARG;
+  if (n_seqs < 1 || n_free < 0 || (n_free && !free_pages) || table_ld < 1 || max_rows < 0 || (max_rows && !slots))
+    return LEDE_E_ARG;
+  CachePlanArgs a{};
+  a.seq_lens = seq_lens; a.new_lens = new_lens; a.held = held; a.n_seqs = n_seqs;
+  a.free_pages = free_pages; a.n_free = n_free; a.free_head = free_head;
+  a.tables = tables; a.table_ld = table_ld; a.max_rows = max_rows;
+  a.kv_lens = kv_lens; a.held_out = held_out; a.row_start = row_start; a.slots = slots; a.status = status;
+  return done(launch_cache_plan(a, S_(stream)));
+}
+
+static int cache_rows(bool append, int32_t dtype, void* k, int64_t ldk, void* v, int64_t ldv, const int64_t* slots,
+                      int32_t n_rows, void* cache, int32_t n_pages, int32_t n_kv, int32_t hd, void* stream) {
+  if (!dtype_ok(dtype) || !cache || n_rows < 0) return LEDE_E_ARG;
+  if (int rc = check_cache(n_pages, n_kv, hd)) return rc;
+  if (!aligned(cache, 16)) return LEDE_E_ARG;
+  if (n_rows == 0) return LEDE_OK;
+  const int64_t width = (int64_t)n_kv * hd;
+  if (!slots || !rows_ok(k, ldk, width, dtype) || !rows_ok(v, ldv, width, dtype)) return LEDE_E_ARG;
+  CacheRowsArgs a{};
+  a.c = cache_view(cache, n_pages, n_kv, hd);
+  a.k = k; a.v = v; a.ldk = ldk; a.ldv = ldv; a.slots = slots; a.n_rows = n_rows;
+  a.window = (int)std::min<int64_t>(CACHE_PAGE, std::max<int64_t>(1, (int64_t)n_rows * n_kv * 2 / 4096));
+  return done(append ? launch_cache_append(dtype, a, S_(stream)) : launch_cache_read(dtype, a, S_(stream)));
+}
+
+int lede_op_cache_append(int32_t dtype, const void* k, int64_t ldk, const void* v, int64_t ldv, const int64_t* slots,
+                         int32_t n_rows, void* cache, int32_t n_pages, int32_t n_kv_heads, int32_t head_dim,
+                         void* stream) {
+  return cache_rows(true, dtype, (void*)k, ldk, (void*)v, ldv, slots, n_rows, cache, n_pages, n_kv_heads, head_dim, stream);
+}
+
+int lede_op_cache_read(int32_t dtype, const void* cache, int32_t n_pages, int32_t n_kv_heads, int32_t head_dim,
+                       const int64_t* slots, int32_t n_rows, void* k, int64_t ldk, void* v, int64_t ldv, void* stream) {
+  return cache_rows(false, dtype, k, ldk, v, ldv, slots, n_rows, (void*)cache, n_pages, n_kv_heads, head_dim, stream);
+}
+
+size_t lede_op_cache_attention_bytes(int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads,
+                                     int32_t head_dim, int32_t max_new, int32_t max_kv) {
+  if (n_seqs < 1 || n_rows < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_kv < 0) return 0;
+  const AttnGrid g = attn_grid(n_seqs, n_heads, n_kv_heads, max_new, max_kv);
+  return g.n_split == 1 ? 0 : (size_t)n_rows * n_heads * g.n_split * (head_dim + 2) * 4;
+}
+
+int lede_op_cache_attention(int32_t dtype, const void* q, int64_t ldq, const void* cache, int32_t n_pages,
+                            const int32_t* tables, int32_t table_ld, const int32_t* kv_lens, const int32_t* row_start,
+                            int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                            float scale, int32_t max_new, int32_t max_kv, void* out, int64_t ldo, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  if (!dtype_ok(dtype) || !cache || !tables || !kv_lens || !row_start || n_seqs < 1 || n_rows < 0 || table_ld < 1)
+    return LEDE_E_ARG;
+  if (int rc = check_cache(n_pages, n_kv_heads, head_dim)) return rc;
+  if (n_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_kv < 0 || !std::isfinite(scale)) return LEDE_E_ARG;
+  if (n_seqs > MOST_SEQS || n_heads > 65536) return LEDE_E_UNSUPPORTED;
+  if (!aligned(cache, 16)) return LEDE_E_ARG;
+  if (n_rows == 0) return LEDE_OK;
+  const int64_t width = (int64_t)n_heads * head_dim;
+  if (!rows_ok(q, ldq, width, dtype) || !rows_ok(out, ldo, width, dtype)) return LEDE_E_ARG;
+  const AttnGrid g = attn_grid(n_seqs, n_heads, n_kv_heads, max_new, max_kv);
+  if (g.blocks > MOST_BLOCKS) return LEDE_E_UNSUPPORTED;
+  const size_t need = lede_op_cache_attention_bytes(n_seqs, n_rows, n_heads, n_kv_heads, head_dim, max_new, max_kv);
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return LEDE_E_ARG;
+  CacheAttnArgs a{};
+  a.c = cache_view((void*)cache, n_pages, n_kv_heads, head_dim);
+  a.q = q; a.ldq = ldq; a.tables = tables; a.table_ld = table_ld; a.kv_lens = kv_lens; a.row_start = row_start;
+  a.n_seqs = n_seqs; a.n_rows = n_rows; a.nq = n_heads;
+  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  a.n_tiles = g.n_tiles; a.n_split = g.n_split; a.min_chunk = g.min_chunk;
+  a.part = (float*)workspace; a.out = out; a.ldo = ldo;
+  return done(launch_cache_attention(dtype, a, S_(stream)));
+}
+
+size_t lede_op_logprobs_bytes(int32_t n_rows, int32_t V, int32_t n_top) {
+  if (n_rows < 0 || V < 1 || V > MOST_VOCAB || n_top < 0 || n_top > MOST_TOP) return 0;
+  return (size_t)n_rows * logprobs_segments(V) * (16 + 8 * (size_t)n_top);
+}
+
+int lede_op_logprobs(int32_t dtype, const void* logits, int64_t ld, int32_t n_rows, int32_t V, float temperature,
+                     const int32_t* tokens, int32_t n_top, float* logprobs, int32_t* ranks, float* entropy,
+                     int32_t* top_ids, float* top_logprobs, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!dtype_ok(dtype) || n_rows < 0 || V < 1 || n_top < 0 || n_top > V || ld < V) return LEDE_E_ARG;
+  if (!(temperature > 0.f) || !std::isfinite(temperature)) return LEDE_E_ARG;
+  if (V > MOST_VOCAB || n_top > MOST_TOP) return LEDE_E_UNSUPPORTED;
+  const float c = (float)(1.4426950408889634 / temperature);
+  if (!std::isfinite(c)) return LEDE_E_ARG;
+  if ((logprobs || ranks) && !tokens) return LEDE_E_ARG;
+  if (n_top && (!top_ids || !top_logprobs)) return LEDE_E_ARG;
+  if (n_rows == 0) return LEDE_OK;
+  if (!logits || !aligned(logits, es_of(dtype))) return LEDE_E_ARG;
+  const size_t need = lede_op_logprobs_bytes(n_rows, V, n_top);
+  if (!workspace || !aligned(workspace, 16) || workspace_bytes < need) return LEDE_E_ARG;
+  LogprobsArgs a{};
+  a.logits = logits; a.ld = ld; a.n_rows = n_rows; a.V = V; a.n_seg = logprobs_segments(V); a.n_top = n_top;
+  if ((int64_t)n_rows * a.n_seg > MOST_BLOCKS) return LEDE_E_UNSUPPORTED;
+  a.c = c; a.tokens = tokens;
+  a.logprobs = logprobs; a.ranks = ranks; a.entropy = entropy; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
+  a.seg_stats = (float4*)workspace;
+  a.seg_keys = (uint64_t*)(a.seg_stats + (size_t)n_rows * a.n_seg);
+  return done(launch_logprobs(dtype, a, S_(stream)));
+}
+
+}  // extern "C"

@@ -83,7 +83,9 @@ EXPORTED = ["lede_region_bytes", "lede_create", "lede_destroy", "lede_last_error
             "lede_get_trace", "lede_set_verify_reuse", "lede_dqn_region_bytes", "lede_dqn_create", "lede_dqn_destroy",
             "lede_dqn_last_error", "lede_dqn_init", "lede_dqn_push", "lede_dqn_record", "lede_dqn_end_episode",
             "lede_dqn_update", "lede_dqn_sync_target", "lede_dqn_act", "lede_dqn_read", "lede_step_submit",
-            "lede_step_collect", "lede_load_weights", "lede_debug_logits", "lede_debug_inject_failure", "lede_op_sample_noalloc"]
+            "lede_step_collect", "lede_load_weights", "lede_debug_logits", "lede_debug_inject_failure", "lede_op_sample_noalloc",
+            "lede_op_cache_bytes", "lede_op_cache_plan", "lede_op_cache_append", "lede_op_cache_read",
+            "lede_op_cache_attention_bytes", "lede_op_cache_attention", "lede_op_logprobs_bytes", "lede_op_logprobs"]
 MAX_IN_FLIGHT = 2
 SAMPLE_SLOTS = 16
 SAMPLE_STRIDE = 33
@@ -155,9 +157,22 @@ def load(path: str = LIB_PATH):
     L.lede_dqn_sync_target.argtypes = [vp, vp]
     L.lede_dqn_act.argtypes = [vp, vp, vp, vp]
     L.lede_dqn_read.argtypes = [vp, i32, fp, sz, P(i32), vp]
+    i64, f32 = ctypes.c_int64, ctypes.c_float
+    L.lede_op_cache_bytes.argtypes = [i32] * 3
+    L.lede_op_cache_plan.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]
+    L.lede_op_cache_append.argtypes = [i32, vp, i64, vp, i64, vp, i32, vp, i32, i32, i32, vp]
+    L.lede_op_cache_read.argtypes = [i32, vp, i32, i32, i32, vp, i32, vp, i64, vp, i64, vp]
+    L.lede_op_cache_attention_bytes.argtypes = [i32] * 7
+    L.lede_op_cache_attention.argtypes = [i32, vp, i64, vp, i32, vp, i32, vp, vp, i32, i32, i32, i32, i32, f32, i32, i32,
+                                          vp, i64, vp, sz, vp]
+    L.lede_op_logprobs_bytes.argtypes = [i32] * 3
+    L.lede_op_logprobs.argtypes = [i32, vp, i64, i32, i32, f32, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    for name in ("lede_op_cache_bytes", "lede_op_cache_attention_bytes", "lede_op_logprobs_bytes"):
+        getattr(L, name).restype = sz
     for name in EXPORTED:
         if name not in ("lede_destroy", "lede_last_error", "lede_op_tiled_bytes", "lede_dqn_region_bytes",
-                        "lede_dqn_destroy", "lede_dqn_last_error"):
+                        "lede_dqn_destroy", "lede_dqn_last_error", "lede_op_cache_bytes",
+                        "lede_op_cache_attention_bytes", "lede_op_logprobs_bytes"):
             getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -574,6 +589,195 @@ def op_sample_noalloc(logits, temperature: float, u) -> List[int]:
     if rc:
         raise LedeError(rc, "op_sample_noalloc")
     return [int(t) for t in out[:rows]]
+
+
+# ---- a batch of requests over one paged 8-bit cache ----------------------------------
+
+def _call(device, what: str, fn, *args):
+    """fn(*args, current stream of device) with that device current; a status
+    other than OK raises."""
+    import torch
+    if device.type != "cuda":
+        raise LedeError(LEDE_E_ARG, what + ": tensors on the GPU")
+    if device.index == torch.cuda.current_device():
+        rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    if rc:
+        raise LedeError(rc, what)
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise LedeError(LEDE_E_ARG, what)
+
+
+def _dense(device, dtype, *tensors) -> bool:
+    return all(t.device == device and t.dtype == dtype and t.is_contiguous() for t in tensors)
+
+
+def _dtype_code(torch, dtype) -> int:
+    _need(dtype in (torch.float32, torch.bfloat16), "dtype must be float32 or bfloat16")
+    return 1 if dtype == torch.bfloat16 else 0
+
+
+class Cache:
+    """One layer's paged 8-bit K/V cache: n_pages pages of 64 tokens, in
+    `region`, a uint8 GPU tensor of lede_op_cache_bytes (allocated and cleared
+    when not given)."""
+
+    def __init__(self, n_pages: int, n_kv: int, head_dim: int, device: int = 0, region=None):
+        import torch
+        nbytes = load().lede_op_cache_bytes(n_pages, n_kv, head_dim)
+        if nbytes == 0:
+            raise LedeError(LEDE_E_UNSUPPORTED, "cache of %d pages, %d heads of %d" % (n_pages, n_kv, head_dim))
+        if region is None:
+            region = torch.zeros(nbytes, dtype=torch.uint8, device=torch.device("cuda", device))
+        _need(region.dtype == torch.uint8 and region.is_contiguous() and region.numel() >= nbytes, "cache region")
+        self.region, self.n_pages, self.n_kv, self.head_dim = region, n_pages, n_kv, head_dim
+
+    @property
+    def device(self):
+        return self.region.device
+
+
+@dataclass
+class CachePlan:
+    kv_lens: object
+    held: object
+    row_start: object
+    slots: object
+    status: object   # code, rows, place in the free list after the call, first failing sequence
+
+
+def op_cache_plan(seq_lens, new_lens, held, free_pages, free_head, tables, max_rows: int,
+                  out: Optional[CachePlan] = None) -> CachePlan:
+    """Pages and slots of a pass in which sequence s gets new_lens[s] tokens
+    behind seq_lens[s] cached ones (int32 GPU tensors; tables [n_seqs][width]
+    is updated).  `out` reuses a plan's tensors, which may be the inputs'
+    own (kv_lens is seq_lens, held is held, free_head is status[2:3])."""
+    import torch
+    dev, n = seq_lens.device, seq_lens.numel()
+    _need(_dense(dev, torch.int32, seq_lens, new_lens, held, free_pages, free_head, tables) and tables.dim() == 2
+          and new_lens.numel() == n and held.numel() == n and tables.shape[0] == n and free_head.numel() == 1, "op_cache_plan")
+    if out is None:
+        buf = torch.empty(3 * n + 5, dtype=torch.int32, device=dev)
+        out = CachePlan(buf[:n], buf[n:2 * n], buf[2 * n:3 * n + 1], torch.empty(max_rows, dtype=torch.int64, device=dev),
+                        buf[3 * n + 1:])
+    _need(_dense(dev, torch.int32, out.kv_lens, out.held, out.row_start, out.status) and _dense(dev, torch.int64, out.slots)
+          and out.kv_lens.numel() == n and out.held.numel() == n and out.row_start.numel() == n + 1
+          and out.slots.numel() >= max_rows and out.status.numel() == 4, "op_cache_plan: out")
+    _call(dev, "op_cache_plan", load().lede_op_cache_plan, seq_lens.data_ptr(), new_lens.data_ptr(), held.data_ptr(), n,
+          free_pages.data_ptr(), free_pages.numel(), free_head.data_ptr(), tables.data_ptr(), tables.shape[1], max_rows,
+          out.kv_lens.data_ptr(), out.held.data_ptr(), out.row_start.data_ptr(), out.slots.data_ptr(), out.status.data_ptr())
+    return out
+
+
+def _cache_rows(cache: Cache, x, what: str):
+    """Row stride of [rows][n_kv][head_dim] with dense heads."""
+    _need(x.dim() == 3 and x.device == cache.device and x.shape[1:] == (cache.n_kv, cache.head_dim)
+          and x.stride(2) == 1 and (x.stride(1) == cache.head_dim or cache.n_kv == 1), what)
+    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), cache.n_kv * cache.head_dim)
+
+
+def op_cache_append(cache: Cache, k, v, slots):
+    """Rows k and v [rows][n_kv][head_dim] (any row stride that is a multiple
+    of 16 bytes) into the cache at slots (int64)."""
+    import torch
+    _need(k.dtype == v.dtype and k.shape == v.shape and _dense(cache.device, torch.int64, slots)
+          and slots.numel() == k.shape[0], "op_cache_append")
+    _call(cache.device, "op_cache_append", load().lede_op_cache_append, _dtype_code(torch, k.dtype), k.data_ptr(),
+          _cache_rows(cache, k, "op_cache_append: k"), v.data_ptr(), _cache_rows(cache, v, "op_cache_append: v"),
+          slots.data_ptr(), slots.numel(), cache.region.data_ptr(), cache.n_pages, cache.n_kv, cache.head_dim)
+
+
+def op_cache_read(cache: Cache, slots, dtype, out=None):
+    """(k, v) [rows][n_kv][head_dim] of `dtype` that the cache holds at slots
+    (int64); `out` gives the two tensors."""
+    import torch
+    _need(_dense(cache.device, torch.int64, slots), "op_cache_read")
+    code, n = _dtype_code(torch, dtype), slots.numel()
+    if out is None:
+        out = torch.empty(2, n, cache.n_kv, cache.head_dim, dtype=dtype, device=cache.device).unbind(0)
+    k, v = out
+    _need(k.dtype == dtype and v.dtype == dtype and k.shape[0] == n and v.shape[0] == n, "op_cache_read: out")
+    _call(cache.device, "op_cache_read", load().lede_op_cache_read, code, cache.region.data_ptr(), cache.n_pages,
+          cache.n_kv, cache.head_dim, slots.data_ptr(), n, k.data_ptr(), _cache_rows(cache, k, "op_cache_read: k"),
+          v.data_ptr(), _cache_rows(cache, v, "op_cache_read: v"))
+    return k, v
+
+
+def _workspace(torch, need: int, workspace, device, what: str):
+    if workspace is None:
+        return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+    _need(workspace.device == device and workspace.is_contiguous(), what)
+    return workspace
+
+
+def op_cache_attention(cache: Cache, q, tables, kv_lens, row_start, max_new: int, max_kv: int, scale: Optional[float] = None,
+                       out=None, workspace=None):
+    """Causal attention of q [rows][n_heads][head_dim], the rows row_start[s] ..
+    row_start[s + 1] - 1 being the last of the kv_lens[s] cached tokens of
+    sequence s, over the pages of tables [n_seqs][width] (int32).  max_new and
+    max_kv: the largest numbers of rows and of tokens expected.  `scale` is
+    head_dim ** -0.5 when not given.  Rows of a new `out` that no sequence has
+    are undefined; a given one's are left as they are."""
+    import torch
+    dev, n = cache.device, kv_lens.numel()
+    _need(q.dim() == 3 and q.device == dev and q.shape[2] == cache.head_dim and q.stride(2) == 1
+          and (q.stride(1) == cache.head_dim or q.shape[1] == 1) and _dense(dev, torch.int32, tables, kv_lens, row_start)
+          and tables.dim() == 2 and tables.shape[0] == n and row_start.numel() == n + 1, "op_cache_attention")
+    rows, heads = q.shape[0], q.shape[1]
+    if out is None:
+        out = torch.empty(rows, heads, cache.head_dim, dtype=q.dtype, device=dev)
+    _need(out.dtype == q.dtype and out.shape == q.shape and out.device == dev and out.stride(2) == 1
+          and (out.stride(1) == cache.head_dim or heads == 1), "op_cache_attention: out")
+    L, width = load(), heads * cache.head_dim
+    need = L.lede_op_cache_attention_bytes(n, rows, heads, cache.n_kv, cache.head_dim, max_new, max_kv)
+    ws = _workspace(torch, need, workspace, dev, "op_cache_attention: workspace")
+    _call(dev, "op_cache_attention", L.lede_op_cache_attention, _dtype_code(torch, q.dtype), q.data_ptr(),
+          q.stride(0) if rows > 1 else max(q.stride(0), width), cache.region.data_ptr(), cache.n_pages, tables.data_ptr(),
+          tables.shape[1], kv_lens.data_ptr(), row_start.data_ptr(), n, rows, heads, cache.n_kv, cache.head_dim,
+          cache.head_dim ** -0.5 if scale is None else float(scale), int(max_new), int(max_kv), out.data_ptr(),
+          out.stride(0) if rows > 1 else max(out.stride(0), width), ws.data_ptr(), ws.numel() * ws.element_size())
+    return out
+
+
+@dataclass
+class Logprobs:
+    logprobs: object
+    ranks: object
+    entropy: object
+    top_ids: object
+    top_logprobs: object
+
+
+def op_logprobs(logits, tokens, n_top: int = 0, temperature: float = 1.0, workspace=None) -> Logprobs:
+    """Log probabilities under softmax(logits / temperature) of the given token
+    of each row (int32 [rows]; None: no token), its rank, the row's entropy and
+    its n_top most likely tokens.  logits [rows][V] is float32 or bfloat16, of
+    any row stride."""
+    import torch
+    dev = logits.device
+    _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1), "op_logprobs: logits")
+    rows, V = logits.shape
+    _need(tokens is None or (_dense(dev, torch.int32, tokens) and tokens.numel() == rows), "op_logprobs: tokens")
+    n_top = int(n_top)
+    buf = torch.empty(rows * (3 + 2 * max(n_top, 0)), dtype=torch.float32, device=dev)
+    cols = buf[:3 * rows].view(3, rows)
+    top = buf[3 * rows:].view(2, rows, max(n_top, 0))
+    r = Logprobs(None if tokens is None else cols[0], None if tokens is None else cols[1].view(torch.int32), cols[2],
+                 top[0].view(torch.int32), top[1])
+    L = load()
+    ws = _workspace(torch, L.lede_op_logprobs_bytes(rows, V, n_top), workspace, dev, "op_logprobs: workspace")
+    at = buf.data_ptr()
+    given = tokens is not None
+    _call(dev, "op_logprobs", L.lede_op_logprobs, _dtype_code(torch, logits.dtype), logits.data_ptr(),
+          logits.stride(0) if rows > 1 else max(logits.stride(0), V), rows, V, float(temperature),
+          tokens.data_ptr() if given else None, n_top, at if given else None, at + 4 * rows if given else None, at + 8 * rows,
+          at + 12 * rows, at + 12 * rows + 4 * rows * n_top, ws.data_ptr(), ws.numel() * ws.element_size())
+    return r
 
 
 def dqn_noise_count(hidden: int) -> int:
