@@ -51,9 +51,20 @@ constexpr int64_t MOST_BLOCKS = 0x7FFFFFFF;
 constexpr int32_t MOST_SEQS = 65535;
 constexpr int32_t MOST_VOCAB = 1 << 20;
 constexpr int32_t MOST_TOP = 32;
-constexpr int LOGPROBS_SEG = 8192;   // entries of a row that one block holds
 
-int logprobs_segments(int32_t V) { return (V + 7 + LOGPROBS_SEG - 1) / LOGPROBS_SEG; }  // (+ 7: a row may begin inside a 16-byte piece)
+// Tiles of a row (its first may begin inside a 16-byte piece: up to 7
+// entries before it), and how many of them a block takes: as many as leave
+// the card about 1024 blocks, and all of up to four (5 rows of 32000: 15.3 us
+// in one launch, 10.1 + 5.2 us with a block per tile and the join).
+struct ScoreGrid { int n_tiles, part_tiles, n_part; };
+ScoreGrid score_grid(int32_t n_rows, int32_t V) {
+  ScoreGrid g;
+  g.n_tiles = (V + 7 + LP_TILE - 1) / LP_TILE;
+  const int parts = g.n_tiles <= 4 ? 1 : std::min(g.n_tiles, std::max(1, (int)((1024 + (int64_t)n_rows - 1) / std::max(n_rows, 1))));
+  g.part_tiles = std::min((g.n_tiles + parts - 1) / parts, LP_PART_TILES);
+  g.n_part = (g.n_tiles + g.part_tiles - 1) / g.part_tiles;
+  return g;
+}
 
 }  // namespace
 
@@ -142,7 +153,8 @@ int lede_op_cache_attention(int32_t dtype, const void* q, int64_t ldq, const voi
 
 size_t lede_op_logprobs_bytes(int32_t n_rows, int32_t V, int32_t n_top) {
   if (n_rows < 0 || V < 1 || V > MOST_VOCAB || n_top < 0 || n_top > MOST_TOP) return 0;
-  return (size_t)n_rows * logprobs_segments(V) * (16 + 8 * (size_t)n_top);
+  const int parts = score_grid(n_rows, V).n_part;
+  return parts == 1 ? 0 : (size_t)n_rows * parts * (16 + 8 * (size_t)n_top);
 }
 
 int lede_op_logprobs(int32_t dtype, const void* logits, int64_t ld, int32_t n_rows, int32_t V, float temperature,
@@ -158,14 +170,16 @@ int lede_op_logprobs(int32_t dtype, const void* logits, int64_t ld, int32_t n_ro
   if (n_rows == 0) return LEDE_OK;
   if (!logits || !aligned(logits, es_of(dtype))) return LEDE_E_ARG;
   const size_t need = lede_op_logprobs_bytes(n_rows, V, n_top);
-  if (!workspace || !aligned(workspace, 16) || workspace_bytes < need) return LEDE_E_ARG;
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return LEDE_E_ARG;
   LogprobsArgs a{};
-  a.logits = logits; a.ld = ld; a.n_rows = n_rows; a.V = V; a.n_seg = logprobs_segments(V); a.n_top = n_top;
-  if ((int64_t)n_rows * a.n_seg > MOST_BLOCKS) return LEDE_E_UNSUPPORTED;
+  const ScoreGrid g = score_grid(n_rows, V);
+  if ((int64_t)n_rows * g.n_part > MOST_BLOCKS) return LEDE_E_UNSUPPORTED;
+  a.logits = logits; a.ld = ld; a.n_rows = n_rows; a.V = V; a.n_top = n_top;
+  a.n_tiles = g.n_tiles; a.part_tiles = g.part_tiles; a.n_part = g.n_part;
   a.c = c; a.tokens = tokens;
   a.logprobs = logprobs; a.ranks = ranks; a.entropy = entropy; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
-  a.seg_stats = (float4*)workspace;
-  a.seg_keys = (uint64_t*)(a.seg_stats + (size_t)n_rows * a.n_seg);
+  a.part_stats = (float4*)workspace;
+  a.part_keys = (uint64_t*)(a.part_stats + (size_t)n_rows * a.n_part);
   return done(launch_logprobs(dtype, a, S_(stream)));
 }
 

@@ -77,18 +77,21 @@ hipError_t launch_cache_append(int dtype, const CacheRowsArgs& a, hipStream_t s)
 hipError_t launch_cache_read(int dtype, const CacheRowsArgs& a, hipStream_t s);
 hipError_t launch_cache_attention(int dtype, const CacheAttnArgs& a, hipStream_t s);
 
+constexpr int LP_TILE = 8192;       // entries of a row that a block holds at a time
+constexpr int LP_PART_TILES = 16;   // tiles that a block takes at most
+
 struct LogprobsArgs {
   const void* logits;
   int64_t ld;
-  int n_rows, V, n_seg, n_top;
+  int n_rows, V, n_tiles, part_tiles, n_part, n_top;   // a block takes part_tiles tiles of a row
   float c;               // log2(e) / temperature
   const int32_t* tokens;
   float *logprobs, *entropy, *top_logprobs;
   int32_t *ranks, *top_ids;
-  // workspace: per (row, segment) {max, sum, weighted sum, rank count},
-  // and the segment's largest keys in descending order
-  float4* seg_stats;     // .w holds the count's bits
-  uint64_t* seg_keys;    // [row][seg][n_top]
+  // workspace (n_part > 1): per (row, part) {max, sum, weighted sum, rank
+  // count} and the part's top keys in descending order
+  float4* part_stats;    // .w holds the count's bits
+  uint64_t* part_keys;   // [row][part][n_top]
 };
 hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t s);
 

@@ -597,13 +597,14 @@ def _call(device, what: str, fn, *args):
     """fn(*args, current stream of device) with that device current; a status
     other than OK raises."""
     import torch
-    if device.type != "cuda":
-        raise LedeError(LEDE_E_ARG, what + ": tensors on the GPU")
-    if device.index == torch.cuda.current_device():
-        rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    index = device.index
+    _need(index is not None, what + ": tensors on the GPU")
+    stream = torch._C._cuda_getCurrentRawStream   # (torch.cuda.current_stream builds an object: 1.9 us against 0.1)
+    if index == torch.cuda.current_device():
+        rc = fn(*args, stream(index))
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+        with torch.cuda.device(index):
+            rc = fn(*args, stream(index))
     if rc:
         raise LedeError(rc, what)
 
@@ -614,12 +615,25 @@ def _need(ok: bool, what: str):
 
 
 def _dense(device, dtype, *tensors) -> bool:
-    return all(t.device == device and t.dtype == dtype and t.is_contiguous() for t in tensors)
+    for t in tensors:
+        if t.dtype != dtype or t.device != device or not t.is_contiguous():
+            return False
+    return True
 
 
 def _dtype_code(torch, dtype) -> int:
-    _need(dtype in (torch.float32, torch.bfloat16), "dtype must be float32 or bfloat16")
-    return 1 if dtype == torch.bfloat16 else 0
+    if dtype is torch.bfloat16:
+        return 1
+    _need(dtype is torch.float32, "dtype must be float32 or bfloat16")
+    return 0
+
+
+def _row_stride(x, heads: int, head_dim: int, what: str) -> int:
+    """Elements between the rows of x [rows][heads][head_dim], whose heads are dense."""
+    rows, h, d = x.shape
+    r, sh, sd = x.stride()
+    _need(h == heads and d == head_dim and sd == 1 and (sh == d or h == 1), what)
+    return r if rows > 1 else max(r, h * d)
 
 
 class Cache:
@@ -636,10 +650,7 @@ class Cache:
             region = torch.zeros(nbytes, dtype=torch.uint8, device=torch.device("cuda", device))
         _need(region.dtype == torch.uint8 and region.is_contiguous() and region.numel() >= nbytes, "cache region")
         self.region, self.n_pages, self.n_kv, self.head_dim = region, n_pages, n_kv, head_dim
-
-    @property
-    def device(self):
-        return self.region.device
+        self.device = region.device
 
 
 @dataclass
@@ -658,61 +669,60 @@ def op_cache_plan(seq_lens, new_lens, held, free_pages, free_head, tables, max_r
     is updated).  `out` reuses a plan's tensors, which may be the inputs'
     own (kv_lens is seq_lens, held is held, free_head is status[2:3])."""
     import torch
-    dev, n = seq_lens.device, seq_lens.numel()
+    dev, n, max_rows = seq_lens.device, seq_lens.numel(), int(max_rows)
     _need(_dense(dev, torch.int32, seq_lens, new_lens, held, free_pages, free_head, tables) and tables.dim() == 2
           and new_lens.numel() == n and held.numel() == n and tables.shape[0] == n and free_head.numel() == 1, "op_cache_plan")
     if out is None:
         buf = torch.empty(3 * n + 5, dtype=torch.int32, device=dev)
-        out = CachePlan(buf[:n], buf[n:2 * n], buf[2 * n:3 * n + 1], torch.empty(max_rows, dtype=torch.int64, device=dev),
-                        buf[3 * n + 1:])
-    _need(_dense(dev, torch.int32, out.kv_lens, out.held, out.row_start, out.status) and _dense(dev, torch.int64, out.slots)
-          and out.kv_lens.numel() == n and out.held.numel() == n and out.row_start.numel() == n + 1
-          and out.slots.numel() >= max_rows and out.status.numel() == 4, "op_cache_plan: out")
+        kv_lens, held_out, row_start, status = buf.split_with_sizes((n, n, n + 1, 4))
+        out = CachePlan(kv_lens, held_out, row_start, torch.empty(max_rows, dtype=torch.int64, device=dev), status)
+    else:
+        _need(_dense(dev, torch.int32, out.kv_lens, out.held, out.row_start, out.status)
+              and _dense(dev, torch.int64, out.slots) and out.kv_lens.numel() == n and out.held.numel() == n
+              and out.row_start.numel() == n + 1 and out.slots.numel() >= max_rows and out.status.numel() == 4,
+              "op_cache_plan: out")
     _call(dev, "op_cache_plan", load().lede_op_cache_plan, seq_lens.data_ptr(), new_lens.data_ptr(), held.data_ptr(), n,
           free_pages.data_ptr(), free_pages.numel(), free_head.data_ptr(), tables.data_ptr(), tables.shape[1], max_rows,
           out.kv_lens.data_ptr(), out.held.data_ptr(), out.row_start.data_ptr(), out.slots.data_ptr(), out.status.data_ptr())
     return out
 
 
-def _cache_rows(cache: Cache, x, what: str):
-    """Row stride of [rows][n_kv][head_dim] with dense heads."""
-    _need(x.dim() == 3 and x.device == cache.device and x.shape[1:] == (cache.n_kv, cache.head_dim)
-          and x.stride(2) == 1 and (x.stride(1) == cache.head_dim or cache.n_kv == 1), what)
-    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), cache.n_kv * cache.head_dim)
-
-
 def op_cache_append(cache: Cache, k, v, slots):
     """Rows k and v [rows][n_kv][head_dim] (any row stride that is a multiple
     of 16 bytes) into the cache at slots (int64)."""
     import torch
-    _need(k.dtype == v.dtype and k.shape == v.shape and _dense(cache.device, torch.int64, slots)
-          and slots.numel() == k.shape[0], "op_cache_append")
-    _call(cache.device, "op_cache_append", load().lede_op_cache_append, _dtype_code(torch, k.dtype), k.data_ptr(),
-          _cache_rows(cache, k, "op_cache_append: k"), v.data_ptr(), _cache_rows(cache, v, "op_cache_append: v"),
-          slots.data_ptr(), slots.numel(), cache.region.data_ptr(), cache.n_pages, cache.n_kv, cache.head_dim)
+    dev, kv, hd, n = cache.device, cache.n_kv, cache.head_dim, slots.numel()
+    _need(_dense(dev, torch.int64, slots) and k.dim() == 3 and v.dim() == 3 and k.shape[0] == n and v.shape[0] == n
+          and k.device == dev and v.device == dev and k.dtype == v.dtype, "op_cache_append")
+    _call(dev, "op_cache_append", load().lede_op_cache_append, _dtype_code(torch, k.dtype), k.data_ptr(),
+          _row_stride(k, kv, hd, "op_cache_append: k"), v.data_ptr(), _row_stride(v, kv, hd, "op_cache_append: v"),
+          slots.data_ptr(), n, cache.region.data_ptr(), cache.n_pages, kv, hd)
 
 
 def op_cache_read(cache: Cache, slots, dtype, out=None):
     """(k, v) [rows][n_kv][head_dim] of `dtype` that the cache holds at slots
     (int64); `out` gives the two tensors."""
     import torch
-    _need(_dense(cache.device, torch.int64, slots), "op_cache_read")
-    code, n = _dtype_code(torch, dtype), slots.numel()
-    if out is None:
-        out = torch.empty(2, n, cache.n_kv, cache.head_dim, dtype=dtype, device=cache.device).unbind(0)
-    k, v = out
-    _need(k.dtype == dtype and v.dtype == dtype and k.shape[0] == n and v.shape[0] == n, "op_cache_read: out")
-    _call(cache.device, "op_cache_read", load().lede_op_cache_read, code, cache.region.data_ptr(), cache.n_pages,
-          cache.n_kv, cache.head_dim, slots.data_ptr(), n, k.data_ptr(), _cache_rows(cache, k, "op_cache_read: k"),
-          v.data_ptr(), _cache_rows(cache, v, "op_cache_read: v"))
+    dev, kv, hd, n = cache.device, cache.n_kv, cache.head_dim, slots.numel()
+    code = _dtype_code(torch, dtype)
+    k, v = torch.empty(2, n, kv, hd, dtype=dtype, device=dev).unbind(0) if out is None else out
+    _need(_dense(dev, torch.int64, slots) and k.dim() == 3 and v.dim() == 3 and k.shape[0] == n and v.shape[0] == n
+          and k.device == dev and v.device == dev and k.dtype == dtype and v.dtype == dtype, "op_cache_read")
+    _call(dev, "op_cache_read", load().lede_op_cache_read, code, cache.region.data_ptr(), cache.n_pages, kv, hd,
+          slots.data_ptr(), n, k.data_ptr(), _row_stride(k, kv, hd, "op_cache_read: k"), v.data_ptr(),
+          _row_stride(v, kv, hd, "op_cache_read: v"))
     return k, v
 
 
 def _workspace(torch, need: int, workspace, device, what: str):
+    """(tensor, address, bytes) of the workspace, the caller's or one of `need` bytes."""
     if workspace is None:
-        return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
-    _need(workspace.device == device and workspace.is_contiguous(), what)
-    return workspace
+        if need == 0:
+            return None, None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    else:
+        _need(workspace.device == device and workspace.is_contiguous(), what)
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def op_cache_attention(cache: Cache, q, tables, kv_lens, row_start, max_new: int, max_kv: int, scale: Optional[float] = None,
@@ -724,23 +734,25 @@ def op_cache_attention(cache: Cache, q, tables, kv_lens, row_start, max_new: int
     head_dim ** -0.5 when not given.  Rows of a new `out` that no sequence has
     are undefined; a given one's are left as they are."""
     import torch
-    dev, n = cache.device, kv_lens.numel()
-    _need(q.dim() == 3 and q.device == dev and q.shape[2] == cache.head_dim and q.stride(2) == 1
-          and (q.stride(1) == cache.head_dim or q.shape[1] == 1) and _dense(dev, torch.int32, tables, kv_lens, row_start)
-          and tables.dim() == 2 and tables.shape[0] == n and row_start.numel() == n + 1, "op_cache_attention")
-    rows, heads = q.shape[0], q.shape[1]
+    dev, kv, hd, n = cache.device, cache.n_kv, cache.head_dim, kv_lens.numel()
+    max_new, max_kv = int(max_new), int(max_kv)
+    _need(_dense(dev, torch.int32, tables, kv_lens, row_start) and q.dim() == 3 and q.device == dev and tables.dim() == 2
+          and tables.shape[0] == n and row_start.numel() == n + 1, "op_cache_attention")
+    rows, heads, _ = q.shape
+    ldq = _row_stride(q, heads, hd, "op_cache_attention: q")
     if out is None:
-        out = torch.empty(rows, heads, cache.head_dim, dtype=q.dtype, device=dev)
-    _need(out.dtype == q.dtype and out.shape == q.shape and out.device == dev and out.stride(2) == 1
-          and (out.stride(1) == cache.head_dim or heads == 1), "op_cache_attention: out")
-    L, width = load(), heads * cache.head_dim
-    need = L.lede_op_cache_attention_bytes(n, rows, heads, cache.n_kv, cache.head_dim, max_new, max_kv)
-    ws = _workspace(torch, need, workspace, dev, "op_cache_attention: workspace")
-    _call(dev, "op_cache_attention", L.lede_op_cache_attention, _dtype_code(torch, q.dtype), q.data_ptr(),
-          q.stride(0) if rows > 1 else max(q.stride(0), width), cache.region.data_ptr(), cache.n_pages, tables.data_ptr(),
-          tables.shape[1], kv_lens.data_ptr(), row_start.data_ptr(), n, rows, heads, cache.n_kv, cache.head_dim,
-          cache.head_dim ** -0.5 if scale is None else float(scale), int(max_new), int(max_kv), out.data_ptr(),
-          out.stride(0) if rows > 1 else max(out.stride(0), width), ws.data_ptr(), ws.numel() * ws.element_size())
+        out = torch.empty(rows, heads, hd, dtype=q.dtype, device=dev)
+        ldo = heads * hd
+    else:
+        _need(out.dtype == q.dtype and out.shape == q.shape and out.device == dev, "op_cache_attention: out")
+        ldo = _row_stride(out, heads, hd, "op_cache_attention: out")
+    L = load()
+    need = L.lede_op_cache_attention_bytes(n, rows, heads, kv, hd, max_new, max_kv)
+    ws, ws_at, ws_bytes = _workspace(torch, need, workspace, dev, "op_cache_attention: workspace")
+    _call(dev, "op_cache_attention", L.lede_op_cache_attention, _dtype_code(torch, q.dtype), q.data_ptr(), ldq,
+          cache.region.data_ptr(), cache.n_pages, tables.data_ptr(), tables.shape[1], kv_lens.data_ptr(),
+          row_start.data_ptr(), n, rows, heads, kv, hd, hd ** -0.5 if scale is None else scale, max_new, max_kv,
+          out.data_ptr(), ldo, ws_at, ws_bytes)
     return out
 
 
@@ -760,24 +772,24 @@ def op_logprobs(logits, tokens, n_top: int = 0, temperature: float = 1.0, worksp
     any row stride."""
     import torch
     dev = logits.device
-    _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1), "op_logprobs: logits")
-    rows, V = logits.shape
-    _need(tokens is None or (_dense(dev, torch.int32, tokens) and tokens.numel() == rows), "op_logprobs: tokens")
     n_top = int(n_top)
-    buf = torch.empty(rows * (3 + 2 * max(n_top, 0)), dtype=torch.float32, device=dev)
-    cols = buf[:3 * rows].view(3, rows)
-    top = buf[3 * rows:].view(2, rows, max(n_top, 0))
-    r = Logprobs(None if tokens is None else cols[0], None if tokens is None else cols[1].view(torch.int32), cols[2],
-                 top[0].view(torch.int32), top[1])
+    rows, V = logits.shape
+    ld, step = logits.stride()
+    _need((step == 1 or V == 1) and (tokens is None or (_dense(dev, torch.int32, tokens) and tokens.numel() == rows)),
+          "op_logprobs")
+    _need(0 <= n_top <= V, "op_logprobs: n_top")
+    given, m = tokens is not None, rows * n_top
+    f = torch.empty(2 * rows + m, dtype=torch.float32, device=dev)
+    i = torch.empty(rows + m, dtype=torch.int32, device=dev)
+    logprobs, entropy, top = f.split_with_sizes((rows, rows, m))
+    ranks, ids = i.split_with_sizes((rows, m))
     L = load()
-    ws = _workspace(torch, L.lede_op_logprobs_bytes(rows, V, n_top), workspace, dev, "op_logprobs: workspace")
-    at = buf.data_ptr()
-    given = tokens is not None
+    ws, ws_at, ws_bytes = _workspace(torch, L.lede_op_logprobs_bytes(rows, V, n_top), workspace, dev, "op_logprobs: workspace")
+    at, at_i = f.data_ptr(), i.data_ptr()
     _call(dev, "op_logprobs", L.lede_op_logprobs, _dtype_code(torch, logits.dtype), logits.data_ptr(),
-          logits.stride(0) if rows > 1 else max(logits.stride(0), V), rows, V, float(temperature),
-          tokens.data_ptr() if given else None, n_top, at if given else None, at + 4 * rows if given else None, at + 8 * rows,
-          at + 12 * rows, at + 12 * rows + 4 * rows * n_top, ws.data_ptr(), ws.numel() * ws.element_size())
-    return r
+          ld if rows > 1 else max(ld, V), rows, V, temperature, tokens.data_ptr() if given else None, n_top,
+          at if given else None, at_i if given else None, at + 4 * rows, at_i + 4 * rows, at + 8 * rows, ws_at, ws_bytes)
+    return Logprobs(logprobs if given else None, ranks if given else None, entropy, ids.view(rows, n_top), top.view(rows, n_top))
 
 
 def dqn_noise_count(hidden: int) -> int:

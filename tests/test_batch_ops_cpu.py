@@ -99,11 +99,11 @@ def test_attention_bytes(lib):
 
 
 LP = ["dtype", "logits", "ld", "n_rows", "V", "T", "tokens", "top", "lp", "ranks", "ent", "ids", "top_lp", "ws", "ws_bytes", "stream"]
-LP_GOOD = [0, P, 1000, 4, 1000, 1.0, P, 5, P, P, P, P, P, P, 1 << 30, NULL]
+LP_GOOD = [0, P, 50000, 4, 50000, 1.0, P, 5, P, P, P, P, P, P, 1 << 30, NULL]
 
 
 @pytest.mark.parametrize("bad,code", [({n: NULL}, lede.LEDE_E_ARG) for n in ("logits", "tokens", "ids", "top_lp", "ws")] + [
-    (dict(dtype=5), lede.LEDE_E_ARG), (dict(n_rows=-1), lede.LEDE_E_ARG), (dict(V=0), lede.LEDE_E_ARG), (dict(ld=999), lede.LEDE_E_ARG),
+    (dict(dtype=5), lede.LEDE_E_ARG), (dict(n_rows=-1), lede.LEDE_E_ARG), (dict(V=0), lede.LEDE_E_ARG), (dict(ld=49999), lede.LEDE_E_ARG),
     (dict(top=-1), lede.LEDE_E_ARG), (dict(top=33), lede.LEDE_E_UNSUPPORTED), (dict(V=4, top=5), lede.LEDE_E_ARG), (dict(T=0.0), lede.LEDE_E_ARG),
     (dict(T=-1.0), lede.LEDE_E_ARG), (dict(T=float("nan")), lede.LEDE_E_ARG), (dict(T=float("inf")), lede.LEDE_E_ARG),
     (dict(T=1e-45), lede.LEDE_E_ARG), (dict(logits=P + 2), lede.LEDE_E_ARG), (dict(ws=P + 8), lede.LEDE_E_ARG), (dict(ws_bytes=8), lede.LEDE_E_ARG),
