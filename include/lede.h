@@ -620,7 +620,8 @@ int lede_op_cache_plan(const int32_t* seq_lens, const int32_t* new_lens, const i
  * Rounding is to nearest, ties to even; an entry that is not finite becomes
  * a NaN.  Tokens of the page that the call does not write keep their values.
  * LEDE_E_ARG: null pointers, a bad dtype, n_rows < 0, a row stride below
- * n_kv * head_dim; k, v, cache or row strides not multiples of 16 bytes. */
+ * n_kv * head_dim; k, v, cache or row strides not multiples of 16 bytes.
+ * LEDE_E_UNSUPPORTED: 2^24 rows or more. */
 int lede_op_cache_append(int32_t dtype, const void* k, int64_t ldk, const void* v, int64_t ldv, const int64_t* slots,
                          int32_t n_rows, void* cache, int32_t n_pages, int32_t n_kv_heads, int32_t head_dim,
                          void* stream);
@@ -649,9 +650,10 @@ int lede_op_cache_read(int32_t dtype, const void* cache, int32_t n_pages, int32_
  * LEDE_E_ARG: null pointers, bad sizes, n_heads not a multiple of n_kv_heads,
  * a scale that is not finite, a small workspace; q, out, cache, workspace or
  * row strides not multiples of 16 bytes.  LEDE_E_UNSUPPORTED: more than 65535
- * sequences, more than 65536 heads, or a grid above 2^31 blocks. */
-size_t lede_op_cache_attention_bytes(int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads,
-                                     int32_t head_dim, int32_t max_new, int32_t max_kv);
+ * sequences, more than 65536 heads, 2^30 (row, head of a group) pairs or 2^23
+ * (sequence, KV head) pairs. */
+size_t lede_op_cache_attention_bytes(int32_t dtype, int32_t n_seqs, int32_t n_rows, int32_t n_heads,
+                                     int32_t n_kv_heads, int32_t head_dim, int32_t max_new, int32_t max_kv);
 int lede_op_cache_attention(int32_t dtype, const void* q, int64_t ldq, const void* cache, int32_t n_pages,
                             const int32_t* tables, int32_t table_ld, const int32_t* kv_lens, const int32_t* row_start,
                             int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -673,7 +675,7 @@ int lede_op_cache_attention(int32_t dtype, const void* q, int64_t ldq, const voi
  * LEDE_E_ARG: null pointers, bad sizes, n_top > V, ld < V, a temperature that
  * is not finite and > 0 (or whose reciprocal overflows), a small or
  * misaligned (16 bytes) workspace.  LEDE_E_UNSUPPORTED: V above 2^20, n_top
- * above 32. */
+ * above 32, 2^24 rows or more. */
 size_t lede_op_logprobs_bytes(int32_t n_rows, int32_t V, int32_t n_top);
 int lede_op_logprobs(int32_t dtype, const void* logits, int64_t ld, int32_t n_rows, int32_t V, float temperature,
                      const int32_t* tokens, int32_t n_top, float* logprobs, int32_t* ranks, float* entropy,

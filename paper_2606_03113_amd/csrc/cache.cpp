@@ -32,22 +32,37 @@ bool rows_ok(const void* p, int64_t ld, int64_t width, int32_t dt) {
   return p && aligned(p, 16) && ld >= width && ld * es_of(dt) % 16 == 0;
 }
 
+// Of 256 threads: a launch has fewer than 2^32 threads.
+constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;
+
 // Row tiles and splits of an attention's grid.  The kernels are right for any
 // lengths; this decides how the work spreads.
-struct AttnGrid { int n_tiles, n_split, min_chunk; int64_t blocks; };
-AttnGrid attn_grid(int32_t n_seqs, int32_t nq, int32_t nkv, int32_t max_new, int32_t max_kv) {
+struct AttnGrid { int tile_rows, n_tiles, n_full, n_cut, n_split, min_chunk; };
+AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32_t max_new, int32_t max_kv) {
   AttnGrid g;
-  const int64_t tiles = std::max<int64_t>(1, ((int64_t)max_new * (nq / nkv) + 15) / 16);
-  g.n_tiles = (int)std::min<int64_t>(tiles, 65536);
-  const int64_t whole = (int64_t)n_seqs * nkv * g.n_tiles;
-  const int64_t pages = ((int64_t)max_kv + CACHE_PAGE - 1) / CACHE_PAGE;
-  g.min_chunk = 4;
-  g.n_split = (int)std::max<int64_t>(1, std::min((2048 + whole - 1) / whole, (pages + g.min_chunk - 1) / g.min_chunk));
-  g.blocks = whole * g.n_split;
+  const int64_t rows = std::max<int64_t>(1, (int64_t)max_new * (nq / nkv));
+  g.tile_rows = rows <= 16 ? 16 : rows <= 64 || dtype == LEDE_DTYPE_F32 ? 64 : 128;
+  // (a task takes every n_tiles-th tile: a grid need not grow with a large max_new)
+  const int64_t groups = (int64_t)n_seqs * nkv;
+  g.n_tiles = (int)std::min((rows + g.tile_rows - 1) / g.tile_rows, 65536 / groups + 1);
+  const int64_t whole = groups * g.n_tiles;
+  const int64_t pages = std::max<int64_t>(1, ((int64_t)max_kv + CACHE_PAGE - 1) / CACHE_PAGE);
+  // The card holds ROUND blocks at a time.  Tasks of whole rounds are blocks
+  // of their own, and the rest, or all where there are fewer, are cut to fill
+  // one.  Few rows behind very long contexts are cut in any case: lengths
+  // differ, and one long sequence must not be a block's alone.
+  constexpr int64_t ROUND = 512, LONG = 128, MOST_CUT = 4096;
+  const int64_t by_length = g.tile_rows == 16 ? (pages + LONG - 1) / LONG : 1;
+  const int64_t cut = by_length > 1 ? whole : whole % ROUND;
+  int64_t split = cut ? std::max(whole < ROUND ? (ROUND + whole - 1) / whole : by_length > 1 ? 1 : ROUND / cut, by_length) : 1;
+  split = std::min(split, std::max<int64_t>(1, MOST_CUT / std::max<int64_t>(cut, 1)));
+  g.min_chunk = (int)std::max<int64_t>(4, (pages + split - 1) / split);
+  g.n_split = (int)((pages + g.min_chunk - 1) / g.min_chunk);
+  g.n_cut = g.n_split > 1 ? (int)cut : 0;
+  g.n_full = (int)(whole - g.n_cut);
   return g;
 }
 
-constexpr int64_t MOST_BLOCKS = 0x7FFFFFFF;
 constexpr int32_t MOST_SEQS = 65535;
 constexpr int32_t MOST_VOCAB = 1 << 20;
 constexpr int32_t MOST_TOP = 32;
@@ -95,6 +110,7 @@ static int cache_rows(bool append, int32_t dtype, void* k, int64_t ldk, void* v,
   if (!dtype_ok(dtype) || !cache || n_rows < 0) return LEDE_E_ARG;
   if (int rc = check_cache(n_pages, n_kv, hd)) return rc;
   if (!aligned(cache, 16)) return LEDE_E_ARG;
+  if (n_rows > MOST_BLOCKS) return LEDE_E_UNSUPPORTED;
   if (n_rows == 0) return LEDE_OK;
   const int64_t width = (int64_t)n_kv * hd;
   if (!slots || !rows_ok(k, ldk, width, dtype) || !rows_ok(v, ldv, width, dtype)) return LEDE_E_ARG;
@@ -116,11 +132,11 @@ int lede_op_cache_read(int32_t dtype, const void* cache, int32_t n_pages, int32_
   return cache_rows(false, dtype, k, ldk, v, ldv, slots, n_rows, (void*)cache, n_pages, n_kv_heads, head_dim, stream);
 }
 
-size_t lede_op_cache_attention_bytes(int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads,
+size_t lede_op_cache_attention_bytes(int32_t dtype, int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads,
                                      int32_t head_dim, int32_t max_new, int32_t max_kv) {
-  if (n_seqs < 1 || n_rows < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_kv < 0) return 0;
-  const AttnGrid g = attn_grid(n_seqs, n_heads, n_kv_heads, max_new, max_kv);
-  return g.n_split == 1 ? 0 : (size_t)n_rows * n_heads * g.n_split * (head_dim + 2) * 4;
+  if (!dtype_ok(dtype) || n_seqs < 1 || n_rows < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_kv < 0) return 0;
+  const AttnGrid g = attn_grid(dtype, n_seqs, n_heads, n_kv_heads, max_new, max_kv);
+  return (size_t)g.n_cut * g.n_split * g.tile_rows * (head_dim + 4) * 4;
 }
 
 int lede_op_cache_attention(int32_t dtype, const void* q, int64_t ldq, const void* cache, int32_t n_pages,
@@ -132,21 +148,22 @@ int lede_op_cache_attention(int32_t dtype, const void* q, int64_t ldq, const voi
     return LEDE_E_ARG;
   if (int rc = check_cache(n_pages, n_kv_heads, head_dim)) return rc;
   if (n_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_kv < 0 || !std::isfinite(scale)) return LEDE_E_ARG;
-  if (n_seqs > MOST_SEQS || n_heads > 65536) return LEDE_E_UNSUPPORTED;
+  if (n_seqs > MOST_SEQS || (int64_t)n_seqs * n_kv_heads > MOST_BLOCKS / 2 || n_heads > 65536 || (int64_t)n_rows * (n_heads / n_kv_heads) >= 1ll << 30) return LEDE_E_UNSUPPORTED;
   if (!aligned(cache, 16)) return LEDE_E_ARG;
   if (n_rows == 0) return LEDE_OK;
   const int64_t width = (int64_t)n_heads * head_dim;
   if (!rows_ok(q, ldq, width, dtype) || !rows_ok(out, ldo, width, dtype)) return LEDE_E_ARG;
-  const AttnGrid g = attn_grid(n_seqs, n_heads, n_kv_heads, max_new, max_kv);
-  if (g.blocks > MOST_BLOCKS) return LEDE_E_UNSUPPORTED;
-  const size_t need = lede_op_cache_attention_bytes(n_seqs, n_rows, n_heads, n_kv_heads, head_dim, max_new, max_kv);
+  const AttnGrid g = attn_grid(dtype, n_seqs, n_heads, n_kv_heads, max_new, max_kv);
+  const size_t need = lede_op_cache_attention_bytes(dtype, n_seqs, n_rows, n_heads, n_kv_heads, head_dim, max_new, max_kv);
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return LEDE_E_ARG;
   CacheAttnArgs a{};
   a.c = cache_view((void*)cache, n_pages, n_kv_heads, head_dim);
   a.q = q; a.ldq = ldq; a.tables = tables; a.table_ld = table_ld; a.kv_lens = kv_lens; a.row_start = row_start;
   a.n_seqs = n_seqs; a.n_rows = n_rows; a.nq = n_heads;
-  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
-  a.n_tiles = g.n_tiles; a.n_split = g.n_split; a.min_chunk = g.min_chunk;
+  a.scale_log2 = (float)(std::fabs((double)scale) * 1.4426950408889634);
+  a.q_sign = scale < 0 ? 0x80008000u : 0;
+  a.tile_rows = g.tile_rows; a.n_tiles = g.n_tiles;
+  a.n_full = g.n_full; a.n_cut = g.n_cut; a.n_split = g.n_split; a.min_chunk = g.min_chunk;
   a.part = (float*)workspace; a.out = out; a.ldo = ldo;
   return done(launch_cache_attention(dtype, a, S_(stream)));
 }

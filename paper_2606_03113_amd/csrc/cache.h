@@ -65,10 +65,12 @@ struct CacheAttnArgs {
   const int32_t* tables; int table_ld;
   const int32_t *kv_lens, *row_start;
   int n_seqs, n_rows, nq;
-  float scale_log2;      // softmax scale times log2(e)
+  float scale_log2;      // magnitude of the softmax scale, times log2(e)
+  uint32_t q_sign;       // 0x80008000 where it is negative: flips bf16 pairs' signs
+  int tile_rows;         // rows a block: 16 (waves take pages), 64 or 128 (waves take rows)
   int n_tiles;           // row tiles per (sequence, KV head) of the grid
-  int n_split, min_chunk;
-  float* part;           // [n_rows][nq][n_split][hd + 2]
+  int n_full, n_cut, n_split, min_chunk;  // blocks of whole tasks; tasks cut into n_split blocks of at least min_chunk pages
+  float* part;           // [n_cut][n_split][tile_rows][hd + 4]
   void* out; int64_t ldo;
 };
 

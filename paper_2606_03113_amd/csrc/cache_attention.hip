@@ -9,18 +9,26 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // For query row i of a sequence with n rows and L cached tokens (its own
 // included), p = L - n + i the row's position and t <= p:
-//   s_t = scale q . k_t,  m = max s_t,  o = sum exp(s_t - m) v_t / sum exp(s_t - m).
+//   o = sum w_t v_t / sum w_t,  w_t = exp(scale q . k_t).
 // A row at a negative position sees nothing: o = 0.
 //
-// Codes become matrix operands in registers: e4m3 is exact in bf16 and fp16,
-// and a block's power-of-two scale multiplies the page's scores (keys) and
-// its value product (values), so no precision is lost there.  q is exact in
-// one bf16 operand (bf16 queries) or in three (fp32 queries).  The weights
-// enter the value product in fp16: 11 bits for bf16 outputs, whose own half
-// step is 8 times larger, and as a high and a low part of 22 bits together
-// for fp32.  They are computed as 2^P_UP exp(s - m), which cancels in the
-// quotient and keeps weights down to 2^-14-P_UP in fp16's normal range.
-constexpr int P_UP = 12;
+// Codes become matrix operands in registers: e4m3 is exact in bf16 and fp16.
+// q is exact in one bf16 operand (bf16 queries) or in three (fp32 queries).
+// With E_k and E_v a page's scale exponents and c_t, d_t its codes, the kernels
+// form the exponent of a whole term of the sum,
+//   x_t = scale log2(e) 2^E_k q . c_t + E_v - B,  o = sum 2^x_t d_t / sum 2^(x_t - E_v),
+// so that the value product's accumulators take any mix of scales, its
+// weights 2^x are as precise as the term's share of the result asks, and both
+// scales cost nothing (one of the multiply, one of the add of a fused step).
+// B is a whole number (its rounding cancels), P_UP below the largest x so
+// far, and follows it only when some x passes P_LIM: until then neither the
+// accumulators nor the maximum across lanes are touched.  The weights enter
+// the product in fp16: 11 bits for bf16 outputs, whose own half step is 8
+// times larger, and a high and a low part, 22 bits, for fp32; between 2^P_LIM
+// and 2^-14 they are normal numbers.  The sum of 2^(x - E_v) is kept in fp32
+// at 2^-SUM_DOWN, which holds every scale's range.
+constexpr int P_UP = 8, P_LIM = 15, SUM_DOWN = 10;
+constexpr float B_NONE = -1e30f;   // B of a row that has seen nothing
 
 // Token of a page that row `r` of its score tile `t` (16 tokens x 16 queries)
 // holds.  A lane then has, of its query, the scores of 16 consecutive tokens
@@ -51,20 +59,48 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
 __device__ __forceinline__ uint32_t keep_bytes(uint32_t x, int n) {
   return n <= 0 ? 0u : n >= 4 ? x : x & (0xFFFFFFFFu >> (32 - 8 * n));
 }
-// 0x80 in every byte whose code is a NaN.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t x) { return ((x & 0x7F7F7F7F) + 0x01010101) & 0x80808080; }
-// fp16 ones where the bits of nan_bytes are set: a matrix operand of eight tokens.
-__device__ __forceinline__ uint4 ones_f16(uint2 m) {
-  auto two = [](uint32_t x, int i) {
-    return ((x >> (8 * i + 7) & 1) ? 0x3C00u : 0u) | ((x >> (8 * i + 15) & 1) ? 0x3C000000u : 0u);
-  };
-  return make_uint4(two(m.x, 0), two(m.x, 2), two(m.y, 0), two(m.y, 2));
+// fp16 ones at an operand's NaNs, and the operand with zeros there.
+__device__ __forceinline__ uint4 nan_ones(uint4 v) {
+  auto one = [](uint32_t u) { return ((u & 0x7FFFu) > 0x7C00u ? 0x3C00u : 0u) | ((u >> 16 & 0x7FFFu) > 0x7C00u ? 0x3C000000u : 0u); };
+  return make_uint4(one(v.x), one(v.y), one(v.z), one(v.w));
+}
+__device__ __forceinline__ uint4 nan_zeros(uint4 v) {
+  auto zero = [](uint32_t u) { return u & (((u & 0x7FFFu) > 0x7C00u ? 0u : 0xFFFFu) | ((u >> 16 & 0x7FFFu) > 0x7C00u ? 0u : 0xFFFF0000u)); };
+  return make_uint4(zero(v.x), zero(v.y), zero(v.z), zero(v.w));
+}
+// Four codes, zero where they are NaNs.
+__device__ __forceinline__ uint32_t nan_codes_zero(uint32_t x) { return x & ~((((x & 0x7F7F7F7F) + 0x01010101) >> 7 & 0x01010101) * 0xFFu); }
+// fp16 ones at the first n of an operand's eight tokens.
+__device__ __forceinline__ uint4 first_ones(int n) {
+  auto two = [n](int i) { return (i < n ? 0x3C00u : 0u) | (i + 1 < n ? 0x3C000000u : 0u); };
+  return make_uint4(two(0), two(2), two(4), two(6));
 }
 
-// The pages of a sequence that one split takes: chunks of at least min_chunk
-// pages, as many pages for each split where there are more.
-__device__ __forceinline__ int split_chunk(const CacheAttnArgs& a, int pages) {
-  return max(a.min_chunk, (pages + a.n_split - 1) / a.n_split);
+// A block's work: a tile of a sequence's (row, query head of the group) pairs
+// for one KV head, and a split of its pages.  The first n_full tasks are
+// blocks of their own; the others, which would leave the card partly idle in
+// a last round, are n_split blocks each.  Tasks with more pages come first.
+struct Task { int s, kvh, tile, split, n_split, slot; };
+__device__ __forceinline__ Task attn_task(const CacheAttnArgs& a, int bid) {
+  Task t;
+  t.slot = bid < a.n_full ? -1 : (bid - a.n_full) / a.n_split;
+  t.n_split = t.slot < 0 ? 1 : a.n_split;
+  t.split = t.slot < 0 ? 0 : (bid - a.n_full) % a.n_split;
+  int i = t.slot < 0 ? bid : a.n_full + t.slot;
+  t.kvh = i % a.c.nkv;
+  i /= a.c.nkv;
+  t.tile = a.n_tiles - 1 - i % a.n_tiles;
+  t.s = i / a.n_tiles;
+  return t;
+}
+// Pages of one split where a tile's rows see `pages`; all of them: no split.
+__device__ __forceinline__ int split_chunk(const CacheAttnArgs& a, int n_split, int pages) {
+  return n_split == 1 ? pages : max(a.min_chunk, (pages + n_split - 1) / n_split);
+}
+// A split's partial results of a tile's row: HD sums, then B and the weights' sum.
+template <int HD>
+__device__ __forceinline__ float* part_of(const CacheAttnArgs& a, int slot, int split, int r) {
+  return a.part + (((int64_t)slot * a.n_split + split) * a.tile_rows + r) * (HD + 4);
 }
 
 // A sequence's rows and cached length, held to the call's own bounds.
@@ -75,58 +111,42 @@ __device__ __forceinline__ AttnSeq attn_seq(const CacheAttnArgs& a, int s) {
   return {r0, r1 - r0, (int)min((int64_t)max(a.kv_lens[s], 0), cap)};
 }
 
-// Up to 16 query rows ((row, query head of the group) pairs of one sequence
-// and KV head) against one split of the sequence's pages.  The four waves
-// take the pages in turn, each with a running maximum, sum and output of its
-// own, all in registers: a page's keys and values are loaded straight into
-// operand order, the scores' result layout is the weights' operand layout,
-// and the next page's keys and values are requested as soon as this one's
-// are used.  The waves meet in LDS once, at the end.
-template <int DT, int HD>
-__global__ __launch_bounds__(256) void k_cache_attn(CacheAttnArgs a) {
-  constexpr int KH = HD / 64;          // 16-byte pieces of a key that a lane loads
-  constexpr int ND = HD / 16;          // 16-dim output tiles
-  constexpr int NQ = DT ? 1 : 3;       // bf16 parts of q
-  constexpr int NP = DT ? 1 : 2;       // fp16 parts of the weights
-  __shared__ float sm[4][16], sl[4][16];
-  __shared__ __align__(16) float so[4][16][HD + 4];
-  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
-  int bid = blockIdx.x;
-  const int split = bid % a.n_split;
-  bid /= a.n_split;
-  const int kvh = bid % a.c.nkv;
-  bid /= a.c.nkv;
-  const int s = bid / a.n_tiles;
-  const AttnSeq q = attn_seq(a, s);
-  const int G = a.nq / a.c.nkv;
-  const int64_t R = (int64_t)q.n * G;
-  const int pages_all = (q.len + CACHE_PAGE - 1) / CACHE_PAGE;
-  const int chunk = split_chunk(a, pages_all);
-  const bool direct = pages_all <= chunk;
-  const int32_t* table = a.tables + (int64_t)s * a.table_ld;
-  const uint8_t* kc = a.c.k + (size_t)kvh * (CACHE_PAGE * HD);
-  const uint8_t* vc = a.c.v + (size_t)kvh * (CACHE_PAGE * HD);
-  const size_t page_bytes = (size_t)a.c.nkv * (CACHE_PAGE * HD);
-  for (int64_t r0 = (int64_t)(bid % a.n_tiles) * 16; r0 < R; r0 += (int64_t)a.n_tiles * 16) {
-    const int nr = (int)min((int64_t)16, R - r0);
-    const int64_t rr = r0 + min(lr, nr - 1);   // rows past nr repeat the last one
-    const int m_row = (int)(rr / G), head = kvh * G + (int)(rr % G);
-    const int row_pos = q.len - q.n + m_row;
-    const int pos_lo = q.len - q.n + (int)(r0 / G), pos_hi = q.len - q.n + (int)((r0 + nr - 1) / G);
-    const int pages = pos_hi < 0 ? 0 : pos_hi / CACHE_PAGE + 1;   // that some row of the tile sees
-    const int j_end = min(pages, (split + 1) * chunk);
-    if (split * chunk >= pages && !(direct && split == 0)) continue;
-    // this lane's query: dims 64 h + 16 lg + 8 half .. + 7 as operand (h, half)
-    uint4 qf[NQ][KH][2];
-    {
-      const int64_t at = (int64_t)(q.row0 + m_row) * a.ldq + head * HD;
+// NT tiles of 16 query rows ((row, query head of the group) pairs of one
+// sequence and KV head), as a wave holds them.  A lane has the query lr = lane
+// % 16 of each tile, and of its outputs the dims 16 d + 4 lg .. + 3, lg = lane
+// / 16: both products' results lie so.
+template <int DT, int HD, int NT>
+struct Tiles {
+  static constexpr int KH = HD / 64;      // 16-byte pieces of a key that a lane loads
+  static constexpr int ND = HD / 16;      // 16-dim output tiles
+  static constexpr int NQ = DT ? 1 : 3;   // bf16 parts of q
+  static constexpr int NP = DT ? 1 : 2;   // fp16 parts of the weights
+  uint4 qf[NT][NQ][KH][2];
+  f32x4 o[NT][ND];
+  float sum[NT], base[NT];
+  int pos[NT];
+
+  // rows r0 .. of the R (row, head) pairs; tiles past R repeat the last
+  __device__ __forceinline__ void init(const CacheAttnArgs& a, const AttnSeq& q, int kvh, int G, int r0, int R) {
+    const int l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int rr = min(r0 + 16 * n + lr, R - 1), m = rr / G, head = kvh * G + (rr - m * G);
+      pos[n] = q.len - q.n + m;
+      sum[n] = 0.f;
+      base[n] = B_NONE;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+      // dims 64 h + 16 lg + 8 half .. + 7 are the operand (h, half)
+      const int64_t at = (int64_t)(q.row0 + m) * a.ldq + head * HD;
 #pragma unroll
       for (int h = 0; h < KH; ++h)
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const int64_t i = at + 64 * h + 16 * lg + 8 * half;
           if (DT == 1) {
-            qf[0][h][half] = ld16((const uint16_t*)a.q + i);
+            const uint4 u = ld16((const uint16_t*)a.q + i);
+            qf[n][0][h][half] = make_uint4(u.x ^ a.q_sign, u.y ^ a.q_sign, u.z ^ a.q_sign, u.w ^ a.q_sign);
           } else {
             float x[8];
             *(float4*)x = *(const float4*)((const float*)a.q + i);
@@ -140,98 +160,97 @@ __global__ __launch_bounds__(256) void k_cache_attn(CacheAttnArgs a) {
                 x[2 * e] -= bf16lo(u[e]);
                 x[2 * e + 1] -= bf16hi(u[e]);
               }
-              qf[p][h][half] = make_uint4(u[0], u[1], u[2], u[3]);
+              qf[n][p][h][half] = make_uint4(u[0] ^ a.q_sign, u[1] ^ a.q_sign, u[2] ^ a.q_sign, u[3] ^ a.q_sign);
             }
           }
         }
     }
-    float mx = -INFINITY, sum = 0.f;
-    f32x4 o[ND];
+  }
+
+  // One page: tokens t0 .. t0 + 63; this lane's key operand (t, h, half) and
+  // value operand (d, half) from kf and vf.  wk and wv: its scale words.
+  // pos_lo: the lowest position of the tiles' rows.  after_keys() once the
+  // keys are used.
+  template <class KF, class VF, class AK>
+  __device__ __forceinline__ void page(const CacheAttnArgs& a, int t0, int pos_lo, bool known, uint32_t wk, uint32_t wv, KF kf, VF vf,
+                                       AK after_keys) {
+    const int lg = (threadIdx.x & 63) >> 4;
+    const float ks = ldexpf(a.scale_log2, (int)(wk & 255) - 127);
+    const int ev = (int)(wv & 255) - 127;
+    // lane: token t0 + 16 lg + 4 t + i of its query.  Two key tiles at a time
+    // (products on one accumulator wait for each other), a step's operands
+    // taken while the step before is multiplied
+    f32x4 x[NT][4];
 #pragma unroll
-    for (int d = 0; d < ND; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    uint4 kf[4][KH], vf[ND];
-    uint2 words = make_uint2(0, 0);
-    int page = -1;
-    auto find = [&](int j) {
-      page = table[j];
-      const int p = page >= 0 && page < a.c.n_pages ? page : 0;
-      return p;
-    };
-    auto load_k = [&](int p) {
-      const uint8_t* base = kc + p * page_bytes + 16 * lg;
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) x[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    uint4 cur[2] = {kf(0, 0, 0), kf(1, 0, 0)};
+#pragma unroll
+    for (int i = 0; i < 4 * KH; ++i) {
+      const int t = i / (2 * KH) * 2, h = i / 2 % KH, half = i & 1;
+      uint4 nxt[2];
+      if (i + 1 < 4 * KH) {
+        const int t1 = (i + 1) / (2 * KH) * 2, h1 = (i + 1) / 2 % KH;
+        nxt[0] = kf(t1, h1, (i + 1) & 1);
+        nxt[1] = kf(t1 + 1, h1, (i + 1) & 1);
+      } else {
+        nxt[0] = vf(0, 0);
+        nxt[1] = vf(1, 0);
+      }
+#pragma unroll
+      for (int p = 0; p < NQ; ++p)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) x[n][t + u] = mfma_tile<1>(cur[u], qf[n][p][h][half], x[n][t + u]);
+      cur[0] = nxt[0];
+      cur[1] = nxt[1];
+      if (NT > 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    after_keys();
+    const bool edge = !known || t0 + CACHE_PAGE - 1 > pos_lo;
+    uint4 pf[NT][NP][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float up = (float)(ev + P_UP) - base[n];
+      float m = -INFINITY, kx = ks;   // x = kx x' + up
+      if (edge) {
+        // a table entry outside the pool: rows that see the page become NaN
+        kx = 1.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[n][t][i] = t0 + 16 * lg + 4 * t + i > pos[n] ? -INFINITY : known ? x[n][t][i] * ks : __builtin_nanf("");
+      }
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int h = 0; h < KH; ++h) kf[t][h] = ld16(base + tile_token(t, lr) * HD + 64 * h);
-    };
-    auto load_v = [&](int p) {
-      const uint8_t* base = vc + p * page_bytes + lr * CACHE_PAGE + 16 * lg;
+        for (int i = 0; i < 4; ++i) m = fmaxf(m, x[n][t][i]);
+      m *= kx;   // (the scale is not negative: q takes its sign)
+      float off = up;
+      if (__ballot(m + up > P_LIM)) {
+        // the row's new B, the same in its four lanes
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const float b = m + up > P_LIM ? ceilf(m + ev) : base[n], f = __builtin_amdgcn_exp2f(base[n] - b);
+        base[n] = b;
+        off = (float)(ev + P_UP) - b;
+        sum[n] *= f;
 #pragma unroll
-      for (int d = 0; d < ND; ++d) vf[d] = ld16(base + d * 16 * CACHE_PAGE);
-    };
-    int j = split * chunk + w;
-    if (j < j_end) {
-      const int p = find(j);
-      load_k(p);
-      load_v(p);
-      words = *(const uint2*)(a.c.words + ((size_t)p * a.c.nkv + kvh) * 2);
-    }
-    for (; j < j_end; j += 4) {
-      const bool known = page >= 0 && page < a.c.n_pages;
-      const uint2 wd = words;
-      const int t0 = j * CACHE_PAGE;
-      const float ks = ldexpf(a.scale_log2, (int)(wd.x & 255) - 127);
-      // scores: token t0 + 16 lg + 4 t + i of this lane's query
-      float sv[16];
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int h = 0; h < KH; ++h) {
-          const uint4 k0 = codes_bf16(make_uint2(kf[t][h].x, kf[t][h].y)), k1 = codes_bf16(make_uint2(kf[t][h].z, kf[t][h].w));
-#pragma unroll
-          for (int p = 0; p < NQ; ++p) {
-            acc = mfma_tile<1>(k0, qf[p][h][0], acc);
-            acc = mfma_tile<1>(k1, qf[p][h][1], acc);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sv[4 * t + i] = acc[i] * ks;
+          for (int i = 0; i < 4; ++i) o[n][d][i] *= f;
       }
-      int next = 0;
-      const bool more = j + 4 < j_end;
-      if (more) {
-        next = find(j + 4);
-        load_k(next);
-        words = *(const uint2*)(a.c.words + ((size_t)next * a.c.nkv + kvh) * 2);
-      }
-      if (!known || t0 + CACHE_PAGE - 1 > pos_lo) {
-        // a table entry outside the pool: rows that see the page become NaN
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sv[i] = t0 + 16 * lg + i > row_pos ? -INFINITY : known ? sv[i] : __builtin_nanf("");
-        // value codes past the sequence's end are whatever the page held before
-        const int nv = known ? q.len - t0 - 16 * lg : 0;
-        if (nv < 16)
-#pragma unroll
-          for (int d = 0; d < ND; ++d)
-            vf[d] = make_uint4(keep_bytes(vf[d].x, nv), keep_bytes(vf[d].y, nv - 4), keep_bytes(vf[d].z, nv - 8), keep_bytes(vf[d].w, nv - 12));
-      }
-      float pm = sv[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) pm = fmaxf(pm, sv[i]);
-      pm = fmaxf(pm, __shfl_xor(pm, 16));
-      pm = fmaxf(pm, __shfl_xor(pm, 32));
-      const float nm = fmaxf(mx, pm);
-      const float base = nm == -INFINITY ? 0.f : nm;   // nothing seen yet: weights 0
-      const float alpha = __builtin_amdgcn_exp2f(mx - base);
-      mx = nm;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sv[i] = __builtin_amdgcn_exp2f(sv[i] - base + P_UP);
       float ps = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) ps += sv[i];
-      sum = fmaf(sum, alpha, ps);
-      uint4 pf[NP][2];
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[n][t][i] = __builtin_amdgcn_exp2f(fmaf(x[n][t][i], kx, off));
+          if (DT == 0) ps += x[n][t][i];
+        }
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -239,135 +258,354 @@ __global__ __launch_bounds__(256) void k_cache_attn(CacheAttnArgs a) {
           uint32_t u[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            float& x0 = sv[8 * half + 2 * e];
-            float& x1 = sv[8 * half + 2 * e + 1];
-            u[e] = pack_f16(x0, x1);
+            const int t = 2 * half + e / 2, i = 2 * (e & 1);
+            u[e] = pack_f16(x[n][t][i], x[n][t][i + 1]);
+            // (the weights as the product takes them, two an operation)
+            if (DT == 1) ps = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, u[e]), f16x2{(_Float16)1.f, (_Float16)1.f}, ps, false);
             if (p + 1 < NP) {
               const f16x2 r = __builtin_bit_cast(f16x2, u[e]);
-              x0 -= (float)r[0];
-              x1 -= (float)r[1];
+              x[n][t][i] -= (float)r[0];
+              x[n][t][i + 1] -= (float)r[1];
             }
           }
-          pf[p][half] = make_uint4(u[0], u[1], u[2], u[3]);
+          pf[n][p][half] = make_uint4(u[0], u[1], u[2], u[3]);
         }
-      const float vs = ldexpf(1.f, (int)(wd.y & 255) - 127);
-      if (__builtin_expect((wd.y & CACHE_NAN) != 0, 0)) {
-        // NaN codes reach the rows that see their tokens, and no others: a
-        // product of indicators finds those rows, and the codes become zero
-        uint4 seen[2];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int t = t0 + 16 * lg + 8 * half;
-          uint2 mk = make_uint2(0, 0);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (t + e <= row_pos) mk.x |= 0x80u << (8 * e);
-            if (t + 4 + e <= row_pos) mk.y |= 0x80u << (8 * e);
-          }
-          seen[half] = ones_f16(mk);
-        }
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          uint32_t c[4] = {vf[d].x, vf[d].y, vf[d].z, vf[d].w}, nb[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            nb[e] = nan_bytes(c[e]);
-            c[e] &= ~((nb[e] >> 7) * 0xFFu);
-          }
-          f32x4 hit = {0.f, 0.f, 0.f, 0.f};
-          hit = mfma_f16(ones_f16(make_uint2(nb[0], nb[1])), seen[0], hit);
-          hit = mfma_f16(ones_f16(make_uint2(nb[2], nb[3])), seen[1], hit);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (hit[i] > 0.f) o[d][i] = __builtin_nanf("");
-          vf[d] = make_uint4(c[0], c[1], c[2], c[3]);
-        }
-      }
-#pragma unroll
-      for (int d = 0; d < ND; ++d) {
-        const uint4 v0 = codes_f16(make_uint2(vf[d].x, vf[d].y)), v1 = codes_f16(make_uint2(vf[d].z, vf[d].w));
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          acc = mfma_f16(v0, pf[p][0], acc);
-          acc = mfma_f16(v1, pf[p][1], acc);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[d][i] = fmaf(acc[i], vs, o[d][i] * alpha);
-      }
-      if (more) load_v(next);
-    }
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if (lg == 0) {
-      sm[w][lr] = mx;
-      sl[w][lr] = sum;
+      sum[n] = fmaf(ps, ldexpf(1.f, -ev - SUM_DOWN), sum[n]);
     }
 #pragma unroll
-    for (int d = 0; d < ND; ++d) *(f32x4*)&so[w][lr][16 * d + 4 * lg] = o[d];
-    __syncthreads();
-    // the waves' states joined, four dims of a row per thread
-    for (int i = threadIdx.x; i < nr * (HD / 4); i += 256) {
-      const int r = i / (HD / 4), d = i % (HD / 4) * 4;
-      const float m4 = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r]));
-      const float base = m4 == -INFINITY ? 0.f : m4;
-      float lsum = 0.f;
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float f = __builtin_amdgcn_exp2f(sm[u][r] - base);
-        lsum = fmaf(sl[u][r], f, lsum);
-        const f32x4 x = *(const f32x4*)&so[u][r][d];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = fmaf(x[e], f, acc[e]);
+    for (int i = 0; i < ND; ++i) {
+      const int d = i / 2 * 2, half = i & 1;
+      uint4 nxt[2] = {cur[0], cur[1]};
+      if (i + 1 < ND) {
+        nxt[0] = vf((i + 1) / 2 * 2, (i + 1) & 1);
+        nxt[1] = vf((i + 1) / 2 * 2 + 1, (i + 1) & 1);
       }
-      const int64_t ri = r0 + r;
-      const int64_t row = q.row0 + ri / G;
-      const int hd = kvh * G + (int)(ri % G);
-      if (direct) {
-        // a row that sees nothing is 0; one whose scores are all -infinity has no softmax
-        const float inv = q.len - q.n + ri / G < 0 ? 0.f : 1.f / lsum;
-        store4<DT>((uint8_t*)a.out + (row * a.ldo + hd * HD) * Elem<DT>::ES_, d,
-                   make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv));
-      } else {
-        float* p = a.part + ((row * a.nq + hd) * a.n_split + split) * (HD + 2);
-        *(float2*)(p + d) = make_float2(acc[0], acc[1]);
-        *(float2*)(p + d + 2) = make_float2(acc[2], acc[3]);
-        if (d == 0) *(float2*)(p + HD) = make_float2(m4, lsum);
-      }
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) o[n][d + u] = mfma_f16(cur[u], pf[n][p][half], o[n][d + u]);
+      cur[0] = nxt[0];
+      cur[1] = nxt[1];
+      if (NT > 1) __builtin_amdgcn_sched_barrier(0);
     }
-    __syncthreads();
+  }
+
+  // A page with NaN values: they reach the rows that see their tokens, and no
+  // others.  A product of indicators finds those rows; page() then takes the
+  // values with zeros in their place.
+  template <class VF>
+  __device__ __forceinline__ void mark_nans(int t0, VF vf) {
+    const int lg = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      const uint4 n0 = nan_ones(vf(d, 0)), n1 = nan_ones(vf(d, 1));
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const int seen = pos[n] - (t0 + 16 * lg) + 1;
+        f32x4 hit = {0.f, 0.f, 0.f, 0.f};
+        hit = mfma_f16(n0, first_ones(seen), hit);
+        hit = mfma_f16(n1, first_ones(seen - 8), hit);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][d][i] = hit[i] > 0.f ? __builtin_nanf("") : o[n][d][i];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
+
+// Value codes of tokens from nv on are whatever the page held before: zero.
+__device__ __forceinline__ uint4 keep_tokens(uint4 v, int nv) {
+  return make_uint4(keep_bytes(v.x, nv), keep_bytes(v.y, nv - 4), keep_bytes(v.z, nv - 8), keep_bytes(v.w, nv - 12));
+}
+
+// The next pages of a walk: 64 at a time, page and scale words in the lanes.
+// An entry outside the pool reads page 0 (and is known to).
+struct Walk {
+  int id = -1;
+  uint2 words = {0, 0};
+  // lane i: logical page j + stride * i, of those below j_end
+  __device__ __forceinline__ void load(const CacheAttnArgs& a, const int32_t* table, int kvh, int j, int stride, int j_end) {
+    const int64_t at = j + (int64_t)stride * (threadIdx.x & 63);
+    id = at < j_end ? table[at] : -1;
+    const int p = id >= 0 && id < a.c.n_pages ? id : 0;
+    words = *(const uint2*)(a.c.words + ((size_t)p * a.c.nkv + kvh) * 2);
+  }
+};
+
+// A result's four dims d .. d + 3: of an output row, or of a split's partial.
+template <int DT, int HD>
+__device__ __forceinline__ void put4(const CacheAttnArgs& a, const AttnSeq& q, int kvh, int G, int ri, int d, float* part, f32x4 acc,
+                                     float base, float sum) {
+  if (!part) {
+    const int m = ri / G, head = kvh * G + (ri - m * G);
+    const int64_t row = q.row0 + m;
+    // a row that sees nothing is 0; one whose scores are all -infinity has no softmax
+    const float inv = q.len - q.n + m < 0 ? 0.f : ldexpf(1.f / sum, -SUM_DOWN);
+    store4<DT>((uint8_t*)a.out + (row * a.ldo + head * HD) * Elem<DT>::ES_, d, make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv));
+  } else {
+    *(f32x4*)(part + d) = acc;
+    if (d == 0) *(float2*)(part + HD) = make_float2(base, sum);
   }
 }
 
-// The splits of a (row, query head) joined in order: a wave each, lanes over
-// the dims, sixteen splits requested at a time.
+// Up to 16 rows: one split of a sequence's pages, which the block's four waves
+// take in turn for all of its rows, each with sums of its own.  Keys and
+// values go from memory straight into the operands' registers (no LDS, no
+// barrier), the next page's requested as soon as this one's are used.  The
+// waves meet in LDS once, at the end.
 template <int DT, int HD>
+__global__ __launch_bounds__(256, DT ? 2 : 1) void k_cache_attn(CacheAttnArgs a) {
+  constexpr int NT = 1;
+  typedef Tiles<DT, HD, NT> T;
+  constexpr int KH = T::KH, ND = T::ND;
+  __shared__ float sm[4][16], sl[4][16];
+  __shared__ __align__(16) float so[4][16][HD + 4];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
+  const Task task = attn_task(a, blockIdx.x);
+  const int s = task.s, kvh = task.kvh;
+  const AttnSeq q = attn_seq(a, s);
+  const int G = a.nq / a.c.nkv;
+  const int R = q.n * G;
+  const int32_t* table = a.tables + (int64_t)s * a.table_ld;
+  const uint8_t* kc = a.c.k + (size_t)kvh * (CACHE_PAGE * HD);
+  const uint8_t* vc = a.c.v + (size_t)kvh * (CACHE_PAGE * HD);
+  const size_t page_bytes = (size_t)a.c.nkv * (CACHE_PAGE * HD);
+  // (rows behind the expected ones: every n_tiles-th tile more, whole)
+  int n_split = task.n_split;
+  for (int r0 = task.tile * (16 * NT); r0 < R; r0 += a.n_tiles * (16 * NT), n_split = 1) {
+    const int nr = min(16 * NT, R - r0);
+    const int pos_lo = q.len - q.n + r0 / G, pos_hi = q.len - q.n + (r0 + nr - 1) / G;
+    const int pages = pos_hi < 0 ? 0 : pos_hi / CACHE_PAGE + 1;   // that some row of the tiles sees
+    const int chunk = split_chunk(a, n_split, pages), j0 = task.split * chunk, j_end = min(pages, j0 + chunk);
+    const bool direct = chunk >= pages;
+    if (direct ? task.split > 0 : j0 >= pages) continue;
+    int j = j0 + w;
+    Walk walk;
+    walk.load(a, table, kvh, j, 4, j_end);
+    T tiles;
+    tiles.init(a, q, kvh, G, r0, R);
+    uint4 kf[4][KH], vf[ND];
+    int id = 0;   // of the page in the registers
+    auto page_at = [&](int i) {
+      const int p = __builtin_amdgcn_readlane(walk.id, i);
+      return p;
+    };
+    auto load_k = [&](int p) {
+      const uint8_t* base = kc + (p >= 0 && p < a.c.n_pages ? p : 0) * page_bytes + 16 * lg;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int h = 0; h < KH; ++h) kf[t][h] = ld16(base + tile_token(t, lr) * HD + 64 * h);
+    };
+    auto load_v = [&](int p) {
+      const uint8_t* base = vc + (p >= 0 && p < a.c.n_pages ? p : 0) * page_bytes + lr * CACHE_PAGE + 16 * lg;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) vf[d] = ld16(base + d * 16 * CACHE_PAGE);
+    };
+    if (j < j_end) {
+      id = page_at(0);
+      load_k(id);
+      load_v(id);
+    }
+    for (int i = 0; j < j_end; j += 4) {
+      const bool known = id >= 0 && id < a.c.n_pages;
+      const uint32_t wk = __builtin_amdgcn_readlane(walk.words.x, i), wv = __builtin_amdgcn_readlane(walk.words.y, i);
+      const int t0 = j * CACHE_PAGE;
+      const bool more = j + 4 < j_end;
+      if (++i == 64) {
+        i = 0;
+        if (more) walk.load(a, table, kvh, j + 4, 4, j_end);
+      }
+      const int next = page_at(i);
+      const int nv = known ? q.len - t0 : 0;
+      if (nv < CACHE_PAGE)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) vf[d] = keep_tokens(vf[d], nv - 16 * lg);
+      const auto value = [&](int d, int half) { return codes_f16(half ? make_uint2(vf[d].z, vf[d].w) : make_uint2(vf[d].x, vf[d].y)); };
+      if (__builtin_expect((wv & CACHE_NAN) != 0, 0)) {
+        tiles.mark_nans(t0, value);
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+          vf[d] = make_uint4(nan_codes_zero(vf[d].x), nan_codes_zero(vf[d].y), nan_codes_zero(vf[d].z), nan_codes_zero(vf[d].w));
+      }
+      tiles.page(a, t0, pos_lo, known, wk, wv,
+                 [&](int t, int h, int half) { return codes_bf16(half ? make_uint2(kf[t][h].z, kf[t][h].w) : make_uint2(kf[t][h].x, kf[t][h].y)); },
+                 value, [&] { if (more) load_k(next); });
+      if (more) load_v(next);
+      id = next;
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (16 * n >= nr) break;
+      float sum = tiles.sum[n];
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (lg == 0) {
+        sm[w][lr] = tiles.base[n];
+        sl[w][lr] = sum;
+      }
+#pragma unroll
+      for (int d = 0; d < ND; ++d) *(f32x4*)&so[w][lr][16 * d + 4 * lg] = tiles.o[n][d];
+      __syncthreads();
+      // the waves' states joined, four dims of a row per thread
+      for (int i = threadIdx.x; i < min(16, nr - 16 * n) * (HD / 4); i += 256) {
+        const int r = i / (HD / 4), d = i % (HD / 4) * 4;
+        const float b = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r]));
+        float lsum = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float f = __builtin_amdgcn_exp2f(sm[u][r] - b);
+          lsum = fmaf(sl[u][r], f, lsum);
+          const f32x4 x = *(const f32x4*)&so[u][r][d];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[e] = fmaf(x[e], f, acc[e]);
+        }
+        put4<DT, HD>(a, q, kvh, G, r0 + 16 * n + r, d, direct ? nullptr : part_of<HD>(a, task.slot, task.split, 16 * n + r), acc, b, lsum);
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// Many rows: four waves with 16 NT rows each walk the same pages.  A page comes
+// into LDS once per block, as 16-bit operands in the order in which the lanes
+// take them (16 bytes per lane, a contiguous KiB per operand: no bank
+// conflict either way), so that each wave converts a quarter of the codes;
+// two pages' room, so one barrier a page.
+template <int DT, int HD, int NT>
+__global__ __launch_bounds__(256, DT ? 2 : 1) void k_cache_attn_rows(CacheAttnArgs a) {
+  typedef Tiles<DT, HD, NT> T;
+  constexpr int KH = T::KH, ND = T::ND, VW = ND / 4;
+  __shared__ uint4 sk[2][8 * KH][64], sv[2][2 * ND][64];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
+  const Task task = attn_task(a, blockIdx.x);
+  const int s = task.s, kvh = task.kvh;
+  const AttnSeq q = attn_seq(a, s);
+  const int G = a.nq / a.c.nkv;
+  const int R = q.n * G;
+  const int32_t* table = a.tables + (int64_t)s * a.table_ld;
+  const uint8_t* kc = a.c.k + (size_t)kvh * (CACHE_PAGE * HD);
+  const uint8_t* vc = a.c.v + (size_t)kvh * (CACHE_PAGE * HD);
+  const size_t page_bytes = (size_t)a.c.nkv * (CACHE_PAGE * HD);
+  constexpr int ROWS = 64 * NT;
+  int n_split = task.n_split;
+  for (int b0 = task.tile * ROWS; b0 < R; b0 += a.n_tiles * ROWS, n_split = 1) {
+    const int pos_top = q.len - q.n + (min(b0 + ROWS, R) - 1) / G;
+    const int pages = pos_top < 0 ? 0 : pos_top / CACHE_PAGE + 1;   // that some row of the block sees
+    const int chunk = split_chunk(a, n_split, pages), j0 = task.split * chunk, j_end = min(pages, j0 + chunk);
+    const bool direct = chunk >= pages;
+    if (direct ? task.split > 0 : j0 >= pages) continue;
+    const int r0 = b0 + w * (16 * NT), nr = min(16 * NT, R - r0);   // of this wave; none or less: it only loads
+    const int pos_lo = q.len - q.n + min(r0, R - 1) / G;
+    Walk walk;
+    T tiles;
+    tiles.init(a, q, kvh, G, r0, R);
+    uint4 kr[KH], vr[VW];   // this wave's part of the next page: key tile w, value tiles VW w ..
+    auto load = [&](int id) {
+      const size_t at = (id >= 0 && id < a.c.n_pages ? id : 0) * page_bytes;
+      const uint8_t* kb = kc + at + tile_token(w, lr) * HD + 16 * lg;
+      const uint8_t* vb = vc + at + (w * VW * 16 + lr) * CACHE_PAGE + 16 * lg;
+#pragma unroll
+      for (int h = 0; h < KH; ++h) kr[h] = ld16(kb + 64 * h);
+#pragma unroll
+      for (int d = 0; d < VW; ++d) vr[d] = ld16(vb + d * 16 * CACHE_PAGE);
+    };
+    auto stage = [&](int buf, int id, int j) {
+      const int nv = id >= 0 && id < a.c.n_pages ? q.len - j * CACHE_PAGE : 0;
+      if (nv < CACHE_PAGE)
+#pragma unroll
+        for (int d = 0; d < VW; ++d) vr[d] = keep_tokens(vr[d], nv - 16 * lg);
+#pragma unroll
+      for (int h = 0; h < KH; ++h) {
+        sk[buf][2 * (w * KH + h)][l] = codes_bf16(make_uint2(kr[h].x, kr[h].y));
+        sk[buf][2 * (w * KH + h) + 1][l] = codes_bf16(make_uint2(kr[h].z, kr[h].w));
+      }
+#pragma unroll
+      for (int d = 0; d < VW; ++d) {
+        sv[buf][2 * (w * VW + d)][l] = codes_f16(make_uint2(vr[d].x, vr[d].y));
+        sv[buf][2 * (w * VW + d) + 1][l] = codes_f16(make_uint2(vr[d].z, vr[d].w));
+      }
+    };
+    int id = 0;
+    if (j0 < j_end) {
+      walk.load(a, table, kvh, j0, 1, j_end);
+      id = __builtin_amdgcn_readlane(walk.id, 0);
+      load(id);
+      stage(0, id, j0);
+    }
+    __syncthreads();
+    for (int j = j0, i = 0, buf = 0; j < j_end; ++j, buf ^= 1) {
+      const bool known = id >= 0 && id < a.c.n_pages;
+      const uint32_t wk = __builtin_amdgcn_readlane(walk.words.x, i), wv = __builtin_amdgcn_readlane(walk.words.y, i);
+      const bool more = j + 1 < j_end;
+      if (++i == 64) {
+        i = 0;
+        if (more) walk.load(a, table, kvh, j + 1, 1, j_end);
+      }
+      id = __builtin_amdgcn_readlane(walk.id, i);
+      if (more) load(id);
+      if (__builtin_expect((wv & CACHE_NAN) != 0, 0)) {   // (the same for the whole block)
+        tiles.mark_nans(j * CACHE_PAGE, [&](int d, int half) { return sv[buf][2 * d + half][l]; });
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < 2 * VW; ++d) sv[buf][2 * w * VW + d][l] = nan_zeros(sv[buf][2 * w * VW + d][l]);
+        __syncthreads();
+      }
+      // (a wave whose rows end before the page, or that has none, computes masked scores: a branch
+      // around the page costs every page a copy of the accumulators)
+      tiles.page(a, j * CACHE_PAGE, pos_lo, known, wk, wv, [&](int t, int h, int half) { return sk[buf][2 * (t * KH + h) + half][l]; },
+                 [&](int d, int half) { return sv[buf][2 * d + half][l]; }, [] {});
+      if (more) stage(buf ^ 1, id, j + 1);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float sum = tiles.sum[n];
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (16 * n + lr < nr) {
+        float* part = direct ? nullptr : part_of<HD>(a, task.slot, task.split, w * (16 * NT) + 16 * n + lr);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) put4<DT, HD>(a, q, kvh, G, r0 + 16 * n + lr, 16 * d + 4 * lg, part, tiles.o[n][d], tiles.base[n], sum);
+      }
+    }
+  }
+}
+
+// The splits of a row of a split task joined in order: a wave each, lanes over
+// the dims, B splits requested at a time.
+template <int DT, int HD, int B>
 __global__ __launch_bounds__(256) void k_cache_attn_join(CacheAttnArgs a) {
   constexpr int DL = HD / 64;
   const int l = threadIdx.x & 63;
-  const int s = blockIdx.y;
-  const AttnSeq q = attn_seq(a, s);
-  const int pages_all = (q.len + CACHE_PAGE - 1) / CACHE_PAGE;
-  const int chunk = split_chunk(a, pages_all);
-  if (pages_all <= chunk) return;
-  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < (int64_t)q.n * a.nq; i += (int64_t)gridDim.x * 4) {
-    const int64_t row = q.row0 + i / a.nq;
-    const int head = (int)(i % a.nq);
-    const int pos = q.len - q.n + (int)(i / a.nq);
+  const int G = a.nq / a.c.nkv;
+  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < (int64_t)a.n_cut * a.tile_rows; i += (int64_t)gridDim.x * 4) {
+    const int slot = (int)(i / a.tile_rows), r = (int)(i % a.tile_rows);
+    const Task t = attn_task(a, a.n_full + slot * a.n_split);
+    const AttnSeq q = attn_seq(a, t.s);
+    const int r0 = t.tile * a.tile_rows, ri = r0 + r, R = q.n * G;
+    if (ri >= R) continue;
+    const int pos_top = q.len - q.n + (min(r0 + a.tile_rows, R) - 1) / G;
+    const int pages = pos_top < 0 ? 0 : pos_top / CACHE_PAGE + 1, chunk = split_chunk(a, a.n_split, pages);
+    if (chunk >= pages) continue;
+    const int m = ri / G, head = t.kvh * G + (ri - m * G), pos = q.len - q.n + m;
+    const int64_t row = q.row0 + m;
     const int n = pos < 0 ? 0 : pos / CACHE_PAGE / chunk + 1;
-    const float* p = a.part + (row * a.nq + head) * a.n_split * (HD + 2);
-    float mx = -INFINITY, sum = 0.f, acc[DL];
+    const float* p = part_of<HD>(a, slot, 0, r);
+    const int64_t pitch = (int64_t)a.tile_rows * (HD + 4);
+    float mx = B_NONE, sum = 0.f, acc[DL];
 #pragma unroll
     for (int d = 0; d < DL; ++d) acc[d] = 0.f;
-    constexpr int B = 16;
     for (int j0 = 0; j0 < n; j0 += B) {
       float pm[B], pl[B], pa[B][DL];
 #pragma unroll
       for (int u = 0; u < B; ++u) {
-        const float* x = p + min(j0 + u, n - 1) * (HD + 2);
+        const float* x = p + min(j0 + u, n - 1) * pitch;
         const float2 ml = *(const float2*)(x + HD);
-        pm[u] = j0 + u < n ? ml.x : -INFINITY;
+        pm[u] = j0 + u < n ? ml.x : B_NONE;
         pl[u] = ml.y;
 #pragma unroll
         for (int d = 0; d < DL; ++d) pa[u][d] = x[l * DL + d];
@@ -375,14 +613,13 @@ __global__ __launch_bounds__(256) void k_cache_attn_join(CacheAttnArgs a) {
       float nm = mx;
 #pragma unroll
       for (int u = 0; u < B; ++u) nm = fmaxf(nm, pm[u]);
-      const float base = nm == -INFINITY ? 0.f : nm;
-      const float f0 = __builtin_amdgcn_exp2f(mx - base);
+      const float f0 = __builtin_amdgcn_exp2f(mx - nm);
       sum *= f0;
 #pragma unroll
       for (int d = 0; d < DL; ++d) acc[d] *= f0;
 #pragma unroll
       for (int u = 0; u < B; ++u) {
-        const float f = __builtin_amdgcn_exp2f(pm[u] - base);
+        const float f = __builtin_amdgcn_exp2f(pm[u] - nm);
         const bool live = j0 + u < n;
         sum = live ? fmaf(pl[u], f, sum) : sum;
 #pragma unroll
@@ -390,7 +627,7 @@ __global__ __launch_bounds__(256) void k_cache_attn_join(CacheAttnArgs a) {
       }
       mx = nm;
     }
-    const float inv = n == 0 ? 0.f : 1.f / sum;
+    const float inv = n == 0 ? 0.f : ldexpf(1.f / sum, -SUM_DOWN);
 #pragma unroll
     for (int d = 0; d < DL; ++d) Elem<DT>::store(a.out, row * a.ldo + head * HD + l * DL + d, acc[d] * inv);
   }
@@ -398,10 +635,16 @@ __global__ __launch_bounds__(256) void k_cache_attn_join(CacheAttnArgs a) {
 
 template <int DT, int HD>
 static hipError_t attention_hd(const CacheAttnArgs& a, hipStream_t s) {
-  k_cache_attn<DT, HD><<<(unsigned)((int64_t)a.n_seqs * a.n_tiles * a.c.nkv * a.n_split), 256, 0, s>>>(a);
-  if (a.n_split > 1) {
-    const int64_t per_seq = ((int64_t)a.n_rows * a.nq / a.n_seqs + 3) / 4;
-    k_cache_attn_join<DT, HD><<<dim3((unsigned)(per_seq < 1 ? 1 : per_seq > 4096 ? 4096 : per_seq), a.n_seqs), 256, 0, s>>>(a);
+  const unsigned blocks = (unsigned)(a.n_full + a.n_cut * a.n_split);
+  if (a.tile_rows == 16) k_cache_attn<DT, HD><<<blocks, 256, 0, s>>>(a);
+  else if (a.tile_rows == 64) k_cache_attn_rows<DT, HD, 1><<<blocks, 256, 0, s>>>(a);
+  else if constexpr (DT == 1) k_cache_attn_rows<DT, HD, 2><<<blocks, 256, 0, s>>>(a);
+  if (a.n_cut > 0) {
+    const int64_t rows = (int64_t)a.n_cut * a.tile_rows;
+    const unsigned grid = (unsigned)(rows / 4 < 16384 ? rows / 4 : 16384);
+    if (a.n_split <= 2) k_cache_attn_join<DT, HD, 2><<<grid, 256, 0, s>>>(a);
+    else if (a.n_split <= 4) k_cache_attn_join<DT, HD, 4><<<grid, 256, 0, s>>>(a);
+    else k_cache_attn_join<DT, HD, 16><<<grid, 256, 0, s>>>(a);
   }
   return hipGetLastError();
 }

@@ -162,7 +162,7 @@ def load(path: str = LIB_PATH):
     L.lede_op_cache_plan.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]
     L.lede_op_cache_append.argtypes = [i32, vp, i64, vp, i64, vp, i32, vp, i32, i32, i32, vp]
     L.lede_op_cache_read.argtypes = [i32, vp, i32, i32, i32, vp, i32, vp, i64, vp, i64, vp]
-    L.lede_op_cache_attention_bytes.argtypes = [i32] * 7
+    L.lede_op_cache_attention_bytes.argtypes = [i32] * 8
     L.lede_op_cache_attention.argtypes = [i32, vp, i64, vp, i32, vp, i32, vp, vp, i32, i32, i32, i32, i32, f32, i32, i32,
                                           vp, i64, vp, sz, vp]
     L.lede_op_logprobs_bytes.argtypes = [i32] * 3
@@ -746,10 +746,10 @@ def op_cache_attention(cache: Cache, q, tables, kv_lens, row_start, max_new: int
     else:
         _need(out.dtype == q.dtype and out.shape == q.shape and out.device == dev, "op_cache_attention: out")
         ldo = _row_stride(out, heads, hd, "op_cache_attention: out")
-    L = load()
-    need = L.lede_op_cache_attention_bytes(n, rows, heads, kv, hd, max_new, max_kv)
+    L, code = load(), _dtype_code(torch, q.dtype)
+    need = L.lede_op_cache_attention_bytes(code, n, rows, heads, kv, hd, max_new, max_kv)
     ws, ws_at, ws_bytes = _workspace(torch, need, workspace, dev, "op_cache_attention: workspace")
-    _call(dev, "op_cache_attention", L.lede_op_cache_attention, _dtype_code(torch, q.dtype), q.data_ptr(), ldq,
+    _call(dev, "op_cache_attention", L.lede_op_cache_attention, code, q.data_ptr(), ldq,
           cache.region.data_ptr(), cache.n_pages, tables.data_ptr(), tables.shape[1], kv_lens.data_ptr(),
           row_start.data_ptr(), n, rows, heads, kv, hd, hd ** -0.5 if scale is None else scale, max_new, max_kv,
           out.data_ptr(), ldo, ws_at, ws_bytes)

@@ -85,17 +85,17 @@ ATTN_GOOD = [1, P, 4096, P, 64, P, 32, P, P, 2, 2, 32, 8, 128, 0.1, 1, 2000, P, 
     (dict(out=P + 8), lede.LEDE_E_ARG), (dict(cache=P + 4), lede.LEDE_E_ARG), (dict(ws=P + 8), lede.LEDE_E_ARG),
     (dict(ws_bytes=16), lede.LEDE_E_ARG), (dict(n_seqs=65536), lede.LEDE_E_UNSUPPORTED), (dict(nq=65544), lede.LEDE_E_UNSUPPORTED)], ids=str)
 def test_attention_refuses(lib, bad, code):
-    assert lib.lede_op_cache_attention_bytes(2, 2, 32, 8, 128, 1, 2000) > 16
+    assert lib.lede_op_cache_attention_bytes(1, 2, 2, 32, 8, 128, 1, 2000) > 16
     assert lib.lede_op_cache_attention(*_change(ATTN_GOOD, ATTN, **bad)) == code
 
 
 def test_attention_bytes(lib):
-    assert lib.lede_op_cache_attention_bytes(1, 1, 4, 4, 64, 1, 100) == 0            # one split
-    assert lib.lede_op_cache_attention_bytes(0, 1, 4, 4, 64, 1, 100) == 0
-    assert lib.lede_op_cache_attention_bytes(1, 1, 5, 4, 64, 1, 100) == 0
+    assert lib.lede_op_cache_attention_bytes(1, 1, 1, 4, 4, 64, 1, 100) == 0            # one split
+    assert lib.lede_op_cache_attention_bytes(1, 0, 1, 4, 4, 64, 1, 100) == 0
+    assert lib.lede_op_cache_attention_bytes(1, 1, 1, 5, 4, 64, 1, 100) == 0
     # sizes that only spread the work may be anything
-    assert lib.lede_op_cache_attention_bytes(1, 1, 64, 8, 128, 1, 2 ** 31 - 1) > 0
-    assert lib.lede_op_cache_attention_bytes(1, 2 ** 31 - 1, 64, 8, 128, 2 ** 31 - 1, 2 ** 31 - 1) >= 0
+    assert lib.lede_op_cache_attention_bytes(1, 1, 1, 64, 8, 128, 1, 2 ** 31 - 1) > 0
+    assert lib.lede_op_cache_attention_bytes(1, 1, 2 ** 31 - 1, 64, 8, 128, 2 ** 31 - 1, 2 ** 31 - 1) >= 0
 
 
 LP = ["dtype", "logits", "ld", "n_rows", "V", "T", "tokens", "top", "lp", "ranks", "ent", "ids", "top_lp", "ws", "ws_bytes", "stream"]

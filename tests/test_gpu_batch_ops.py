@@ -420,7 +420,7 @@ def test_attention_strides_and_workspace(dtype):
     wide = torch.full((3, 6 * 64 + 8), 3.0, dtype=DT[dtype], device="cuda")
     wide[:, 8:8 + 256] = d.view(3, -1)
     out = torch.full((3, 5 * 64), 3.0, dtype=DT[dtype], device="cuda")
-    need = m.load().lede_op_cache_attention_bytes(2, 3, 4, 2, 64, 2, 1300)
+    need = m.load().lede_op_cache_attention_bytes(int(dtype == "bf16"), 2, 3, 4, 2, 64, 2, 1300)
     assert need > 0
     ws = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device="cuda")
     for _ in range(2):
