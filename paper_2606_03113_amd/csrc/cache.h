@@ -47,7 +47,6 @@ struct CachePlanArgs {
   int32_t *kv_lens, *held_out, *row_start;    // may be seq_lens and held
   int64_t* slots;
   int32_t* status;                            // [4]: code, rows, free_head after, first failing sequence
-  int n_slot_blocks;                          // k_cache_slots blocks; 0: k_cache_plan writes the slots itself
 };
 
 struct CacheRowsArgs {   // append (rows in) and read (rows out)

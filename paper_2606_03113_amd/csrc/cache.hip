@@ -10,23 +10,34 @@ namespace lede {
 
 constexpr int PLAN_THREADS = 1024;
 
-// Inclusive prefix sum over the block, in thread order; `total` to everyone.
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* red, int64_t& total) {
+// Inclusive prefix sums of two values over the block, in thread order, and
+// their totals.
+struct Pair { int64_t x, y; };
+__device__ __forceinline__ Pair block_scan(Pair v, Pair* red, Pair& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(v, o);
-    if (lane >= o) v += y;
+    const int64_t x = __shfl_up(v.x, o), y = __shfl_up(v.y, o);
+    if (lane >= o) {
+      v.x += x;
+      v.y += y;
+    }
   }
   __syncthreads();
   if (lane == 63) red[wave] = v;
   __syncthreads();
-  int64_t base = 0, all = 0;
+  Pair base{0, 0};
+  total = Pair{0, 0};
+#pragma unroll
   for (int w = 0; w < PLAN_THREADS / 64; ++w) {
-    if (w < wave) base += red[w];
-    all += red[w];
+    const Pair r = red[w];
+    if (w < wave) {
+      base.x += r.x;
+      base.y += r.y;
+    }
+    total.x += r.x;
+    total.y += r.y;
   }
-  total = all;
-  return base + v;
+  return Pair{base.x + v.x, base.y + v.y};
 }
 
 __device__ __forceinline__ int pages_of(int64_t tokens) { return (int)((tokens + CACHE_PAGE - 1) / CACHE_PAGE); }
@@ -46,92 +57,125 @@ __device__ __forceinline__ PlanAsk plan_ask(const CachePlanArgs& a, int s) {
   return r;
 }
 
-__device__ __forceinline__ int64_t plan_slot(const CachePlanArgs& a, int s, int pos) {
-  const int64_t page = a.tables[(int64_t)s * a.table_ld + pos / CACHE_PAGE];
-  return page * CACHE_PAGE + pos % CACHE_PAGE;
+// How many of n ascending values are at most i.
+__device__ __forceinline__ int at_most(const int32_t* v, int n, int i) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (v[mid] <= i) lo = mid + 1; else hi = mid;
+  }
+  return lo;
 }
 
 // One block: prefix sums of the rows and of the pages to take, in sequence
-// order; a first pass finds the first sequence that fails, a second writes.
-// Latency-bound: three loads, two scans and the stores.
+// order, PLAN_THREADS sequences at a time; a first pass finds the first
+// sequence that fails, a second writes (one chunk: the first's sums serve).
+// The taken pages' table entries, and with SLOTS the rows' slots, are spread
+// over the threads whatever the sequences' sizes.  Latency-bound: two rounds of
+// loads, a scan and the stores; 64 sequences of one row each 5 us.
+template <bool SLOTS>
 __global__ __launch_bounds__(PLAN_THREADS) void k_cache_plan(CachePlanArgs a) {
-  __shared__ int64_t red[PLAN_THREADS / 64];
+  __shared__ Pair red[PLAN_THREADS / 64];
   __shared__ int bad_seq, bad_code;
+  __shared__ int32_t row_end[PLAN_THREADS], page_end[PLAN_THREADS], seq_len[PLAN_THREADS], held[PLAN_THREADS];
   const int tid = threadIdx.x;
   const int head = *a.free_head;
   const int64_t avail = head >= 0 && head <= a.n_free ? a.n_free - head : -1;
   if (tid == 0) bad_seq = INT_MAX;
   __syncthreads();
-  int64_t rows = 0, taken = 0;
+  PlanAsk q;
+  Pair end, total, done{0, 0};   // rows, pages
   for (int s0 = 0; s0 < a.n_seqs; s0 += PLAN_THREADS) {
     const int s = s0 + tid;
-    const PlanAsk q = plan_ask(a, s);
-    int64_t t_rows, t_taken;
-    const int64_t r_end = rows + block_scan(q.fresh, red, t_rows);
-    const int64_t p_end = taken + block_scan(q.need, red, t_taken);
-    const int code = q.code              ? q.code
-                     : avail < 0         ? LEDE_E_ARG
-                     : p_end > avail     ? LEDE_E_KV_FULL
-                     : r_end > a.max_rows ? LEDE_E_ARG
-                                         : 0;
+    q = plan_ask(a, s);
+    end = block_scan(Pair{q.fresh, q.need}, red, total);
+    const int code = q.code                          ? q.code
+                     : avail < 0                     ? LEDE_E_ARG
+                     : done.y + end.y > avail        ? LEDE_E_KV_FULL
+                     : done.x + end.x > a.max_rows   ? LEDE_E_ARG
+                                                     : 0;
     if (s < a.n_seqs && code) atomicMin(&bad_seq, s);
     __syncthreads();
     if (s == bad_seq) bad_code = code;
-    rows += t_rows;
-    taken += t_taken;
+    done.x += total.x;
+    done.y += total.y;
     __syncthreads();
     if (bad_seq != INT_MAX) break;
   }
   const bool ok = bad_seq == INT_MAX;
-  rows = taken = 0;
-  for (int s0 = 0; s0 < a.n_seqs; s0 += PLAN_THREADS) {
-    const int s = s0 + tid;
-    const PlanAsk q = plan_ask(a, s);
-    int64_t t_rows = 0, t_taken = 0, r_end = 0, p_end = 0;
-    if (ok) {
-      r_end = rows + block_scan(q.fresh, red, t_rows);
-      p_end = taken + block_scan(q.need, red, t_taken);
-    }
-    if (s < a.n_seqs) {
-      if (ok)
-        for (int j = 0; j < q.need; ++j) a.tables[(int64_t)s * a.table_ld + q.held + j] = a.free_pages[head + p_end - q.need + j];
-      a.kv_lens[s] = ok ? q.seq + q.fresh : a.seq_lens[s];
-      a.held_out[s] = ok ? q.held + q.need : a.held[s];
-      a.row_start[s + 1] = (int)r_end;
-    }
-    rows += t_rows;
-    taken += t_taken;
-  }
+  if (!ok) done = Pair{0, 0};
   if (tid == 0) {
     a.row_start[0] = 0;
     a.status[0] = ok ? 0 : bad_code;
-    a.status[1] = (int)rows;
-    a.status[2] = head + (int)taken;
+    a.status[1] = (int)done.x;
+    a.status[2] = head + (int)done.y;
     a.status[3] = ok ? -1 : bad_seq;
   }
+  int rows = 0, taken = 0;   // (they fit: the first pass held them to max_rows and n_free)
+  for (int s0 = 0; s0 < a.n_seqs; s0 += PLAN_THREADS) {
+    const int s = s0 + tid;
+    if (ok && a.n_seqs > PLAN_THREADS) {
+      q = plan_ask(a, s);
+      end = block_scan(Pair{q.fresh, q.need}, red, total);
+    }
+    if (s < a.n_seqs) {
+      if (ok) {
+        row_end[tid] = (int)end.x;
+        page_end[tid] = (int)end.y;
+        seq_len[tid] = q.seq;
+        held[tid] = q.held;
+      }
+      a.kv_lens[s] = ok ? q.seq + q.fresh : a.seq_lens[s];
+      a.held_out[s] = ok ? q.held + q.need : a.held[s];
+      a.row_start[s + 1] = ok ? rows + (int)end.x : 0;
+    }
+    if (!ok) continue;
+    __syncthreads();
+    const int n = min(PLAN_THREADS, a.n_seqs - s0);
+    for (int i = tid; i < (int)total.y; i += PLAN_THREADS) {
+      const int j = at_most(page_end, n, i), from = j ? page_end[j - 1] : 0;
+      a.tables[(int64_t)(s0 + j) * a.table_ld + held[j] + i - from] = a.free_pages[head + taken + i];
+    }
+    if (SLOTS) {
+      for (int r = tid; r < (int)total.x; r += PLAN_THREADS) {
+        const int j = at_most(row_end, n, r), pos = seq_len[j] + r - (j ? row_end[j - 1] : 0);
+        const int i = pos / CACHE_PAGE - held[j];   // taken in this call: its entry may not be written yet
+        const int64_t page = i < 0 ? a.tables[(int64_t)(s0 + j) * a.table_ld + pos / CACHE_PAGE]
+                                   : a.free_pages[head + taken + (j ? page_end[j - 1] : 0) + i];
+        a.slots[rows + r] = page * CACHE_PAGE + pos % CACHE_PAGE;
+      }
+    }
+    rows += (int)total.x;
+    taken += (int)total.y;
+    __syncthreads();
+  }
+  if (SLOTS)
+    for (int r = rows + tid; r < a.max_rows; r += PLAN_THREADS) a.slots[r] = -1;
 }
 
-// The slot of every row: the row's sequence by binary search of row_start.
+// The slot of every row, by many blocks: the row's sequence from row_start.
 __global__ __launch_bounds__(256) void k_cache_slots(CachePlanArgs a) {
   const int rows = a.status[1];
   for (int r = blockIdx.x * 256 + threadIdx.x; r < a.max_rows; r += gridDim.x * 256) {
     int64_t slot = -1;
     if (r < rows) {
-      int lo = 0, hi = a.n_seqs;   // row_start[lo] <= r < row_start[hi]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (a.row_start[mid] <= r) lo = mid; else hi = mid;
-      }
-      const int n = a.row_start[lo + 1] - a.row_start[lo];
-      slot = plan_slot(a, lo, a.kv_lens[lo] - n + (r - a.row_start[lo]));
+      const int s = at_most(a.row_start + 1, a.n_seqs, r);
+      const int pos = a.kv_lens[s] - a.row_start[s + 1] + r;
+      slot = (int64_t)a.tables[(int64_t)s * a.table_ld + pos / CACHE_PAGE] * CACHE_PAGE + pos % CACHE_PAGE;
     }
     a.slots[r] = slot;
   }
 }
 
+// Few rows: one launch (64 rows: 6 us, and 8 in two); many: a second spreads them
+// over the card.
 hipError_t launch_cache_plan(const CachePlanArgs& a, hipStream_t s) {
-  k_cache_plan<<<1, PLAN_THREADS, 0, s>>>(a);
-  if (a.max_rows > 0) k_cache_slots<<<(int)min((a.max_rows + 255ll) / 256, 2048ll), 256, 0, s>>>(a);
+  if (a.max_rows <= 4 * PLAN_THREADS) {
+    k_cache_plan<true><<<1, PLAN_THREADS, 0, s>>>(a);
+  } else {
+    k_cache_plan<false><<<1, PLAN_THREADS, 0, s>>>(a);
+    k_cache_slots<<<(int)min((a.max_rows + 255ll) / 256, 2048ll), 256, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 
@@ -158,189 +202,306 @@ __device__ __forceinline__ float to_scale(float x, int e) {
 }
 template <int I> __device__ __forceinline__ float decode1(uint32_t w) { return __builtin_amdgcn_cvt_f32_fp8((int)w, I); }
 
-// Eight consecutive elements of a row.
-template <int DT> __device__ __forceinline__ void row8(const void* p, int64_t i, float* o) {
-  if (DT == 1) {
-    const uint4 u = ld16((const uint16_t*)p + i);
-    o[0] = bf16lo(u.x); o[1] = bf16hi(u.x); o[2] = bf16lo(u.y); o[3] = bf16hi(u.y);
-    o[4] = bf16lo(u.z); o[5] = bf16hi(u.z); o[6] = bf16lo(u.w); o[7] = bf16hi(u.w);
-  } else {
-    const float4 a = *(const float4*)((const float*)p + i), b = *(const float4*)((const float*)p + i + 4);
-    o[0] = a.x; o[1] = a.y; o[2] = a.z; o[3] = a.w; o[4] = b.x; o[5] = b.y; o[6] = b.z; o[7] = b.w;
+// Eight consecutive elements of a row, as they came (half the registers of
+// their values, for bf16).
+template <int DT> struct Eight {
+  uint4 u[DT ? 1 : 2];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < (DT ? 1 : 2); ++i) u[i] = make_uint4(0, 0, 0, 0);
   }
+  __device__ __forceinline__ void load(const void* p, int64_t i) {
+    u[0] = ld16((const uint8_t*)p + i * Elem<DT>::ES_);
+    if (DT == 0) u[DT ? 0 : 1] = ld16((const uint8_t*)p + i * Elem<DT>::ES_ + 16);
+  }
+  // The largest magnitude's fp32 bits: from 0x7F800000 on, one is not finite.
+  __device__ __forceinline__ uint32_t most(uint32_t m) const {
+    if (DT == 1) {
+      typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+      auto low = [](uint32_t x) { return __builtin_bit_cast(u16x2, x & 0x7FFF7FFFu); };
+      const u16x2 x = __builtin_elementwise_max(__builtin_elementwise_max(low(u[0].x), low(u[0].y)), __builtin_elementwise_max(low(u[0].z), low(u[0].w)));
+      return max(m, (uint32_t)max(x[0], x[1]) << 16);
+    }
+#pragma unroll
+    for (int i = 0; i < (DT ? 1 : 2); ++i) m = max(max(max(m, u[i].x & 0x7FFFFFFF), u[i].y & 0x7FFFFFFF), max(u[i].z & 0x7FFFFFFF, u[i].w & 0x7FFFFFFF));
+    return m;
+  }
+  __device__ __forceinline__ float operator[](int e) const {   // (e is a constant of an unrolled loop)
+    const uint4 q = DT ? u[0] : u[DT ? 0 : e / 4];
+    const int w = DT ? e / 2 : e % 4;
+    const uint32_t x = w == 0 ? q.x : w == 1 ? q.y : w == 2 ? q.z : q.w;
+    return DT == 0 ? __uint_as_float(x) : e & 1 ? bf16hi(x) : bf16lo(x);
+  }
+};
+
+// Four codes re-scaled by 2^d (d <= 0), rounded to the nearest code.
+__device__ __forceinline__ uint32_t rescale4(uint32_t w, int d) {
+  return encode4(scale_by(decode1<0>(w), d), scale_by(decode1<1>(w), d), scale_by(decode1<2>(w), d), scale_by(decode1<3>(w), d));
 }
 
-// Sixteen codes re-scaled by 2^d (d <= 0), rounded to the nearest code.
-__device__ __forceinline__ uint4 rescale16(uint4 c, int d) {
-  uint32_t w[4] = {c.x, c.y, c.z, c.w};
+// A block of 2 HD threads works on a page's (KV head, keys or values) block:
+// a thread has the four tokens 4 g .. 4 g + 3 and eight dims 8 c .. 8 c + 7.
+// Keys: neighbouring threads have neighbouring dims (a token's codes are
+// contiguous); values: neighbouring token groups (a dim's codes are), and four
+// tokens' codes of a dim are one dword, so that nothing is transposed.
+template <int HD> struct BlockPart {
+  int c, g;
+  __device__ __forceinline__ explicit BlockPart(bool values) {
+    const int tid = threadIdx.x;
+    c = values ? tid / 16 : tid % (HD / 8);
+    g = values ? tid % 16 : tid / (HD / 8);
+  }
+};
+
+// Rows whose slots lie in one page and follow each other in a call: a run.
+// ASCENDING: with rising places, too (a place then has one row).  A wave's
+// view from row w0 on: lane i has the slots of rows w0 + i and of the one
+// before it.
+template <bool ASCENDING> struct Rows {
+  const CacheRowsArgs& a;
+  int64_t n_slots, at, prev;
+  __device__ __forceinline__ Rows(const CacheRowsArgs& a_, int w0) : a(a_), n_slots((int64_t)a_.c.n_pages * CACHE_PAGE) { load(w0); }
+  __device__ __forceinline__ void load(int w0) {
+    const int r = w0 + (threadIdx.x & 63);
+    at = r < a.n_rows ? a.slots[r] : -1;
+    prev = r < a.n_rows && r > 0 ? a.slots[r - 1] : -1;
+  }
+  __device__ __forceinline__ bool valid(int64_t s) const { return s >= 0 && s < n_slots; }
+  __device__ __forceinline__ bool joins() const {
+    return valid(prev) && valid(at) && prev / CACHE_PAGE == at / CACHE_PAGE && !(ASCENDING && at <= prev);
+  }
+  // Which of the first n rows begin a run.
+  __device__ __forceinline__ uint64_t leaders(int n) const { return __ballot((int)(threadIdx.x & 63) < n && valid(at) && !joins()); }
+  // The run at w0: its length (at most 64), its page, lane i its row i's place (-1 behind it).
+  __device__ __forceinline__ int run(int64_t& page, int& place) const {
+    const int lane = threadIdx.x & 63;
+    const uint64_t out = ~__ballot(lane == 0 || joins());
+    const int n = out ? __ffsll((unsigned long long)out) - 1 : 64;
+    place = lane < n ? (int)(at % CACHE_PAGE) : -1;
+    page = __shfl(at, 0) / CACHE_PAGE;
+    return n;
+  }
+};
+
+// The run's row of every place of the page (-1: none), by the first wave.
+__device__ __forceinline__ void place_rows(int8_t* row_of, int n, int place) {
+  if (threadIdx.x < 64) row_of[threadIdx.x] = -1;
+  __syncthreads();
+  if (threadIdx.x < n && threadIdx.x < 64) row_of[place] = (int8_t)threadIdx.x;
+  __syncthreads();
+}
+
+// The block's maximum.
+template <int NW> __device__ __forceinline__ uint32_t block_most(uint32_t v, uint32_t* red) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    w[i] = encode4(scale_by(decode1<0>(w[i]), d), scale_by(decode1<1>(w[i]), d), scale_by(decode1<2>(w[i]), d),
-                   scale_by(decode1<3>(w[i]), d));
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  for (int o = 32; o; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (int i = 1; i < NW; ++i) v = max(v, red[i]);
+  return v;
 }
 
 // The rows of a call that lie in one page are a run of consecutive rows; a
 // block handles the runs that begin in its window of rows, for one KV head
 // and for keys or values.  A run that holds the page's first token starts the
 // block's scale anew; any other run keeps the old scale, or, where its rows
-// need a larger one, re-scales the page's codes first.
+// need a larger one, re-scales the page's other codes.  Memory-bound for
+// prompts; a step's single rows wait for three dependent loads.
 template <int DT, int HD>
-__global__ __launch_bounds__(256) void k_cache_append(CacheRowsArgs a) {
-  constexpr int TPR = HD / 8, RPP = 256 / TPR, NP = CACHE_PAGE / RPP;  // threads per row, rows per pass, passes
-  __shared__ float red[4];
-  __shared__ int red_bad[4];
-  __shared__ __align__(16) uint8_t stage[CACHE_PAGE][HD + 16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+__global__ __launch_bounds__(2 * HD) void k_cache_append(CacheRowsArgs a) {
+  constexpr int NW = 2 * HD / 64;
+  __shared__ uint32_t red[NW];
+  __shared__ __align__(4) int8_t row_of[CACHE_PAGE];
   const int head = blockIdx.y, which = blockIdx.z;
   const void* src = which ? a.v : a.k;
   const int64_t ld = which ? a.ldv : a.ldk;
-  const int64_t n_slots = (int64_t)a.c.n_pages * CACHE_PAGE;
+  const BlockPart<HD> my(which);
   const int w0 = blockIdx.x * a.window;
-  for (int r0 = w0; r0 < min(w0 + a.window, a.n_rows); ++r0) {
-    const int64_t first = a.slots[r0];
-    if (first < 0 || first >= n_slots) continue;
-    const int64_t page = first / CACHE_PAGE;
-    if (r0 > 0) {
-      const int64_t prev = a.slots[r0 - 1];
-      if (prev >= 0 && prev < n_slots && prev / CACHE_PAGE == page) continue;  // inside a run
-    }
-    // lane i holds the place of the run's row i
-    const int64_t mine = r0 + lane < a.n_rows ? a.slots[r0 + lane] : -1;
-    const bool in = mine >= 0 && mine < n_slots && mine / CACHE_PAGE == page;
-    const uint64_t mask = __ballot(in);
-    const int n = ~mask ? __ffsll((unsigned long long)~mask) - 1 : 64;
-    const int off = lane < n ? (int)(mine % CACHE_PAGE) : -1;
-    const bool fresh = __ballot(off == 0) != 0;
-    uint32_t* word = a.c.words + (page * a.c.nkv + head) * 2 + which;
+  Rows<false> rows(a, w0);
+  for (uint64_t left = rows.leaders(a.window); left; left &= left - 1) {
+    const int r0 = w0 + __ffsll((unsigned long long)left) - 1;
+    if (r0 > w0) rows.load(r0);
+    int64_t page;
+    int place;
+    const int n = rows.run(page, place);
+    const int64_t block = page * a.c.nkv + head;
+    const bool fresh = __ballot(place == 0) != 0;
+    uint32_t* word = a.c.words + block * 2 + which;
     const uint32_t old = *word;
+    place_rows(row_of, n, place);
     // this thread's pieces of the rows, their largest finite magnitude
-    const int part = tid % TPR;
-    float x[NP][8];
-    float amax = 0.f;
-    bool bad = false;
+    Eight<DT> x[4];
+    uint32_t in = 0;   // which of the four tokens the run has
+    uint32_t most = 0;
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      const int r = p * RPP + tid / TPR;
-      if (r < n) {
-        row8<DT>(src, (r0 + r) * ld + head * HD + part * 8, x[p]);
+    for (int p = 0; p < 4; ++p) {
+      const int r = row_of[4 * my.g + p];
+      x[p].zero();
+      if (r >= 0) {
+        in |= 1u << p;
+        x[p].load(src, (r0 + r) * ld + head * HD + my.c * 8);
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < 4; ++p) most = x[p].most(most);
+    most = block_most<NW>(most, red);
+    const bool bad = most >= 0x7F800000u;
+    if (__builtin_expect(bad, 0)) {   // of the finite ones
+      most = 0;
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float m = fabsf(x[p][e]);
-          if (m < INFINITY) amax = fmaxf(amax, m); else bad = true;
+          const uint32_t m = __float_as_uint(x[p][e]) & 0x7FFFFFFF;
+          most = m < 0x7F800000u ? max(most, m) : most;
         }
-      }
+      most = block_most<NW>(most, red);
     }
-    amax = wave_max(amax);
-    bad = __ballot(bad) != 0;
-    __syncthreads();
-    if (lane == 0) {
-      red[wave] = amax;
-      red_bad[wave] = bad;
-    }
-    __syncthreads();
-    amax = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    bad = red_bad[0] | red_bad[1] | red_bad[2] | red_bad[3];
+    const float amax = __uint_as_float(most);
     const int e_old = max((int)(old & 255) - 127, CACHE_E_MIN), e_new = block_exponent(amax);
     const int e = fresh ? e_new : max(e_old, e_new);
-    uint8_t* codes = (which ? a.c.v : a.c.k) + (page * a.c.nkv + head) * (size_t)(CACHE_PAGE * HD);
-    if (!fresh && e > e_old) {
+    const bool grew = !fresh && e > e_old;
+    uint8_t* codes = (which ? a.c.v : a.c.k) + block * (size_t)(CACHE_PAGE * HD);
+    if (in || grew) {
+      if (!which) {
 #pragma unroll
-      for (int i = tid * 16; i < CACHE_PAGE * HD; i += 256 * 16) *(uint4*)(codes + i) = rescale16(ld16(codes + i), e_old - e);
-    }
+        for (int p = 0; p < 4; ++p) {
+          uint2* at = (uint2*)(codes + (4 * my.g + p) * HD + my.c * 8);
+          if (in >> p & 1) {
+            *at = make_uint2(encode4(to_scale(x[p][0], e), to_scale(x[p][1], e), to_scale(x[p][2], e), to_scale(x[p][3], e)),
+                             encode4(to_scale(x[p][4], e), to_scale(x[p][5], e), to_scale(x[p][6], e), to_scale(x[p][7], e)));
+          } else if (grew) {
+            const uint2 c = *at;
+            *at = make_uint2(rescale4(c.x, e_old - e), rescale4(c.y, e_old - e));
+          }
+        }
+      } else {
+        uint32_t had[8], keep = 0;   // bytes of the tokens that the run does not have
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      const int r = p * RPP + tid / TPR;
-      const int o = __shfl(off, r & 63);
-      if (r < n) {
-        const uint2 c = make_uint2(encode4(to_scale(x[p][0], e), to_scale(x[p][1], e), to_scale(x[p][2], e), to_scale(x[p][3], e)),
-                                   encode4(to_scale(x[p][4], e), to_scale(x[p][5], e), to_scale(x[p][6], e), to_scale(x[p][7], e)));
-        *(uint2*)&stage[o][part * 8] = c;
-      }
-    }
-    __syncthreads();  // (the re-scaled codes are written, too)
-    uint64_t have = 0;   // tokens of the page that the run holds
-    for (int i = 0; i < n; ++i) have |= 1ull << __shfl(off, i);
-    if (!which) {
-      for (int i = tid; i < CACHE_PAGE * HD / 16; i += 256) {
-        const int t = i / (HD / 16), d = i % (HD / 16) * 16;
-        if (have >> t & 1) *(uint4*)(codes + t * HD + d) = *(const uint4*)&stage[t][d];
-      }
-    } else {
-      for (int i = tid; i < CACHE_PAGE * HD / 16; i += 256) {
-        const int d = i / 4, t0 = i % 4 * 16;
-        const uint32_t h = (uint32_t)(have >> t0) & 0xFFFF;
-        if (h == 0xFFFF) {
-          uint32_t w[4];
+        for (int p = 0; p < 4; ++p) keep |= in >> p & 1 ? 0u : 0xFFu << (8 * p);
+        uint32_t* at = (uint32_t*)(codes + my.c * 8 * CACHE_PAGE) + my.g;
+        if (grew && keep)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            w[j] = stage[t0 + 4 * j][d] | stage[t0 + 4 * j + 1][d] << 8 | stage[t0 + 4 * j + 2][d] << 16 | (uint32_t)stage[t0 + 4 * j + 3][d] << 24;
-          *(uint4*)(codes + d * CACHE_PAGE + t0) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else if (h) {
-          for (int j = 0; j < 16; ++j)
-            if (h >> j & 1) codes[d * CACHE_PAGE + t0 + j] = stage[t0 + j][d];
+          for (int d = 0; d < 8; ++d) had[d] = at[d * (CACHE_PAGE / 4)];
+        uint32_t w[8];
+#pragma unroll
+        for (int d = 0; d < 8; ++d) w[d] = encode4(to_scale(x[0][d], e), to_scale(x[1][d], e), to_scale(x[2][d], e), to_scale(x[3][d], e));
+        if (grew && keep)
+#pragma unroll
+          for (int d = 0; d < 8; ++d) w[d] = (w[d] & ~keep) | (rescale4(had[d], e_old - e) & keep);
+        if (grew || !keep) {
+#pragma unroll
+          for (int d = 0; d < 8; ++d) at[d * (CACHE_PAGE / 4)] = w[d];
+        } else {
+#pragma unroll
+          for (int p = 0; p < 4; ++p)
+            if (in >> p & 1)
+#pragma unroll
+              for (int d = 0; d < 8; ++d) ((uint8_t*)(at + d * (CACHE_PAGE / 4)))[p] = (uint8_t)(w[d] >> (8 * p));
         }
       }
     }
-    if (tid == 0) *word = (uint32_t)(e + 127) | (bad || (!fresh && (old & CACHE_NAN)) ? CACHE_NAN : 0);
+    if (threadIdx.x == 0) *word = (uint32_t)(e + 127) | (bad || (!fresh && (old & CACHE_NAN)) ? CACHE_NAN : 0);
     __syncthreads();
   }
 }
 
 // ---- read-back ----------------------------------------------------------------------
 
-template <int DT, int HD>
-__global__ __launch_bounds__(256) void k_cache_read(CacheRowsArgs a) {
-  constexpr int TPR = HD / 8;
-  const int head = blockIdx.y;
-  const int r = blockIdx.x * (256 / TPR) + threadIdx.x / TPR, part = threadIdx.x % TPR;
-  if (r >= a.n_rows) return;
-  const int64_t slot = a.slots[r];
-  if (slot < 0 || slot >= (int64_t)a.c.n_pages * CACHE_PAGE) return;
-  const int64_t block = slot / CACHE_PAGE * a.c.nkv + head;
-  const int t = (int)(slot % CACHE_PAGE);
-  const uint2 words = *(const uint2*)(a.c.words + block * 2);
-  const int ek = (int)(words.x & 255) - 127, ev = (int)(words.y & 255) - 127;
-  const uint2 kc = *(const uint2*)(a.c.k + block * (size_t)(CACHE_PAGE * HD) + t * HD + part * 8);
-  const uint8_t* vp = a.c.v + block * (size_t)(CACHE_PAGE * HD) + part * 8 * CACHE_PAGE + t;
-  uint32_t vc[2];
+// Byte I of a dword as the value of its code times 2^e.
+template <int I> __device__ __forceinline__ float value_of(uint32_t w, int e) { return scale_by(decode1<I>(w), e); }
+
+// A thread's four tokens and eight dims of a page's block, to their rows (r: the
+// run's row of each token, -1 none).
+template <int DT, int HD, bool VALUES>
+__device__ __forceinline__ void read_part(const uint8_t* codes, const BlockPart<HD>& my, const int (&r)[4], int e, uint8_t* dst, int64_t pitch) {
+  float x[4][8];
+  if (VALUES) {
+    uint32_t w[8];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    vc[i] = vp[(4 * i) * CACHE_PAGE] | vp[(4 * i + 1) * CACHE_PAGE] << 8 | vp[(4 * i + 2) * CACHE_PAGE] << 16 |
-            (uint32_t)vp[(4 * i + 3) * CACHE_PAGE] << 24;
+    for (int d = 0; d < 8; ++d) w[d] = *((const uint32_t*)(codes + (my.c * 8 + d) * CACHE_PAGE) + my.g);
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    const uint32_t lo = which ? vc[0] : kc.x, hi = which ? vc[1] : kc.y;
-    const int e = which ? ev : ek;
-    const float4 x = make_float4(scale_by(decode1<0>(lo), e), scale_by(decode1<1>(lo), e), scale_by(decode1<2>(lo), e), scale_by(decode1<3>(lo), e));
-    const float4 y = make_float4(scale_by(decode1<0>(hi), e), scale_by(decode1<1>(hi), e), scale_by(decode1<2>(hi), e), scale_by(decode1<3>(hi), e));
-    uint8_t* dst = (uint8_t*)(which ? a.v : a.k) + (r * (which ? a.ldv : a.ldk) + head * HD) * Elem<DT>::ES_;
-    store4<DT>(dst, part * 8, x);
-    store4<DT>(dst, part * 8 + 4, y);
+    for (int d = 0; d < 8; ++d) {
+      x[0][d] = value_of<0>(w[d], e);
+      x[1][d] = value_of<1>(w[d], e);
+      x[2][d] = value_of<2>(w[d], e);
+      x[3][d] = value_of<3>(w[d], e);
+    }
+  } else {
+    uint2 w[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) w[p] = *(const uint2*)(codes + (4 * my.g + p) * HD + my.c * 8);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      x[p][0] = value_of<0>(w[p].x, e); x[p][1] = value_of<1>(w[p].x, e); x[p][2] = value_of<2>(w[p].x, e); x[p][3] = value_of<3>(w[p].x, e);
+      x[p][4] = value_of<0>(w[p].y, e); x[p][5] = value_of<1>(w[p].y, e); x[p][6] = value_of<2>(w[p].y, e); x[p][7] = value_of<3>(w[p].y, e);
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    if (r[p] < 0) continue;
+    uint8_t* at = dst + r[p] * pitch + my.c * 8 * Elem<DT>::ES_;
+    if (DT == 1) {
+      *(uint4*)at = make_uint4(f32_to_bf16x2(x[p][0], x[p][1]), f32_to_bf16x2(x[p][2], x[p][3]), f32_to_bf16x2(x[p][4], x[p][5]),
+                               f32_to_bf16x2(x[p][6], x[p][7]));
+    } else {
+      *(float4*)at = make_float4(x[p][0], x[p][1], x[p][2], x[p][3]);
+      *(float4*)(at + 16) = make_float4(x[p][4], x[p][5], x[p][6], x[p][7]);
+    }
   }
 }
 
-template <int DT>
-static hipError_t append_hd(const CacheRowsArgs& a, hipStream_t s) {
+// Runs as those of an append (of rising places), values the other way.
+template <int DT, int HD>
+__global__ __launch_bounds__(2 * HD) void k_cache_read(CacheRowsArgs a) {
+  __shared__ __align__(4) int8_t row_of[CACHE_PAGE];
+  const int head = blockIdx.y, which = blockIdx.z;
+  const int64_t ld = which ? a.ldv : a.ldk;
+  const BlockPart<HD> my(which);
+  const int w0 = blockIdx.x * a.window;
+  Rows<true> rows(a, w0);
+  for (uint64_t left = rows.leaders(a.window); left; left &= left - 1) {
+    const int r0 = w0 + __ffsll((unsigned long long)left) - 1;
+    if (r0 > w0) rows.load(r0);
+    int64_t page;
+    int place;
+    const int n = rows.run(page, place);
+    const int64_t block = page * a.c.nkv + head;
+    const int e = (int)(a.c.words[block * 2 + which] & 255) - 127;
+    place_rows(row_of, n, place);
+    int r[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) r[p] = row_of[4 * my.g + p];
+    if (max(max(r[0], r[1]), max(r[2], r[3])) >= 0) {
+      const uint8_t* codes = (which ? a.c.v : a.c.k) + block * (size_t)(CACHE_PAGE * HD);
+      uint8_t* dst = (uint8_t*)(which ? a.v : a.k) + (r0 * ld + head * HD) * Elem<DT>::ES_;
+      if (which) read_part<DT, HD, true>(codes, my, r, e, dst, ld * Elem<DT>::ES_);
+      else read_part<DT, HD, false>(codes, my, r, e, dst, ld * Elem<DT>::ES_);
+    }
+    __syncthreads();
+  }
+}
+
+template <int DT, bool APPEND>
+static hipError_t rows_hd(const CacheRowsArgs& a, hipStream_t s) {
   const dim3 grid((a.n_rows + a.window - 1) / a.window, a.c.nkv, 2);
-  if (a.c.hd == 128) k_cache_append<DT, 128><<<grid, 256, 0, s>>>(a);
-  else k_cache_append<DT, 64><<<grid, 256, 0, s>>>(a);
+  if (APPEND) {
+    if (a.c.hd == 128) k_cache_append<DT, 128><<<grid, 256, 0, s>>>(a);
+    else k_cache_append<DT, 64><<<grid, 128, 0, s>>>(a);
+  } else {
+    if (a.c.hd == 128) k_cache_read<DT, 128><<<grid, 256, 0, s>>>(a);
+    else k_cache_read<DT, 64><<<grid, 128, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 hipError_t launch_cache_append(int dtype, const CacheRowsArgs& a, hipStream_t s) {
-  return dtype ? append_hd<1>(a, s) : append_hd<0>(a, s);
-}
-
-template <int DT>
-static hipError_t read_hd(const CacheRowsArgs& a, hipStream_t s) {
-  const int rpb = 256 / (a.c.hd / 8);
-  const dim3 grid((a.n_rows + rpb - 1) / rpb, a.c.nkv);
-  if (a.c.hd == 128) k_cache_read<DT, 128><<<grid, 256, 0, s>>>(a);
-  else k_cache_read<DT, 64><<<grid, 256, 0, s>>>(a);
-  return hipGetLastError();
+  return dtype ? rows_hd<1, true>(a, s) : rows_hd<0, true>(a, s);
 }
 hipError_t launch_cache_read(int dtype, const CacheRowsArgs& a, hipStream_t s) {
-  return dtype ? read_hd<1>(a, s) : read_hd<0>(a, s);
+  return dtype ? rows_hd<1, false>(a, s) : rows_hd<0, false>(a, s);
 }
 
 }  // namespace lede
