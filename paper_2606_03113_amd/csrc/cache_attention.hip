@@ -356,7 +356,7 @@ __device__ __forceinline__ void put4(const CacheAttnArgs& a, const AttnSeq& q, i
 // barrier), the next page's requested as soon as this one's are used.  The
 // waves meet in LDS once, at the end.
 template <int DT, int HD>
-__global__ __launch_bounds__(256, DT ? 2 : 1) void k_cache_attn(CacheAttnArgs a) {
+__global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
   constexpr int NT = 1;
   typedef Tiles<DT, HD, NT> T;
   constexpr int KH = T::KH, ND = T::ND;
@@ -476,7 +476,7 @@ __global__ __launch_bounds__(256, DT ? 2 : 1) void k_cache_attn(CacheAttnArgs a)
 // conflict either way), so that each wave converts a quarter of the codes;
 // two pages' room, so one barrier a page.
 template <int DT, int HD, int NT>
-__global__ __launch_bounds__(256, DT ? 2 : 1) void k_cache_attn_rows(CacheAttnArgs a) {
+__global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
   typedef Tiles<DT, HD, NT> T;
   constexpr int KH = T::KH, ND = T::ND, VW = ND / 4;
   __shared__ uint4 sk[2][8 * KH][64], sv[2][2 * ND][64];
@@ -575,14 +575,14 @@ __global__ __launch_bounds__(256, DT ? 2 : 1) void k_cache_attn_rows(CacheAttnAr
   }
 }
 
-// The splits of a row of a split task joined in order: a wave each, lanes over
-// the dims, B splits requested at a time.
+// The splits of a row of a cut task joined in order: HD / 4 lanes a row, four
+// dims each, B splits requested at a time.
 template <int DT, int HD, int B>
 __global__ __launch_bounds__(256) void k_cache_attn_join(CacheAttnArgs a) {
-  constexpr int DL = HD / 64;
-  const int l = threadIdx.x & 63;
+  constexpr int LANES = HD / 4, ROWS = 256 / LANES;
+  const int d = threadIdx.x % LANES * 4;
   const int G = a.nq / a.c.nkv;
-  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < (int64_t)a.n_cut * a.tile_rows; i += (int64_t)gridDim.x * 4) {
+  for (int64_t i = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; i < (int64_t)a.n_cut * a.tile_rows; i += (int64_t)gridDim.x * ROWS) {
     const int slot = (int)(i / a.tile_rows), r = (int)(i % a.tile_rows);
     const Task t = attn_task(a, a.n_full + slot * a.n_split);
     const AttnSeq q = attn_seq(a, t.s);
@@ -591,45 +591,39 @@ __global__ __launch_bounds__(256) void k_cache_attn_join(CacheAttnArgs a) {
     const int pos_top = q.len - q.n + (min(r0 + a.tile_rows, R) - 1) / G;
     const int pages = pos_top < 0 ? 0 : pos_top / CACHE_PAGE + 1, chunk = split_chunk(a, a.n_split, pages);
     if (chunk >= pages) continue;
-    const int m = ri / G, head = t.kvh * G + (ri - m * G), pos = q.len - q.n + m;
-    const int64_t row = q.row0 + m;
+    const int pos = q.len - q.n + ri / G;
     const int n = pos < 0 ? 0 : pos / CACHE_PAGE / chunk + 1;
     const float* p = part_of<HD>(a, slot, 0, r);
     const int64_t pitch = (int64_t)a.tile_rows * (HD + 4);
-    float mx = B_NONE, sum = 0.f, acc[DL];
-#pragma unroll
-    for (int d = 0; d < DL; ++d) acc[d] = 0.f;
+    float b = B_NONE, sum = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int j0 = 0; j0 < n; j0 += B) {
-      float pm[B], pl[B], pa[B][DL];
+      float2 bs[B];
+      f32x4 pa[B];
 #pragma unroll
       for (int u = 0; u < B; ++u) {
         const float* x = p + min(j0 + u, n - 1) * pitch;
-        const float2 ml = *(const float2*)(x + HD);
-        pm[u] = j0 + u < n ? ml.x : B_NONE;
-        pl[u] = ml.y;
-#pragma unroll
-        for (int d = 0; d < DL; ++d) pa[u][d] = x[l * DL + d];
+        bs[u] = *(const float2*)(x + HD);
+        pa[u] = *(const f32x4*)(x + d);
       }
-      float nm = mx;
+      float nb = b;
 #pragma unroll
-      for (int u = 0; u < B; ++u) nm = fmaxf(nm, pm[u]);
-      const float f0 = __builtin_amdgcn_exp2f(mx - nm);
+      for (int u = 0; u < B; ++u) nb = fmaxf(nb, j0 + u < n ? bs[u].x : B_NONE);
+      const float f0 = __builtin_amdgcn_exp2f(b - nb);
       sum *= f0;
 #pragma unroll
-      for (int d = 0; d < DL; ++d) acc[d] *= f0;
+      for (int e = 0; e < 4; ++e) acc[e] *= f0;
 #pragma unroll
       for (int u = 0; u < B; ++u) {
-        const float f = __builtin_amdgcn_exp2f(pm[u] - nm);
         const bool live = j0 + u < n;
-        sum = live ? fmaf(pl[u], f, sum) : sum;
+        const float f = __builtin_amdgcn_exp2f(bs[u].x - nb);
+        sum = live ? fmaf(bs[u].y, f, sum) : sum;
 #pragma unroll
-        for (int d = 0; d < DL; ++d) acc[d] = live ? fmaf(pa[u][d], f, acc[d]) : acc[d];
+        for (int e = 0; e < 4; ++e) acc[e] = live ? fmaf(pa[u][e], f, acc[e]) : acc[e];
       }
-      mx = nm;
+      b = nb;
     }
-    const float inv = n == 0 ? 0.f : ldexpf(1.f / sum, -SUM_DOWN);
-#pragma unroll
-    for (int d = 0; d < DL; ++d) Elem<DT>::store(a.out, row * a.ldo + head * HD + l * DL + d, acc[d] * inv);
+    put4<DT, HD>(a, q, t.kvh, G, ri, d, nullptr, acc, b, sum);
   }
 }
 
@@ -641,7 +635,8 @@ static hipError_t attention_hd(const CacheAttnArgs& a, hipStream_t s) {
   else if constexpr (DT == 1) k_cache_attn_rows<DT, HD, 2><<<blocks, 256, 0, s>>>(a);
   if (a.n_cut > 0) {
     const int64_t rows = (int64_t)a.n_cut * a.tile_rows;
-    const unsigned grid = (unsigned)(rows / 4 < 16384 ? rows / 4 : 16384);
+    const int64_t need = rows * (HD / 4) / 256;
+    const unsigned grid = (unsigned)(need < 16384 ? need : 16384);
     if (a.n_split <= 2) k_cache_attn_join<DT, HD, 2><<<grid, 256, 0, s>>>(a);
     else if (a.n_split <= 4) k_cache_attn_join<DT, HD, 4><<<grid, 256, 0, s>>>(a);
     else k_cache_attn_join<DT, HD, 16><<<grid, 256, 0, s>>>(a);
