@@ -598,8 +598,8 @@ size_t lede_op_cache_bytes(int32_t n_pages, int32_t n_kv_heads, int32_t head_dim
  *              -1.  free_head may be status + 2.
  * Errors of the lengths are found on the device: LEDE_E_ARG (a negative
  * length, held outside [pages of seq_lens, table_ld], free_head outside [0,
- * n_free], more rows than max_rows), LEDE_E_CTX_OVERFLOW (table_ld pages do
- * not hold the sequence), LEDE_E_KV_FULL (no page left).  Then nothing is
+ * n_free], more rows than max_rows), LEDE_E_CTX_OVERFLOW (table_ld pages or
+ * 2^31 - 1 tokens do not hold the sequence), LEDE_E_KV_FULL (no page left).  Then nothing is
  * taken: kv_lens = seq_lens, held_out = held, status[2] = *free_head, every
  * row_start is 0 and every slot -1, so that the pass behind it has no rows.
  * Returns LEDE_E_ARG on null pointers (free_pages may be null with n_free =

@@ -182,9 +182,9 @@ int lede_op_logprobs(int32_t dtype, const void* logits, int64_t ld, int32_t n_ro
   if (V > MOST_VOCAB || n_top > MOST_TOP) return LEDE_E_UNSUPPORTED;
   const float c = (float)(1.4426950408889634 / temperature);
   if (!std::isfinite(c)) return LEDE_E_ARG;
+  if (n_rows == 0) return LEDE_OK;
   if ((logprobs || ranks) && !tokens) return LEDE_E_ARG;
   if (n_top && (!top_ids || !top_logprobs)) return LEDE_E_ARG;
-  if (n_rows == 0) return LEDE_OK;
   if (!logits || !aligned(logits, es_of(dtype))) return LEDE_E_ARG;
   const size_t need = lede_op_logprobs_bytes(n_rows, V, n_top);
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return LEDE_E_ARG;

@@ -51,7 +51,7 @@ __device__ __forceinline__ PlanAsk plan_ask(const CachePlanArgs& a, int s) {
   r.fresh = a.new_lens[s];
   r.held = a.held[s];
   if (r.seq < 0 || r.fresh < 0 || r.held < 0 || r.held > a.table_ld || pages_of(r.seq) > r.held) r.code = LEDE_E_ARG;
-  else if (pages_of((int64_t)r.seq + r.fresh) > a.table_ld) r.code = LEDE_E_CTX_OVERFLOW;
+  else if ((int64_t)r.seq + r.fresh > INT32_MAX || pages_of((int64_t)r.seq + r.fresh) > a.table_ld) r.code = LEDE_E_CTX_OVERFLOW;
   else r.need = max(0, pages_of((int64_t)r.seq + r.fresh) - r.held);
   if (r.code) r.fresh = 0;
   return r;

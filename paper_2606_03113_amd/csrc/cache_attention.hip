@@ -24,11 +24,17 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // far, and follows it only when some x passes P_LIM: until then neither the
 // accumulators nor the maximum across lanes are touched.  The weights enter
 // the product in fp16: 11 bits for bf16 outputs, whose own half step is 8
-// times larger, and a high and a low part, 22 bits, for fp32; between 2^P_LIM
-// and 2^-14 they are normal numbers.  The sum of 2^(x - E_v) is kept in fp32
-// at 2^-SUM_DOWN, which holds every scale's range.
-constexpr int P_UP = 8, P_LIM = 15, SUM_DOWN = 10;
+// times larger, and a high and a low part, 22 bits, for fp32.  Below 2^-14
+// they lose bits, below 2^-25 they vanish: 2^-33 (bf16) or 2^-38 (fp32) of
+// the largest term, from a million tokens together less than the rounding of
+// the output.  The sum of 2^(x - E_v) is kept in fp32 at 2^-SUM_DOWN, which
+// holds every scale's range.
+constexpr int P_LIM = 15, SUM_DOWN = 10;
 constexpr float B_NONE = -1e30f;   // B of a row that has seen nothing
+// From scores of 2^22 on, where fp32 has no room for B's whole part, the
+// multiply and the add are rounded one by one, so that the largest score
+// itself comes out as it went into B.
+constexpr float B_FAR = 4194304.f;
 
 // Token of a page that row `r` of its score tile `t` (16 tokens x 16 queries)
 // holds.  A lane then has, of its query, the scores of 16 consecutive tokens
@@ -121,6 +127,7 @@ struct Tiles {
   static constexpr int ND = HD / 16;      // 16-dim output tiles
   static constexpr int NQ = DT ? 1 : 3;   // bf16 parts of q
   static constexpr int NP = DT ? 1 : 2;   // fp16 parts of the weights
+  static constexpr int P_UP = DT ? 8 : 13;
   uint4 qf[NT][NQ][KH][2];
   f32x4 o[NT][ND];
   float sum[NT], base[NT];
@@ -186,6 +193,7 @@ struct Tiles {
 #pragma unroll
       for (int t = 0; t < 4; ++t) x[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     uint4 cur[2] = {kf(0, 0, 0), kf(1, 0, 0)};
+    __builtin_amdgcn_s_setprio(1);   // a wave in its products goes first; the SIMD's other has its exponentials (3%)
 #pragma unroll
     for (int i = 0; i < 4 * KH; ++i) {
       const int t = i / (2 * KH) * 2, h = i / 2 % KH, half = i & 1;
@@ -208,14 +216,16 @@ struct Tiles {
       cur[1] = nxt[1];
       if (NT > 1) __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
     after_keys();
     const bool edge = !known || t0 + CACHE_PAGE - 1 > pos_lo;
     uint4 pf[NT][NP][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const float up = (float)(ev + P_UP) - base[n];
+      const bool far = __ballot(fabsf(up) > B_FAR) != 0;
       float m = -INFINITY, kx = ks;   // x = kx x' + up
-      if (edge) {
+      if (edge || far) {
         // a table entry outside the pool: rows that see the page become NaN
         kx = 1.f;
 #pragma unroll
@@ -234,7 +244,8 @@ struct Tiles {
         // the row's new B, the same in its four lanes
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
-        const float b = m + up > P_LIM ? ceilf(m + ev) : base[n], f = __builtin_amdgcn_exp2f(base[n] - b);
+        const float b = !(m + up > P_LIM) ? base[n] : fabsf(m) < B_FAR ? ceilf(m + ev) : m + (float)(ev + P_UP);
+        const float f = __builtin_amdgcn_exp2f(base[n] - b);
         base[n] = b;
         off = (float)(ev + P_UP) - b;
         sum[n] *= f;
@@ -242,6 +253,17 @@ struct Tiles {
         for (int d = 0; d < ND; ++d)
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[n][d][i] *= f;
+        if (__ballot(fabsf(off) > B_FAR)) {   // a step of such scores may be more than P_LIM
+          const float most = P_LIM - off;
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float y = x[n][t][i] * kx;
+              x[n][t][i] = y > most ? most : y;
+            }
+          kx = 1.f;
+        }
       }
       float ps = 0.f;
 #pragma unroll
@@ -272,6 +294,7 @@ struct Tiles {
         }
       sum[n] = fmaf(ps, ldexpf(1.f, -ev - SUM_DOWN), sum[n]);
     }
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
       const int d = i / 2 * 2, half = i & 1;
@@ -290,6 +313,7 @@ struct Tiles {
       cur[1] = nxt[1];
       if (NT > 1) __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
   }
 
   // A page with NaN values: they reach the rows that see their tokens, and no

@@ -333,6 +333,96 @@ def test_attention_peaked_flat_and_scaled(dtype):
         _attend(cache, model, tables, lens, new, 4, dtype, r, scale=scale, q=q)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 70])
+def test_attention_many_small_weights(dtype, rows):
+    """One token with most of the weight, and thousands whose weights are below fp16's normal range beside it."""
+    m = lede()
+    r = np.random.default_rng(rows)
+    kv, hd, length = 1, 64, 6000
+    cache, model = m.Cache(length // 64 + 1, kv, hd), ref.CacheModel(length // 64 + 1, kv, hd)
+    for gap in (12, 17, 20, 24):      # nats below the first token: e^-17 = 2^-24.5
+        x = np.zeros((length, 2, kv, hd))
+        x[:, 0, :, 0] = -gap
+        x[:rows, 0, :, 0] = 0.0       # (every row sees one)
+        x[:, 1] = 1.0 + r.random((length, kv, hd))
+        d, val = rounded(x, "bf16")
+        m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(np.arange(length)))
+        model = ref.CacheModel(length // 64 + 1, kv, hd)
+        model.append(val[:, 0], val[:, 1], np.arange(length))
+        q = np.zeros((rows + 2, 2, hd))
+        q[:, :, 0] = 1.0
+        _attend(cache, model, np.arange(length // 64 + 1, dtype=np.int32)[None], [length], [rows], 2, dtype, r, scale=1.0, q=q)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [2, 70])
+def test_attention_huge_scores(dtype, rows):
+    """Scores far beyond fp32's whole numbers: the largest one's value, to the output's rounding."""
+    m = lede()
+    kv, hd, length = 1, 64, 300
+    r = np.random.default_rng(rows)
+    cache, model = m.Cache(5, kv, hd), ref.CacheModel(5, kv, hd)
+    x = np.zeros((length, 2, kv, hd))
+    x[:, 0, 0, 0] = 1.0 + np.arange(length) % 7 / 8        # distinct sizes; the largest is one token's
+    best = 150
+    x[best, 0, 0, 0] = 4.0
+    x[:, 1] = r.standard_normal((length, kv, hd)) * np.exp2(np.arange(length) // 64 * 3)[:, None, None]   # blocks of several scales
+    d, val = rounded(x, "bf16")
+    m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(np.arange(length)))
+    model.append(val[:, 0], val[:, 1], np.arange(length))
+    value = model.read([best])[1][0, 0]
+    table = np.arange(5, dtype=np.int32)[None]
+    for size in (3e3, 1e6, 3e7, 1e8, 3e8, 1e9, 1e11, 1e20, 1e30):
+        q = np.zeros((rows, 1, hd), np.float32)
+        q[:, 0, 0] = size
+        got = m.op_cache_attention(cache, rounded(q, dtype)[0], gpu(table), i32([length]), i32([0, rows]), rows, length, scale=1.0)
+        got = got.double().cpu().numpy()
+        assert (np.abs(got - value) <= ref.HALF_STEP[dtype] * 2 * np.abs(value)).all(), size
+        # the other way, the largest scores are the most negative ones' opposites
+        got = m.op_cache_attention(cache, rounded(-q, dtype)[0], gpu(table), i32([length]), i32([0, rows]), rows, length, scale=-1.0)
+        assert (np.abs(got.double().cpu().numpy() - value) <= ref.HALF_STEP[dtype] * 2 * np.abs(value)).all(), size
+
+
+@pytest.mark.parametrize("dtype,seqs,nq,kv,new", [("bf16", 131, 4, 4, 1), ("f32", 200, 3, 3, 2), ("bf16", 9, 60, 60, 70), ("bf16", 70, 8, 8, 9), ("f32", 70, 8, 8, 17),
+                                                  ("bf16", 3, 60, 60, 400)])
+def test_attention_more_tasks_than_a_round(dtype, seqs, nq, kv, new):
+    """Whole rounds of blocks and a cut rest, few and many rows."""
+    say("attention tasks", dtype, seqs, nq, kv, new)
+    r = np.random.default_rng(seqs)
+    lens = [int(x) for x in r.integers(new, new + (900 if seqs < 10 else 400), seqs)]
+    news = [int(x) for x in r.integers(max(1, new - 3), new + 1, seqs)]
+    cache, model, tables = _fill(kv, 64, lens, r)
+    m = lede()
+    assert m.load().lede_op_cache_attention_bytes(int(dtype == "bf16"), seqs, sum(news), nq, kv, 64, max(news), max(lens)) > 0
+    start = np.concatenate([[0], np.cumsum(news)])
+    d, val = rounded(r.standard_normal((int(start[-1]), nq, 64)), dtype)
+    got = m.op_cache_attention(cache, d, gpu(tables), i32(lens), i32(start), max(news), max(lens)).double().cpu().numpy()
+    for s in np.unique(np.concatenate([[0, seqs - 1], r.integers(0, seqs, 12)])):     # some of them: the reference takes its time
+        rows = np.unique(np.concatenate([[start[s], start[s + 1] - 1], r.integers(start[s], start[s + 1], 6)]))
+        heads = np.unique(r.integers(0, nq, 5))
+        k, v = model.sequence(tables[s], lens[s])
+        for row in rows:
+            seen = lens[s] - (start[s + 1] - row) + 1
+            for h in heads:
+                z = 0.125 * (k[:seen, h // (nq // kv)] @ val[row, h])
+                w = np.exp(z - z.max())
+                w /= w.sum()
+                want = w @ v[:seen, h // (nq // kv)]
+                eps = 2.0 ** -23 * (200 * 0.125 * (np.abs(k[:seen, h // (nq // kv)]) @ np.abs(val[row, h])).max() + 200) + (2.0 ** -12 if dtype == "bf16" else 2.0 ** -22)
+                tol = 2 * eps * (w @ np.abs(v[:seen, h // (nq // kv)])) + ref.HALF_STEP[dtype] * np.abs(want) * (1 + 2 ** -6)
+                assert (np.abs(got[row, h] - want) <= tol).all(), (s, row, h)
+
+
+def test_attention_one_long_sequence_among_short_ones():
+    """Contexts of which one is far longer: its pages are spread over many blocks, the others are whole."""
+    r = np.random.default_rng(21)
+    lens, new = [20000, 64, 700, 1, 129], [1, 1, 1, 1, 1]
+    cache, model, tables = _fill(2, 64, lens, r)
+    for dtype in ("bf16", "f32"):
+        _attend(cache, model, tables, lens, new, 4, dtype, r)
+
+
 def test_attention_blocks_of_different_scale():
     """Pages whose values differ by 2^60: a row that attends to the small one alone sees its own precision."""
     m = lede()
@@ -522,6 +612,43 @@ def test_logprobs_ties_masks_and_what_is_not_finite(dtype):
     _score(z, tokens, 32, 1.0, dtype)
     _score(z, [V, -1, 17, -5, 99, 5, 5, 5, 0, 8999, 50, 0, 0, 8200], 3, 0.7, dtype)
     _score(z[:, :200], None, 20, 1.0, dtype)
+
+
+def test_logprobs_largest_vocabulary():
+    """The most entries and top tokens that are taken: rows of random logits, of equal ones, and with a mask of all but a few."""
+    V = 1 << 20
+    r = np.random.default_rng(6)
+    z = r.standard_normal((3, V))
+    z[1] = -1.25
+    z[2] = -np.inf
+    z[2, [5, 70000, V - 1]] = [1.0, 2.0, 1.0]
+    _score(z, [V - 1, 12345, 70000], 32, 1.0, "bf16")
+    _score(z, [0, V - 1, 5], 7, 0.8, "f32")
+
+
+def test_logprobs_rising_rows():
+    """Logits that rise or fall along the row: every tile holds larger ones than those before."""
+    V = 30000
+    z = np.stack([np.linspace(-5, 5, V), np.linspace(5, -5, V), np.sin(np.arange(V) / 300.0), np.floor(np.linspace(0, 40, V))])
+    for dtype in ("f32", "bf16"):
+        _score(z, [V - 1, V - 1, 471, 100], 32, 1.0, dtype)
+
+
+def test_logprobs_many_rows():
+    """More rows than a round of blocks, a row a block and with rows cut in parts: each against the same row alone."""
+    m = lede()
+    r = np.random.default_rng(7)
+    z = gpu(r.standard_normal((1100, 40001)).astype(np.float32) * 2)
+    tok = i32(r.integers(0, 40001, 1100))
+    all_rows, few = m.op_logprobs(z, tok, 9, 0.7), m.op_logprobs(z[300:340], tok[300:340], 9, 0.7)
+    for a, b in ((all_rows.ranks, few.ranks), (all_rows.top_ids, few.top_ids)):
+        assert torch.equal(a[300:340], b)
+    lp = torch.log_softmax(z.double() / 0.7, 1)
+    want = lp.gather(1, tok.long()[:, None])[:, 0]
+    tol = ref.score_tolerance(want.cpu().numpy(), 40001)
+    assert (np.abs(all_rows.logprobs.double().cpu().numpy() - want.cpu().numpy()) <= tol).all()
+    ids = torch.sort(z, dim=1, descending=True, stable=True).indices[:, :9]
+    assert torch.equal(all_rows.top_ids.long(), ids)
 
 
 def test_logprobs_extreme_temperatures_and_logits():
