@@ -41,7 +41,7 @@ struct AttnGrid { int tile_rows, n_tiles, n_full, n_cut, n_split, min_chunk; };
 AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32_t max_new, int32_t max_kv) {
   AttnGrid g;
   const int64_t rows = std::max<int64_t>(1, (int64_t)max_new * (nq / nkv));
-  g.tile_rows = rows <= 16 ? 16 : rows <= 64 || dtype == LEDE_DTYPE_F32 ? 64 : 128;
+  g.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || dtype == LEDE_DTYPE_F32 ? 64 : 128;
   // (a task takes every n_tiles-th tile: a grid need not grow with a large max_new)
   const int64_t groups = (int64_t)n_seqs * nkv;
   g.n_tiles = (int)std::min((rows + g.tile_rows - 1) / g.tile_rows, 65536 / groups + 1);
@@ -52,7 +52,7 @@ AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32
   // one.  Few rows behind very long contexts are cut in any case: lengths
   // differ, and one long sequence must not be a block's alone.
   constexpr int64_t ROUND = 512, LONG = 128, MOST_CUT = 4096;
-  const int64_t by_length = g.tile_rows == 16 ? (pages + LONG - 1) / LONG : 1;
+  const int64_t by_length = g.tile_rows <= 32 ? (pages + LONG - 1) / LONG : 1;
   const int64_t cut = by_length > 1 ? whole : whole % ROUND;
   int64_t split = cut ? std::max(whole < ROUND ? (ROUND + whole - 1) / whole : by_length > 1 ? 1 : ROUND / cut, by_length) : 1;
   split = std::min(split, std::max<int64_t>(1, MOST_CUT / std::max<int64_t>(cut, 1)));

@@ -120,58 +120,72 @@ __device__ __forceinline__ AttnSeq attn_seq(const CacheAttnArgs& a, int s) {
 // NT tiles of 16 query rows ((row, query head of the group) pairs of one
 // sequence and KV head), as a wave holds them.  A lane has the query lr = lane
 // % 16 of each tile, and of its outputs the dims 16 d + 4 lg .. + 3, lg = lane
-// / 16: both products' results lie so.
-template <int DT, int HD, int NT>
+// / 16: both products' results lie so.  QL: the queries' operands are in LDS,
+// for waves that share their rows.
+template <int DT, int HD, int NT, bool QL = false>
 struct Tiles {
   static constexpr int KH = HD / 64;      // 16-byte pieces of a key that a lane loads
   static constexpr int ND = HD / 16;      // 16-dim output tiles
   static constexpr int NQ = DT ? 1 : 3;   // bf16 parts of q
   static constexpr int NP = DT ? 1 : 2;   // fp16 parts of the weights
   static constexpr int P_UP = DT ? 8 : 13;
-  uint4 qf[NT][NQ][KH][2];
+  static constexpr bool PIPE = !QL;       // operands come from LDS: a step's taken while the one before is multiplied
+  uint4 qf[QL ? 1 : NT][NQ][KH][2];
+  const uint4 (*ql)[NQ][KH][2][64];   // [NT]
   f32x4 o[NT][ND];
   float sum[NT], base[NT];
-  int pos[NT];
+  int pos[QL ? 1 : NT];
+  const int (*pl)[16];                // [NT]: positions, beside the queries
 
-  // rows r0 .. of the R (row, head) pairs; tiles past R repeat the last
+  // Tile n of rows r0 .. of the R (row, head) pairs; tiles past R repeat the last.
+  __device__ __forceinline__ static int row_at(int r0, int n, int R) { return min(r0 + 16 * n + (int)(threadIdx.x & 15), R - 1); }
+
+  // Dims 64 h + 16 lg + 8 half .. + 7 of a tile's queries are the operand (h, half).
+  __device__ __forceinline__ static void load_q(const CacheAttnArgs& a, const AttnSeq& q, int kvh, int G, int rr, uint4 (&f)[NQ][KH][2]) {
+    const int lg = (threadIdx.x & 63) >> 4, m = rr / G, head = kvh * G + (rr - m * G);
+    const int64_t at = (int64_t)(q.row0 + m) * a.ldq + head * HD;
+#pragma unroll
+    for (int h = 0; h < KH; ++h)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int64_t i = at + 64 * h + 16 * lg + 8 * half;
+        if (DT == 1) {
+          const uint4 u = ld16((const uint16_t*)a.q + i);
+          f[0][h][half] = make_uint4(u.x ^ a.q_sign, u.y ^ a.q_sign, u.z ^ a.q_sign, u.w ^ a.q_sign);
+        } else {
+          float x[8];
+          *(float4*)x = *(const float4*)((const float*)a.q + i);
+          *(float4*)(x + 4) = *(const float4*)((const float*)a.q + i + 4);
+#pragma unroll
+          for (int p = 0; p < NQ; ++p) {
+            uint32_t u[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              u[e] = f32_to_bf16x2(x[2 * e], x[2 * e + 1]);
+              x[2 * e] -= bf16lo(u[e]);
+              x[2 * e + 1] -= bf16hi(u[e]);
+            }
+            f[p][h][half] = make_uint4(u[0] ^ a.q_sign, u[1] ^ a.q_sign, u[2] ^ a.q_sign, u[3] ^ a.q_sign);
+          }
+        }
+      }
+  }
+
   __device__ __forceinline__ void init(const CacheAttnArgs& a, const AttnSeq& q, int kvh, int G, int r0, int R) {
-    const int l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int rr = min(r0 + 16 * n + lr, R - 1), m = rr / G, head = kvh * G + (rr - m * G);
-      pos[n] = q.len - q.n + m;
+      const int rr = row_at(r0, n, R);
+      if (!QL) pos[QL ? 0 : n] = q.len - q.n + rr / G;
       sum[n] = 0.f;
       base[n] = B_NONE;
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-      // dims 64 h + 16 lg + 8 half .. + 7 are the operand (h, half)
-      const int64_t at = (int64_t)(q.row0 + m) * a.ldq + head * HD;
-#pragma unroll
-      for (int h = 0; h < KH; ++h)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int64_t i = at + 64 * h + 16 * lg + 8 * half;
-          if (DT == 1) {
-            const uint4 u = ld16((const uint16_t*)a.q + i);
-            qf[n][0][h][half] = make_uint4(u.x ^ a.q_sign, u.y ^ a.q_sign, u.z ^ a.q_sign, u.w ^ a.q_sign);
-          } else {
-            float x[8];
-            *(float4*)x = *(const float4*)((const float*)a.q + i);
-            *(float4*)(x + 4) = *(const float4*)((const float*)a.q + i + 4);
-#pragma unroll
-            for (int p = 0; p < NQ; ++p) {
-              uint32_t u[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                u[e] = f32_to_bf16x2(x[2 * e], x[2 * e + 1]);
-                x[2 * e] -= bf16lo(u[e]);
-                x[2 * e + 1] -= bf16hi(u[e]);
-              }
-              qf[n][p][h][half] = make_uint4(u[0] ^ a.q_sign, u[1] ^ a.q_sign, u[2] ^ a.q_sign, u[3] ^ a.q_sign);
-            }
-          }
-        }
+      if (!QL) load_q(a, q, kvh, G, rr, qf[QL ? 0 : n]);
     }
+  }
+  __device__ __forceinline__ int position(int n) const { return QL ? pl[n][threadIdx.x & 15] : pos[QL ? 0 : n]; }
+  __device__ __forceinline__ uint4 query(int n, int p, int h, int half) const {
+    return QL ? ql[n][p][h][half][threadIdx.x & 63] : qf[QL ? 0 : n][p][h][half];
   }
 
   // One page: tokens t0 .. t0 + 63; this lane's key operand (t, h, half) and
@@ -184,21 +198,27 @@ struct Tiles {
     const int lg = (threadIdx.x & 63) >> 4;
     const float ks = ldexpf(a.scale_log2, (int)(wk & 255) - 127);
     const int ev = (int)(wv & 255) - 127;
-    // lane: token t0 + 16 lg + 4 t + i of its query.  Two key tiles at a time
-    // (products on one accumulator wait for each other), a step's operands
-    // taken while the step before is multiplied
+    // lane: token t0 + 16 lg + 4 t + i of its query.  Two key tiles at a time:
+    // products on one accumulator wait for each other
     f32x4 x[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int t = 0; t < 4; ++t) x[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    uint4 cur[2] = {kf(0, 0, 0), kf(1, 0, 0)};
+    uint4 cur[2];
+    if (PIPE) {
+      cur[0] = kf(0, 0, 0);
+      cur[1] = kf(1, 0, 0);
+    }
     __builtin_amdgcn_s_setprio(1);   // a wave in its products goes first; the SIMD's other has its exponentials (3%)
 #pragma unroll
     for (int i = 0; i < 4 * KH; ++i) {
       const int t = i / (2 * KH) * 2, h = i / 2 % KH, half = i & 1;
       uint4 nxt[2];
-      if (i + 1 < 4 * KH) {
+      if (!PIPE) {
+        cur[0] = kf(t, h, half);
+        cur[1] = kf(t + 1, h, half);
+      } else if (i + 1 < 4 * KH) {
         const int t1 = (i + 1) / (2 * KH) * 2, h1 = (i + 1) / 2 % KH;
         nxt[0] = kf(t1, h1, (i + 1) & 1);
         nxt[1] = kf(t1 + 1, h1, (i + 1) & 1);
@@ -209,11 +229,15 @@ struct Tiles {
 #pragma unroll
       for (int p = 0; p < NQ; ++p)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n) {
+          const uint4 qo = query(n, p, h, half);
 #pragma unroll
-          for (int u = 0; u < 2; ++u) x[n][t + u] = mfma_tile<1>(cur[u], qf[n][p][h][half], x[n][t + u]);
-      cur[0] = nxt[0];
-      cur[1] = nxt[1];
+          for (int u = 0; u < 2; ++u) x[n][t + u] = mfma_tile<1>(cur[u], qo, x[n][t + u]);
+        }
+      if (PIPE) {
+        cur[0] = nxt[0];
+        cur[1] = nxt[1];
+      }
       if (NT > 1) __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
@@ -228,11 +252,12 @@ struct Tiles {
       if (edge || far) {
         // a table entry outside the pool: rows that see the page become NaN
         kx = 1.f;
+        const int last = position(n);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            x[n][t][i] = t0 + 16 * lg + 4 * t + i > pos[n] ? -INFINITY : known ? x[n][t][i] * ks : __builtin_nanf("");
+            x[n][t][i] = t0 + 16 * lg + 4 * t + i > last ? -INFINITY : known ? x[n][t][i] * ks : __builtin_nanf("");
       }
 #pragma unroll
       for (int t = 0; t < 4; ++t)
@@ -298,8 +323,11 @@ struct Tiles {
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
       const int d = i / 2 * 2, half = i & 1;
-      uint4 nxt[2] = {cur[0], cur[1]};
-      if (i + 1 < ND) {
+      uint4 nxt[2];
+      if (!PIPE) {
+        cur[0] = vf(d, half);
+        cur[1] = vf(d + 1, half);
+      } else if (i + 1 < ND) {
         nxt[0] = vf((i + 1) / 2 * 2, (i + 1) & 1);
         nxt[1] = vf((i + 1) / 2 * 2 + 1, (i + 1) & 1);
       }
@@ -309,8 +337,10 @@ struct Tiles {
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int u = 0; u < 2; ++u) o[n][d + u] = mfma_f16(cur[u], pf[n][p][half], o[n][d + u]);
-      cur[0] = nxt[0];
-      cur[1] = nxt[1];
+      if (PIPE && i + 1 < ND) {
+        cur[0] = nxt[0];
+        cur[1] = nxt[1];
+      }
       if (NT > 1) __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
@@ -327,7 +357,7 @@ struct Tiles {
       const uint4 n0 = nan_ones(vf(d, 0)), n1 = nan_ones(vf(d, 1));
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const int seen = pos[n] - (t0 + 16 * lg) + 1;
+        const int seen = position(n) - (t0 + 16 * lg) + 1;
         f32x4 hit = {0.f, 0.f, 0.f, 0.f};
         hit = mfma_f16(n0, first_ones(seen), hit);
         hit = mfma_f16(n1, first_ones(seen - 8), hit);
@@ -374,16 +404,18 @@ __device__ __forceinline__ void put4(const CacheAttnArgs& a, const AttnSeq& q, i
   }
 }
 
-// Up to 16 rows: one split of a sequence's pages, which the block's four waves
-// take in turn for all of its rows, each with sums of its own.  Keys and
+// Few rows, 16 NT a tile: one split of a sequence's pages, which the block's four
+// waves take in turn for all of its rows, each with sums of its own.  Keys and
 // values go from memory straight into the operands' registers (no LDS, no
-// barrier), the next page's requested as soon as this one's are used.  The
-// waves meet in LDS once, at the end.
-template <int DT, int HD>
+// barrier), the next page's requested as soon as this one's are used; of two
+// tiles the queries are in LDS, to leave them room.  The waves meet in LDS
+// once, at the end.
+template <int DT, int HD, int NT>
 __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
-  constexpr int NT = 1;
-  typedef Tiles<DT, HD, NT> T;
+  typedef Tiles<DT, HD, NT, (NT > 1)> T;
   constexpr int KH = T::KH, ND = T::ND;
+  __shared__ uint4 ql[NT > 1 ? NT : 1][T::NQ][KH][2][NT > 1 ? 64 : 1];
+  __shared__ int pl[NT][16];
   __shared__ float sm[4][16], sl[4][16];
   __shared__ __align__(16) float so[4][16][HD + 4];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
@@ -410,6 +442,22 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
     walk.load(a, table, kvh, j, 4, j_end);
     T tiles;
     tiles.init(a, q, kvh, G, r0, R);
+    if constexpr (NT > 1) {
+      if (w < NT) {
+        uint4 f[T::NQ][KH][2];
+        T::load_q(a, q, kvh, G, T::row_at(r0, w, R), f);
+#pragma unroll
+        for (int p = 0; p < T::NQ; ++p)
+#pragma unroll
+          for (int h = 0; h < KH; ++h)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) ql[w][p][h][half][l] = f[p][h][half];
+        if (l < 16) pl[w][l] = q.len - q.n + T::row_at(r0, w, R) / G;
+      }
+      tiles.ql = ql;
+      tiles.pl = pl;
+      __syncthreads();
+    }
     uint4 kf[4][KH], vf[ND];
     int id = 0;   // of the page in the registers
     auto page_at = [&](int i) {
@@ -654,7 +702,8 @@ __global__ __launch_bounds__(256) void k_cache_attn_join(CacheAttnArgs a) {
 template <int DT, int HD>
 static hipError_t attention_hd(const CacheAttnArgs& a, hipStream_t s) {
   const unsigned blocks = (unsigned)(a.n_full + a.n_cut * a.n_split);
-  if (a.tile_rows == 16) k_cache_attn<DT, HD><<<blocks, 256, 0, s>>>(a);
+  if (a.tile_rows == 16) k_cache_attn<DT, HD, 1><<<blocks, 256, 0, s>>>(a);
+  else if (a.tile_rows == 32) k_cache_attn<DT, HD, 2><<<blocks, 256, 0, s>>>(a);
   else if (a.tile_rows == 64) k_cache_attn_rows<DT, HD, 1><<<blocks, 256, 0, s>>>(a);
   else if constexpr (DT == 1) k_cache_attn_rows<DT, HD, 2><<<blocks, 256, 0, s>>>(a);
   if (a.n_cut > 0) {
