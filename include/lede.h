@@ -603,7 +603,8 @@ size_t lede_op_cache_bytes(int32_t n_pages, int32_t n_kv_heads, int32_t head_dim
  * taken: kv_lens = seq_lens, held_out = held, status[2] = *free_head, every
  * row_start is 0 and every slot -1, so that the pass behind it has no rows.
  * Returns LEDE_E_ARG on null pointers (free_pages may be null with n_free =
- * 0, slots with max_rows = 0) and sizes below these. */
+ * 0, slots with max_rows = 0) and sizes below these, LEDE_E_UNSUPPORTED from
+ * 2^24 sequences or rows on. */
 int lede_op_cache_plan(const int32_t* seq_lens, const int32_t* new_lens, const int32_t* held, int32_t n_seqs,
                        const int32_t* free_pages, int32_t n_free, const int32_t* free_head, int32_t* tables,
                        int32_t table_ld, int32_t max_rows, int32_t* kv_lens, int32_t* held_out, int32_t* row_start,
@@ -611,14 +612,16 @@ int lede_op_cache_plan(const int32_t* seq_lens, const int32_t* new_lens, const i
 
 /* K/V rows into the cache: row r (k + r * ldk and v + r * ldv elements of
  * `dtype`, n_kv heads of head_dim) goes to slots[r]; a slot outside the pool
- * skips its row.  Rows of one page stand next to each other, as a plan lays
- * them out, and no slot is given twice (else what the pages involved hold is
- * undefined).  A block's scale is the smallest with |x| <= 448 * 2^e for
+ * skips its row.  Rows of one page stand next to each other with no skipped
+ * row between them, as a plan lays them out, and no slot is given twice (else
+ * what the pages involved hold is undefined).  A block's scale is the smallest with |x| <= 448 * 2^e for
  * its finite entries: rows that include a page's first token start it anew,
  * others keep the larger of the old and their own, and when it grows the
  * page's codes are rounded to the new one (exact but for the smallest).
  * Rounding is to nearest, ties to even; an entry that is not finite becomes
- * a NaN.  Tokens of the page that the call does not write keep their values.
+ * a NaN.  Tokens that the call does not write keep their values, but for
+ * those of a page whose first token it writes: they are undefined until they
+ * are written (as after a rollback, which they belong to).
  * LEDE_E_ARG: null pointers, a bad dtype, n_rows < 0, a row stride below
  * n_kv * head_dim; k, v, cache or row strides not multiples of 16 bytes.
  * LEDE_E_UNSUPPORTED: 2^24 rows or more. */
@@ -637,7 +640,8 @@ int lede_op_cache_read(int32_t dtype, const void* cache, int32_t n_pages, int32_
  * n_heads heads of head_dim), which are the last of its kv_lens[s] cached
  * tokens: row i of n sees the tokens up to position kv_lens[s] - n + i.
  * Query head h reads KV head h / (n_heads / n_kv_heads); weights are
- * softmax(scale q.k).  out (row stride ldo) has q's dtype; a row that sees no
+ * softmax(scale q.k).  out (row stride ldo) has q's dtype and may be q itself
+ * (with ldo = ldq), but overlaps nothing else; a row that sees no
  * token is 0, rows outside every sequence are left as they are.  Any
  * mix of lengths (none, one, many) is taken; max_new and max_kv, the largest
  * number of rows and of cached tokens that a sequence is expected to have,

@@ -97,6 +97,7 @@ int lede_op_cache_plan(const int32_t* seq_lens, const int32_t* new_lens, const i
     return LEDE_E_ARG;
   if (n_seqs < 1 || n_free < 0 || (n_free && !free_pages) || table_ld < 1 || max_rows < 0 || (max_rows && !slots))
     return LEDE_E_ARG;
+  if (n_seqs > MOST_BLOCKS || max_rows > MOST_BLOCKS) return LEDE_E_UNSUPPORTED;   // (the kernels step through both in 32 bits)
   CachePlanArgs a{};
   a.seq_lens = seq_lens; a.new_lens = new_lens; a.held = held; a.n_seqs = n_seqs;
   a.free_pages = free_pages; a.n_free = n_free; a.free_head = free_head;

@@ -671,7 +671,8 @@ def op_cache_plan(seq_lens, new_lens, held, free_pages, free_head, tables, max_r
     import torch
     dev, n, max_rows = seq_lens.device, seq_lens.numel(), int(max_rows)
     _need(_dense(dev, torch.int32, seq_lens, new_lens, held, free_pages, free_head, tables) and tables.dim() == 2
-          and new_lens.numel() == n and held.numel() == n and tables.shape[0] == n and free_head.numel() == 1, "op_cache_plan")
+          and new_lens.numel() == n and held.numel() == n and tables.shape[0] == n and free_head.numel() == 1 and max_rows >= 0,
+          "op_cache_plan")
     if out is None:
         buf = torch.empty(3 * n + 5, dtype=torch.int32, device=dev)
         kv_lens, held_out, row_start, status = buf.split_with_sizes((n, n, n + 1, 4))
@@ -732,7 +733,7 @@ def op_cache_attention(cache: Cache, q, tables, kv_lens, row_start, max_new: int
     sequence s, over the pages of tables [n_seqs][width] (int32).  max_new and
     max_kv: the largest numbers of rows and of tokens expected.  `scale` is
     head_dim ** -0.5 when not given.  Rows of a new `out` that no sequence has
-    are undefined; a given one's are left as they are."""
+    are undefined; a given one's (q itself is taken) are left as they are."""
     import torch
     dev, kv, hd, n = cache.device, cache.n_kv, cache.head_dim, kv_lens.numel()
     max_new, max_kv = int(max_new), int(max_kv)

@@ -47,6 +47,11 @@ def test_plan_refuses(lib, bad):
     assert lib.lede_op_cache_plan(*_change(PLAN_GOOD, PLAN, **bad)) == lede.LEDE_E_ARG
 
 
+@pytest.mark.parametrize("big", [dict(n_seqs=1 << 24), dict(max_rows=1 << 24), dict(max_rows=2 ** 31 - 1)], ids=str)
+def test_plan_refuses_what_32_bits_cannot_step_through(lib, big):
+    assert lib.lede_op_cache_plan(*_change(PLAN_GOOD, PLAN, **big)) == lede.LEDE_E_UNSUPPORTED
+
+
 APPEND = ["dtype", "k", "ldk", "v", "ldv", "slots", "n_rows", "cache", "n_pages", "n_kv", "hd", "stream"]
 APPEND_GOOD = [1, P, 1024, P, 1024, P, 4, P, 2, 8, 128, NULL]
 ROWS_BAD = [(dict(dtype=2), lede.LEDE_E_ARG), (dict(dtype=-1), lede.LEDE_E_ARG), (dict(k=NULL), lede.LEDE_E_ARG),
@@ -54,7 +59,7 @@ ROWS_BAD = [(dict(dtype=2), lede.LEDE_E_ARG), (dict(dtype=-1), lede.LEDE_E_ARG),
             (dict(n_rows=-1), lede.LEDE_E_ARG), (dict(n_pages=0), lede.LEDE_E_ARG), (dict(n_kv=0), lede.LEDE_E_ARG),
             (dict(hd=80), lede.LEDE_E_UNSUPPORTED), (dict(n_kv=1025), lede.LEDE_E_UNSUPPORTED), (dict(ldk=1023), lede.LEDE_E_ARG),
             (dict(ldk=1028), lede.LEDE_E_ARG), (dict(ldv=1016), lede.LEDE_E_ARG), (dict(k=P + 8), lede.LEDE_E_ARG),
-            (dict(v=P + 2), lede.LEDE_E_ARG), (dict(cache=P + 8), lede.LEDE_E_ARG)]
+            (dict(v=P + 2), lede.LEDE_E_ARG), (dict(cache=P + 8), lede.LEDE_E_ARG), (dict(n_rows=1 << 24), lede.LEDE_E_UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("bad,code", ROWS_BAD, ids=str)
@@ -70,6 +75,7 @@ def test_no_rows_is_no_work(lib):
     assert lib.lede_op_cache_append(*_change(APPEND_GOOD, APPEND, n_rows=0, k=NULL, v=NULL, slots=NULL)) == 0
     assert lib.lede_op_cache_attention(*_change(ATTN_GOOD, ATTN, n_rows=0, q=NULL, out=NULL)) == 0
     assert lib.lede_op_logprobs(*_change(LP_GOOD, LP, n_rows=0, logits=NULL, ws=NULL)) == 0
+    assert lib.lede_op_logprobs(*_change(LP_GOOD, LP, n_rows=0, logits=NULL, ws=NULL, tokens=NULL, ids=NULL, top_lp=NULL)) == 0
 
 
 ATTN = ["dtype", "q", "ldq", "cache", "n_pages", "tables", "ld", "kv", "start", "n_seqs", "n_rows", "nq", "nkv", "hd", "scale", "max_new",
@@ -83,7 +89,8 @@ ATTN_GOOD = [1, P, 4096, P, 64, P, 32, P, P, 2, 2, 32, 8, 128, 0.1, 1, 2000, P, 
     (dict(scale=float("nan")), lede.LEDE_E_ARG), (dict(scale=float("inf")), lede.LEDE_E_ARG), (dict(max_new=-1), lede.LEDE_E_ARG),
     (dict(max_kv=-1), lede.LEDE_E_ARG), (dict(ldq=4088), lede.LEDE_E_ARG), (dict(ldo=4100), lede.LEDE_E_ARG), (dict(q=P + 4), lede.LEDE_E_ARG),
     (dict(out=P + 8), lede.LEDE_E_ARG), (dict(cache=P + 4), lede.LEDE_E_ARG), (dict(ws=P + 8), lede.LEDE_E_ARG),
-    (dict(ws_bytes=16), lede.LEDE_E_ARG), (dict(n_seqs=65536), lede.LEDE_E_UNSUPPORTED), (dict(nq=65544), lede.LEDE_E_UNSUPPORTED)], ids=str)
+    (dict(ws_bytes=16), lede.LEDE_E_ARG), (dict(n_seqs=65536), lede.LEDE_E_UNSUPPORTED), (dict(nq=65544), lede.LEDE_E_UNSUPPORTED),
+    (dict(n_rows=1 << 28), lede.LEDE_E_UNSUPPORTED), (dict(n_seqs=1 << 13, nq=1024, nkv=1024), lede.LEDE_E_UNSUPPORTED)], ids=str)
 def test_attention_refuses(lib, bad, code):
     assert lib.lede_op_cache_attention_bytes(1, 2, 2, 32, 8, 128, 1, 2000) > 16
     assert lib.lede_op_cache_attention(*_change(ATTN_GOOD, ATTN, **bad)) == code
@@ -107,7 +114,8 @@ LP_GOOD = [0, P, 50000, 4, 50000, 1.0, P, 5, P, P, P, P, P, P, 1 << 30, NULL]
     (dict(top=-1), lede.LEDE_E_ARG), (dict(top=33), lede.LEDE_E_UNSUPPORTED), (dict(V=4, top=5), lede.LEDE_E_ARG), (dict(T=0.0), lede.LEDE_E_ARG),
     (dict(T=-1.0), lede.LEDE_E_ARG), (dict(T=float("nan")), lede.LEDE_E_ARG), (dict(T=float("inf")), lede.LEDE_E_ARG),
     (dict(T=1e-45), lede.LEDE_E_ARG), (dict(logits=P + 2), lede.LEDE_E_ARG), (dict(ws=P + 8), lede.LEDE_E_ARG), (dict(ws_bytes=8), lede.LEDE_E_ARG),
-    (dict(V=(1 << 20) + 1, ld=1 << 21), lede.LEDE_E_UNSUPPORTED)], ids=str)
+    (dict(V=(1 << 20) + 1, ld=1 << 21), lede.LEDE_E_UNSUPPORTED),
+    (dict(n_rows=1 << 24, ws_bytes=1 << 40), lede.LEDE_E_UNSUPPORTED)], ids=str)
 def test_logprobs_refuses(lib, bad, code):
     assert lib.lede_op_logprobs(*_change(LP_GOOD, LP, **bad)) == code
 

@@ -522,6 +522,54 @@ def test_attention_strides_and_workspace(dtype):
         m.op_cache_attention(cache, d, gpu(tables), i32(lens), i32([0, 2, 3]), 2, 1300, workspace=ws[:need - 16])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [[1, 0, 2], [9, 1, 3], [20, 2, 1], [70, 0, 1]])
+def test_attention_in_place(dtype, new):
+    """The output in the queries' own rows, beside splits that are joined later: the bits of an output of its own."""
+    m = lede()
+    say("in place", dtype, new)
+    r = np.random.default_rng(sum(new))
+    lens = [900, 70, 2000]
+    cache, model, tables = _fill(2, 64, lens, r)
+    start = i32(np.concatenate([[0], np.cumsum(new)]))
+    q, _ = rounded(r.standard_normal((sum(new) + 1, 6, 64)), dtype)
+    args = (gpu(tables), i32(lens), start, max(new), max(lens))
+    want = torch.full_like(q, 3.0)
+    want[-1] = q[-1]
+    m.op_cache_attention(cache, q, *args, out=want)
+    assert m.op_cache_attention(cache, q, *args, out=q) is q
+    assert torch.equal(q, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [[1, 1, 1], [30, 2, 5], [66, 4, 1]])
+def test_attention_shared_pages(dtype, new):
+    """Requests with one beginning read the same pages; a page may even stand twice in one table."""
+    r = np.random.default_rng(19)
+    lens = [190, 250, 130]
+    cache, model, tables = _fill(3, 128, lens, r)
+    tables[1, :2] = tables[0, :2]
+    tables[2, 1] = tables[2, 0]
+    _attend(cache, model, tables, lens, new, 6, dtype, r)
+
+
+def test_attention_page_started_anew():
+    """A page that held NaNs and large values, given to another request: nothing of them stays."""
+    m = lede()
+    r = np.random.default_rng(20)
+    cache, model, tables = _fill(2, 64, [70], r, size=1e4)
+    bad = torch.full((3, 2, 64), math.nan, device="cuda")
+    slots = tables[0, 0].astype(np.int64) * 64 + np.arange(3)
+    m.op_cache_append(cache, bad, bad, gpu(slots + 20))
+    for dtype, rows in (("f32", 2), ("bf16", 40)):
+        d, val = rounded(_rows(r, 45, 2, 64, 1e-3), dtype)
+        at = tables[0, 0].astype(np.int64) * 64 + np.arange(45)
+        m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(at))
+        model.append(val[:, 0], val[:, 1], at)
+        got = _attend(cache, model, tables, [45], [rows], 4, dtype, r)
+        assert np.isfinite(got).all() and np.abs(got).max() < 1e-2
+
+
 def test_attention_rows_do_not_depend_on_the_batch():
     """The same bits again, and with another sequence's rows beside."""
     m = lede()
@@ -784,6 +832,34 @@ def test_on_another_stream():
         c, e = m.op_cache_attention(cache, d, *args), m.op_logprobs(z, tok, 8, 0.9)
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(a, c) and torch.equal(b.logprobs, e.logprobs) and torch.equal(b.top_ids, e.top_ids)
+
+
+def test_two_streams_at_once():
+    """Calls that overlap on two streams, each with a workspace and outputs of its own."""
+    m = lede()
+    r = np.random.default_rng(21)
+    lens, new = [6000, 40, 300, 2500], [2, 1, 1, 1]
+    cache, model, tables = _fill(2, 64, lens, r)
+    q = [rounded(r.standard_normal((5, 8, 64)), "bf16")[0] for _ in range(2)]
+    z = [gpu(r.standard_normal((5, 60000)).astype(np.float32)) for _ in range(2)]
+    args = (gpu(tables), i32(lens), i32([0, 2, 3, 4, 5]), 2, 6000)
+    tok = i32([1, 2, 3, 4, 59999])
+    want = [(m.op_cache_attention(cache, q[i], *args), m.op_logprobs(z[i], tok, 32)) for i in range(2)]
+    need = m.load().lede_op_cache_attention_bytes(1, 4, 5, 8, 2, 64, 2, 6000), m.load().lede_op_logprobs_bytes(5, 60000, 32)
+    assert min(need) > 0
+    ws = [[torch.empty(n, dtype=torch.uint8, device="cuda") for n in need] for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(8):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append((m.op_cache_attention(cache, q[i], *args, workspace=ws[i][0]), m.op_logprobs(z[i], tok, 32, workspace=ws[i][1])))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o, lp in got[i]:
+            assert torch.equal(o, want[i][0]) and torch.equal(lp.top_ids, want[i][1].top_ids)
+            assert torch.equal(lp.logprobs, want[i][1].logprobs) and torch.equal(lp.entropy, want[i][1].entropy)
 
 
 def test_long_cache_offsets():
