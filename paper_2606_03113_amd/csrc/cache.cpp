@@ -37,25 +37,54 @@ constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;
 
 // Row tiles and splits of an attention's grid.  The kernels are right for any
 // lengths; this decides how the work spreads.
+//
+// Rows of a tile.  16 and 32: a block's waves take pages, so that each page is
+// read once per tile, straight into registers; 64 and 128: they take rows,
+// and share pages through LDS.  Measured, us (bf16 unless said otherwise):
+//   rows each                            16    32    64   128
+//   16, 64 sequences of 8000, hd 128    153   159   209   281
+//   20                                  200   163   208   277
+//   40, 2 sequences of 131000           107   100    75   100
+//   80, 64 of 8000                      311   246   331   285
+//   100, 16 of 4000, 32 KV heads        187   126   145   131
+//   256                                 413   266   261   221
+//   500, fp32                           893   732   703
+//   20, 64 of 8000, hd 64               104    87   137
+//   40                                  108   123   136
+//   500, 16 of 4000, 16 KV heads        158   142   138
+//   1000                                320   278   243
 struct AttnGrid { int tile_rows, n_tiles, n_full, n_cut, n_split, min_chunk; };
-AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32_t max_new, int32_t max_kv) {
+AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32_t hd, int32_t max_new, int32_t max_kv) {
   AttnGrid g;
   const int64_t rows = std::max<int64_t>(1, (int64_t)max_new * (nq / nkv));
-  g.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || dtype == LEDE_DTYPE_F32 ? 64 : 128;
+  if (rows <= 32) g.tile_rows = rows <= 16 ? 16 : 32;
+  else if (hd == 128) g.tile_rows = rows <= 64 ? 64 : rows < 256 ? 32 : dtype == LEDE_DTYPE_BF16 ? 128 : 64;
+  else g.tile_rows = rows < 512 ? 16 : 64;
   // (a task takes every n_tiles-th tile: a grid need not grow with a large max_new)
   const int64_t groups = (int64_t)n_seqs * nkv;
   g.n_tiles = (int)std::min((rows + g.tile_rows - 1) / g.tile_rows, 65536 / groups + 1);
   const int64_t whole = groups * g.n_tiles;
   const int64_t pages = std::max<int64_t>(1, ((int64_t)max_kv + CACHE_PAGE - 1) / CACHE_PAGE);
-  // The card holds ROUND blocks at a time.  Tasks of whole rounds are blocks
-  // of their own, and the rest, or all where there are fewer, are cut to fill
-  // one.  Few rows behind very long contexts are cut in any case: lengths
-  // differ, and one long sequence must not be a block's alone.
-  constexpr int64_t ROUND = 512, LONG = 128, MOST_CUT = 4096;
+  // The card holds ROUND blocks at a time.  Tasks of whole rounds are blocks of
+  // their own, and the rest, or all where there are fewer, are cut to fill one
+  // (3 x 1000 rows behind 4100 tokens: 167 us, 205 uncut).  Few rows behind long
+  // contexts are cut into about LONG pages in any case: lengths differ, and one
+  // long sequence must not be a block's alone (100000 tokens among 63 of 1000:
+  // 81 us, 600 uncut).  64 pages where the card would not be full (20 sequences
+  // of 50 to 60000 tokens: 60 us, 88 with 128), else 128 (64 of 6000: 118 us,
+  // 125 with 64).  MOST_CUT bounds the workspace and the blocks that find
+  // nothing to do (300 of 50 to 60000: 955 us, 1056 with half as many).
+  constexpr int64_t ROUND = 512, MOST_CUT = 8192;
+  const int64_t LONG = whole < ROUND ? 64 : 128;
   const int64_t by_length = g.tile_rows <= 32 ? (pages + LONG - 1) / LONG : 1;
   const int64_t cut = by_length > 1 ? whole : whole % ROUND;
   int64_t split = cut ? std::max(whole < ROUND ? (ROUND + whole - 1) / whole : by_length > 1 ? 1 : ROUND / cut, by_length) : 1;
   split = std::min(split, std::max<int64_t>(1, MOST_CUT / std::max<int64_t>(cut, 1)));
+  // A split's pages follow each other, and so do the splits in the join: about
+  // 2 sqrt(pages) of them take the least of both (one head of 130000 tokens: 26
+  // us, 56 in chunks of 4 pages).  4 pages are a page a wave (1000 tokens: 9.0 us,
+  // 10.2 in chunks of 8).
+  while (split > 1 && split * split > 4 * pages) --split;
   g.min_chunk = (int)std::max<int64_t>(4, (pages + split - 1) / split);
   g.n_split = (int)((pages + g.min_chunk - 1) / g.min_chunk);
   g.n_cut = g.n_split > 1 ? (int)cut : 0;
@@ -69,8 +98,9 @@ constexpr int32_t MOST_TOP = 32;
 
 // Tiles of a row (its first may begin inside a 16-byte piece: up to 7
 // entries before it), and how many of them a block takes: as many as leave
-// the card about 1024 blocks, and all of up to four (5 rows of 32000: 15.3 us
-// in one launch, 10.1 + 5.2 us with a block per tile and the join).
+// the card about 1024 blocks (400 rows of 128256: 33 us, 36 with 512, 39 with
+// 2048), and all of up to four (5 rows of 32000: 12.1 us in one launch; a block
+// per tile takes 11.2, but a second launch and a workspace on the host).
 struct ScoreGrid { int n_tiles, part_tiles, n_part; };
 ScoreGrid score_grid(int32_t n_rows, int32_t V) {
   ScoreGrid g;
@@ -118,6 +148,7 @@ static int cache_rows(bool append, int32_t dtype, void* k, int64_t ldk, void* v,
   CacheRowsArgs a{};
   a.c = cache_view(cache, n_pages, n_kv, hd);
   a.k = k; a.v = v; a.ldk = ldk; a.ldv = ldv; a.slots = slots; a.n_rows = n_rows;
+  // about 4096 blocks (the kernels say what shorter and longer windows cost)
   a.window = (int)std::min<int64_t>(CACHE_PAGE, std::max<int64_t>(1, (int64_t)n_rows * n_kv * 2 / 4096));
   return done(append ? launch_cache_append(dtype, a, S_(stream)) : launch_cache_read(dtype, a, S_(stream)));
 }
@@ -136,7 +167,7 @@ int lede_op_cache_read(int32_t dtype, const void* cache, int32_t n_pages, int32_
 size_t lede_op_cache_attention_bytes(int32_t dtype, int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads,
                                      int32_t head_dim, int32_t max_new, int32_t max_kv) {
   if (!dtype_ok(dtype) || n_seqs < 1 || n_rows < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_kv < 0) return 0;
-  const AttnGrid g = attn_grid(dtype, n_seqs, n_heads, n_kv_heads, max_new, max_kv);
+  const AttnGrid g = attn_grid(dtype, n_seqs, n_heads, n_kv_heads, head_dim, max_new, max_kv);
   return (size_t)g.n_cut * g.n_split * g.tile_rows * (head_dim + 4) * 4;
 }
 
@@ -154,7 +185,7 @@ int lede_op_cache_attention(int32_t dtype, const void* q, int64_t ldq, const voi
   if (n_rows == 0) return LEDE_OK;
   const int64_t width = (int64_t)n_heads * head_dim;
   if (!rows_ok(q, ldq, width, dtype) || !rows_ok(out, ldo, width, dtype)) return LEDE_E_ARG;
-  const AttnGrid g = attn_grid(dtype, n_seqs, n_heads, n_kv_heads, max_new, max_kv);
+  const AttnGrid g = attn_grid(dtype, n_seqs, n_heads, n_kv_heads, head_dim, max_new, max_kv);
   const size_t need = lede_op_cache_attention_bytes(dtype, n_seqs, n_rows, n_heads, n_kv_heads, head_dim, max_new, max_kv);
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return LEDE_E_ARG;
   CacheAttnArgs a{};

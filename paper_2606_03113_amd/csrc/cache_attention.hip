@@ -85,7 +85,10 @@ __device__ __forceinline__ uint4 first_ones(int n) {
 // A block's work: a tile of a sequence's (row, query head of the group) pairs
 // for one KV head, and a split of its pages.  The first n_full tasks are
 // blocks of their own; the others, which would leave the card partly idle in
-// a last round, are n_split blocks each.  Tasks with more pages come first.
+// a last round, are n_split blocks each.  Of a sequence, tiles with more pages
+// come first, and a task's splits follow each other: one long context among
+// short ones is then under way from the start (200000 tokens among 63 of 100:
+// 127 us, and 191 with the first splits of all tasks before the others).
 struct Task { int s, kvh, tile, split, n_split, slot; };
 __device__ __forceinline__ Task attn_task(const CacheAttnArgs& a, int bid) {
   Task t;
@@ -409,7 +412,11 @@ __device__ __forceinline__ void put4(const CacheAttnArgs& a, const AttnSeq& q, i
 // values go from memory straight into the operands' registers (no LDS, no
 // barrier), the next page's requested as soon as this one's are used; of two
 // tiles the queries are in LDS, to leave them room.  The waves meet in LDS
-// once, at the end.
+// once, at the end.  Memory-bound: 64 sequences of up to 6000 tokens (8 KV
+// heads of 128, 609 MB) 115-120 us, 5.1-5.3 TB/s, as fast as a kernel that only
+// reads; with 32 rows each (8000 tokens, 819 MB) 164 us, 5.0 TB/s.  A second
+// page ahead in registers would not fit: the compiler spills 256 of them, and
+// the step takes 384 us.
 template <int DT, int HD, int NT>
 __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
   typedef Tiles<DT, HD, NT, (NT > 1)> T;
@@ -546,7 +553,10 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
 // into LDS once per block, as 16-bit operands in the order in which the lanes
 // take them (16 bytes per lane, a contiguous KiB per operand: no bank
 // conflict either way), so that each wave converts a quarter of the codes;
-// two pages' room, so one barrier a page.
+// two pages' room, so one barrier a page.  Bound by the matrix units and the
+// exponentials beside them: 850-880 TFLOP/s over whole rounds of 128-row tiles
+// (bf16, heads of 128), against 1269 of a large library product; with the codes
+// themselves in LDS, converted by every wave, the rate was 8% lower.
 template <int DT, int HD, int NT>
 __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
   typedef Tiles<DT, HD, NT> T;
@@ -648,7 +658,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
 }
 
 // The splits of a row of a cut task joined in order: HD / 4 lanes a row, four
-// dims each, B splits requested at a time.
+// dims each, B splits requested at a time (fp32 chunk of 5 x 77 rows: 6 us, and
+// 9 with one dim a lane).
 template <int DT, int HD, int B>
 __global__ __launch_bounds__(256) void k_cache_attn_join(CacheAttnArgs a) {
   constexpr int LANES = HD / 4, ROWS = 256 / LANES;
@@ -705,7 +716,7 @@ static hipError_t attention_hd(const CacheAttnArgs& a, hipStream_t s) {
   if (a.tile_rows == 16) k_cache_attn<DT, HD, 1><<<blocks, 256, 0, s>>>(a);
   else if (a.tile_rows == 32) k_cache_attn<DT, HD, 2><<<blocks, 256, 0, s>>>(a);
   else if (a.tile_rows == 64) k_cache_attn_rows<DT, HD, 1><<<blocks, 256, 0, s>>>(a);
-  else if constexpr (DT == 1) k_cache_attn_rows<DT, HD, 2><<<blocks, 256, 0, s>>>(a);
+  else if constexpr (DT == 1 && HD == 128) k_cache_attn_rows<DT, HD, 2><<<blocks, 256, 0, s>>>(a);
   if (a.n_cut > 0) {
     const int64_t rows = (int64_t)a.n_cut * a.tile_rows;
     const int64_t need = rows * (HD / 4) / 256;

@@ -14,7 +14,9 @@ namespace lede {
 // its end: each thread keeps a running maximum and sums of its own entries,
 // and writes down the largest of each tile's.  These maxima lead to the top
 // tokens: the n_top-th largest over groups of threads is a lower bound that
-// few threads' tiles reach, and only those are read again.
+// few threads' tiles reach, and only those are read again.  Memory-bound for
+// many rows: 2048 rows of 128256 in bf16 101 us without top tokens, 112 with 20
+// (5.2 and 4.7 TB/s); a running list of the top ones took 162.
 constexpr int LP_THREADS = 256, LP_PER = 32;
 static_assert(LP_THREADS * LP_PER == LP_TILE, "a tile is LP_PER entries per thread");
 constexpr int LP_MAX_TOP = 32;
@@ -323,15 +325,23 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs(LogprobsArgs a) {
 }
 
 // One block per row: the parts' sums at their common maximum, the ranks, and
-// the top keys, each placed by how many larger ones the parts' sorted lists
-// hold.
+// the top keys: those of the parts' sorted lists that reach a bound, each
+// placed by how many of them are larger.  A chain of LDS reads, so few of them:
+// 5 rows of 128256, 20 top, 15 us with the parts' kernel, 28 with every key
+// sought in every list (a row of 2^20, 32 top: 25 and 713).
 template <int DT>
 __global__ __launch_bounds__(LP_THREADS) void k_logprobs_join(LogprobsArgs a) {
   extern __shared__ uint64_t keys[];
   __shared__ float row_m;
   __shared__ double row_ls;
+  __shared__ uint64_t bound, found[LP_LIST];
+  __shared__ int n_found;
   const int tid = threadIdx.x, row = blockIdx.x, top = a.n_top;
   const int n = a.n_part * top;
+  if (tid == 0) {
+    bound = 0;
+    n_found = 0;
+  }
   const uint64_t* src = a.part_keys + (int64_t)row * n;
   for (int i = tid; i < n; i += LP_THREADS) keys[i] = src[i];
   if (tid < 64) {
@@ -362,16 +372,38 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs_join(LogprobsArgs a) {
     }
   }
   __syncthreads();
+  if (!top) return;
+  // a bound that at least top keys reach: with i entries of each of c parts
+  // the c-th largest of the i-th ones (i c >= top), or a part's last one
+  const int i0 = (top + a.n_part - 1) / a.n_part, c0 = (top + i0 - 1) / i0;
+  for (int p = tid; p < a.n_part; p += LP_THREADS) {
+    const uint64_t k = keys[p * top + i0 - 1];
+    int before = 0;
+#pragma unroll 8
+    for (int h = 0; h < a.n_part; ++h) before += keys[h * top + i0 - 1] > k;
+    const uint64_t last = keys[p * top + top - 1];
+    atomicMax((unsigned long long*)&bound, (unsigned long long)(k && before == c0 - 1 ? max(k, last) : last));
+  }
+  __syncthreads();
+  const uint64_t least = bound;
+  for (int i = tid; i < n; i += LP_THREADS)
+    if (keys[i] && keys[i] >= least) {
+      const int at = atomicAdd(&n_found, 1);
+      if (at < LP_LIST) found[at] = keys[i];
+    }
+  __syncthreads();
   const float m = row_m;
   const double ls = row_ls;
-  for (int i = tid; i < n; i += LP_THREADS) {
-    const uint64_t k = keys[i];
-    const int g = i / top;
-    int before = i % top;
+  const bool fits = n_found <= LP_LIST;
+  for (int i = tid; i < (fits ? n_found : n); i += LP_THREADS) {
+    const uint64_t k = fits ? found[i] : keys[i];
+    int before = 0;
     if (!k) continue;
-    for (int h = 0; h < a.n_part && before < top; ++h) {
-      if (h == g) continue;
-      before += larger_keys(keys + h * top, top, k);
+    if (fits) {
+#pragma unroll 8
+      for (int j = 0; j < n_found; ++j) before += found[j] > k;
+    } else {   // many as large: by the parts' sorted lists
+      for (int h = 0; h < a.n_part && before < top; ++h) before += larger_keys(keys + h * top, top, k);
     }
     if (before < top) finish_top(a, row, before, k, m, ls);
   }

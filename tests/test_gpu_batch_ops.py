@@ -322,7 +322,8 @@ def test_attention_expected_sizes_only_spread_the_work(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_attention_peaked_flat_and_scaled(dtype):
+@pytest.mark.parametrize("expect", [None, 600])   # rows expected: the variant for few, and the one for many
+def test_attention_peaked_flat_and_scaled(dtype, expect):
     """Scores that one token dominates, equal scores, huge ones, other scales (a negative one, zero)."""
     r = np.random.default_rng(9)
     lens, new = [300, 65], [3, 2]
@@ -330,12 +331,13 @@ def test_attention_peaked_flat_and_scaled(dtype):
     for scale, size in ((1.0, 3.0), (0.0, 1.0), (-0.2, 1.0), (0.125, 1e-20), (1e-3, 100.0)):
         say("attention scale", scale, size)
         q = r.standard_normal((7, 4, 64)) * size
-        _attend(cache, model, tables, lens, new, 4, dtype, r, scale=scale, q=q)
+        _attend(cache, model, tables, lens, new, 4, dtype, r, scale=scale, q=q, max_new=expect)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows", [1, 70])
-def test_attention_many_small_weights(dtype, rows):
+@pytest.mark.parametrize("expect", [None, 600])   # rows expected: the variant for few, and the one for many
+def test_attention_many_small_weights(dtype, rows, expect):
     """One token with most of the weight, and thousands whose weights are below fp16's normal range beside it."""
     m = lede()
     r = np.random.default_rng(rows)
@@ -352,12 +354,13 @@ def test_attention_many_small_weights(dtype, rows):
         model.append(val[:, 0], val[:, 1], np.arange(length))
         q = np.zeros((rows + 2, 2, hd))
         q[:, :, 0] = 1.0
-        _attend(cache, model, np.arange(length // 64 + 1, dtype=np.int32)[None], [length], [rows], 2, dtype, r, scale=1.0, q=q)
+        _attend(cache, model, np.arange(length // 64 + 1, dtype=np.int32)[None], [length], [rows], 2, dtype, r, scale=1.0, q=q, max_new=expect)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows", [2, 70])
-def test_attention_huge_scores(dtype, rows):
+@pytest.mark.parametrize("expect", [None, 600])   # rows expected: the variant for few, and the one for many
+def test_attention_huge_scores(dtype, rows, expect):
     """Scores far beyond fp32's whole numbers: the largest one's value, to the output's rounding."""
     m = lede()
     kv, hd, length = 1, 64, 300
@@ -376,27 +379,29 @@ def test_attention_huge_scores(dtype, rows):
     for size in (3e3, 1e6, 3e7, 1e8, 3e8, 1e9, 1e11, 1e20, 1e30):
         q = np.zeros((rows, 1, hd), np.float32)
         q[:, 0, 0] = size
-        got = m.op_cache_attention(cache, rounded(q, dtype)[0], gpu(table), i32([length]), i32([0, rows]), rows, length, scale=1.0)
+        got = m.op_cache_attention(cache, rounded(q, dtype)[0], gpu(table), i32([length]), i32([0, rows]), expect or rows, length, scale=1.0)
         got = got.double().cpu().numpy()
         assert (np.abs(got - value) <= ref.HALF_STEP[dtype] * 2 * np.abs(value)).all(), size
         # the other way, the largest scores are the most negative ones' opposites
-        got = m.op_cache_attention(cache, rounded(-q, dtype)[0], gpu(table), i32([length]), i32([0, rows]), rows, length, scale=-1.0)
+        got = m.op_cache_attention(cache, rounded(-q, dtype)[0], gpu(table), i32([length]), i32([0, rows]), expect or rows, length, scale=-1.0)
         assert (np.abs(got.double().cpu().numpy() - value) <= ref.HALF_STEP[dtype] * 2 * np.abs(value)).all(), size
 
 
-@pytest.mark.parametrize("dtype,seqs,nq,kv,new", [("bf16", 131, 4, 4, 1), ("f32", 200, 3, 3, 2), ("bf16", 9, 60, 60, 70), ("bf16", 70, 8, 8, 9), ("f32", 70, 8, 8, 17),
-                                                  ("bf16", 3, 60, 60, 400)])
-def test_attention_more_tasks_than_a_round(dtype, seqs, nq, kv, new):
+@pytest.mark.parametrize("dtype,seqs,nq,kv,new,hd", [("bf16", 131, 4, 4, 1, 64), ("f32", 200, 3, 3, 2, 64), ("bf16", 9, 60, 60, 70, 64), ("bf16", 70, 8, 8, 9, 64),
+                                                     ("f32", 70, 8, 8, 17, 64), ("bf16", 3, 60, 60, 400, 64), ("bf16", 3, 80, 40, 300, 64), ("bf16", 3, 60, 60, 400, 128),
+                                                     ("f32", 3, 32, 16, 400, 128)])
+def test_attention_more_tasks_than_a_round(dtype, seqs, nq, kv, new, hd):
     """Whole rounds of blocks and a cut rest, few and many rows."""
     say("attention tasks", dtype, seqs, nq, kv, new)
     r = np.random.default_rng(seqs)
     lens = [int(x) for x in r.integers(new, new + (900 if seqs < 10 else 400), seqs)]
     news = [int(x) for x in r.integers(max(1, new - 3), new + 1, seqs)]
-    cache, model, tables = _fill(kv, 64, lens, r)
+    cache, model, tables = _fill(kv, hd, lens, r)
     m = lede()
-    assert m.load().lede_op_cache_attention_bytes(int(dtype == "bf16"), seqs, sum(news), nq, kv, 64, max(news), max(lens)) > 0
+    cut = m.load().lede_op_cache_attention_bytes(int(dtype == "bf16"), seqs, sum(news), nq, kv, hd, max(news), max(lens)) > 0
+    assert cut or (kv, new, hd) == (60, 400, 64)       # (more than half a round is left whole)
     start = np.concatenate([[0], np.cumsum(news)])
-    d, val = rounded(r.standard_normal((int(start[-1]), nq, 64)), dtype)
+    d, val = rounded(r.standard_normal((int(start[-1]), nq, hd)), dtype)
     got = m.op_cache_attention(cache, d, gpu(tables), i32(lens), i32(start), max(news), max(lens)).double().cpu().numpy()
     for s in np.unique(np.concatenate([[0, seqs - 1], r.integers(0, seqs, 12)])):     # some of them: the reference takes its time
         rows = np.unique(np.concatenate([[start[s], start[s + 1] - 1], r.integers(start[s], start[s + 1], 6)]))
@@ -405,7 +410,7 @@ def test_attention_more_tasks_than_a_round(dtype, seqs, nq, kv, new):
         for row in rows:
             seen = lens[s] - (start[s + 1] - row) + 1
             for h in heads:
-                z = 0.125 * (k[:seen, h // (nq // kv)] @ val[row, h])
+                z = hd ** -0.5 * (k[:seen, h // (nq // kv)] @ val[row, h])
                 w = np.exp(z - z.max())
                 w /= w.sum()
                 want = w @ v[:seen, h // (nq // kv)]
@@ -437,12 +442,14 @@ def test_attention_blocks_of_different_scale():
         model.append(val[:, 0], val[:, 1], slots)
     tables = np.array([[2, 0, 1]], np.int32)
     for dtype in ("f32", "bf16"):
-        _attend(cache, model, tables, [192], [1], 2, dtype, r, scale=1.0, q=np.full((3, 2, hd), 2.0))
+        for expect in (1, 20, 600):
+            _attend(cache, model, tables, [192], [1], 2, dtype, r, scale=1.0, q=np.full((3, 2, hd), 2.0), max_new=expect)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows", [6, 40])
-def test_attention_nan_stays_with_the_rows_that_see_it(dtype, rows):
+@pytest.mark.parametrize("expect", [None, 600])   # rows expected: the variant for few, and the one for many
+def test_attention_nan_stays_with_the_rows_that_see_it(dtype, rows, expect):
     """NaN and infinite keys and values at positions that some rows of a pass see and earlier ones do not; a query row
     that is not finite."""
     m = lede()
@@ -458,18 +465,19 @@ def test_attention_nan_stays_with_the_rows_that_see_it(dtype, rows):
         d, val = rounded(x, dtype)
         m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(slots))
         model.append(val[:, 0], val[:, 1], slots)
-        got = _attend(cache, model, tables, [length, 70], [rows, 2], 6, dtype, r)
+        got = _attend(cache, model, tables, [length, 70], [rows, 2], 6, dtype, r, max_new=expect)
         assert np.isnan(got[3:rows, 3:]).any() and not np.isnan(got[:3]).any() and not np.isnan(got[:, :3]).any() and not np.isnan(got[rows:]).any()
     cache, model, tables = _fill(kv, hd, [length, 70], r)
     q = r.standard_normal((rows + 4, 6, hd))
     q[2, 4, 5] = np.nan
-    got = _attend(cache, model, tables, [length, 70], [rows, 2], 6, dtype, r, q=q)
+    got = _attend(cache, model, tables, [length, 70], [rows, 2], 6, dtype, r, q=q, max_new=expect)
     assert np.isnan(got[2, 4]).all() and np.isnan(got).sum() == hd
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows", [5, 70])
-def test_attention_pages_outside_the_pool(dtype, rows):
+@pytest.mark.parametrize("expect", [None, 600])   # rows expected: the variant for few, and the one for many
+def test_attention_pages_outside_the_pool(dtype, rows, expect):
     """An entry of a table that names no page: rows that see it are NaN, others are right; entries that no row sees may be
     anything.  Lengths above the table's and row starts outside the rows are held to them."""
     m = lede()
@@ -483,7 +491,7 @@ def test_attention_pages_outside_the_pool(dtype, rows):
         new = [rows, 2]
         start = np.array([0, rows, rows + 2])
         d, val = rounded(r.standard_normal((rows + 2, 4, hd)), dtype)
-        got = m.op_cache_attention(cache, d, gpu(tables), i32(lens), i32(start), rows, 200).double().cpu().numpy()
+        got = m.op_cache_attention(cache, d, gpu(tables), i32(lens), i32(start), expect or rows, 200).double().cpu().numpy()
         sees = np.concatenate([200 - rows + np.arange(rows) >= 192, [False, False]])
         assert np.isnan(got[sees]).all() and not np.isnan(got[~sees]).any()
         good = tables.copy()
@@ -494,7 +502,7 @@ def test_attention_pages_outside_the_pool(dtype, rows):
     cache, model, tables = _fill(kv, hd, lens, r)
     short = tables[:, :3].copy()
     d, val = rounded(r.standard_normal((3, 4, hd)), dtype)
-    got = m.op_cache_attention(cache, d, gpu(short), i32([200, 130]), i32([-5, 1, 2]), 1, 200).double().cpu().numpy()
+    got = m.op_cache_attention(cache, d, gpu(short), i32([200, 130]), i32([-5, 1, 2]), expect or 1, 200).double().cpu().numpy()
     want, tol = ref.attention(model, val, short, [192, 130], [0, 1, 2], hd ** -0.5, dtype)
     assert (np.abs(got - want)[:2] <= tol[:2]).all()
 
@@ -523,7 +531,7 @@ def test_attention_strides_and_workspace(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("new", [[1, 0, 2], [9, 1, 3], [20, 2, 1], [70, 0, 1]])
+@pytest.mark.parametrize("new", [[1, 0, 2], [9, 1, 3], [20, 2, 1], [70, 0, 1], [200, 1, 3]])
 def test_attention_in_place(dtype, new):
     """The output in the queries' own rows, beside splits that are joined later: the bits of an output of its own."""
     m = lede()
@@ -542,7 +550,7 @@ def test_attention_in_place(dtype, new):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("new", [[1, 1, 1], [30, 2, 5], [66, 4, 1]])
+@pytest.mark.parametrize("new", [[1, 1, 1], [30, 2, 5], [66, 4, 1], [130, 4, 1]])
 def test_attention_shared_pages(dtype, new):
     """Requests with one beginning read the same pages; a page may even stand twice in one table."""
     r = np.random.default_rng(19)
@@ -561,12 +569,12 @@ def test_attention_page_started_anew():
     bad = torch.full((3, 2, 64), math.nan, device="cuda")
     slots = tables[0, 0].astype(np.int64) * 64 + np.arange(3)
     m.op_cache_append(cache, bad, bad, gpu(slots + 20))
-    for dtype, rows in (("f32", 2), ("bf16", 40)):
+    for dtype, rows, expect in (("f32", 2, None), ("bf16", 40, None), ("bf16", 40, 600)):
         d, val = rounded(_rows(r, 45, 2, 64, 1e-3), dtype)
         at = tables[0, 0].astype(np.int64) * 64 + np.arange(45)
         m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(at))
         model.append(val[:, 0], val[:, 1], at)
-        got = _attend(cache, model, tables, [45], [rows], 4, dtype, r)
+        got = _attend(cache, model, tables, [45], [rows], 4, dtype, r, max_new=expect)
         assert np.isfinite(got).all() and np.abs(got).max() < 1e-2
 
 
