@@ -86,20 +86,29 @@ __device__ __forceinline__ uint4 first_ones(int n) {
 // for one KV head, and a split of its pages.  The first n_full tasks are
 // blocks of their own; the others, which would leave the card partly idle in
 // a last round, are n_split blocks each.  Of a sequence, tiles with more pages
-// come first, and a task's splits follow each other: one long context among
-// short ones is then under way from the start (200000 tokens among 63 of 100:
-// 127 us, and 191 with the first splits of all tasks before the others).
+// come first.
 struct Task { int s, kvh, tile, split, n_split, slot; };
-__device__ __forceinline__ Task attn_task(const CacheAttnArgs& a, int bid) {
-  Task t;
-  t.slot = bid < a.n_full ? -1 : (bid - a.n_full) / a.n_split;
-  t.n_split = t.slot < 0 ? 1 : a.n_split;
-  t.split = t.slot < 0 ? 0 : (bid - a.n_full) % a.n_split;
-  int i = t.slot < 0 ? bid : a.n_full + t.slot;
+__device__ __forceinline__ Task attn_task(const CacheAttnArgs& a, int i) {   // task i, whole
+  Task t{0, 0, 0, 0, 1, i - a.n_full};
   t.kvh = i % a.c.nkv;
   i /= a.c.nkv;
   t.tile = a.n_tiles - 1 - i % a.n_tiles;
   t.s = i / a.n_tiles;
+  return t;
+}
+// Blocks of cut tasks: as many tasks as a sequence has together, one split
+// after the other.  One long context among short ones is then under way from
+// the start (30000 tokens among 63 of 1000: 67 us, and 99 with the first splits
+// of all sequences before the others), and blocks that run together read
+// neighbouring heads of the same pages (40 heads, 58590 tokens, fp32: 131 us,
+// and 139 with a task's splits together).
+__device__ __forceinline__ Task attn_block(const CacheAttnArgs& a, int bid) {
+  const int x = bid - a.n_full;
+  if (x < 0) return attn_task(a, bid);
+  const int per = a.n_tiles * a.c.nkv, g = x / (per * a.n_split), n = min(per, a.n_cut - g * per), y = x - g * per * a.n_split;
+  Task t = attn_task(a, a.n_full + g * per + y % n);
+  t.split = y / n;
+  t.n_split = a.n_split;
   return t;
 }
 // Pages of one split where a tile's rows see `pages`; all of them: no split.
@@ -426,7 +435,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
   __shared__ float sm[4][16], sl[4][16];
   __shared__ __align__(16) float so[4][16][HD + 4];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
-  const Task task = attn_task(a, blockIdx.x);
+  const Task task = attn_block(a, blockIdx.x);
   const int s = task.s, kvh = task.kvh;
   const AttnSeq q = attn_seq(a, s);
   const int G = a.nq / a.c.nkv;
@@ -563,7 +572,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
   constexpr int KH = T::KH, ND = T::ND, VW = ND / 4;
   __shared__ uint4 sk[2][8 * KH][64], sv[2][2 * ND][64];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
-  const Task task = attn_task(a, blockIdx.x);
+  const Task task = attn_block(a, blockIdx.x);
   const int s = task.s, kvh = task.kvh;
   const AttnSeq q = attn_seq(a, s);
   const int G = a.nq / a.c.nkv;
@@ -667,7 +676,7 @@ __global__ __launch_bounds__(256) void k_cache_attn_join(CacheAttnArgs a) {
   const int G = a.nq / a.c.nkv;
   for (int64_t i = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; i < (int64_t)a.n_cut * a.tile_rows; i += (int64_t)gridDim.x * ROWS) {
     const int slot = (int)(i / a.tile_rows), r = (int)(i % a.tile_rows);
-    const Task t = attn_task(a, a.n_full + slot * a.n_split);
+    const Task t = attn_task(a, a.n_full + slot);
     const AttnSeq q = attn_seq(a, t.s);
     const int r0 = t.tile * a.tile_rows, ri = r0 + r, R = q.n * G;
     if (ri >= R) continue;
