@@ -40,7 +40,8 @@ constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;
 //
 // Rows of a tile.  16 and 32: a block's waves take pages, so that each page is
 // read once per tile, straight into registers; 64 and 128: they take rows,
-// and share pages through LDS.  Measured, us (bf16 unless said otherwise):
+// and share pages through LDS.  Measured, us (bf16 unless said otherwise; up to
+// so many rows and tokens a sequence, from half of them on):
 //   rows each                            16    32    64   128
 //   16, 64 sequences of 8000, hd 128    153   159   209   281
 //   20                                  200   163   208   277
@@ -67,11 +68,11 @@ AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32
   const int64_t pages = std::max<int64_t>(1, ((int64_t)max_kv + CACHE_PAGE - 1) / CACHE_PAGE);
   // The card holds ROUND blocks at a time.  Tasks of whole rounds are blocks of
   // their own, and the rest, or all where there are fewer, are cut to fill one
-  // (3 x 1000 rows behind 4100 tokens: 167 us, 205 uncut).  Few rows behind long
+  // (3 x up to 1000 rows behind up to 4100 tokens: 167 us, 205 uncut).  Few rows behind long
   // contexts are cut into about LONG pages in any case: lengths differ, and one
   // long sequence must not be a block's alone (100000 tokens among 63 of 1000:
   // 81 us, 600 uncut).  64 pages where the card would not be full (20 sequences
-  // of 50 to 60000 tokens: 60 us, 88 with 128), else 128 (64 of 6000: 118 us,
+  // of 50 to 60000 tokens: 60 us, 88 with 128), else 128 (64 of up to 6000: 118 us,
   // 125 with 64).  MOST_CUT bounds the workspace and the blocks that find
   // nothing to do (300 of 50 to 60000: 955 us, 1056 with half as many).
   constexpr int64_t ROUND = 512, MOST_CUT = 8192;

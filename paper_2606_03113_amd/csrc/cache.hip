@@ -308,8 +308,8 @@ template <int NW> __device__ __forceinline__ uint32_t block_most(uint32_t v, uin
 // block handles the runs that begin in its window of rows, for one KV head
 // and for keys or values.  A run that holds the page's first token starts the
 // block's scale anew; any other run keeps the old scale, or, where its rows
-// need a larger one, re-scales the page's other codes.  A prompt's rows (8193
-// of 32 heads of 128, bf16: 170 MB) are memory-bound, 33 us, 5.1 TB/s; a step's
+// need a larger one, re-scales the page's other codes.  A prompt's rows (6406
+// of 32 heads of 128, bf16: 157 MB) are memory-bound, 33 us, 4.8 TB/s; a step's
 // single rows wait for three dependent loads, 5.2 us.  The window is short
 // where blocks are few and a run's search would be repeated (48 rows: 5 us
 // with one row, 44 with 16), long where rows fill pages (the prompt: 32 us with

