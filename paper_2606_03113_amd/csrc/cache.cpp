@@ -47,8 +47,11 @@ constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;
 //   20                                  200   163   208   277
 //   40, 2 sequences of 131000           107   100    75   100
 //   80, 64 of 8000                      311   246   331   285
-//   100, 16 of 4000, 32 KV heads        187   126   145   131
-//   256                                 413   266   261   221
+//   96, 16 of 12000                           101   137   107
+//   120, 8 of 30000                           150   158   124
+//   160, 4 of 15000                            53    65    72
+//   240, 2 of 130000                          210   214   166
+//   256, 16 of 4000, 32 KV heads        413   266   261   221
 //   500, fp32                           893   732   703
 //   20, 64 of 8000, hd 64               104    87   137
 //   40                                  108   123   136
@@ -58,24 +61,31 @@ struct AttnGrid { int tile_rows, n_tiles, n_full, n_cut, n_split, min_chunk; };
 AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32_t hd, int32_t max_new, int32_t max_kv) {
   AttnGrid g;
   const int64_t rows = std::max<int64_t>(1, (int64_t)max_new * (nq / nkv));
-  if (rows <= 32) g.tile_rows = rows <= 16 ? 16 : 32;
-  else if (hd == 128) g.tile_rows = rows <= 64 ? 64 : rows < 256 ? 32 : dtype == LEDE_DTYPE_BF16 ? 128 : 64;
-  else g.tile_rows = rows < 512 ? 16 : 64;
-  // (a task takes every n_tiles-th tile: a grid need not grow with a large max_new)
+  const auto up = [](int64_t n, int64_t to) { return (n + to - 1) / to * to; };
   const int64_t groups = (int64_t)n_seqs * nkv;
+  const int64_t pages = std::max<int64_t>(1, ((int64_t)max_kv + CACHE_PAGE - 1) / CACHE_PAGE);
+  constexpr int64_t ROUND = 512, MOST_CUT = 8192;   // the card holds ROUND blocks at a time
+  // Tiles of 128: unless much of them would be empty, or a round's blocks have
+  // less than 16 pages each (8 sequences of up to 1000, 100 rows, 32 KV heads: 36
+  // us, 29 in tiles of 32).
+  const bool wide = up(rows, 128) * 4 <= up(rows, 32) * 5 && groups * (up(rows, 128) / 128) * pages >= 16 * ROUND;
+  if (rows <= 32) g.tile_rows = rows <= 16 ? 16 : 32;
+  else if (hd == 64) g.tile_rows = rows < 512 ? 16 : 64;
+  else if (rows <= 64) g.tile_rows = 64;
+  else if (dtype == LEDE_DTYPE_BF16) g.tile_rows = wide ? 128 : 32;
+  else g.tile_rows = rows < 256 ? 32 : 64;
+  // (a task takes every n_tiles-th tile: a grid need not grow with a large max_new)
   g.n_tiles = (int)std::min((rows + g.tile_rows - 1) / g.tile_rows, 65536 / groups + 1);
   const int64_t whole = groups * g.n_tiles;
-  const int64_t pages = std::max<int64_t>(1, ((int64_t)max_kv + CACHE_PAGE - 1) / CACHE_PAGE);
-  // The card holds ROUND blocks at a time.  Tasks of whole rounds are blocks of
-  // their own, and the rest, or all where there are fewer, are cut to fill one
-  // (3 x up to 1000 rows behind up to 4100 tokens: 167 us, 205 uncut).  Few rows behind long
-  // contexts are cut into about LONG pages in any case: lengths differ, and one
-  // long sequence must not be a block's alone (100000 tokens among 63 of 1000:
-  // 81 us, 600 uncut).  64 pages where the card would not be full (20 sequences
-  // of 50 to 60000 tokens: 60 us, 88 with 128), else 128 (64 of up to 6000: 118 us,
-  // 125 with 64).  MOST_CUT bounds the workspace and the blocks that find
-  // nothing to do (300 of 50 to 60000: 955 us, 1056 with half as many).
-  constexpr int64_t ROUND = 512, MOST_CUT = 8192;
+  // Tasks of whole rounds are blocks of their own, and the rest, or all where
+  // there are fewer, are cut to fill one (3 x up to 1000 rows behind up to 4100
+  // tokens: 167 us, 205 uncut).  Few rows behind long contexts are cut into about
+  // LONG pages in any case: lengths differ, and one long sequence must not be a
+  // block's alone (100000 tokens among 63 of 1000: 81 us, 600 uncut).  64 pages
+  // where the card would not be full (20 sequences of 50 to 60000 tokens: 60 us,
+  // 88 with 128), else 128 (64 of up to 6000: 118 us, 125 with 64).  MOST_CUT
+  // bounds the workspace and the blocks that find nothing to do (300 of 50 to
+  // 60000: 955 us, 1056 with half as many).
   const int64_t LONG = whole < ROUND ? 64 : 128;
   const int64_t by_length = g.tile_rows <= 32 ? (pages + LONG - 1) / LONG : 1;
   const int64_t cut = by_length > 1 ? whole : whole % ROUND;
