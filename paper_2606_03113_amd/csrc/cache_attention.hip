@@ -421,21 +421,25 @@ __device__ __forceinline__ void put4(const CacheAttnArgs& a, const AttnSeq& q, i
 // values go from memory straight into the operands' registers (no LDS, no
 // barrier), the next page's requested as soon as this one's are used; of two
 // tiles the queries are in LDS, to leave them room.  The waves meet in LDS
-// once, at the end.  Memory-bound: 64 sequences of up to 6000 tokens (8 KV
+// once, at the end.  ALONE: each wave has a task of its own, and nothing to do
+// with the others.  Memory-bound: 64 sequences of up to 6000 tokens (8 KV
 // heads of 128, 609 MB) 115-120 us, 5.1-5.3 TB/s, as fast as a kernel that only
 // reads; with 32 rows each (up to 8000 tokens, 819 MB) 164 us, 5.0 TB/s.  A second
 // page ahead in registers would not fit: the compiler spills 256 of them, and
 // the step takes 384 us.
-template <int DT, int HD, int NT>
+template <int DT, int HD, int NT, bool ALONE>
 __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
+  static_assert(!ALONE || NT == 1, "queries in LDS are the block's");
+  constexpr int STEP = ALONE ? 1 : 4;   // a wave takes every STEP-th page
   typedef Tiles<DT, HD, NT, (NT > 1)> T;
   constexpr int KH = T::KH, ND = T::ND;
   __shared__ uint4 ql[NT > 1 ? NT : 1][T::NQ][KH][2][NT > 1 ? 64 : 1];
   __shared__ int pl[NT][16];
-  __shared__ float sm[4][16], sl[4][16];
-  __shared__ __align__(16) float so[4][16][HD + 4];
+  __shared__ float sm[STEP][16], sl[STEP][16];
+  __shared__ __align__(16) float so[STEP][16][HD + 4];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
-  const Task task = attn_block(a, blockIdx.x);
+  if (ALONE && (int)blockIdx.x * 4 + w >= a.n_full) return;
+  const Task task = attn_block(a, ALONE ? blockIdx.x * 4 + w : blockIdx.x);
   const int s = task.s, kvh = task.kvh;
   const AttnSeq q = attn_seq(a, s);
   const int G = a.nq / a.c.nkv;
@@ -453,9 +457,9 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
     const int chunk = split_chunk(a, n_split, pages), j0 = task.split * chunk, j_end = min(pages, j0 + chunk);
     const bool direct = chunk >= pages;
     if (direct ? task.split > 0 : j0 >= pages) continue;
-    int j = j0 + w;
+    int j = ALONE ? j0 : j0 + w;
     Walk walk;
-    walk.load(a, table, kvh, j, 4, j_end);
+    walk.load(a, table, kvh, j, STEP, j_end);
     T tiles;
     tiles.init(a, q, kvh, G, r0, R);
     if constexpr (NT > 1) {
@@ -497,14 +501,14 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
       load_k(id);
       load_v(id);
     }
-    for (int i = 0; j < j_end; j += 4) {
+    for (int i = 0; j < j_end; j += STEP) {
       const bool known = id >= 0 && id < a.c.n_pages;
       const uint32_t wk = __builtin_amdgcn_readlane(walk.words.x, i), wv = __builtin_amdgcn_readlane(walk.words.y, i);
       const int t0 = j * CACHE_PAGE;
-      const bool more = j + 4 < j_end;
+      const bool more = j + STEP < j_end;
       if (++i == 64) {
         i = 0;
-        if (more) walk.load(a, table, kvh, j + 4, 4, j_end);
+        if (more) walk.load(a, table, kvh, j + STEP, STEP, j_end);
       }
       const int next = page_at(i);
       const int nv = known ? q.len - t0 : 0;
@@ -530,6 +534,12 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
       float sum = tiles.sum[n];
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
+      if (ALONE) {
+        if (lr < nr)
+#pragma unroll
+          for (int d = 0; d < ND; ++d) put4<DT, HD>(a, q, kvh, G, r0 + lr, 16 * d + 4 * lg, nullptr, tiles.o[n][d], tiles.base[n], sum);
+        continue;
+      }
       if (lg == 0) {
         sm[w][lr] = tiles.base[n];
         sl[w][lr] = sum;
@@ -540,11 +550,11 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
       // the waves' states joined, four dims of a row per thread
       for (int i = threadIdx.x; i < min(16, nr - 16 * n) * (HD / 4); i += 256) {
         const int r = i / (HD / 4), d = i % (HD / 4) * 4;
-        const float b = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r]));
+        const float b = fmaxf(fmaxf(sm[0][r], sm[1 % STEP][r]), fmaxf(sm[2 % STEP][r], sm[3 % STEP][r]));
         float lsum = 0.f;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < STEP; ++u) {
           const float f = __builtin_amdgcn_exp2f(sm[u][r] - b);
           lsum = fmaf(sl[u][r], f, lsum);
           const f32x4 x = *(const f32x4*)&so[u][r][d];
@@ -722,8 +732,9 @@ __global__ __launch_bounds__(256) void k_cache_attn_join(CacheAttnArgs a) {
 template <int DT, int HD>
 static hipError_t attention_hd(const CacheAttnArgs& a, hipStream_t s) {
   const unsigned blocks = (unsigned)(a.n_full + a.n_cut * a.n_split);
-  if (a.tile_rows == 16) k_cache_attn<DT, HD, 1><<<blocks, 256, 0, s>>>(a);
-  else if (a.tile_rows == 32) k_cache_attn<DT, HD, 2><<<blocks, 256, 0, s>>>(a);
+  if (a.alone) k_cache_attn<DT, HD, 1, true><<<(blocks + 3) / 4, 256, 0, s>>>(a);
+  else if (a.tile_rows == 16) k_cache_attn<DT, HD, 1, false><<<blocks, 256, 0, s>>>(a);
+  else if (a.tile_rows == 32) k_cache_attn<DT, HD, 2, false><<<blocks, 256, 0, s>>>(a);
   else if (a.tile_rows == 64) k_cache_attn_rows<DT, HD, 1><<<blocks, 256, 0, s>>>(a);
   else if constexpr (DT == 1 && HD == 128) k_cache_attn_rows<DT, HD, 2><<<blocks, 256, 0, s>>>(a);
   if (a.n_cut > 0) {

@@ -398,11 +398,11 @@ def test_attention_more_tasks_than_a_round(dtype, seqs, nq, kv, new, hd):
     news = [int(x) for x in r.integers(max(1, new - 3), new + 1, seqs)]
     cache, model, tables = _fill(kv, hd, lens, r)
     m = lede()
-    cut = m.load().lede_op_cache_attention_bytes(int(dtype == "bf16"), seqs, sum(news), nq, kv, hd, max(news), max(lens)) > 0
-    assert cut or (kv, new, hd) == (60, 400, 64)       # (more than half a round is left whole)
+    cut = [m.load().lede_op_cache_attention_bytes(int(dtype == "bf16"), seqs, sum(news), nq, kv, hd, max(news), n) > 0 for n in (max(lens), 4000)]
+    assert cut[1] or (kv, new, hd) == (60, 400, 64)       # (more than half a round is left whole)
     start = np.concatenate([[0], np.cumsum(news)])
     d, val = rounded(r.standard_normal((int(start[-1]), nq, hd)), dtype)
-    got = m.op_cache_attention(cache, d, gpu(tables), i32(lens), i32(start), max(news), max(lens)).double().cpu().numpy()
+    both = [m.op_cache_attention(cache, d, gpu(tables), i32(lens), i32(start), max(news), n).double().cpu().numpy() for n in (max(lens), 4000)]
     for s in np.unique(np.concatenate([[0, seqs - 1], r.integers(0, seqs, 12)])):     # some of them: the reference takes its time
         rows = np.unique(np.concatenate([[start[s], start[s + 1] - 1], r.integers(start[s], start[s + 1], 6)]))
         heads = np.unique(r.integers(0, nq, 5))
@@ -416,7 +416,39 @@ def test_attention_more_tasks_than_a_round(dtype, seqs, nq, kv, new, hd):
                 want = w @ v[:seen, h // (nq // kv)]
                 eps = 2.0 ** -23 * (200 * 0.125 * (np.abs(k[:seen, h // (nq // kv)]) @ np.abs(val[row, h])).max() + 200) + (2.0 ** -12 if dtype == "bf16" else 2.0 ** -22)
                 tol = 2 * eps * (w @ np.abs(v[:seen, h // (nq // kv)])) + ref.HALF_STEP[dtype] * np.abs(want) * (1 + 2 ** -6)
-                assert (np.abs(got[row, h] - want) <= tol).all(), (s, row, h)
+                for got in both:
+                    assert (np.abs(got[row, h] - want) <= tol).all(), (s, row, h)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nq,kv,hd", HEADS)
+def test_attention_many_short_sequences(dtype, nq, kv, hd):
+    """More tasks than a round of short contexts, most of them with nothing to do; rows above the expected number, an
+    infinite value that some rows see, a page outside the pool, output in place."""
+    m = lede()
+    say("attention short", dtype, nq, kv, hd)
+    r = np.random.default_rng(nq + hd)
+    none = [0] * (600 // kv)
+    lens, new = [1, 63, 64, 65, 0, 0, 128, 450, 3, 131, 5] + none, [1, 1, 1, 2, 0, 3, 0, 5, 3, 17, 9] + none
+    cache, model, tables = _fill(kv, hd, lens, r)
+    assert m.load().lede_op_cache_attention_bytes(int(dtype == "bf16"), len(lens), sum(new), nq, kv, hd, 16 // (nq // kv), 450) == 0
+    _attend(cache, model, tables, lens, new, nq, dtype, r, max_new=16 // (nq // kv))
+    slot = np.array([tables[9, 120 // 64].astype(np.int64) * 64 + 120 % 64])       # rows of the tenth sequence end at 130
+    x = _rows(r, 1, kv, hd)
+    x[0, 1, kv - 1, 17] = np.inf
+    d, val = rounded(x, dtype)
+    m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(slot))
+    model.append(val[:, 0], val[:, 1], slot)
+    got = _attend(cache, model, tables, lens, new, nq, dtype, r, max_new=16 // (nq // kv))
+    assert 0 < np.isnan(got).sum() < got.size / 3
+    start = np.concatenate([[0], np.cumsum(new)])
+    q, _ = rounded(r.standard_normal((int(start[-1]), nq, hd)), dtype)
+    tables[7, 7] = cache.n_pages       # tokens 448 ..: its last two rows
+    args = (gpu(tables), i32(lens), i32(start), 16 // (nq // kv), 450)
+    out = m.op_cache_attention(cache, q, *args)
+    rows = int(start[8])
+    assert torch.isnan(out[rows - 2:rows]).all() and not torch.isnan(out[rows - 5:rows - 2]).any()
+    assert torch.equal(torch.nan_to_num(m.op_cache_attention(cache, q, *args, out=q), 7.0), torch.nan_to_num(out, 7.0))
 
 
 def test_attention_one_long_sequence_among_short_ones():
