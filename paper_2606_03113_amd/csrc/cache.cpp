@@ -99,7 +99,7 @@ AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32
   // 2 sqrt(pages) of them take the least of both (one head of 130000 tokens: 26
   // us, 56 in chunks of 4 pages).  4 pages are a page a wave (1000 tokens: 9.0 us,
   // 10.2 in chunks of 8).
-  while (split > 1 && split * split > 4 * pages) --split;
+  split = std::min(split, (int64_t)std::sqrt(4.0 * pages));
   g.min_chunk = (int)std::max<int64_t>(4, (pages + split - 1) / split);
   g.n_split = (int)((pages + g.min_chunk - 1) / g.min_chunk);
   g.n_cut = g.n_split > 1 && !g.alone ? (int)cut : 0;

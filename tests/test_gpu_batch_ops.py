@@ -610,16 +610,21 @@ def test_attention_page_started_anew():
         assert np.isfinite(got).all() and np.abs(got).max() < 1e-2
 
 
-def test_attention_rows_do_not_depend_on_the_batch():
-    """The same bits again, and with another sequence's rows beside."""
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("expect", [4, 8, 600])
+def test_attention_rows_do_not_depend_on_the_batch(dtype, expect):
+    """The same bits again, and with other lengths, rows and queries beside."""
     m = lede()
     r = np.random.default_rng(13)
     lens, new = [2000, 500, 77], [1, 4, 1]
     cache, model, tables = _fill(4, 128, lens, r)
-    d, _ = rounded(r.standard_normal((6, 16, 128)), "bf16")
-    args = (gpu(tables), i32(lens), i32([0, 1, 5, 6]), 4, 2000)
+    d, _ = rounded(r.standard_normal((6, 16, 128)), dtype)
+    args = (gpu(tables), i32(lens), i32([0, 1, 5, 6]), expect, 2000)
     a, b = m.op_cache_attention(cache, d, *args), m.op_cache_attention(cache, d, *args)
     assert torch.equal(a, b)
+    e = torch.cat([d[:1], 30 * d[1:3], d[5:]])
+    c = m.op_cache_attention(cache, e, gpu(tables), i32([2000, 130, 77]), i32([0, 1, 3, 4]), expect, 2000)
+    assert torch.equal(c[0], a[0]) and torch.equal(c[3], a[5]) and not torch.equal(c[1], a[1])
 
 
 # ---- scores ----------------------------------------------------------------------------------------------
