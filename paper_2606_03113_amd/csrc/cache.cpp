@@ -57,7 +57,7 @@ constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;
 //   40                                  108   123   136
 //   500, 16 of 4000, 16 KV heads        158   142   138
 //   1000                                320   278   243
-struct AttnGrid { int tile_rows; bool alone; int n_tiles, n_full, n_cut, n_split, min_chunk; };
+struct AttnGrid { int tile_rows; bool alone, raw; int n_tiles, n_full, n_cut, n_split, min_chunk; };
 AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32_t hd, int32_t max_new, int32_t max_kv) {
   AttnGrid g;
   const int64_t rows = std::max<int64_t>(1, (int64_t)max_new * (nq / nkv));
@@ -104,6 +104,7 @@ AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32
   g.n_split = (int)((pages + g.min_chunk - 1) / g.min_chunk);
   g.n_cut = g.n_split > 1 && !g.alone ? (int)cut : 0;
   g.n_full = (int)(whole - g.n_cut);
+  g.raw = g.tile_rows == 64 && dtype == LEDE_DTYPE_BF16 && hd == 128 && g.n_full + (int64_t)g.n_cut * g.n_split > ROUND;
   return g;
 }
 
@@ -209,7 +210,7 @@ int lede_op_cache_attention(int32_t dtype, const void* q, int64_t ldq, const voi
   a.n_seqs = n_seqs; a.n_rows = n_rows; a.nq = n_heads;
   a.scale_log2 = (float)(std::fabs((double)scale) * 1.4426950408889634);
   a.q_sign = scale < 0 ? 0x80008000u : 0;
-  a.tile_rows = g.tile_rows; a.alone = g.alone; a.n_tiles = g.n_tiles;
+  a.tile_rows = g.tile_rows; a.alone = g.alone; a.raw = g.raw; a.n_tiles = g.n_tiles;
   a.n_full = g.n_full; a.n_cut = g.n_cut; a.n_split = g.n_split; a.min_chunk = g.min_chunk;
   a.part = (float*)workspace; a.out = out; a.ldo = ldo;
   return done(launch_cache_attention(dtype, a, S_(stream)));

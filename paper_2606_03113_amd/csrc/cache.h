@@ -68,6 +68,7 @@ struct CacheAttnArgs {
   uint32_t q_sign;       // 0x80008000 where it is negative: flips bf16 pairs' signs
   int tile_rows;         // rows a block: 16 or 32 (waves take pages), 64 or 128 (waves take rows)
   bool alone;            // 16 rows a wave, with all of their pages (n_cut = 0)
+  bool raw;              // (64 rows, bf16, heads of 128) pages as codes in LDS
   int n_tiles;           // row tiles per (sequence, KV head) of the grid
   int n_full, n_cut, n_split, min_chunk;  // blocks of whole tasks; tasks cut into n_split blocks of at least min_chunk pages
   float* part;           // [n_cut][n_split][tile_rows][hd + 4]

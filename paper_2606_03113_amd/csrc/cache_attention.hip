@@ -74,8 +74,9 @@ __device__ __forceinline__ uint4 nan_zeros(uint4 v) {
   auto zero = [](uint32_t u) { return u & (((u & 0x7FFFu) > 0x7C00u ? 0u : 0xFFFFu) | ((u >> 16 & 0x7FFFu) > 0x7C00u ? 0u : 0xFFFF0000u)); };
   return make_uint4(zero(v.x), zero(v.y), zero(v.z), zero(v.w));
 }
-// Four codes, zero where they are NaNs.
+// Four codes, and eight, zero where they are NaNs.
 __device__ __forceinline__ uint32_t nan_codes_zero(uint32_t x) { return x & ~((((x & 0x7F7F7F7F) + 0x01010101) >> 7 & 0x01010101) * 0xFFu); }
+__device__ __forceinline__ uint2 nan_zeros(uint2 c) { return make_uint2(nan_codes_zero(c.x), nan_codes_zero(c.y)); }
 // fp16 ones at the first n of an operand's eight tokens.
 __device__ __forceinline__ uint4 first_ones(int n) {
   auto two = [n](int i) { return (i < n ? 0x3C00u : 0u) | (i + 1 < n ? 0x3C000000u : 0u); };
@@ -568,6 +569,17 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
   }
 }
 
+// What a staged piece holds, codes (uint2) or their operand (uint4), from
+// codes, and its operand.
+template <bool B, class X, class Y> struct Pick { typedef X type; };
+template <class X, class Y> struct Pick<false, X, Y> { typedef Y type; };
+template <class T, bool KEYS> __device__ __forceinline__ T hold(uint2 c) {
+  if constexpr (sizeof(T) == 8) return c;
+  else return KEYS ? codes_bf16(c) : codes_f16(c);
+}
+template <bool KEYS> __device__ __forceinline__ uint4 operand(uint4 x) { return x; }
+template <bool KEYS> __device__ __forceinline__ uint4 operand(uint2 c) { return KEYS ? codes_bf16(c) : codes_f16(c); }
+
 // Many rows: four waves with 16 NT rows each walk the same pages.  A page comes
 // into LDS once per block, as 16-bit operands in the order in which the lanes
 // take them (16 bytes per lane, a contiguous KiB per operand: no bank
@@ -575,12 +587,17 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
 // two pages' room, so one barrier a page.  Bound by the matrix units and the
 // exponentials beside them: 1008 TFLOP/s over whole rounds of 128-row tiles
 // (bf16, heads of 128), against 1269 of a large library product; with the codes
-// themselves in LDS, converted by every wave, 920.
-template <int DT, int HD, int NT>
+// themselves in LDS, converted by every wave, 920.  RAW: codes all the same, for
+// 64 bf16 rows and heads of 128 behind long contexts, bound by memory: half the
+// LDS makes room for a third block, where there is one (30 sequences of up to
+// 20000 tokens: 229 us, 266 with operands; 2 of up to 131000, one round of
+// blocks: 81 and 79).
+template <int DT, int HD, int NT, bool RAW>
 __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
   typedef Tiles<DT, HD, NT> T;
   constexpr int KH = T::KH, ND = T::ND, VW = ND / 4;
-  __shared__ uint4 sk[2][8 * KH][64], sv[2][2 * ND][64];
+  typedef typename Pick<RAW, uint2, uint4>::type Held;
+  __shared__ Held sk[2][8 * KH][64], sv[2][2 * ND][64];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
   const Task task = attn_block(a, blockIdx.x);
   const int s = task.s, kvh = task.kvh;
@@ -621,13 +638,13 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
         for (int d = 0; d < VW; ++d) vr[d] = keep_tokens(vr[d], nv - 16 * lg);
 #pragma unroll
       for (int h = 0; h < KH; ++h) {
-        sk[buf][2 * (w * KH + h)][l] = codes_bf16(make_uint2(kr[h].x, kr[h].y));
-        sk[buf][2 * (w * KH + h) + 1][l] = codes_bf16(make_uint2(kr[h].z, kr[h].w));
+        sk[buf][2 * (w * KH + h)][l] = hold<Held, true>(make_uint2(kr[h].x, kr[h].y));
+        sk[buf][2 * (w * KH + h) + 1][l] = hold<Held, true>(make_uint2(kr[h].z, kr[h].w));
       }
 #pragma unroll
       for (int d = 0; d < VW; ++d) {
-        sv[buf][2 * (w * VW + d)][l] = codes_f16(make_uint2(vr[d].x, vr[d].y));
-        sv[buf][2 * (w * VW + d) + 1][l] = codes_f16(make_uint2(vr[d].z, vr[d].w));
+        sv[buf][2 * (w * VW + d)][l] = hold<Held, false>(make_uint2(vr[d].x, vr[d].y));
+        sv[buf][2 * (w * VW + d) + 1][l] = hold<Held, false>(make_uint2(vr[d].z, vr[d].w));
       }
     };
     int id = 0;
@@ -649,7 +666,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
       id = __builtin_amdgcn_readlane(walk.id, i);
       if (more) load(id);
       if (__builtin_expect((wv & CACHE_NAN) != 0, 0)) {   // (the same for the whole block)
-        tiles.mark_nans(j * CACHE_PAGE, [&](int d, int half) { return sv[buf][2 * d + half][l]; });
+        tiles.mark_nans(j * CACHE_PAGE, [&](int d, int half) { return operand<false>(sv[buf][2 * d + half][l]); });
         __syncthreads();
 #pragma unroll
         for (int d = 0; d < 2 * VW; ++d) sv[buf][2 * w * VW + d][l] = nan_zeros(sv[buf][2 * w * VW + d][l]);
@@ -657,8 +674,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
       }
       // (a wave whose rows end before the page, or that has none, computes masked scores: a branch
       // around the page costs every page a copy of the accumulators)
-      tiles.page(a, j * CACHE_PAGE, pos_lo, known, wk, wv, [&](int t, int h, int half) { return sk[buf][2 * (t * KH + h) + half][l]; },
-                 [&](int d, int half) { return sv[buf][2 * d + half][l]; }, [] {});
+      tiles.page(a, j * CACHE_PAGE, pos_lo, known, wk, wv, [&](int t, int h, int half) { return operand<true>(sk[buf][2 * (t * KH + h) + half][l]); },
+                 [&](int d, int half) { return operand<false>(sv[buf][2 * d + half][l]); }, [] {});
       if (more) stage(buf ^ 1, id, j + 1);
       __syncthreads();
     }
@@ -735,8 +752,11 @@ static hipError_t attention_hd(const CacheAttnArgs& a, hipStream_t s) {
   if (a.alone) k_cache_attn<DT, HD, 1, true><<<(blocks + 3) / 4, 256, 0, s>>>(a);
   else if (a.tile_rows == 16) k_cache_attn<DT, HD, 1, false><<<blocks, 256, 0, s>>>(a);
   else if (a.tile_rows == 32) k_cache_attn<DT, HD, 2, false><<<blocks, 256, 0, s>>>(a);
-  else if (a.tile_rows == 64) k_cache_attn_rows<DT, HD, 1><<<blocks, 256, 0, s>>>(a);
-  else if constexpr (DT == 1 && HD == 128) k_cache_attn_rows<DT, HD, 2><<<blocks, 256, 0, s>>>(a);
+  else if (a.tile_rows == 64 && !a.raw) k_cache_attn_rows<DT, HD, 1, false><<<blocks, 256, 0, s>>>(a);
+  else if constexpr (DT == 1 && HD == 128) {
+    if (a.raw) k_cache_attn_rows<DT, HD, 1, true><<<blocks, 256, 0, s>>>(a);
+    else k_cache_attn_rows<DT, HD, 2, false><<<blocks, 256, 0, s>>>(a);
+  }
   if (a.n_cut > 0) {
     const int64_t rows = (int64_t)a.n_cut * a.tile_rows;
     const int64_t need = rows * (HD / 4) / 256;

@@ -389,7 +389,7 @@ def test_attention_huge_scores(dtype, rows, expect):
 
 @pytest.mark.parametrize("dtype,seqs,nq,kv,new,hd", [("bf16", 131, 4, 4, 1, 64), ("f32", 200, 3, 3, 2, 64), ("bf16", 9, 60, 60, 70, 64), ("bf16", 70, 8, 8, 9, 64),
                                                      ("f32", 70, 8, 8, 17, 64), ("bf16", 3, 60, 60, 400, 64), ("bf16", 3, 80, 40, 300, 64), ("bf16", 3, 60, 60, 400, 128),
-                                                     ("f32", 3, 32, 16, 400, 128)])
+                                                     ("f32", 3, 32, 16, 400, 128), ("bf16", 70, 48, 8, 8, 128)])
 def test_attention_more_tasks_than_a_round(dtype, seqs, nq, kv, new, hd):
     """Whole rounds of blocks and a cut rest, few and many rows."""
     say("attention tasks", dtype, seqs, nq, kv, new)
@@ -422,32 +422,33 @@ def test_attention_more_tasks_than_a_round(dtype, seqs, nq, kv, new, hd):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("nq,kv,hd", HEADS)
-def test_attention_many_short_sequences(dtype, nq, kv, hd):
+@pytest.mark.parametrize("rows", [16, 64])
+def test_attention_many_short_sequences(dtype, nq, kv, hd, rows):
     """More tasks than a round of short contexts, most of them with nothing to do; rows above the expected number, an
     infinite value that some rows see, a page outside the pool, output in place."""
-    m = lede()
+    m, most = lede(), rows // (nq // kv)
     say("attention short", dtype, nq, kv, hd)
     r = np.random.default_rng(nq + hd)
     none = [0] * (600 // kv)
     lens, new = [1, 63, 64, 65, 0, 0, 128, 450, 3, 131, 5] + none, [1, 1, 1, 2, 0, 3, 0, 5, 3, 17, 9] + none
     cache, model, tables = _fill(kv, hd, lens, r)
-    assert m.load().lede_op_cache_attention_bytes(int(dtype == "bf16"), len(lens), sum(new), nq, kv, hd, 16 // (nq // kv), 450) == 0
-    _attend(cache, model, tables, lens, new, nq, dtype, r, max_new=16 // (nq // kv))
+    assert rows > 16 or m.load().lede_op_cache_attention_bytes(int(dtype == "bf16"), len(lens), sum(new), nq, kv, hd, most, 450) == 0
+    _attend(cache, model, tables, lens, new, nq, dtype, r, max_new=most)
     slot = np.array([tables[9, 120 // 64].astype(np.int64) * 64 + 120 % 64])       # rows of the tenth sequence end at 130
     x = _rows(r, 1, kv, hd)
     x[0, 1, kv - 1, 17] = np.inf
     d, val = rounded(x, dtype)
     m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(slot))
     model.append(val[:, 0], val[:, 1], slot)
-    got = _attend(cache, model, tables, lens, new, nq, dtype, r, max_new=16 // (nq // kv))
+    got = _attend(cache, model, tables, lens, new, nq, dtype, r, max_new=most)
     assert 0 < np.isnan(got).sum() < got.size / 3
     start = np.concatenate([[0], np.cumsum(new)])
     q, _ = rounded(r.standard_normal((int(start[-1]), nq, hd)), dtype)
     tables[7, 7] = cache.n_pages       # tokens 448 ..: its last two rows
-    args = (gpu(tables), i32(lens), i32(start), 16 // (nq // kv), 450)
+    args = (gpu(tables), i32(lens), i32(start), most, 450)
     out = m.op_cache_attention(cache, q, *args)
-    rows = int(start[8])
-    assert torch.isnan(out[rows - 2:rows]).all() and not torch.isnan(out[rows - 5:rows - 2]).any()
+    end = int(start[8])
+    assert torch.isnan(out[end - 2:end]).all() and not torch.isnan(out[end - 5:end - 2]).any()
     assert torch.equal(torch.nan_to_num(m.op_cache_attention(cache, q, *args, out=q), 7.0), torch.nan_to_num(out, 7.0))
 
 
