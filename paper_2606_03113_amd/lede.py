@@ -600,7 +600,7 @@ def _call(device, what: str, fn, *args):
     index = device.index
     _need(index is not None, what + ": tensors on the GPU")
     stream = torch._C._cuda_getCurrentRawStream   # (torch.cuda.current_stream builds an object: 1.9 us against 0.1)
-    if index == torch.cuda.current_device():
+    if index == torch._C._cuda_getDevice():       # (torch.cuda.current_device checks for initialisation first: 0.7 us against 0.2)
         rc = fn(*args, stream(index))
     else:
         with torch.cuda.device(index):
