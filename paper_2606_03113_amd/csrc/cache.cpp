@@ -57,6 +57,13 @@ constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;
 //   40                                  108   123   136
 //   500, 16 of 4000, 16 KV heads        158   142   138
 //   1000                                320   278   243
+// Time of a page in a block that has its CU to itself, us (measured over 150
+// pages, the fewest rows of hd 128 from memory).
+double page_us(int32_t dtype, int32_t hd, int tile_rows) {
+  static const double T[2][2][4] = {{{.33, .45, 1.03, 0}, {.22, .30, .79, 0}}, {{.65, .70, 1.6, 0}, {.50, .42, 1.12, 1.45}}};
+  return T[hd == 128][dtype == LEDE_DTYPE_BF16][tile_rows == 16 ? 0 : tile_rows == 32 ? 1 : tile_rows == 64 ? 2 : 3];
+}
+
 struct AttnGrid { int tile_rows; bool alone, raw; int n_tiles, n_full, n_cut, n_split, min_chunk; };
 AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32_t hd, int32_t max_new, int32_t max_kv) {
   AttnGrid g;
@@ -77,32 +84,46 @@ AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32
   // (a task takes every n_tiles-th tile: a grid need not grow with a large max_new)
   g.n_tiles = (int)std::min((rows + g.tile_rows - 1) / g.tile_rows, 65536 / groups + 1);
   const int64_t whole = groups * g.n_tiles;
+  // Short contexts of many tasks: a wave each, without a block's start, meeting
+  // and end (2560 tasks of up to 128 tokens: 21 us, 28 with a block each; up to
+  // 400: 45 and 43, and 18 and 20 with 640 tasks; up to 800: 93 and 81).
+  g.alone = g.tile_rows == 16 && pages <= 8 && whole > ROUND;
   // Tasks of whole rounds are blocks of their own, and the rest, or all where
   // there are fewer, are cut to fill one (3 x up to 1000 rows behind up to 4100
-  // tokens: 167 us, 205 uncut).  Few rows behind long contexts are cut into about
+  // tokens: 157 us, 205 uncut).  Few rows behind long contexts are cut into about
   // LONG pages in any case: lengths differ, and one long sequence must not be a
   // block's alone (100000 tokens among 63 of 1000: 81 us, 600 uncut).  64 pages
   // where the card would not be full (20 sequences of 50 to 60000 tokens: 60 us,
   // 88 with 128), else 128 (64 of up to 6000: 118 us, 125 with 64).  MOST_CUT
   // bounds the workspace and the blocks that find nothing to do (300 of 50 to
-  // 60000: 955 us, 1056 with half as many).
-  // Short contexts of many tasks: a wave each, without a block's start, meeting
-  // and end (2560 tasks of up to 128 tokens: 21 us, 28 with a block each; up to
-  // 400: 45 and 43, and 18 and 20 with 640 tasks; up to 800: 93 and 81).
-  g.alone = g.tile_rows == 16 && pages <= 8 && whole > ROUND;
+  // 60000: 955 us, 1056 with half as many).  A split's pages follow each other,
+  // and so do the splits in the join: 2 sqrt(pages) of them at most (one head of
+  // 130000 tokens: 26 us in 90 splits, 56 in 512).
   const int64_t LONG = whole < ROUND ? 64 : 128;
   const int64_t by_length = g.tile_rows <= 32 ? (pages + LONG - 1) / LONG : 1;
-  const int64_t cut = by_length > 1 ? whole : whole % ROUND;
+  const int64_t cut = g.alone ? 0 : by_length > 1 ? whole : whole % ROUND;
   int64_t split = cut ? std::max(whole < ROUND ? (ROUND + whole - 1) / whole : by_length > 1 ? 1 : ROUND / cut, by_length) : 1;
-  split = std::min(split, std::max<int64_t>(1, MOST_CUT / std::max<int64_t>(cut, 1)));
-  // A split's pages follow each other, and so do the splits in the join: about
-  // 2 sqrt(pages) of them take the least of both (one head of 130000 tokens: 26
-  // us, 56 in chunks of 4 pages).  4 pages are a page a wave (1000 tokens: 9.0 us,
-  // 10.2 in chunks of 8).
-  split = std::min(split, (int64_t)std::sqrt(4.0 * pages));
-  g.min_chunk = (int)std::max<int64_t>(4, (pages + split - 1) / split);
-  g.n_split = (int)((pages + g.min_chunk - 1) / g.min_chunk);
-  g.n_cut = g.n_split > 1 && !g.alone ? (int)cut : 0;
+  split = std::min({split, std::max<int64_t>(1, MOST_CUT / std::max<int64_t>(cut, 1)), (int64_t)std::sqrt(4.0 * pages)});
+  // A join costs its launch, its splits and its bytes, and short splits do not
+  // earn it back: fewer (half, a quarter, ..) where a model of both says so (5 x
+  // 100 rows, 16 pages: 15.6 us whole, 25 in four; 64 pages: 38 whole, 36 in two).
+  const double page = page_us(dtype, hd, g.tile_rows), page_full = std::max(1.5 * page, ROUND * 128.0 * hd / 5.3e6);
+  double best = INFINITY;
+  for (int64_t k = split;; k = std::max<int64_t>(1, k / 2)) {
+    const int64_t chunk = std::max<int64_t>(4, (pages + k - 1) / k), n = (pages + chunk - 1) / chunk, c = n > 1 ? cut : 0;
+    const int64_t blocks = whole - c + c * n;
+    const double steps = double(whole - c) * pages + double(c) * n * chunk;
+    double us = 4 * std::max(1.0, blocks / double(ROUND)) + std::max((c < whole ? pages : chunk) * page, steps / ROUND * page_full);
+    if (blocks > ROUND) us += 0.3 * (c ? chunk : pages) * page;
+    if (c) us += 2 + 0.07 * n + c * n * g.tile_rows * (hd + 4) * 8 / 8e6;
+    if (us < best) {
+      best = us;
+      g.n_cut = (int)c;
+      g.n_split = c ? (int)n : 1;
+      g.min_chunk = (int)chunk;
+    }
+    if (k == 1 || k / 2 < by_length) break;
+  }
   g.n_full = (int)(whole - g.n_cut);
   g.raw = g.tile_rows == 64 && dtype == LEDE_DTYPE_BF16 && hd == 128 && g.n_full + (int64_t)g.n_cut * g.n_split > ROUND;
   return g;
