@@ -135,14 +135,15 @@ constexpr int32_t MOST_TOP = 32;
 
 // Tiles of a row (its first may begin inside a 16-byte piece: up to 7
 // entries before it), and how many of them a block takes: as many as leave
-// the card about 1024 blocks (400 rows of 128256: 33 us, 36 with 512, 39 with
-// 2048), and all of up to four (5 rows of 32000: 12.1 us in one launch; a block
-// per tile takes 11.2, but a second launch and a workspace on the host).
+// the card about 1024 blocks (400 rows of 128256: 34 us, 37 with 512, 40 with
+// 2048), all of them from 512 rows on (1000 rows: 60 us, 69 in two parts), and all
+// of up to four (5 rows of 32000: 13.3 us in one launch; a block per tile takes
+// 12.8, but a second launch and a workspace on the host).
 struct ScoreGrid { int n_tiles, part_tiles, n_part; };
 ScoreGrid score_grid(int32_t n_rows, int32_t V) {
   ScoreGrid g;
   g.n_tiles = (V + 7 + LP_TILE - 1) / LP_TILE;
-  const int parts = g.n_tiles <= 4 ? 1 : std::min(g.n_tiles, std::max(1, (int)((1024 + (int64_t)n_rows - 1) / std::max(n_rows, 1))));
+  const int parts = g.n_tiles <= 4 || n_rows >= 512 ? 1 : std::min(g.n_tiles, std::max(1, (int)((1024 + (int64_t)n_rows - 1) / std::max(n_rows, 1))));
   g.part_tiles = std::min((g.n_tiles + parts - 1) / parts, LP_PART_TILES);
   g.n_part = (g.n_tiles + g.part_tiles - 1) / g.part_tiles;
   return g;
