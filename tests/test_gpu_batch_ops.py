@@ -728,18 +728,32 @@ def test_logprobs_rising_rows():
         _score(z, [V - 1, V - 1, 471, 100], 32, 1.0, dtype)
 
 
-def test_logprobs_many_rows():
-    """More rows than a round of blocks, a row a block and with rows cut in parts: each against the same row alone."""
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("each", [1, 17, 31, 32, 40])
+def test_logprobs_equal_tops_in_every_part(dtype, each):
+    """As many largest entries, equal or nearly, in every part of a long row: none of the parts has the row's top tokens."""
+    V = 1 << 20
+    r = np.random.default_rng(each)
+    z = -1.0 - r.random((2, V))
+    at = (np.arange(0, V - 8192, 8192)[:, None] + 100 + 3 * np.arange(each)).reshape(-1)
+    z[0, at] = 5.0
+    z[1, at] = 5.0 + r.integers(0, 2, len(at)) / 32
+    _score(z, [at[-1], 0], 32, 1.0, dtype)
+
+
+@pytest.mark.parametrize("rows,V", [(1100, 40001), (530, 135001)])
+def test_logprobs_many_rows(rows, V):
+    """More rows than a round of blocks, a row a block and with rows cut in parts (few rows, or longer than a block takes): each against the same row alone."""
     m = lede()
     r = np.random.default_rng(7)
-    z = gpu(r.standard_normal((1100, 40001)).astype(np.float32) * 2)
-    tok = i32(r.integers(0, 40001, 1100))
+    z = gpu(r.standard_normal((rows, V)).astype(np.float32) * 2)
+    tok = i32(r.integers(0, V, rows))
     all_rows, few = m.op_logprobs(z, tok, 9, 0.7), m.op_logprobs(z[300:340], tok[300:340], 9, 0.7)
     for a, b in ((all_rows.ranks, few.ranks), (all_rows.top_ids, few.top_ids)):
         assert torch.equal(a[300:340], b)
     lp = torch.log_softmax(z.double() / 0.7, 1)
     want = lp.gather(1, tok.long()[:, None])[:, 0]
-    tol = ref.score_tolerance(want.cpu().numpy(), 40001)
+    tol = ref.score_tolerance(want.cpu().numpy(), V)
     assert (np.abs(all_rows.logprobs.double().cpu().numpy() - want.cpu().numpy()) <= tol).all()
     ids = torch.sort(z, dim=1, descending=True, stable=True).indices[:, :9]
     assert torch.equal(all_rows.top_ids.long(), ids)
