@@ -27,14 +27,25 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // times larger, and a high and a low part, 22 bits, for fp32.  Below 2^-14
 // they lose bits, below 2^-25 they vanish: 2^-33 (bf16) or 2^-38 (fp32) of
 // the largest term, from a million tokens together less than the rounding of
-// the output.  The sum of 2^(x - E_v) is kept in fp32 at 2^-SUM_DOWN, which
-// holds every scale's range.
-constexpr int P_LIM = 15, SUM_DOWN = 10;
+// the output.
+// A page of small values (E_v = -100 if all are zero) has small terms, but its
+// full part in the sum of 2^(x - E_v).  Where E_v is more than EV_NEAR below
+// the largest so far, that part is formed in fp32 from exponents without the
+// difference; nearer pages' weights give theirs as the product takes them, and
+// lose less than 2^-28 of the largest weight each.  The sum is kept in fp32 at
+// 2^-SUM_DOWN, and where B moves or sums of different B meet, it takes the
+// factor in two halves: E_v goes from -100 to 120, so sums from 2^-122 to
+// 2^105, for one token of the largest weight.
+constexpr int P_LIM = 15, SUM_DOWN = 10, EV_NEAR = 4;
 constexpr float B_NONE = -1e30f;   // B of a row that has seen nothing
 // From scores of 2^22 on, where fp32 has no room for B's whole part, the
 // multiply and the add are rounded one by one, so that the largest score
 // itself comes out as it went into B.
 constexpr float B_FAR = 4194304.f;
+
+// The square root of 2^d: a sum that is re-based takes it twice, since it may
+// be as large as 2^d is small (B follows the values' scales, 2^-100 to 2^120).
+__device__ __forceinline__ float half_step(float d) { return __builtin_amdgcn_exp2f(0.5f * d); }
 
 // Token of a page that row `r` of its score tile `t` (16 tokens x 16 queries)
 // holds.  A lane then has, of its query, the scores of 16 consecutive tokens
@@ -147,6 +158,7 @@ struct Tiles {
   const uint4 (*ql)[NQ][KH][2][64];   // [NT]
   f32x4 o[NT][ND];
   float sum[NT], base[NT];
+  int ev_most;                        // the largest value exponent of the pages so far
   int pos[QL ? 1 : NT];
   const int (*pl)[16];                // [NT]: positions, beside the queries
 
@@ -185,6 +197,7 @@ struct Tiles {
   }
 
   __device__ __forceinline__ void init(const CacheAttnArgs& a, const AttnSeq& q, int kvh, int G, int r0, int R) {
+    ev_most = INT_MIN / 2;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int rr = row_at(r0, n, R);
@@ -211,6 +224,9 @@ struct Tiles {
     const int lg = (threadIdx.x & 63) >> 4;
     const float ks = ldexpf(a.scale_log2, (int)(wk & 255) - 127);
     const int ev = (int)(wv & 255) - 127;
+    const int gap = ev_most - ev;
+    const bool small = gap > EV_NEAR;
+    ev_most = max(ev_most, ev);
     // lane: token t0 + 16 lg + 4 t + i of its query.  Two key tiles at a time:
     // products on one accumulator wait for each other
     f32x4 x[NT][4];
@@ -278,15 +294,15 @@ struct Tiles {
         for (int i = 0; i < 4; ++i) m = fmaxf(m, x[n][t][i]);
       m *= kx;   // (the scale is not negative: q takes its sign)
       float off = up;
-      if (__ballot(m + up > P_LIM)) {
+      if (small || __ballot(m + up > P_LIM)) {
         // the row's new B, the same in its four lanes
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
         const float b = !(m + up > P_LIM) ? base[n] : fabsf(m) < B_FAR ? ceilf(m + ev) : m + (float)(ev + P_UP);
-        const float f = __builtin_amdgcn_exp2f(base[n] - b);
+        const float h = half_step(base[n] - b), f = h * h;
         base[n] = b;
         off = (float)(ev + P_UP) - b;
-        sum[n] *= f;
+        sum[n] = sum[n] * h * h;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -301,6 +317,18 @@ struct Tiles {
               x[n][t][i] = y > most ? most : y;
             }
           kx = 1.f;
+        }
+        if (small) {
+          // a small page's part of the sum, 2^more times as large, where the
+          // row's limit leaves room
+          const float more = fminf((float)gap, fmaxf(P_LIM - ceilf(m + off), 0.f));
+          const float near = fabsf(off) > B_FAR ? 0.f : more, rest = more - near;   // (whole numbers, while off is one)
+          float own = 0.f;
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) own += __builtin_amdgcn_exp2f(fmaf(x[n][t][i], kx, off + near) + rest);
+          sum[n] += ldexpf(own, -ev - SUM_DOWN - (int)more);
         }
       }
       float ps = 0.f;
@@ -330,7 +358,7 @@ struct Tiles {
           }
           pf[n][p][half] = make_uint4(u[0], u[1], u[2], u[3]);
         }
-      sum[n] = fmaf(ps, ldexpf(1.f, -ev - SUM_DOWN), sum[n]);
+      sum[n] = fmaf(ps, small ? 0.f : ldexpf(1.f, -ev - SUM_DOWN), sum[n]);
     }
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -556,8 +584,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < STEP; ++u) {
-          const float f = __builtin_amdgcn_exp2f(sm[u][r] - b);
-          lsum = fmaf(sl[u][r], f, lsum);
+          const float h = half_step(sm[u][r] - b), f = h * h;
+          lsum = fmaf(sl[u][r] * h, h, lsum);
           const f32x4 x = *(const f32x4*)&so[u][r][d];
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[e] = fmaf(x[e], f, acc[e]);
@@ -725,13 +753,17 @@ __global__ __launch_bounds__(256) void k_cache_attn_join(CacheAttnArgs a) {
         bs[u] = *(const float2*)(x + HD);
         pa[u] = *(const f32x4*)(x + d);
       }
-      float nb = b;
+      float nb = b, low = INFINITY;
 #pragma unroll
-      for (int u = 0; u < B; ++u) nb = fmaxf(nb, j0 + u < n ? bs[u].x : B_NONE);
-      const float f0 = __builtin_amdgcn_exp2f(b - nb);
-      sum *= f0;
+      for (int u = 0; u < B; ++u) {
+        nb = fmaxf(nb, j0 + u < n ? bs[u].x : B_NONE);
+        low = fminf(low, j0 + u < n ? bs[u].x : INFINITY);
+      }
+      const float h0 = half_step(b - nb), f0 = h0 * h0;
+      sum = sum * h0 * h0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] *= f0;
+      const float before = sum;
 #pragma unroll
       for (int u = 0; u < B; ++u) {
         const bool live = j0 + u < n;
@@ -739,6 +771,14 @@ __global__ __launch_bounds__(256) void k_cache_attn_join(CacheAttnArgs a) {
         sum = live ? fmaf(bs[u].y, f, sum) : sum;
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] = live ? fmaf(pa[u][e], f, acc[e]) : acc[e];
+      }
+      if (__ballot(low - nb < -120.f)) {   // 2^(low - nb) is no number, its part of the sum may be one
+        sum = before;
+#pragma unroll
+        for (int u = 0; u < B; ++u) {
+          const float h = half_step(bs[u].x - nb);
+          sum = j0 + u < n ? fmaf(bs[u].y * h, h, sum) : sum;
+        }
       }
       b = nb;
     }

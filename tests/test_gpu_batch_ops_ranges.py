@@ -1,0 +1,88 @@
+"""The batch operators where magnitudes are far apart, against their plain fp64 counterparts: pages whose values differ by
+many powers of two, in every variant of the attention."""
+import numpy as np
+import pytest
+
+from tests import batch_reference as ref
+from tests.parity import say
+from tests.test_gpu_batch_ops import _attend, _fill, gpu, lede, rounded
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+# (sequences, rows and cached tokens expected), which choose the variant and how pages are split; the work itself is
+# that of a few rows behind some pages
+VARIANTS = {
+    "rows16": (2, 1, 40000),          # a block's waves take every fourth page
+    "rows16-cut": (2, 1, 768),        # and a page each, three splits joined
+    "alone": (300, 1, 400),           # a wave has all pages
+    "rows32": (2, 12, 40000),
+    "rows32-cut": (2, 12, 768),
+    "rows64": (2, 30, 40000),         # waves take rows, and all of them every page
+    "rows64-cut": (2, 30, 768),
+    "rows64-more": (300, 30, 768),    # more blocks than a round: pages as codes (bf16)
+    "rows128": (2, 2000, 40000),      # (bf16)
+    "rows128-more": (60, 1000, 768),
+}
+KV, NQ = 2, 4
+
+
+def _check(variant, dtype, hd, sizes, r, keys=None, q=None, values=None):
+    """One sequence whose pages' values have the given sizes (0: all zero), beside a short one and empty ones."""
+    m = lede()
+    seqs, max_new, max_kv = VARIANTS[variant]
+    length = 64 * len(sizes) - 5
+    lens, new = [length, 70] + [0] * (seqs - 2), [3, 1] + [0] * (seqs - 2)
+    cache, model, tables = _fill(KV, hd, lens, r)
+    x = r.standard_normal((length, 2, KV, hd)) if values is None else values(length)
+    x[:, 0] *= 0.3
+    if keys is not None:
+        x[:, 0] = keys(length)[:, None, None]
+    x[:, 1] *= np.repeat(np.asarray(sizes, float), 64)[:length, None, None]
+    d, val = rounded(x, "bf16")
+    p = np.arange(length)
+    slots = tables[0, p // 64].astype(np.int64) * 64 + p % 64
+    m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(slots))
+    model.append(val[:, 0], val[:, 1], slots)
+    return _attend(cache, model, tables, lens, new, NQ, dtype, r, max_new=max_new, max_kv=max_kv, q=q)
+
+
+def _sizes(pattern, n=12):
+    """The sizes of a sequence's pages."""
+    if pattern == "zeros-behind":
+        return [1.0 if p % 3 == 0 else 0.0 for p in range(n)]
+    if pattern == "zeros-before":
+        return [0.0 if p < 5 else 1.0 for p in range(n)]
+    if pattern == "zero-last":
+        return [1.0] * 6 + [0.0] + [1.0] * (n - 7)
+    where, ratio = pattern.split("/")
+    at = {"first": (0, 1, 2, 3), "middle": (2, 5, 8), "last": (6, n - 1), "one": (1,)}[where]
+    small, large = {"20": (-10, 10), "33": (0, 33), "60": (-30, 30), "100": (-60, 40), "190": (-90, 100)}[ratio]
+    return [2.0 ** (large if p in at else small) for p in range(n)]
+
+
+PATTERNS = ["zeros-behind", "zeros-before", "zero-last"] + [w + "/" + x for x in ("20", "33", "60", "100", "190") for w in ("first", "middle", "last", "one")]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("variant", list(VARIANTS))
+def test_attention_pages_of_any_size_keep_their_weight(dtype, hd, variant):
+    """A page has its part of the softmax whatever its values are: all zero, or smaller or larger than others' by many
+    powers of two, before and behind them."""
+    r = np.random.default_rng(hd)
+    for pattern in PATTERNS:
+        say("attention sizes", dtype, hd, variant, pattern)
+        _check(variant, dtype, hd, _sizes(pattern), r)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("variant", list(VARIANTS))
+def test_attention_small_weights_of_small_pages(dtype, variant):
+    """Thousands of tokens 12 nats below one whose page has values 2^16 larger hold some percent of the weight."""
+    r = np.random.default_rng(31)
+    q = np.full((6, NQ, 64), 0.25)
+    for gap in (10.0, 12.0, 13.0):
+        say("attention gap", dtype, variant, gap)
+        # (scores 64^-0.5 q.k = 2 k: the first page's are `gap` nats larger)
+        _check(variant, dtype, 64, [2.0 ** 16] * 4 + [1.0] * 60, r, keys=lambda n: np.where(np.arange(n) == 0, gap / 4, -gap / 4), q=q)
