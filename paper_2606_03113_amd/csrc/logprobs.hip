@@ -19,6 +19,7 @@ namespace lede {
 // (5.2 and 4.7 TB/s); a running list of the top ones took 162.
 constexpr int LP_THREADS = 256, LP_PER = 32;
 static_assert(LP_THREADS * LP_PER == LP_TILE, "a tile is LP_PER entries per thread");
+constexpr float LP_FAR = 65536.f;   // |max c| from which the difference comes before the product everywhere
 constexpr int LP_MAX_TOP = 32;
 constexpr int LP_LIST = 512;     // candidates
 constexpr int LP_SETS = 128;     // (tile, thread) pairs that are read again
@@ -174,10 +175,11 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs(LogprobsArgs a) {
     if (tm > r.m) rebase(r, tm, c);
     const float shift = r.m == -INFINITY ? 0.f : r.m, sc = shift * c;
     const int v0 = t * LP_TILE - lead;
-    if (v0 >= 0 && v0 + LP_TILE <= V && (tok < v0 || tok >= v0 + LP_TILE) && __ballot(fabsf(sc) < 1e30f) == ~0ull) {
+    if (v0 >= 0 && v0 + LP_TILE <= V && (tok < v0 || tok >= v0 + LP_TILE) && __ballot(fabsf(sc) < LP_FAR) == ~0ull) {
       // a whole tile before or behind the token: one bound for all, counted
       // on the scalar unit.  x = z c - sc, one operation; sc's rounding,
-      // the same for all of them, is put right at the end of the tile
+      // the same for all of them, is put right at the end of the tile: it is
+      // at most 2^-9, and 2^off = 1 + g + g^2 / 2 to 2^-31, g = off ln 2
       const float thr = v0 < tok ? thr_before : zt;
       float s = 0.f, w = 0.f;
       int n = 0;
@@ -193,9 +195,10 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs(LogprobsArgs a) {
         __builtin_amdgcn_sched_barrier(0);   // (pieces one after the other: all at once take twice the registers)
       }
       const float off = -fmaf(shift, c, -sc);   // the true x is off larger
+      const float g1 = off * 0.6931472f, g = fmaf(0.5f * g1, g1, g1);
       w = fmaf(off, s, w);
-      r.s += fmaf(s, off * 0.6931472f, s);
-      r.w += fmaf(w, off * 0.6931472f, w);
+      r.s += fmaf(s, g, s);
+      r.w += fmaf(w, g, w);
       if (!(nan_tok && v0 > tok)) before_wave += n;
     } else {
 #pragma unroll

@@ -1,5 +1,5 @@
 """The batch operators where magnitudes are far apart, against their plain fp64 counterparts: pages whose values differ by
-many powers of two, in every variant of the attention."""
+many powers of two, in every variant of the attention, and scores of logits far from zero or of low temperatures."""
 import numpy as np
 import pytest
 
@@ -86,3 +86,51 @@ def test_attention_small_weights_of_small_pages(dtype, variant):
         say("attention gap", dtype, variant, gap)
         # (scores 64^-0.5 q.k = 2 k: the first page's are `gap` nats larger)
         _check(variant, dtype, 64, [2.0 ** 16] * 4 + [1.0] * 60, r, keys=lambda n: np.where(np.arange(n) == 0, gap / 4, -gap / 4), q=q)
+
+
+# ---- scores ----------------------------------------------------------------------------------------------------
+
+
+def _close(got, z, T, tokens, top):
+    for i in range(len(z)):
+        lp, rank, h, ids, tlp = ref.scores(z[i], T, -1 if tokens is None else int(tokens[i]), top)
+        for a, b in ((got.entropy[i], h), (got.top_logprobs[i], tlp)) + (((got.logprobs[i], lp),) if tokens is not None else ()):
+            a, b = np.asarray(a.cpu(), np.float64), np.asarray(b, np.float64)
+            assert (np.abs(a - b) <= ref.score_tolerance(b, z.shape[1])).all(), (i, a, b)
+        assert tokens is None or int(got.ranks[i]) == rank
+        assert got.top_ids[i].tolist() == list(ids)
+
+
+def _far_rows(r, V, size):
+    """Logits whose magnitude is far above their differences, the largest at different places, and equal ones."""
+    z = r.standard_normal((5, V)) * 5 * max(1.0, size / 2 ** 22)
+    z[1, V // 2] = z[1].max() + 30
+    z[2] = 0.0
+    z[3, : V - 8192] = -3.0
+    return z + np.array([size, size, size, -size, -size])[:, None]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [3 * 8192 + 40, 60001])        # whole rows, and rows in parts that are joined
+def test_logprobs_temperatures_near_zero(dtype, V):
+    """Low temperatures over rows of whole tiles: the largest products of a logit and 1/T, small differences among them."""
+    r = np.random.default_rng(V)
+    z, val = rounded(np.concatenate([r.standard_normal((2, V)) * 5, r.standard_normal((1, V)) * 1e-5 + 12.0, np.full((1, V), -7.3)]), dtype)
+    tokens = np.array([3, int(val[1].argmax()), V - 1, 20000], np.int32)
+    for T in (1e-2, 1e-3, 1e-4, 1e-5, 1e-6, 1e-7, 1e-12, 1e-30):
+        for given in (tokens, None):
+            say("logprobs", dtype, V, T, given is None)
+            _close(lede().op_logprobs(z, None if given is None else gpu(given), 8, T), val, T, given, 8)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [3 * 8192 + 40, 60001])
+def test_logprobs_far_logits(dtype, V):
+    """Logits far from zero, as masks and offsets leave them, over rows of whole tiles."""
+    r = np.random.default_rng(V + 1)
+    for size in (1e3, 65504.0, 1e6, 1e7, 1e9, 1e20, 1e36):
+        z, val = rounded(_far_rows(r, V, size), dtype)
+        tokens = np.array([V - 1, 0, 9000, V - 1, 5], np.int32)
+        for given in (tokens, None):
+            say("logprobs", dtype, V, size, given is None)
+            _close(lede().op_logprobs(z, None if given is None else gpu(given), 8), val, 1.0, given, 8)
