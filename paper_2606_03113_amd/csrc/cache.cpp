@@ -230,7 +230,7 @@ int lede_op_cache_attention(int32_t dtype, const void* q, int64_t ldq, const voi
   a.c = cache_view((void*)cache, n_pages, n_kv_heads, head_dim);
   a.q = q; a.ldq = ldq; a.tables = tables; a.table_ld = table_ld; a.kv_lens = kv_lens; a.row_start = row_start;
   a.n_seqs = n_seqs; a.n_rows = n_rows; a.nq = n_heads;
-  a.scale_log2 = (float)(std::fabs((double)scale) * 1.4426950408889634);
+  a.scale_log2x2 = (float)(std::fabs((double)scale) * 2 * 1.4426950408889634);
   a.q_sign = scale < 0 ? 0x80008000u : 0;
   a.tile_rows = g.tile_rows; a.alone = g.alone; a.raw = g.raw; a.n_tiles = g.n_tiles;
   a.n_full = g.n_full; a.n_cut = g.n_cut; a.n_split = g.n_split; a.min_chunk = g.min_chunk;

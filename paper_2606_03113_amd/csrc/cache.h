@@ -64,7 +64,7 @@ struct CacheAttnArgs {
   const int32_t* tables; int table_ld;
   const int32_t *kv_lens, *row_start;
   int n_seqs, n_rows, nq;
-  float scale_log2;      // magnitude of the softmax scale, times log2(e)
+  float scale_log2x2;    // magnitude of the softmax scale, times 2 log2(e)
   uint32_t q_sign;       // 0x80008000 where it is negative: flips bf16 pairs' signs
   int tile_rows;         // rows a block: 16 or 32 (waves take pages), 64 or 128 (waves take rows)
   bool alone;            // 16 rows a wave, with all of their pages (n_cut = 0)

@@ -16,10 +16,11 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // q is exact in one bf16 operand (bf16 queries) or in three (fp32 queries).
 // With E_k and E_v a page's scale exponents and c_t, d_t its codes, the kernels
 // form the exponent of a whole term of the sum,
-//   x_t = scale log2(e) 2^E_k q . c_t + E_v - B,  o = sum 2^x_t d_t / sum 2^(x_t - E_v),
+//   x_t = scale log2(e) q . (2^E_k c_t) + E_v - B,  o = sum 2^x_t d_t / sum 2^(x_t - E_v),
 // so that the value product's accumulators take any mix of scales, its
 // weights 2^x are as precise as the term's share of the result asks, and both
-// scales cost nothing (one of the multiply, one of the add of a fused step).
+// scales cost nothing (one an operand of the codes' conversion, one of the add
+// of a fused step).
 // B is a whole number (its rounding cancels), P_UP below the largest x so
 // far, and follows it only when some x passes P_LIM: until then neither the
 // accumulators nor the maximum across lanes are touched.  The weights enter
@@ -52,12 +53,18 @@ __device__ __forceinline__ float half_step(float d) { return __builtin_amdgcn_ex
 // (16 lg + 4 t + i from rows 4 lg + i), which is the value product's operand.
 __device__ __forceinline__ int tile_token(int t, int r) { return (r >> 2) * 16 + 4 * t + (r & 3); }
 
-// Eight codes as a bf16 or fp16 matrix operand.
-__device__ __forceinline__ uint4 codes_bf16(uint2 c) {
-  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, 1.f, false)),
-                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, 1.f, true)),
-                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, 1.f, false)),
-                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, 1.f, true)));
+// Half the scale of a page's keys, from its scale word: codes times it are the
+// keys' halves, which bf16 holds for every scale (448 2^120 is above its
+// largest number), so that a product overflows where half the score does.
+__device__ __forceinline__ float key_scale(uint32_t word) { return __uint_as_float((max(word & 255, 127u + CACHE_E_MIN) - 1) << 23); }
+
+// Eight codes times a power of two as a bf16 matrix operand, and as they are
+// as an fp16 one.
+__device__ __forceinline__ uint4 codes_bf16(uint2 c, float scale) {
+  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, scale, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, scale, true)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, scale, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, scale, true)));
 }
 __device__ __forceinline__ uint4 codes_f16(uint2 c) {
   return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c.x, 1.f, false)),
@@ -214,15 +221,15 @@ struct Tiles {
     return QL ? ql[n][p][h][half][threadIdx.x & 63] : qf[QL ? 0 : n][p][h][half];
   }
 
-  // One page: tokens t0 .. t0 + 63; this lane's key operand (t, h, half) and
-  // value operand (d, half) from kf and vf.  wk and wv: its scale words.
+  // One page: tokens t0 .. t0 + 63; this lane's key operand (t, h, half), times
+  // key_scale, and value operand (d, half) from kf and vf.  wv: its values'
+  // scale word.
   // pos_lo: the lowest position of the tiles' rows.  after_keys() once the
   // keys are used.
   template <class KF, class VF, class AK>
-  __device__ __forceinline__ void page(const CacheAttnArgs& a, int t0, int pos_lo, bool known, uint32_t wk, uint32_t wv, KF kf, VF vf,
+  __device__ __forceinline__ void page(const CacheAttnArgs& a, int t0, int pos_lo, bool known, uint32_t wv, KF kf, VF vf,
                                        AK after_keys) {
     const int lg = (threadIdx.x & 63) >> 4;
-    const float ks = ldexpf(a.scale_log2, (int)(wk & 255) - 127);
     const int ev = (int)(wv & 255) - 127;
     const int gap = ev_most - ev;
     const bool small = gap > EV_NEAR;
@@ -277,7 +284,7 @@ struct Tiles {
     for (int n = 0; n < NT; ++n) {
       const float up = (float)(ev + P_UP) - base[n];
       const bool far = __ballot(fabsf(up) > B_FAR) != 0;
-      float m = -INFINITY, kx = ks;   // x = kx x' + up
+      float m = -INFINITY, kx = a.scale_log2x2;   // x = kx x' + up
       if (edge || far) {
         // a table entry outside the pool: rows that see the page become NaN
         kx = 1.f;
@@ -286,7 +293,7 @@ struct Tiles {
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            x[n][t][i] = t0 + 16 * lg + 4 * t + i > last ? -INFINITY : known ? x[n][t][i] * ks : __builtin_nanf("");
+            x[n][t][i] = t0 + 16 * lg + 4 * t + i > last ? -INFINITY : known ? x[n][t][i] * a.scale_log2x2 : __builtin_nanf("");
       }
 #pragma unroll
       for (int t = 0; t < 4; ++t)
@@ -551,8 +558,9 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
         for (int d = 0; d < ND; ++d)
           vf[d] = make_uint4(nan_codes_zero(vf[d].x), nan_codes_zero(vf[d].y), nan_codes_zero(vf[d].z), nan_codes_zero(vf[d].w));
       }
-      tiles.page(a, t0, pos_lo, known, wk, wv,
-                 [&](int t, int h, int half) { return codes_bf16(half ? make_uint2(kf[t][h].z, kf[t][h].w) : make_uint2(kf[t][h].x, kf[t][h].y)); },
+      const float ks = key_scale(wk);
+      tiles.page(a, t0, pos_lo, known, wv,
+                 [&](int t, int h, int half) { return codes_bf16(half ? make_uint2(kf[t][h].z, kf[t][h].w) : make_uint2(kf[t][h].x, kf[t][h].y), ks); },
                  value, [&] { if (more) load_k(next); });
       if (more) load_v(next);
       id = next;
@@ -598,15 +606,15 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
 }
 
 // What a staged piece holds, codes (uint2) or their operand (uint4), from
-// codes, and its operand.
+// codes, and its operand.  ks: the keys' scale.
 template <bool B, class X, class Y> struct Pick { typedef X type; };
 template <class X, class Y> struct Pick<false, X, Y> { typedef Y type; };
-template <class T, bool KEYS> __device__ __forceinline__ T hold(uint2 c) {
+template <class T, bool KEYS> __device__ __forceinline__ T hold(uint2 c, float ks = 1.f) {
   if constexpr (sizeof(T) == 8) return c;
-  else return KEYS ? codes_bf16(c) : codes_f16(c);
+  else return KEYS ? codes_bf16(c, ks) : codes_f16(c);
 }
-template <bool KEYS> __device__ __forceinline__ uint4 operand(uint4 x) { return x; }
-template <bool KEYS> __device__ __forceinline__ uint4 operand(uint2 c) { return KEYS ? codes_bf16(c) : codes_f16(c); }
+template <bool KEYS> __device__ __forceinline__ uint4 operand(uint4 x, float = 1.f) { return x; }
+template <bool KEYS> __device__ __forceinline__ uint4 operand(uint2 c, float ks = 1.f) { return KEYS ? codes_bf16(c, ks) : codes_f16(c); }
 
 // Many rows: four waves with 16 NT rows each walk the same pages.  A page comes
 // into LDS once per block, as 16-bit operands in the order in which the lanes
@@ -659,15 +667,16 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
 #pragma unroll
       for (int d = 0; d < VW; ++d) vr[d] = ld16(vb + d * 16 * CACHE_PAGE);
     };
-    auto stage = [&](int buf, int id, int j) {
+    auto stage = [&](int buf, int id, int j, uint32_t wk) {
+      const float ks = key_scale(wk);
       const int nv = id >= 0 && id < a.c.n_pages ? q.len - j * CACHE_PAGE : 0;
       if (nv < CACHE_PAGE)
 #pragma unroll
         for (int d = 0; d < VW; ++d) vr[d] = keep_tokens(vr[d], nv - 16 * lg);
 #pragma unroll
       for (int h = 0; h < KH; ++h) {
-        sk[buf][2 * (w * KH + h)][l] = hold<Held, true>(make_uint2(kr[h].x, kr[h].y));
-        sk[buf][2 * (w * KH + h) + 1][l] = hold<Held, true>(make_uint2(kr[h].z, kr[h].w));
+        sk[buf][2 * (w * KH + h)][l] = hold<Held, true>(make_uint2(kr[h].x, kr[h].y), ks);
+        sk[buf][2 * (w * KH + h) + 1][l] = hold<Held, true>(make_uint2(kr[h].z, kr[h].w), ks);
       }
 #pragma unroll
       for (int d = 0; d < VW; ++d) {
@@ -676,22 +685,26 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
       }
     };
     int id = 0;
+    uint32_t wk = 0;   // of the page in LDS, as id
     if (j0 < j_end) {
       walk.load(a, table, kvh, j0, 1, j_end);
       id = __builtin_amdgcn_readlane(walk.id, 0);
+      wk = __builtin_amdgcn_readlane(walk.words.x, 0);
       load(id);
-      stage(0, id, j0);
+      stage(0, id, j0, wk);
     }
     __syncthreads();
     for (int j = j0, i = 0, buf = 0; j < j_end; ++j, buf ^= 1) {
       const bool known = id >= 0 && id < a.c.n_pages;
-      const uint32_t wk = __builtin_amdgcn_readlane(walk.words.x, i), wv = __builtin_amdgcn_readlane(walk.words.y, i);
+      const uint32_t wv = __builtin_amdgcn_readlane(walk.words.y, i);
+      const float ks = key_scale(wk);   // (of codes in LDS)
       const bool more = j + 1 < j_end;
       if (++i == 64) {
         i = 0;
         if (more) walk.load(a, table, kvh, j + 1, 1, j_end);
       }
       id = __builtin_amdgcn_readlane(walk.id, i);
+      wk = __builtin_amdgcn_readlane(walk.words.x, i);
       if (more) load(id);
       if (__builtin_expect((wv & CACHE_NAN) != 0, 0)) {   // (the same for the whole block)
         tiles.mark_nans(j * CACHE_PAGE, [&](int d, int half) { return operand<false>(sv[buf][2 * d + half][l]); });
@@ -702,9 +715,9 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
       }
       // (a wave whose rows end before the page, or that has none, computes masked scores: a branch
       // around the page costs every page a copy of the accumulators)
-      tiles.page(a, j * CACHE_PAGE, pos_lo, known, wk, wv, [&](int t, int h, int half) { return operand<true>(sk[buf][2 * (t * KH + h) + half][l]); },
+      tiles.page(a, j * CACHE_PAGE, pos_lo, known, wv, [&](int t, int h, int half) { return operand<true>(sk[buf][2 * (t * KH + h) + half][l], ks); },
                  [&](int d, int half) { return operand<false>(sv[buf][2 * d + half][l]); }, [] {});
-      if (more) stage(buf ^ 1, id, j + 1);
+      if (more) stage(buf ^ 1, id, j + 1, wk);
       __syncthreads();
     }
 #pragma unroll

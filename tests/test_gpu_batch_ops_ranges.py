@@ -88,6 +88,45 @@ def test_attention_small_weights_of_small_pages(dtype, variant):
         _check(variant, dtype, 64, [2.0 ** 16] * 4 + [1.0] * 60, r, keys=lambda n: np.where(np.arange(n) == 0, gap / 4, -gap / 4), q=q)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("variant", list(VARIANTS))
+def test_attention_scores_as_large_as_fp32_holds(dtype, variant):
+    """Scores up to fp32's largest, and ordinary ones of the largest and smallest keys."""
+    m = lede()
+    seqs, max_new, max_kv = VARIANTS[variant]
+    r = np.random.default_rng(55)
+    hd, length, best = 64, 300, 150
+    lens, start = np.array([length] + [0] * (seqs - 1), np.int32), np.array([0] + [3] * seqs, np.int32)
+    table = np.tile(np.arange(5, dtype=np.int32), (seqs, 1))
+    cache, model = m.Cache(5, KV, hd), ref.CacheModel(5, KV, hd)
+    x = np.zeros((length, 2, KV, hd))
+    x[:, 0, :, 0] = (1.0 + np.arange(length) % 7 / 8)[:, None]
+    x[best, 0, :, 0] = 2.25
+    x[:, 1] = r.standard_normal((length, KV, hd))
+    d, val = rounded(x, "bf16")
+    m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(np.arange(length)))
+    model.append(val[:, 0], val[:, 1], np.arange(length))
+    for size in (1e35, 3e36, 1e37, 1e38):
+        say("attention largest", dtype, variant, size)
+        q = np.zeros((3, NQ, hd), np.float32)
+        q[:, :, 0] = size
+        got = m.op_cache_attention(cache, rounded(q, dtype)[0], gpu(table), gpu(lens), gpu(start), max_new, max_kv, scale=1.0)
+        got = got.double().cpu().numpy()
+        for h in range(NQ):      # (the best token's weight is a power of two: two half steps are the quotient's and the output's)
+            want = model.read([best])[1][0, h // (NQ // KV)]
+            assert (np.abs(got[:, h] - want) <= ref.HALF_STEP[dtype] * 2 * np.abs(want)).all(), (size, h)
+    for k in (-90, 100, 118):
+        say("attention keys", dtype, variant, k)
+        cache, model = m.Cache(5, KV, hd), ref.CacheModel(5, KV, hd)
+        x = r.standard_normal((length, 2, KV, hd))
+        x[:, 0] *= 0.3 * 2.0 ** k
+        d, val = rounded(x, "bf16")
+        m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(np.arange(length)))
+        model.append(val[:, 0], val[:, 1], np.arange(length))
+        q = r.standard_normal((5, NQ, hd)) * 2.0 ** -k
+        _attend(cache, model, table, lens.tolist(), [3] + [0] * (seqs - 1), NQ, dtype, r, max_new=max_new, max_kv=max_kv, q=q)
+
+
 # ---- scores ----------------------------------------------------------------------------------------------------
 
 
