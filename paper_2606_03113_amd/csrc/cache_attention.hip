@@ -38,7 +38,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // factor in two halves: E_v goes from -100 to 120, so sums from 2^-122 to
 // 2^105, for one token of the largest weight.
 constexpr int P_LIM = 15, SUM_DOWN = 10, EV_NEAR = 4;
-constexpr float B_NONE = -1e30f;   // B of a row that has seen nothing
+constexpr float B_NONE = -__FLT_MAX__;   // B of a row that has seen nothing (any finite score sets B, this one too)
 // From scores of 2^22 on, where fp32 has no room for B's whole part, the
 // multiply and the add are rounded one by one, so that the largest score
 // itself comes out as it went into B.
@@ -282,12 +282,16 @@ struct Tiles {
     uint4 pf[NT][NP][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const float up = (float)(ev + P_UP) - base[n];
+      float up = (float)(ev + P_UP) - base[n], off = up;
       const bool far = __ballot(fabsf(up) > B_FAR) != 0;
       float m = -INFINITY, kx = a.scale_log2x2;   // x = kx x' + up
       if (edge || far) {
         // a table entry outside the pool: rows that see the page become NaN
         kx = 1.f;
+        if (base[n] == B_NONE) {
+          up = INFINITY;
+          off = 0.f;
+        }
         const int last = position(n);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -300,7 +304,6 @@ struct Tiles {
 #pragma unroll
         for (int i = 0; i < 4; ++i) m = fmaxf(m, x[n][t][i]);
       m *= kx;   // (the scale is not negative: q takes its sign)
-      float off = up;
       if (small || __ballot(m + up > P_LIM)) {
         // the row's new B, the same in its four lanes
         m = fmaxf(m, __shfl_xor(m, 16));

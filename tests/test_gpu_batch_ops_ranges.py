@@ -127,6 +127,41 @@ def test_attention_scores_as_large_as_fp32_holds(dtype, variant):
         _attend(cache, model, table, lens.tolist(), [3] + [0] * (seqs - 1), NQ, dtype, r, max_new=max_new, max_kv=max_kv, q=q)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("variant", list(VARIANTS))
+def test_attention_hugely_negative_scores(dtype, variant):
+    """Rows all of whose scores are far below zero: the largest one's value, as long as fp32 holds the scores."""
+    m = lede()
+    seqs, max_new, max_kv = VARIANTS[variant]
+    r = np.random.default_rng(61)
+    kv, hd, length, best = 2, 64, 300, 150
+    cache, model = m.Cache(5, kv, hd), ref.CacheModel(5, kv, hd)
+    x = np.zeros((length, 2, kv, hd))
+    x[:, 0, :, 0] = (1.0 + np.arange(length) % 7 / 8)[:, None]
+    x[best, 0, :, 0] = 0.5
+    x[:, 1] = r.standard_normal((length, kv, hd)) * np.exp2(np.arange(length) // 64 * 3)[:, None, None]
+    d, val = rounded(x, "bf16")
+    m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(np.arange(length)))
+    model.append(val[:, 0], val[:, 1], np.arange(length))
+    value = model.read([best])[1][0, 0], model.read([best])[1][0, 1]
+    # The best token's weight is the sum.  bf16: both are the same 11 bits, so the output's rounding is all, with room for as
+    # much again.  fp32: half steps of the weight in two parts (2 x 11 bits, 1), of its two products in the accumulator, whose
+    # additions may cut off (2 each), of the reciprocal, of the product with it and of the exponential in the sum (1 each).
+    steps = 2 if dtype == "bf16" else 8
+    table = np.tile(np.arange(5, dtype=np.int32), (seqs, 1))
+    start = np.array([0] + [3] * seqs, np.int32)
+    lens = np.array([length] + [0] * (seqs - 1), np.int32)
+    for size in (1e3, 1e8, 1e20, 1e29, 1e30, 3e30, 1e32, 1e35, 1e37, 1e38):
+        say("attention negative", dtype, variant, size)
+        q = np.zeros((3, NQ, hd), np.float32)
+        q[:, :, 0] = -size
+        got = m.op_cache_attention(cache, rounded(q, dtype)[0], gpu(table), gpu(lens), gpu(start), max_new, max_kv, scale=1.0)
+        got = got.double().cpu().numpy()
+        for h in range(NQ):
+            want = value[h // (NQ // kv)]
+            assert (np.abs(got[:, h] - want) <= ref.HALF_STEP[dtype] * steps * np.abs(want)).all(), (size, h)
+
+
 # ---- scores ----------------------------------------------------------------------------------------------------
 
 
