@@ -576,7 +576,7 @@ int lede_op_read_groups(const void* src, int32_t n_groups, int32_t tiles, uint32
  * the values code * 2^e.  Layout: key codes [n_pages][n_kv][64][head_dim],
  * value codes [n_pages][n_kv][head_dim][64], scale words
  * [n_pages][n_kv][2] (uint32: keys, values) of e + 127, plus 256 when the
- * block holds a NaN.  head_dim is 64 or 128, n_kv at most 1024
+ * block holds a NaN; a block of the cleared region holds zeros.  head_dim is 64 or 128, n_kv at most 1024
  * (LEDE_E_UNSUPPORTED; lede_op_cache_bytes returns 0). */
 size_t lede_op_cache_bytes(int32_t n_pages, int32_t n_kv_heads, int32_t head_dim);
 

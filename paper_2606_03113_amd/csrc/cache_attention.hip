@@ -230,7 +230,7 @@ struct Tiles {
   __device__ __forceinline__ void page(const CacheAttnArgs& a, int t0, int pos_lo, bool known, uint32_t wv, KF kf, VF vf,
                                        AK after_keys) {
     const int lg = (threadIdx.x & 63) >> 4;
-    const int ev = (int)(wv & 255) - 127;
+    const int ev = max((int)(wv & 255) - 127, CACHE_E_MIN);   // (a word of a block never written is 0)
     const int gap = ev_most - ev;
     const bool small = gap > EV_NEAR;
     ev_most = max(ev_most, ev);

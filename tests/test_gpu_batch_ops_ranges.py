@@ -162,6 +162,27 @@ def test_attention_hugely_negative_scores(dtype, variant):
             assert (np.abs(got[:, h] - want) <= ref.HALF_STEP[dtype] * steps * np.abs(want)).all(), (size, h)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("variant", list(VARIANTS))
+def test_attention_pages_never_written(dtype, variant):
+    """Pages of a cleared cache that no append has reached are tokens of zero keys and values."""
+    m = lede()
+    seqs, max_new, max_kv = VARIANTS[variant]
+    r = np.random.default_rng(51)
+    n, hd = 7, 64
+    length = 64 * n - 9
+    for written in ((1, 2, 3, 4, 5, 6), (0, 5), (6,)):
+        say("attention cleared", dtype, variant, written)
+        cache, model = m.Cache(n + 1, KV, hd), ref.CacheModel(n + 1, KV, hd)
+        for page in written:
+            d, val = rounded(r.standard_normal((64, 2, KV, hd)), "bf16")
+            slots = page * 64 + np.arange(64)
+            m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(slots))
+            model.append(val[:, 0], val[:, 1], slots)
+        tables = np.tile(np.arange(n, dtype=np.int32), (seqs, 1))
+        _attend(cache, model, tables, [length, 70] + [0] * (seqs - 2), [3, 1] + [0] * (seqs - 2), NQ, dtype, r, max_new=max_new, max_kv=max_kv)
+
+
 # ---- scores ----------------------------------------------------------------------------------------------------
 
 
