@@ -33,11 +33,14 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // full part in the sum of 2^(x - E_v).  Where E_v is more than EV_NEAR below
 // the largest so far, that part is formed in fp32 from exponents without the
 // difference; nearer pages' weights give theirs as the product takes them, and
-// lose less than 2^-28 of the largest weight each.  The sum is kept in fp32 at
+// lose less than 2^-28 of the largest weight each.  Its product has dims, too,
+// in which the large pages hold zeros: its weights are 2^lift as large, and so
+// is o while they are added (2^O_LIFT at most, below which o has room: 2^15 448
+// and 2^24 tokens).  The sum is kept in fp32 at
 // 2^-SUM_DOWN, and where B moves or sums of different B meet, it takes the
 // factor in two halves: E_v goes from -100 to 120, so sums from 2^-122 to
 // 2^105, for one token of the largest weight.
-constexpr int P_LIM = 15, SUM_DOWN = 10, EV_NEAR = 4;
+constexpr int P_LIM = 15, SUM_DOWN = 10, EV_NEAR = 4, O_LIFT = 64;
 constexpr float B_NONE = -__FLT_MAX__;   // B of a row that has seen nothing (any finite score sets B, this one too)
 // From scores of 2^22 on, where fp32 has no room for B's whole part, the
 // multiply and the add are rounded one by one, so that the largest score
@@ -166,6 +169,8 @@ struct Tiles {
   f32x4 o[NT][ND];
   float sum[NT], base[NT];
   int ev_most;                        // the largest value exponent of the pages so far
+  float lift[NT];                     // o is at 2^lift
+  bool lifted;                        // (otherwise all are 0)
   int pos[QL ? 1 : NT];
   const int (*pl)[16];                // [NT]: positions, beside the queries
 
@@ -205,11 +210,12 @@ struct Tiles {
 
   __device__ __forceinline__ void init(const CacheAttnArgs& a, const AttnSeq& q, int kvh, int G, int r0, int R) {
     ev_most = INT_MIN / 2;
+    lifted = false;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int rr = row_at(r0, n, R);
       if (!QL) pos[QL ? 0 : n] = q.len - q.n + rr / G;
-      sum[n] = 0.f;
+      sum[n] = lift[n] = 0.f;
       base[n] = B_NONE;
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -219,6 +225,21 @@ struct Tiles {
   __device__ __forceinline__ int position(int n) const { return QL ? pl[n][threadIdx.x & 15] : pos[QL ? 0 : n]; }
   __device__ __forceinline__ uint4 query(int n, int p, int h, int half) const {
     return QL ? ql[n][p][h][half][threadIdx.x & 63] : qf[QL ? 0 : n][p][h][half];
+  }
+
+  // The value sums of tile n at 2^to, and all at 1.
+  __device__ __forceinline__ void lift_sums(int n, float to) {
+    const float f = __builtin_amdgcn_exp2f(to - lift[n]);
+    lift[n] = to;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[n][d][i] *= f;
+  }
+  __device__ __forceinline__ void settle() {
+    if (lifted)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) lift_sums(n, 0.f);
   }
 
   // One page: tokens t0 .. t0 + 63; this lane's key operand (t, h, half), times
@@ -304,7 +325,7 @@ struct Tiles {
 #pragma unroll
         for (int i = 0; i < 4; ++i) m = fmaxf(m, x[n][t][i]);
       m *= kx;   // (the scale is not negative: q takes its sign)
-      if (small || __ballot(m + up > P_LIM)) {
+      if (small || lifted || __ballot(m + up > P_LIM)) {
         // the row's new B, the same in its four lanes
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
@@ -328,17 +349,28 @@ struct Tiles {
             }
           kx = 1.f;
         }
-        if (small) {
-          // a small page's part of the sum, 2^more times as large, where the
-          // row's limit leaves room
-          const float more = fminf((float)gap, fmaxf(P_LIM - ceilf(m + off), 0.f));
-          const float near = fabsf(off) > B_FAR ? 0.f : more, rest = more - near;   // (whole numbers, while off is one)
-          float own = 0.f;
+        if (small || lifted) {
+          // a small page's weights as if its values were the largest, 2^more
+          // times as large, where the row's limit leaves room
+          float next = 0.f;
+          if (small) {
+            const float more = fminf((float)gap, fmaxf(P_LIM - ceilf(m + off), 0.f));
+            const float near = fabsf(off) > B_FAR ? 0.f : more, rest = more - near;   // (whole numbers, while off is one)
+            next = fminf(more, (float)O_LIFT);
+            float own = 0.f;
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) own += __builtin_amdgcn_exp2f(fmaf(x[n][t][i], kx, off + near) + rest);
-          sum[n] += ldexpf(own, -ev - SUM_DOWN - (int)more);
+              for (int i = 0; i < 4; ++i) {
+                const float y = fmaf(x[n][t][i], kx, off + near) + rest;
+                own += __builtin_amdgcn_exp2f(y);
+                x[n][t][i] = y - (more - next);
+              }
+            kx = 1.f;
+            off = 0.f;
+            sum[n] += ldexpf(own, -ev - SUM_DOWN - (int)more);
+          }
+          lift_sums(n, next);
         }
       }
       float ps = 0.f;
@@ -395,6 +427,7 @@ struct Tiles {
       if (NT > 1) __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
+    lifted = small;
   }
 
   // A page with NaN values: they reach the rows that see their tokens, and no
@@ -568,6 +601,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
       if (more) load_v(next);
       id = next;
     }
+    tiles.settle();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       if (16 * n >= nr) break;
@@ -723,6 +757,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
       if (more) stage(buf ^ 1, id, j + 1, wk);
       __syncthreads();
     }
+    tiles.settle();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       float sum = tiles.sum[n];

@@ -183,6 +183,23 @@ def test_attention_pages_never_written(dtype, variant):
         _attend(cache, model, tables, [length, 70] + [0] * (seqs - 2), [3, 1] + [0] * (seqs - 2), NQ, dtype, r, max_new=max_new, max_kv=max_kv)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("variant", list(VARIANTS))
+def test_attention_dims_that_only_small_pages_have(dtype, variant):
+    """Large pages whose values are zero but for one dim: the others' sums are the small pages' alone."""
+    r = np.random.default_rng(41)
+    for ratio in (10, 25, 40, 60):
+        for at in ((0,), (3, 4), (0, 2, 5)):
+            say("attention dims", dtype, variant, ratio, at)
+
+            def values(n):
+                x = r.standard_normal((n, 2, KV, 128))
+                x[np.isin(np.arange(n) // 64, at), 1, :, 1:] = 0.0
+                return x
+            sizes = [2.0 ** (ratio - ratio // 2 if p in at else -(ratio // 2)) for p in range(12)]
+            _check(variant, dtype, 128, sizes, r, values=values)
+
+
 # ---- scores ----------------------------------------------------------------------------------------------------
 
 
