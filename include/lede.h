@@ -576,8 +576,9 @@ int lede_op_read_groups(const void* src, int32_t n_groups, int32_t tiles, uint32
  * the values code * 2^e.  Layout: key codes [n_pages][n_kv][64][head_dim],
  * value codes [n_pages][n_kv][head_dim][64], scale words
  * [n_pages][n_kv][2] (uint32: keys, values) of e + 127, plus 256 when the
- * block holds a NaN; a block of the cleared region holds zeros.  head_dim is 64 or 128, n_kv at most 1024
- * (LEDE_E_UNSUPPORTED; lede_op_cache_bytes returns 0). */
+ * block holds a NaN; a block of the cleared region holds zeros.  head_dim is
+ * 64 or 128, n_kv at most 1024 (LEDE_E_UNSUPPORTED; lede_op_cache_bytes
+ * returns 0). */
 size_t lede_op_cache_bytes(int32_t n_pages, int32_t n_kv_heads, int32_t head_dim);
 
 /* Page tables and the slot map of a pass.  Sequence s has seq_lens[s] cached
@@ -652,7 +653,7 @@ int lede_op_cache_read(int32_t dtype, const void* cache, int32_t n_pages, int32_
  * stays with the rows that see it.
  * workspace: lede_op_cache_attention_bytes of the same sizes (may be 0).
  * LEDE_E_ARG: null pointers, bad sizes, n_heads not a multiple of n_kv_heads,
- * a scale that is not finite, a small workspace; q, out, cache, workspace or
+ * a scale that is not within +-1e38, a small workspace; q, out, cache, workspace or
  * row strides not multiples of 16 bytes.  LEDE_E_UNSUPPORTED: more than 65535
  * sequences, more than 65536 heads, 2^30 (row, head of a group) pairs or 2^23
  * (sequence, KV head) pairs. */

@@ -217,7 +217,7 @@ int lede_op_cache_attention(int32_t dtype, const void* q, int64_t ldq, const voi
   if (!dtype_ok(dtype) || !cache || !tables || !kv_lens || !row_start || n_seqs < 1 || n_rows < 0 || table_ld < 1)
     return LEDE_E_ARG;
   if (int rc = check_cache(n_pages, n_kv_heads, head_dim)) return rc;
-  if (n_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_kv < 0 || !std::isfinite(scale)) return LEDE_E_ARG;
+  if (n_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_kv < 0 || !(std::fabs(scale) <= 1e38f)) return LEDE_E_ARG;   // (2 log2(e) scale is finite)
   if (n_seqs > MOST_SEQS || (int64_t)n_seqs * n_kv_heads > MOST_BLOCKS / 2 || n_heads > 65536 || (int64_t)n_rows * (n_heads / n_kv_heads) >= 1ll << 30) return LEDE_E_UNSUPPORTED;
   if (!aligned(cache, 16)) return LEDE_E_ARG;
   if (n_rows == 0) return LEDE_OK;
