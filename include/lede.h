@@ -651,7 +651,8 @@ int lede_op_cache_read(int32_t dtype, const void* cache, int32_t n_pages, int32_
  * NaN.  kv_lens above 64 * table_ld count as that, row_start is held to [0,
  * n_rows].  Scores, softmax statistics and sums are fp32; a NaN or infinity
  * stays with the rows that see it.
- * workspace: lede_op_cache_attention_bytes of the same sizes (may be 0).
+ * workspace: lede_op_cache_attention_bytes of the same sizes (may be 0, as it
+ * is for sizes that the call refuses).
  * LEDE_E_ARG: null pointers, bad sizes, n_heads not a multiple of n_kv_heads,
  * a scale that is not within +-1e38, a small workspace; q, out, cache, workspace or
  * row strides not multiples of 16 bytes.  LEDE_E_UNSUPPORTED: more than 65535

@@ -75,7 +75,7 @@ AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32
   // Tiles of 128: unless much of them would be empty, or a round's blocks have
   // less than 16 pages each (8 sequences of up to 1000, 100 rows, 32 KV heads: 36
   // us, 29 in tiles of 32).
-  const bool wide = up(rows, 128) * 4 <= up(rows, 32) * 5 && groups * (up(rows, 128) / 128) * pages >= 16 * ROUND;
+  const bool wide = up(rows, 128) * 4 <= up(rows, 32) * 5 && double(groups) * double(up(rows, 128) / 128) * double(pages) >= 16.0 * ROUND;
   if (rows <= 32) g.tile_rows = rows <= 16 ? 16 : 32;
   else if (hd == 64) g.tile_rows = rows < 512 ? 16 : 64;
   else if (rows <= 64) g.tile_rows = 64;
@@ -130,6 +130,9 @@ AttnGrid attn_grid(int32_t dtype, int32_t n_seqs, int32_t nq, int32_t nkv, int32
 }
 
 constexpr int32_t MOST_SEQS = 65535;
+bool attention_too_large(int32_t n_seqs, int32_t n_rows, int32_t nq, int32_t nkv) {
+  return n_seqs > MOST_SEQS || (int64_t)n_seqs * nkv > MOST_BLOCKS / 2 || nq > 65536 || (int64_t)n_rows * (nq / nkv) >= 1ll << 30;
+}
 constexpr int32_t MOST_VOCAB = 1 << 20;
 constexpr int32_t MOST_TOP = 32;
 
@@ -205,6 +208,7 @@ int lede_op_cache_read(int32_t dtype, const void* cache, int32_t n_pages, int32_
 size_t lede_op_cache_attention_bytes(int32_t dtype, int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads,
                                      int32_t head_dim, int32_t max_new, int32_t max_kv) {
   if (!dtype_ok(dtype) || n_seqs < 1 || n_rows < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_kv < 0) return 0;
+  if (check_cache(1, n_kv_heads, head_dim) || attention_too_large(n_seqs, n_rows, n_heads, n_kv_heads)) return 0;
   const AttnGrid g = attn_grid(dtype, n_seqs, n_heads, n_kv_heads, head_dim, max_new, max_kv);
   return (size_t)g.n_cut * g.n_split * g.tile_rows * (head_dim + 4) * 4;
 }
@@ -218,7 +222,7 @@ int lede_op_cache_attention(int32_t dtype, const void* q, int64_t ldq, const voi
     return LEDE_E_ARG;
   if (int rc = check_cache(n_pages, n_kv_heads, head_dim)) return rc;
   if (n_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_kv < 0 || !(std::fabs(scale) <= 1e38f)) return LEDE_E_ARG;   // (2 log2(e) scale is finite)
-  if (n_seqs > MOST_SEQS || (int64_t)n_seqs * n_kv_heads > MOST_BLOCKS / 2 || n_heads > 65536 || (int64_t)n_rows * (n_heads / n_kv_heads) >= 1ll << 30) return LEDE_E_UNSUPPORTED;
+  if (attention_too_large(n_seqs, n_rows, n_heads, n_kv_heads)) return LEDE_E_UNSUPPORTED;
   if (!aligned(cache, 16)) return LEDE_E_ARG;
   if (n_rows == 0) return LEDE_OK;
   const int64_t width = (int64_t)n_heads * head_dim;
