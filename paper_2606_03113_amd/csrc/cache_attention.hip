@@ -41,7 +41,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // factor in two halves: E_v goes from -100 to 120, so sums from 2^-122 to
 // 2^105, for one token of the largest weight.
 constexpr int P_LIM = 15, SUM_DOWN = 10, EV_NEAR = 4, O_LIFT = 64;
-constexpr float B_NONE = -__FLT_MAX__;   // B of a row that has seen nothing (any finite score sets B, this one too)
+constexpr float B_NONE = -__FLT_MAX__;   // B of a row that has seen nothing: any finite score moves it, or has the weight 1
 // From scores of 2^22 on, where fp32 has no room for B's whole part, the
 // multiply and the add are rounded one by one, so that the largest score
 // itself comes out as it went into B.
@@ -170,7 +170,7 @@ struct Tiles {
   float sum[NT], base[NT];
   int ev_most;                        // the largest value exponent of the pages so far
   float lift[NT];                     // o is at 2^lift
-  bool lifted;                        // (otherwise all are 0)
+  bool lifted;                        // the last page was a small one
   int pos[QL ? 1 : NT];
   const int (*pl)[16];                // [NT]: positions, beside the queries
 
@@ -237,9 +237,9 @@ struct Tiles {
       for (int i = 0; i < 4; ++i) o[n][d][i] *= f;
   }
   __device__ __forceinline__ void settle() {
-    if (lifted)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) lift_sums(n, 0.f);
+    for (int n = 0; n < NT; ++n)
+      if (__ballot(lift[n] != 0.f)) lift_sums(n, 0.f);
   }
 
   // One page: tokens t0 .. t0 + 63; this lane's key operand (t, h, half), times
@@ -253,7 +253,9 @@ struct Tiles {
     const int lg = (threadIdx.x & 63) >> 4;
     const int ev = max((int)(wv & 255) - 127, CACHE_E_MIN);   // (a word of a block never written is 0)
     const int gap = ev_most - ev;
-    const bool small = gap > EV_NEAR;
+    const bool small = gap > EV_NEAR, rare = small || lifted;
+    const float lim = rare ? -INFINITY : P_LIM;   // (a tile with no row that sees the page has none that sees later ones)
+    const float unit = small ? 0.f : ldexpf(1.f, -ev - SUM_DOWN);
     ev_most = max(ev_most, ev);
     // lane: token t0 + 16 lg + 4 t + i of its query.  Two key tiles at a time:
     // products on one accumulator wait for each other
@@ -303,16 +305,12 @@ struct Tiles {
     uint4 pf[NT][NP][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float up = (float)(ev + P_UP) - base[n], off = up;
+      const float up = (float)(ev + P_UP) - base[n];
       const bool far = __ballot(fabsf(up) > B_FAR) != 0;
       float m = -INFINITY, kx = a.scale_log2x2;   // x = kx x' + up
       if (edge || far) {
         // a table entry outside the pool: rows that see the page become NaN
         kx = 1.f;
-        if (base[n] == B_NONE) {
-          up = INFINITY;
-          off = 0.f;
-        }
         const int last = position(n);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -325,7 +323,8 @@ struct Tiles {
 #pragma unroll
         for (int i = 0; i < 4; ++i) m = fmaxf(m, x[n][t][i]);
       m *= kx;   // (the scale is not negative: q takes its sign)
-      if (small || lifted || __ballot(m + up > P_LIM)) {
+      float off = up;
+      if (__ballot(m + up > lim)) {
         // the row's new B, the same in its four lanes
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
@@ -349,7 +348,7 @@ struct Tiles {
             }
           kx = 1.f;
         }
-        if (small || lifted) {
+        if (rare) {
           // a small page's weights as if its values were the largest, 2^more
           // times as large, where the row's limit leaves room
           float next = 0.f;
@@ -400,7 +399,7 @@ struct Tiles {
           }
           pf[n][p][half] = make_uint4(u[0], u[1], u[2], u[3]);
         }
-      sum[n] = fmaf(ps, small ? 0.f : ldexpf(1.f, -ev - SUM_DOWN), sum[n]);
+      sum[n] = fmaf(ps, unit, sum[n]);
     }
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
