@@ -30,16 +30,17 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // the largest term, from a million tokens together less than the rounding of
 // the output.
 // A page of small values (E_v = -100 if all are zero) has small terms, but its
-// full part in the sum of 2^(x - E_v).  Where E_v is more than EV_NEAR below
-// the largest so far, that part is formed in fp32 from exponents without the
-// difference; nearer pages' weights give theirs as the product takes them, and
-// lose less than 2^-28 of the largest weight each.  Its product has dims, too,
-// in which the large pages hold zeros: its weights are 2^lift as large, and so
-// is o while they are added (2^O_LIFT at most, below which o has room: 2^15 448
-// and 2^24 tokens).  The sum is kept in fp32 at
+// full part in the sum of 2^(x - E_v), and the result's dims in which the
+// large pages hold zeros.  Where E_v is more than EV_NEAR below the largest so
+// far, its weights are 2^lift as large, and so is o while they are added
+// (2^O_LIFT at most: o is below 2^15 448 times the number of tokens); where
+// that does not reach, its part of the sum is formed in fp32 apart.  Nearer
+// pages' weights go in as they are, and lose less than 2^-28 of the largest
+// weight each.  (A chunk of 3 x 1000 rows behind 4100 tokens: 157 us, 187 with
+// values 2^12 larger in each first page.)  The sum is kept in fp32 at
 // 2^-SUM_DOWN, and where B moves or sums of different B meet, it takes the
-// factor in two halves: E_v goes from -100 to 120, so sums from 2^-122 to
-// 2^105, for one token of the largest weight.
+// factor in two halves: E_v goes from -100 to 120, so sums from 2^-122 to 2^105
+// a token of the largest weight.
 constexpr int P_LIM = 15, SUM_DOWN = 10, EV_NEAR = 4, O_LIFT = 64;
 constexpr float B_NONE = -__FLT_MAX__;   // B of a row that has seen nothing: any finite score moves it, or has the weight 1
 // From scores of 2^22 on, where fp32 has no room for B's whole part, the
@@ -169,8 +170,8 @@ struct Tiles {
   f32x4 o[NT][ND];
   float sum[NT], base[NT];
   int ev_most;                        // the largest value exponent of the pages so far
-  float lift[NT];                     // o is at 2^lift
-  bool lifted;                        // the last page was a small one
+  int lift[NT];                       // o is at 2^lift
+  bool lifted;                        // the last page was a small one (otherwise all lifts are 0)
   int pos[QL ? 1 : NT];
   const int (*pl)[16];                // [NT]: positions, beside the queries
 
@@ -215,7 +216,8 @@ struct Tiles {
     for (int n = 0; n < NT; ++n) {
       const int rr = row_at(r0, n, R);
       if (!QL) pos[QL ? 0 : n] = q.len - q.n + rr / G;
-      sum[n] = lift[n] = 0.f;
+      sum[n] = 0.f;
+      lift[n] = 0;
       base[n] = B_NONE;
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -228,8 +230,8 @@ struct Tiles {
   }
 
   // The value sums of tile n at 2^to, and all at 1.
-  __device__ __forceinline__ void lift_sums(int n, float to) {
-    const float f = __builtin_amdgcn_exp2f(to - lift[n]);
+  __device__ __forceinline__ void lift_sums(int n, int to) {
+    const float f = ldexpf(1.f, to - lift[n]);
     lift[n] = to;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -237,9 +239,9 @@ struct Tiles {
       for (int i = 0; i < 4; ++i) o[n][d][i] *= f;
   }
   __device__ __forceinline__ void settle() {
+    if (lifted)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-      if (__ballot(lift[n] != 0.f)) lift_sums(n, 0.f);
+      for (int n = 0; n < NT; ++n) lift_sums(n, 0);
   }
 
   // One page: tokens t0 .. t0 + 63; this lane's key operand (t, h, half), times
@@ -254,8 +256,8 @@ struct Tiles {
     const int ev = max((int)(wv & 255) - 127, CACHE_E_MIN);   // (a word of a block never written is 0)
     const int gap = ev_most - ev;
     const bool small = gap > EV_NEAR, rare = small || lifted;
-    const float lim = rare ? -INFINITY : P_LIM;   // (a tile with no row that sees the page has none that sees later ones)
-    const float unit = small ? 0.f : ldexpf(1.f, -ev - SUM_DOWN);
+    const float lim = rare ? -INFINITY : P_LIM;
+    const int unit = gap > O_LIFT ? -1000 : -ev - SUM_DOWN;   // (of the weights' sum; O_LIFT above: not taken)
     ev_most = max(ev_most, ev);
     // lane: token t0 + 16 lg + 4 t + i of its query.  Two key tiles at a time:
     // products on one accumulator wait for each other
@@ -324,52 +326,58 @@ struct Tiles {
         for (int i = 0; i < 4; ++i) m = fmaxf(m, x[n][t][i]);
       m *= kx;   // (the scale is not negative: q takes its sign)
       float off = up;
-      if (__ballot(m + up > lim)) {
-        // the row's new B, the same in its four lanes
+      if (__ballot(m + up >= lim)) {
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
-        const float b = !(m + up > P_LIM) ? base[n] : fabsf(m) < B_FAR ? ceilf(m + ev) : m + (float)(ev + P_UP);
-        const float h = half_step(base[n] - b), f = h * h;
-        base[n] = b;
-        off = (float)(ev + P_UP) - b;
-        sum[n] = sum[n] * h * h;
+        if (!rare || __ballot(m + up > P_LIM)) {
+          // the row's new B, the same in its four lanes
+          const float b = !(m + up > P_LIM) ? base[n] : fabsf(m) < B_FAR ? ceilf(m + ev) : m + (float)(ev + P_UP);
+          const float h = half_step(base[n] - b), f = h * h;
+          base[n] = b;
+          off = (float)(ev + P_UP) - b;
+          sum[n] = sum[n] * h * h;
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+          for (int d = 0; d < ND; ++d)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[n][d][i] *= f;
-        if (__ballot(fabsf(off) > B_FAR)) {   // a step of such scores may be more than P_LIM
-          const float most = P_LIM - off;
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float y = x[n][t][i] * kx;
-              x[n][t][i] = y > most ? most : y;
-            }
-          kx = 1.f;
-        }
-        if (rare) {
-          // a small page's weights as if its values were the largest, 2^more
-          // times as large, where the row's limit leaves room
-          float next = 0.f;
-          if (small) {
-            const float more = fminf((float)gap, fmaxf(P_LIM - ceilf(m + off), 0.f));
-            const float near = fabsf(off) > B_FAR ? 0.f : more, rest = more - near;   // (whole numbers, while off is one)
-            next = fminf(more, (float)O_LIFT);
-            float own = 0.f;
+            for (int i = 0; i < 4; ++i) o[n][d][i] *= f;
+          if (__ballot(fabsf(off) > B_FAR)) {   // a step of such scores may be more than P_LIM
+            const float most = P_LIM - off;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const float y = fmaf(x[n][t][i], kx, off + near) + rest;
-                own += __builtin_amdgcn_exp2f(y);
-                x[n][t][i] = y - (more - next);
+                const float y = x[n][t][i] * kx;
+                x[n][t][i] = y > most ? most : y;
               }
             kx = 1.f;
-            off = 0.f;
-            sum[n] += ldexpf(own, -ev - SUM_DOWN - (int)more);
           }
-          lift_sums(n, next);
+        }
+        if (rare) {
+          // a small page's weights as if its values were the largest, 2^more
+          // times as large, where the row's limit leaves room
+          int next = 0;
+          if (small) {
+            const float more = fminf((float)gap, fmaxf(P_LIM - ceilf(m + off), 0.f));
+            next = min((int)more, O_LIFT);
+            if (__ballot(fabsf(off) > B_FAR)) {   // (no room for a few powers of two more)
+#pragma unroll
+              for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[n][t][i] = fmaf(x[n][t][i], kx, off);
+              kx = 1.f;
+              off = 0.f;
+            }
+            if (gap > O_LIFT) {   // the weights are not 2^more larger, but the sum's
+              float own = 0.f;
+#pragma unroll
+              for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) own += __builtin_amdgcn_exp2f(fmaf(x[n][t][i], kx, off + more));
+              sum[n] += ldexpf(own, -ev - SUM_DOWN - (int)more);
+            }
+            off += (float)next;
+          }
+          if (__ballot(next != lift[n])) lift_sums(n, next);
         }
       }
       float ps = 0.f;
@@ -399,7 +407,7 @@ struct Tiles {
           }
           pf[n][p][half] = make_uint4(u[0], u[1], u[2], u[3]);
         }
-      sum[n] = fmaf(ps, unit, sum[n]);
+      sum[n] += ldexpf(ps, unit - lift[n]);
     }
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll

@@ -27,7 +27,7 @@ VARIANTS = {
 KV, NQ = 2, 4
 
 
-def _check(variant, dtype, hd, sizes, r, keys=None, q=None, values=None):
+def _check(variant, dtype, hd, sizes, r, keys=None, q=None, values=None, scale=None):
     """One sequence whose pages' values have the given sizes (0: all zero), beside a short one and empty ones."""
     m = lede()
     seqs, max_new, max_kv = VARIANTS[variant]
@@ -44,7 +44,7 @@ def _check(variant, dtype, hd, sizes, r, keys=None, q=None, values=None):
     slots = tables[0, p // 64].astype(np.int64) * 64 + p % 64
     m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(slots))
     model.append(val[:, 0], val[:, 1], slots)
-    return _attend(cache, model, tables, lens, new, NQ, dtype, r, max_new=max_new, max_kv=max_kv, q=q)
+    return _attend(cache, model, tables, lens, new, NQ, dtype, r, max_new=max_new, max_kv=max_kv, q=q, scale=scale)
 
 
 def _sizes(pattern, n=12):
@@ -77,25 +77,27 @@ def test_attention_pages_of_any_size_keep_their_weight(dtype, hd, variant):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("variant", list(VARIANTS))
-def test_attention_small_weights_of_small_pages(dtype, variant):
+def test_attention_small_weights_of_small_pages(dtype, hd, variant):
     """Thousands of tokens 12 nats below one whose page has values 2^16 larger hold some percent of the weight."""
     r = np.random.default_rng(31)
-    q = np.full((6, NQ, 64), 0.25)
+    q = np.full((6, NQ, hd), 16.0 / hd)
     for gap in (10.0, 12.0, 13.0):
         say("attention gap", dtype, variant, gap)
-        # (scores 64^-0.5 q.k = 2 k: the first page's are `gap` nats larger)
-        _check(variant, dtype, 64, [2.0 ** 16] * 4 + [1.0] * 60, r, keys=lambda n: np.where(np.arange(n) == 0, gap / 4, -gap / 4), q=q)
+        # (q.k = 16 k: the first token's score is `gap` nats larger)
+        _check(variant, dtype, hd, [2.0 ** 16] * 4 + [1.0] * 60, r, keys=lambda n: np.where(np.arange(n) == 0, gap / 4, -gap / 4), q=q, scale=0.125)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("variant", list(VARIANTS))
-def test_attention_scores_as_large_as_fp32_holds(dtype, variant):
+def test_attention_scores_as_large_as_fp32_holds(dtype, hd, variant):
     """Scores up to fp32's largest, and ordinary ones of the largest and smallest keys."""
     m = lede()
     seqs, max_new, max_kv = VARIANTS[variant]
     r = np.random.default_rng(55)
-    hd, length, best = 64, 300, 150
+    length, best = 300, 150
     lens, start = np.array([length] + [0] * (seqs - 1), np.int32), np.array([0] + [3] * seqs, np.int32)
     table = np.tile(np.arange(5, dtype=np.int32), (seqs, 1))
     cache, model = m.Cache(5, KV, hd), ref.CacheModel(5, KV, hd)
@@ -128,13 +130,14 @@ def test_attention_scores_as_large_as_fp32_holds(dtype, variant):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("variant", list(VARIANTS))
-def test_attention_hugely_negative_scores(dtype, variant):
+def test_attention_hugely_negative_scores(dtype, hd, variant):
     """Rows all of whose scores are far below zero: the largest one's value, as long as fp32 holds the scores."""
     m = lede()
     seqs, max_new, max_kv = VARIANTS[variant]
     r = np.random.default_rng(61)
-    kv, hd, length, best = 2, 64, 300, 150
+    kv, length, best = 2, 300, 150
     cache, model = m.Cache(5, kv, hd), ref.CacheModel(5, kv, hd)
     x = np.zeros((length, 2, kv, hd))
     x[:, 0, :, 0] = (1.0 + np.arange(length) % 7 / 8)[:, None]
@@ -163,13 +166,14 @@ def test_attention_hugely_negative_scores(dtype, variant):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("variant", list(VARIANTS))
-def test_attention_pages_never_written(dtype, variant):
+def test_attention_pages_never_written(dtype, hd, variant):
     """Pages of a cleared cache that no append has reached are tokens of zero keys and values."""
     m = lede()
     seqs, max_new, max_kv = VARIANTS[variant]
     r = np.random.default_rng(51)
-    n, hd = 7, 64
+    n = 7
     length = 64 * n - 9
     for written in ((1, 2, 3, 4, 5, 6), (0, 5), (6,)):
         say("attention cleared", dtype, variant, written)
@@ -198,6 +202,51 @@ def test_attention_dims_that_only_small_pages_have(dtype, variant):
                 return x
             sizes = [2.0 ** (ratio - ratio // 2 if p in at else -(ratio // 2)) for p in range(12)]
             _check(variant, dtype, 128, sizes, r, values=values)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("variant", list(VARIANTS))
+def test_attention_pages_of_no_weight_beside_small_ones(dtype, hd, variant):
+    """Pages all of whose scores fp32 does not hold, -infinity, behind and before pages of small values: no weight, and the
+    others keep theirs."""
+    m = lede()
+    seqs, max_new, max_kv = VARIANTS[variant]
+    r = np.random.default_rng(71)
+    n = 12
+    length = 64 * n
+    for far, small in (((2, 5, 8, 9, 10), (1, 4, 7)), ((4, 5, 6, 7), (1, 2, 3)), ((11,), (7, 8, 9, 10)), ((0, 1, 2, 3), (4, 5, 6, 7))):
+        say("attention no weight", dtype, variant, far, small)
+        x = r.standard_normal((length, 2, KV, hd))
+        page = np.arange(length) // 64
+        x[:, 0, :, 0] = np.where(np.isin(page, far), 30.0, 0.0)[:, None]      # times q's 1e38: beyond fp32, or nothing
+        x[:, 0, :, 1:] *= 0.3
+        x[np.isin(page, small), 1] *= 2.0 ** -30
+        cache, model = m.Cache(n, KV, hd), ref.CacheModel(n, KV, hd)
+        d, val = rounded(x, "bf16")
+        m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(np.arange(length)))
+        model.append(val[:, 0], val[:, 1], np.arange(length))
+        q = r.standard_normal((6, NQ, hd))
+        q[:, :, 0] = -1e38
+        start = [0, 4] + [4] * (seqs - 1)
+        got = m.op_cache_attention(cache, rounded(q, dtype)[0], gpu(np.tile(np.arange(n, dtype=np.int32), (seqs, 1))), gpu(np.array([length] + [0] * (seqs - 1), np.int32)),
+                                   gpu(np.array(start, np.int32)), max_new, max_kv).double().cpu().numpy()[:4]
+        # the others' keys have a zero against 1e38
+        kk, vv = model.read(np.arange(length))
+        qv = rounded(q, dtype)[1][:4]
+        for i in range(4):
+            seen = ~np.isin(page, far) & (np.arange(length) <= length - 4 + i)
+            for h in range(NQ):
+                k, v = kk[seen, h // 2, 1:], vv[seen, h // 2]
+                z = hd ** -0.5 * (k @ qv[i, h, 1:])
+                w = np.exp(z - z.max())
+                w /= w.sum()
+                want = w @ v
+                # (as ref.attention counts)
+                terms = (3 * hd + 4) * hd ** -0.5 * (np.abs(k) @ np.abs(qv[i, h, 1:])).max() + 4 + 2 * (80 + n)
+                eps = 2.0 ** -23 * terms + (2.0 ** -12 if dtype == "bf16" else 2.0 ** -22)
+                tol = 2 * eps * (w @ np.abs(v)) + ref.HALF_STEP[dtype] * np.abs(want) * (1 + 2 ** -6)
+                assert (np.abs(got[i, h] - want) <= tol).all(), (i, h)
 
 
 # ---- scores ----------------------------------------------------------------------------------------------------
