@@ -199,7 +199,8 @@ struct Tiles {
             uint32_t u[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              u[e] = f32_to_bf16x2(x[2 * e], x[2 * e + 1]);
+              // (cut off, 8 bits a part: rounded, a number above bf16's largest would become infinite)
+              u[e] = __builtin_amdgcn_perm(__float_as_uint(x[2 * e + 1]), __float_as_uint(x[2 * e]), 0x07060302);
               x[2 * e] -= bf16lo(u[e]);
               x[2 * e + 1] -= bf16hi(u[e]);
             }

@@ -249,6 +249,33 @@ def test_attention_pages_of_no_weight_beside_small_ones(dtype, hd, variant):
                 assert (np.abs(got[i, h] - want) <= tol).all(), (i, h)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("variant", list(VARIANTS))
+def test_attention_largest_fp32_queries(hd, variant):
+    """fp32 queries between bf16's largest number and their own."""
+    m = lede()
+    seqs, max_new, max_kv = VARIANTS[variant]
+    r = np.random.default_rng(81)
+    length, best = 300, 100
+    cache, model = m.Cache(5, KV, hd), ref.CacheModel(5, KV, hd)
+    x = r.standard_normal((length, 2, KV, hd))
+    x[:, 0] = 0.0
+    x[:, 0, :, 0] = 0.25
+    x[best, 0, :, 0] = 0.5
+    d, val = rounded(x, "bf16")
+    m.op_cache_append(cache, d[:, 0], d[:, 1], gpu(np.arange(length)))
+    model.append(val[:, 0], val[:, 1], np.arange(length))
+    q = np.zeros((3, NQ, hd), np.float32)
+    for size in (3.39e38, 3.3999e38, -3.4e38):
+        say("attention queries", hd, variant, size)
+        q[:, :, 0] = size
+        got = m.op_cache_attention(cache, gpu(q), gpu(np.tile(np.arange(5, dtype=np.int32), (seqs, 1))), gpu(np.array([length] + [0] * (seqs - 1), np.int32)),
+                                   gpu(np.array([0] + [3] * seqs, np.int32)), max_new, max_kv, scale=float(np.sign(size))).double().cpu().numpy()
+        for h in range(NQ):      # (the best token's weight is a power of two: two half steps are the quotient's and the output's)
+            want = model.read([best])[1][0, h // (NQ // KV)]
+            assert (np.abs(got[:, h] - want) <= ref.HALF_STEP["f32"] * 2 * np.abs(want)).all(), (size, h)
+
+
 # ---- scores ----------------------------------------------------------------------------------------------------
 
 
