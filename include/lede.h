@@ -649,8 +649,11 @@ int lede_op_cache_read(int32_t dtype, const void* cache, int32_t n_pages, int32_
  * only spread the work: larger lengths are right, too, if slower.  Table
  * entries outside the pool are never followed: rows that see such a page are
  * NaN.  kv_lens above 64 * table_ld count as that, row_start is held to [0,
- * n_rows].  Scores, softmax statistics and sums are fp32; a NaN or infinity
- * stays with the rows that see it.
+ * n_rows].  Scores, softmax statistics and sums are fp32; weights enter the
+ * value product with 11 bits (bf16 queries) or 22 (fp32), and those below 2^-28
+ * or 2^-33 of a row's largest, as values below 2^-70 of its largest, may count
+ * as 0 there.  A NaN or infinity stays with the rows that see it, and so does
+ * a score that fp32 does not hold.
  * workspace: lede_op_cache_attention_bytes of the same sizes (may be 0, as it
  * is for sizes that the call refuses).
  * LEDE_E_ARG: null pointers, bad sizes, n_heads not a multiple of n_kv_heads,

@@ -57,6 +57,8 @@ constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;
 //   40                                  108   123   136
 //   500, 16 of 4000, 16 KV heads        158   142   138
 //   1000                                320   278   243
+//   200, fp32                            98         127
+//   400                                 176         193
 // Time of a page in a block that has its CU to itself, us (measured over 150
 // pages, the fewest rows of hd 128 from memory).
 double page_us(int32_t dtype, int32_t hd, int tile_rows) {

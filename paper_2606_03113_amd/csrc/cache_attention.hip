@@ -665,14 +665,14 @@ template <bool KEYS> __device__ __forceinline__ uint4 operand(uint2 c, float ks 
 // into LDS once per block, as 16-bit operands in the order in which the lanes
 // take them (16 bytes per lane, a contiguous KiB per operand: no bank
 // conflict either way), so that each wave converts a quarter of the codes;
-// two pages' room, so one barrier a page.  Bound by the matrix units and the
-// exponentials beside them: 1008 TFLOP/s over whole rounds of 128-row tiles
-// (bf16, heads of 128), against 1269 of a large library product; with the codes
-// themselves in LDS, converted by every wave, 920.  RAW: codes all the same, for
-// 64 bf16 rows and heads of 128 behind long contexts, bound by memory: half the
-// LDS makes room for a third block, where there is one (30 sequences of up to
-// 20000 tokens: 229 us, 266 with operands; 2 of up to 131000, one round of
-// blocks: 81 and 79).
+// two pages' room, so one barrier a page.  Bound by the matrix units (41% of
+// the SIMDs' clocks) and the vector instructions beside them (51%; both at once
+// 7%): 995 TFLOP/s over whole rounds of 128-row tiles (bf16, heads of 128),
+// against 1269 of a large library product; with the codes themselves in LDS,
+// converted by every wave, 890.  RAW: codes all the same, for 64 bf16 rows and
+// heads of 128 behind long contexts, bound by memory: half the LDS makes room
+// for a third block, where there is one (30 sequences of up to 20000 tokens:
+// 239 us, 271 with operands; 2 of up to 131000, one round of blocks: 77 and 75).
 template <int DT, int HD, int NT, bool RAW>
 __global__ __launch_bounds__(256, 2) void k_cache_attn_rows(CacheAttnArgs a) {
   typedef Tiles<DT, HD, NT> T;

@@ -667,7 +667,8 @@ def op_cache_plan(seq_lens, new_lens, held, free_pages, free_head, tables, max_r
     """Pages and slots of a pass in which sequence s gets new_lens[s] tokens
     behind seq_lens[s] cached ones (int32 GPU tensors; tables [n_seqs][width]
     is updated).  `out` reuses a plan's tensors, which may be the inputs'
-    own (kv_lens is seq_lens, held is held, free_head is status[2:3])."""
+    own (kv_lens is seq_lens, held is held, free_head is status[2:3]); of
+    longer slots the first max_rows are written, and only those are the plan's."""
     import torch
     dev, n, max_rows = seq_lens.device, seq_lens.numel(), int(max_rows)
     _need(_dense(dev, torch.int32, seq_lens, new_lens, held, free_pages, free_head, tables) and tables.dim() == 2
