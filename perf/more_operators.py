@@ -1,0 +1,567 @@
+"""Further operators of a batch of requests, as cases that can be timed and compared: the life of the cache's pages,
+linear products with 4-bit weights, and the loss of the vocabulary head with its gradient.
+
+A case is a dict of plain values.  Five kinds, each one pass through calls of paper_2606_03113_amd.lede:
+
+  fork     op_cache_fork, op_cache_own and op_cache_copy: sequences that share the pages of others, and the pages that
+           their next tokens fall into made their own
+  free     op_cache_free: pages that their sequences no longer need go back to the pool
+  compact  op_cache_compact and op_cache_copy: live pages moved to the pool's front
+  linear   op_quant_linear: rows times a matrix of 4-bit codes with a scale for each group of columns
+  loss     op_head_loss, and op_head_loss_grad where the case has a gradient: -log softmax(hidden head^T)[target] of
+           every row without its logits, and what it makes of hidden and head
+
+`run` computes them in elementary torch operations, or, where `own` is true, by those calls.  Passes of the first three
+change the page tables in place; they begin by putting back what `prepare` made (one copy of a few kilobytes).
+
+A page holds 64 tokens.  tables [sequence][place] are pool pages, of which a sequence has the first held[s]; shares[page]
+counts the holders of a page besides one; free_pages[free_head ..] are the pages that nobody has.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+PAGE = 64
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+# (KV heads, head dim) of the repository's workloads, and narrow ones
+CACHES = [(4, 64), (32, 128), (8, 128), (40, 128), (4, 128), (2, 64)]
+# (outputs, inputs) of their products
+MATRICES = [(688, 256), (1024, 256), (4096, 4096), (22016, 4096), (4096, 11008), (5120, 5120), (6144, 4096), (28672, 4096), (4096, 14336)]
+E2M1 = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0]
+LOSS_PRODUCTS = 3 * 2048 * 32000 * 4096      # multiply-adds of a drawn loss
+LINEAR_PRODUCTS = 64 * 28672 * 4096
+REGION_BYTES = 6.5e8
+
+
+def listed():
+    return [
+        # one request's prompt answered by four samples, before their first step: the smallest call, where latency counts
+        {"name": "fork-sample", "kind": "fork", "groups": 1, "children": 3, "ctx": 700, "kv": 4, "hd": 64},
+        # a full server: every prompt with seven siblings, some of them from a prefix
+        {"name": "fork-batch", "kind": "fork", "groups": 32, "children": 7, "ctx": 2000, "kv": 8, "hd": 128},
+        # a step of a batch after which a few requests have ended
+        {"name": "free-step", "kind": "free", "seqs": 64, "ctx": 4096, "gone": 0.05, "family": 1},
+        # a thousand samples in families that share their prompts' pages, half of them ended and others rolled back
+        {"name": "free-batch", "kind": "free", "seqs": 1001, "ctx": 2000, "gone": 0.5, "family": 4},
+        # the few requests left of a small model's pool
+        {"name": "compact-few", "kind": "compact", "seqs": 9, "ctx": 900, "pool": 2.0, "kv": 4, "hd": 64},
+        # a pool that is to shrink by a third behind a batch of long requests
+        {"name": "compact-batch", "kind": "compact", "seqs": 150, "ctx": 2000, "pool": 1.45, "kv": 8, "hd": 128},
+        # the smallest product: three fp32 rows of the smallest model's feed-forward
+        {"name": "linear-tiny", "kind": "linear", "dtype": "f32", "rows": 3, "n": 688, "k": 256, "group": 32},
+        # the ordinary one: one token through a down projection
+        {"name": "linear-token", "kind": "linear", "dtype": "bf16", "rows": 1, "n": 4096, "k": 11008, "group": 128},
+        # a decoding step of 64 requests through gate and up
+        {"name": "linear-batch", "kind": "linear", "dtype": "bf16", "rows": 64, "n": 28672, "k": 4096, "group": 32},
+        # the smallest model's prompt, trained in fp32
+        {"name": "loss-tiny", "kind": "loss", "dtype": "f32", "rows": 32, "vocab": 1024, "d": 256, "grad": True},
+        # a prompt's tokens scored over the largest vocabulary: no gradient
+        {"name": "loss-score", "kind": "loss", "dtype": "bf16", "rows": 700, "vocab": 128256, "d": 4096, "grad": False},
+        # a training step of the shared head
+        {"name": "loss-train", "kind": "loss", "dtype": "bf16", "rows": 2048, "vocab": 32000, "d": 4096, "grad": True},
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, round(math.exp(rng.uniform(math.log(lo), math.log(hi + 0.49))))))
+
+
+def draw(rng):
+    kind = rng.choice(["fork", "free", "compact", "linear", "linear", "linear", "loss", "loss", "loss"])
+    if kind in ("fork", "compact"):
+        kv, hd = rng.choice(CACHES)
+        most = int(REGION_BYTES / (2 * PAGE * kv * hd))          # pages
+    if kind == "fork":
+        groups, children = _log_int(rng, 1, 48), _log_int(rng, 1, 12)
+        ctx = _log_int(rng, 1, max(1, min(6000, (most // groups - children - 3) * PAGE)))
+        return {"kind": kind, "groups": groups, "children": children, "ctx": ctx, "kv": kv, "hd": hd}
+    if kind == "free":
+        seqs = _log_int(rng, 1, 1200)
+        return {"kind": kind, "seqs": seqs, "ctx": _log_int(rng, 1, 2400000 // max(seqs, 300)), "gone": rng.choice([0.0, 0.1, 0.5, 1.0]),
+                "family": rng.choice([1, 1, 2, 5])}
+    if kind == "compact":
+        seqs, pool = _log_int(rng, 1, 256), rng.choice([1.0, 1.1, 1.4, 3.0])
+        return {"kind": kind, "seqs": seqs, "ctx": _log_int(rng, 1, max(1, min(8000, int(most / pool / seqs - 4) * PAGE))), "pool": pool,
+                "kv": kv, "hd": hd}
+    dtype = rng.choice(["f32", "bf16", "bf16"])
+    if kind == "linear":
+        n, k = rng.choice(MATRICES) if rng.random() < 0.6 else (_log_int(rng, 1, 30000), _log_int(rng, 1, 12000))
+        rows = rng.choice([1, 1, rng.randint(2, 16), _log_int(rng, 1, 64)])
+        return {"kind": kind, "dtype": dtype, "rows": max(1, min(rows, LINEAR_PRODUCTS // (n * k))), "n": n, "k": k, "group": rng.choice([32, 64, 128])}
+    grad = rng.random() < 0.7
+    d = 8 * _log_int(rng, 4, 640) if rng.random() < 0.5 else rng.choice([256, 4096, 5120])
+    vocab = rng.choice([1024, 32000, 128256, _log_int(rng, 50, 130000)])
+    most = LOSS_PRODUCTS // (3 if grad else 1) // (vocab * d) // (6 if dtype == "f32" else 1)
+    return {"kind": kind, "dtype": dtype, "rows": _log_int(rng, 1, max(1, min(3000, most))), "vocab": vocab, "d": d, "grad": grad}
+
+
+# ---- inputs ----------------------------------------------------------------------------
+
+
+def _generator(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _fork_lengths(case):
+    """Rows of parents and children, each child's parent (-1: a parent), cached tokens, tokens to share, tokens to come."""
+    r = np.random.default_rng(17)
+    g, c = case["groups"], case["children"]
+    n = g * (1 + c)
+    row = r.permutation(n).reshape(g, 1 + c)
+    source, seq, lens = np.full(n, -1), np.zeros(n, np.int64), np.zeros(n, np.int64)
+    for i in range(g):
+        seq[row[i, 0]] = case["ctx"] if g == 1 else r.integers((case["ctx"] + 1) // 2, case["ctx"] + 1)
+        source[row[i, 1:]] = row[i, 0]
+        lens[row[i, 1:]] = seq[row[i, 0]]
+        cut = row[i, 1:][r.random(c) < 0.2]      # some from a prefix
+        lens[cut] = (lens[cut] * r.random(len(cut))).astype(np.int64)
+    new = (r.random(n) < 0.95).astype(np.int64)
+    return source, seq, lens, new
+
+
+def _free_lengths(case):
+    """Tokens before and after, pages held, and the first row of each family, whose leading pages its others share."""
+    r = np.random.default_rng(19)
+    n, f = case["seqs"], case["family"]
+    before = r.integers((case["ctx"] + 1) // 2, case["ctx"] + 1, n)
+    first = np.arange(n) // f * f
+    shared = np.minimum(before, before[first]) * 3 // 4 // PAGE      # whole pages, of rows other than the first
+    shared[first == np.arange(n)] = 0
+    held = -(-before // PAGE) + r.integers(0, 2, n)
+    after = np.maximum(before - r.integers(0, 6, n), 0)              # rejected drafts
+    after[r.random(n) < case["gone"]] = 0
+    return before, after, held, first, shared
+
+
+def _compact_lengths(case):
+    r = np.random.default_rng(23)
+    n = case["seqs"]
+    seq = r.integers((case["ctx"] + 1) // 2, case["ctx"] + 1, n)
+    return -(-seq // PAGE), int(math.ceil(int((-(-seq // PAGE)).sum()) * case["pool"])) + 2
+
+
+def _book(**parts):
+    """The int32 arrays of a case as views of one buffer, and a copy of it."""
+    flat = torch.from_numpy(np.concatenate([np.asarray(a, np.int32).reshape(-1) for a in parts.values()])).to("cuda")
+    kept, out, at = flat.clone(), {}, 0
+    for name, a in parts.items():
+        n = np.asarray(a).size
+        out[name] = flat[at:at + n].view(np.asarray(a).shape)
+        at += n
+    return dict(out, book=flat, kept=kept)
+
+
+def _region(n_pages, kv, hd, g):
+    """A cache of random contents: the pages' operators move its bytes and never look at them."""
+    return torch.randint(0, 256, (2 * n_pages * kv * PAGE * hd + n_pages * kv * 8,), dtype=torch.uint8, device="cuda", generator=g)
+
+
+def prepare(case, seed):
+    g, r, kind = _generator(seed), np.random.default_rng(seed + 5), case["kind"]
+    s = {"case": case}
+    if kind == "fork":
+        source, seq, lens, new = _fork_lengths(case)
+        held = -(-seq // PAGE)
+        n, width = len(seq), int(held.max()) + 1
+        n_pages = int(held.sum()) + n + 3
+        order, tables, at = r.permutation(n_pages), np.full((n, width), -1), 0
+        for i in range(n):
+            tables[i, :held[i]] = order[at:at + held[i]]
+            at += held[i]
+        s.update(_book(seq_lens=seq, held=held, tables=tables, shares=np.zeros(n_pages), free_pages=order, free_head=[at], source=source,
+                       lens=lens, new_lens=new), n_pages=n_pages, region=_region(n_pages, case["kv"], case["hd"], g), max_moves=n)
+    elif kind == "free":
+        before, after, held, first, shared = _free_lengths(case)
+        n, width = len(before), int(held.max())
+        n_pages = int((held - shared).sum()) + 5
+        order, tables, at, shares = r.permutation(n_pages), np.full((n, width), -1), 0, np.zeros(n_pages)
+        for i in range(n):
+            tables[i, :shared[i]] = tables[first[i], :shared[i]]
+            shares[tables[i, :shared[i]]] += 1
+            k = held[i] - shared[i]
+            tables[i, shared[i]:held[i]] = order[at:at + k]
+            at += k
+        s.update(_book(seq_lens=after, held=held, tables=tables, shares=shares, free_pages=order, free_head=[at]), n_pages=n_pages)
+    elif kind == "compact":
+        held, n_pages = _compact_lengths(case)
+        order, tables, at = r.permutation(n_pages), np.full((len(held), int(held.max())), -1), 0
+        for i in range(len(held)):
+            tables[i, :held[i]] = order[at:at + held[i]]
+            at += held[i]
+        shares = np.zeros(n_pages)
+        if len(held) > 1:                        # a fork among them
+            tables[1, 0] = tables[0, 0]
+            shares[tables[0, 0]] = 1
+        s.update(_book(held=held, tables=tables, shares=shares, free_pages=order, free_head=[at]), n_pages=n_pages,
+                 region=_region(n_pages, case["kv"], case["hd"], g), max_moves=n_pages // 2)
+    elif kind == "linear":
+        n, k, group, dt = case["n"], case["k"], case["group"], DTYPES[case["dtype"]]
+        x = torch.empty(case["rows"], k, device="cuda").normal_(0.0, 1.0, generator=g)
+        x[:, 5::97] *= 12.0                      # channels of large activations
+        # codes as rounding leaves them: normal weights over a scale that their group's largest takes to 6
+        codes = torch.randint(0, 16, (n, k), dtype=torch.uint8, device="cuda", generator=g)
+        scales = torch.empty(n, -(-k // group), device="cuda").uniform_(0.004, 0.016, generator=g).to(torch.bfloat16)
+        if k % 2:
+            codes = torch.nn.functional.pad(codes, (0, 1))
+        s.update(x=x.to(dt), codes=codes[:, ::2] | codes[:, 1::2] << 4, scales=scales)
+        if own:
+            from paper_2606_03113_amd import lede
+            s["matrix"] = lede.QuantMatrix(s["codes"], s["scales"], k, group)
+    else:
+        rows, V, d, dt = case["rows"], case["vocab"], case["d"], DTYPES[case["dtype"]]
+        head = torch.empty(V, d, device="cuda").normal_(0.0, 0.02, generator=g).to(dt)
+        targets = torch.randint(0, V, (rows,), device="cuda", generator=g)
+        hidden = torch.empty(rows, d, device="cuda").normal_(0.0, 1.0, generator=g)
+        # what was learned: every other row has its target's logit about 6 higher
+        hidden[::2] += head[targets[::2]].float() * (6.0 / (0.0004 * d))
+        targets[torch.rand(rows, device="cuda", generator=g) < 0.1] = -1      # rows of the prompt, which are not trained on
+        weights = torch.empty(rows, device="cuda").uniform_(0.5, 1.5, generator=g) / rows
+        s.update(hidden=hidden.to(dt), head=head, targets=targets.to(torch.int32), weights=weights)
+    if own and "region" in s:
+        from paper_2606_03113_amd import lede
+        s["cache"] = lede.Cache(s["n_pages"], case["kv"], case["hd"], region=s["region"])
+    return s
+
+
+# ---- the operators in elementary operations ------------------------------------------------
+
+
+def _pages(tokens):
+    return (tokens + PAGE - 1) // PAGE
+
+
+def _count(pages, which, n_pages):
+    """How often each pool page is among the entries that `which` selects."""
+    return torch.zeros(n_pages + 1, dtype=torch.long, device="cuda").scatter_add_(0, torch.where(which, pages, n_pages).reshape(-1),
+                                                                                 which.long().reshape(-1))[:n_pages]
+
+
+def _first(pages, which, n_pages):
+    """Whether an entry is the first, in reading order, of those selected that have its page."""
+    at = torch.arange(pages.numel(), device="cuda").view(pages.shape)
+    least = torch.full((n_pages + 1,), pages.numel(), dtype=torch.long, device="cuda")
+    least.scatter_reduce_(0, torch.where(which, pages, n_pages).reshape(-1), at.reshape(-1), "amin")
+    return which & (least[torch.where(which, pages, n_pages)] == at)
+
+
+def _copy_pages(s, pairs):
+    kv, hd, n = s["case"]["kv"], s["case"]["hd"], s["n_pages"]
+    size = kv * PAGE * hd
+    pairs = pairs[pairs[:, 0] >= 0].long()
+    for at, width in ((0, size), (n * size, size), (2 * n * size, kv * 8)):
+        part = s["region"][at:at + n * width].view(n, width)
+        part[pairs[:, 1]] = part[pairs[:, 0]]
+
+
+def _listed_pairs(which, src, dst, room):
+    """(src, dst) of the selected entries in reading order, -1 behind them, and how many they are."""
+    rank = torch.cumsum(which.reshape(-1).long(), 0) - 1
+    pairs = torch.full((room + 1, 2), -1, dtype=torch.long, device="cuda")
+    at = torch.where(which.reshape(-1), rank, room)
+    pairs[at] = torch.stack([src.reshape(-1), dst.reshape(-1)], 1)
+    return pairs[:room].int(), which.sum()
+
+
+def _status(*values):
+    return torch.stack([torch.as_tensor(v, device="cuda").long() for v in values]).int()
+
+
+def _plain_fork(s):
+    n_pages, tables, shares = s["n_pages"], s["tables"], s["shares"]
+    col = torch.arange(tables.shape[1], device="cuda")
+    source, lens = s["source"].long(), s["lens"].long()
+    fork = source >= 0
+    shared = fork[:, None] & (col < _pages(lens)[:, None])
+    tables.copy_(torch.where(shared, tables[source.clamp(min=0)], tables))
+    shares += _count(tables.long(), shared, n_pages).int()
+    s["seq_lens"].copy_(torch.where(fork, lens, s["seq_lens"]))
+    s["held"].copy_(torch.where(fork, _pages(lens), s["held"]))
+    forked = _status(0, shared.sum(), -1)
+    # the pages that new tokens fall into
+    seq, new, held, head = s["seq_lens"].long(), s["new_lens"].long(), s["held"].long(), s["free_head"].long()[0]
+    page = tables.long()
+    writes = (new > 0)[:, None] & (col >= (seq // PAGE)[:, None]) & (col < torch.minimum(held, _pages(seq + new))[:, None])
+    x = shares.long()
+    writes = writes & (x[page.clamp(min=0)] > 0)
+    left = x - _count(page, writes, n_pages)
+    keeps = _first(page, writes, n_pages) & (left[page.clamp(min=0)] < 0)
+    takes = writes & ~keeps
+    shares.copy_(left.clamp(min=0))
+    rank = (torch.cumsum(takes.reshape(-1).long(), 0) - 1).view(takes.shape)
+    fresh = s["free_pages"].long()[(head + rank).clamp(0, s["free_pages"].numel() - 1)]
+    pairs, count = _listed_pairs(takes & (col * PAGE < seq[:, None]), page, fresh, s["max_moves"])
+    tables.copy_(torch.where(takes, fresh, page))
+    _copy_pages(s, pairs)
+    return s["seq_lens"], s["held"], tables, shares, forked, pairs, _status(0, count, head + takes.sum(), -1), s["region"].view(torch.int32)
+
+
+def _plain_free(s):
+    n_pages, tables, shares = s["n_pages"], s["tables"], s["shares"]
+    col = torch.arange(tables.shape[1], device="cuda")
+    keep, held, head, page = _pages(s["seq_lens"].long()), s["held"].long(), s["free_head"].long()[0], tables.long()
+    drops = (col >= keep[:, None]) & (col < held[:, None])
+    left = shares.long() - _count(page, drops, n_pages)
+    frees = _first(page, drops, n_pages) & (left[page.clamp(min=0)] < 0)
+    shares.copy_(left.clamp(min=0))
+    total = frees.sum()
+    rank = torch.cumsum(frees.reshape(-1).long(), 0) - 1
+    size = s["free_pages"].numel()
+    room = torch.cat([s["free_pages"].long(), torch.zeros(1, dtype=torch.long, device="cuda")])
+    room[torch.where(frees.reshape(-1), head - total + rank, size)] = page.reshape(-1)
+    s["free_pages"].copy_(room[:size])
+    s["held"].copy_(torch.minimum(held, keep))
+    return s["held"], shares, s["free_pages"], _status(0, total, head - total, -1)
+
+
+def _plain_compact(s):
+    n_pages, tables, shares = s["n_pages"], s["tables"], s["shares"]
+    col, p = torch.arange(tables.shape[1], device="cuda"), torch.arange(n_pages, device="cuda")
+    has = col < s["held"].long()[:, None]
+    live = _count(tables.long(), has, n_pages) > 0
+    n_live = live.sum()
+    moves, holes = live & (p >= n_live), ~live & (p < n_live)
+    hole = torch.zeros(n_pages + 1, dtype=torch.long, device="cuda")
+    hole[torch.where(holes, torch.cumsum(holes.long(), 0) - 1, n_pages)] = p
+    dst = torch.where(moves, hole[(torch.cumsum(moves.long(), 0) - 1).clamp(min=0)], p)
+    pairs, count = _listed_pairs(moves, p, dst, s["max_moves"])
+    tables.copy_(torch.where(has, dst[tables.long().clamp(min=0)], tables.long()))
+    at = torch.cat([torch.where(live, dst, n_pages)])
+    shares.copy_(torch.zeros(n_pages + 1, dtype=torch.long, device="cuda").scatter_(0, at, shares.long())[:n_pages])
+    size = s["free_pages"].numel()
+    head = size - (n_pages - n_live)
+    place = torch.arange(size, device="cuda")
+    s["free_pages"].copy_(torch.where(place >= head, n_live + place - head, s["free_pages"].long()))
+    _copy_pages(s, pairs)
+    return tables, shares, s["free_pages"], pairs, _status(0, count, head, n_live), s["region"].view(torch.int32)
+
+
+def _unpacked(s):
+    """The values of the 4-bit codes, without their scales."""
+    codes = torch.stack([s["codes"] & 15, s["codes"] >> 4], 2).reshape(s["codes"].shape[0], -1)[:, :s["case"]["k"]]
+    return torch.tensor(E2M1, device="cuda")[codes.int()]
+
+
+def _plain_linear(s):
+    scale = torch.repeat_interleave(s["scales"].float(), s["case"]["group"], 1)[:, :s["case"]["k"]]
+    w = _unpacked(s) * scale
+    return torch.matmul(s["x"].float(), w.t()).to(s["x"].dtype)
+
+
+def _plain_loss(s):
+    h, w = s["hidden"].float(), s["head"].float()
+    t = s["targets"].long()
+    trained = (t >= 0) & (t < w.shape[0])
+    at = t.clamp(min=0)[:, None]
+    z = torch.matmul(h, w.t())
+    m = z.amax(1, keepdim=True)
+    lse = m + torch.log(torch.exp(z - m).sum(1, keepdim=True))
+    loss = torch.where(trained, (lse - z.gather(1, at))[:, 0], 0.0)
+    if not s["case"]["grad"]:
+        return loss, lse[:, 0]
+    weight = torch.where(trained, s["weights"], 0.0)[:, None]
+    p = torch.exp(z - lse)
+    p[torch.arange(len(t), device="cuda"), at[:, 0]] -= 1.0
+    p *= weight
+    return loss, lse[:, 0], torch.matmul(p, w).to(s["hidden"].dtype), torch.matmul(p.t(), h).to(s["head"].dtype)
+
+
+def run(s):
+    kind = s["case"]["kind"]
+    if "book" in s:
+        s["book"].copy_(s["kept"])
+    if not own:
+        return {"fork": _plain_fork, "free": _plain_free, "compact": _plain_compact, "linear": _plain_linear, "loss": _plain_loss}[kind](s)
+    from paper_2606_03113_amd import lede
+    if kind == "fork":
+        status = lede.op_cache_fork(s["source"], s["seq_lens"], s["held"], s["tables"], s["shares"], lens=s["lens"])
+        m = lede.op_cache_own(s["seq_lens"], s["new_lens"], s["held"], s["free_pages"], s["free_head"], s["tables"], s["shares"], s["max_moves"])
+        lede.op_cache_copy(s["cache"], m.pairs, m.status[1:2])
+        return s["seq_lens"], s["held"], s["tables"], s["shares"], status, m.pairs, m.status, s["region"].view(torch.int32)
+    if kind == "free":
+        status = lede.op_cache_free(s["seq_lens"], s["held"], s["free_pages"], s["free_head"], s["tables"], s["shares"])
+        return s["held"], s["shares"], s["free_pages"], status
+    if kind == "compact":
+        m = lede.op_cache_compact(s["held"], s["free_pages"], s["free_head"], s["tables"], s["shares"], s["max_moves"])
+        lede.op_cache_copy(s["cache"], m.pairs, m.status[1:2])
+        return s["tables"], s["shares"], s["free_pages"], m.pairs, m.status, s["region"].view(torch.int32)
+    if kind == "linear":
+        return lede.op_quant_linear(s["matrix"], s["x"])
+    r = lede.op_head_loss(s["hidden"], s["head"], s["targets"])
+    if not s["case"]["grad"]:
+        return r.loss, r.lse
+    return (r.loss, r.lse) + lede.op_head_loss_grad(s["hidden"], s["head"], s["targets"], r.lse, s["weights"])
+
+
+# ---- what a pass cannot do without -----------------------------------------------------------
+
+
+def work(case):
+    kind = case["kind"]
+    if kind == "linear":
+        m, n, k, es = case["rows"], case["n"], case["k"], 4 if case["dtype"] == "f32" else 2
+        return {"bytes": n * ((k + 1) // 2 + 2 * -(-k // case["group"])) + m * (k + n) * es, "flops": 2 * m * n * k}
+    if kind == "loss":
+        m, V, d, es = case["rows"], case["vocab"], case["d"], 4 if case["dtype"] == "f32" else 2
+        both = 2 if case["grad"] else 1
+        return {"bytes": both * (m + V) * d * es + 12 * m + (4 * m if case["grad"] else 0), "flops": 2 * m * V * d * (3 if case["grad"] else 1)}
+    if kind == "free":
+        before, after, held, first, shared = _free_lengths(case)
+        drops = int(np.maximum(held - -(-after // PAGE), 0).sum())
+        return {"bytes": 16 * drops + 12 * len(held) + 20, "flops": 4 * drops}
+    page = 2 * PAGE * case["kv"] * case["hd"] + 8 * case["kv"]
+    if kind == "compact":
+        held, n_pages = _compact_lengths(case)
+        live = int(held.sum()) - (len(held) > 1)
+        moved = live * (n_pages - live) // n_pages      # about: a live page lies behind the live ones' number as often
+        return {"bytes": 8 * int(held.sum()) + 8 * (n_pages - live) + moved * (16 + 2 * page) + 4 * len(held) + 20, "flops": 4 * int(held.sum())}
+    source, seq, lens, new = _fork_lengths(case)
+    entries = int((-(-lens[source >= 0] // PAGE)).sum())
+    # a page that tokens share and fall into is copied for every holder but one
+    copies, writers = 0, {}
+    for i in np.nonzero(new)[0]:
+        n = int(lens[i] if source[i] >= 0 else seq[i])
+        if n % PAGE:
+            key = (int(source[i]) if source[i] >= 0 else int(i), n // PAGE)
+            writers.setdefault(key, []).append(i)
+    for (parent, place), who in writers.items():
+        holders = int(((source == parent) & (-(-lens // PAGE) > place)).sum()) + 1
+        copies += 0 if holders == 1 else len(who) - (len(who) == holders)
+    return {"bytes": 16 * entries + 32 * len(seq) + copies * (20 + 2 * page) + 32, "flops": 4 * entries}
+
+
+# ---- the operators from their definitions, in 64 bits ------------------------------------------
+
+
+def _arrays(s, *names):
+    return [s[n].cpu().numpy().astype(np.int64) for n in names]
+
+
+def _exact_moved(s, pairs):
+    """The cache's bytes after one page after the other has been copied."""
+    kv, hd, n = s["case"]["kv"], s["case"]["hd"], s["n_pages"]
+    region, size = s["region"].clone(), kv * PAGE * hd
+    for a, b in pairs:
+        for at, w in ((0, size), (n * size, size), (2 * n * size, 8 * kv)):
+            region[at + b * w:at + (b + 1) * w] = region[at + a * w:at + (a + 1) * w].clone()
+    return region.view(torch.int32)
+
+
+def _padded(pairs, room):
+    return np.array(list(pairs) + [(-1, -1)] * (room - len(pairs)), np.int32).reshape(room, 2)
+
+
+def _exact_fork(s):
+    source, lens, seq, held, new, tables, shares, free, head = _arrays(s, "source", "lens", "seq_lens", "held", "new_lens", "tables", "shares",
+                                                                     "free_pages", "free_head")
+    owners = {}
+    shared = 0
+    for i in range(len(seq)):
+        if source[i] >= 0:
+            seq[i], held[i] = lens[i], -(-lens[i] // PAGE)
+            tables[i, :held[i]] = tables[source[i], :held[i]]
+            shared += held[i]
+        for place in range(held[i]):
+            if tables[i, place] >= 0:
+                owners.setdefault(int(tables[i, place]), []).append(i)
+    writers = {}
+    for i in range(len(seq)):
+        for place in range(seq[i] // PAGE, min(held[i], -(-(seq[i] + new[i]) // PAGE)) if new[i] else 0):
+            page = int(tables[i, place])
+            if len(owners[page]) > 1:
+                writers.setdefault(page, []).append((i, place))
+    keeper = {page: min(w) for page, w in writers.items() if len(w) == len(owners[page])}
+    at, pairs = int(head[0]), []
+    for i, place, page in sorted((i, place, page) for page, w in writers.items() for i, place in w):
+        if keeper.get(page) == (i, place):
+            continue
+        tables[i, place] = free[at]
+        if place * PAGE < seq[i]:
+            pairs.append((page, int(free[at])))
+        owners[page].remove(i)
+        at += 1
+    for page, who in owners.items():
+        shares[page] = len(who) - 1
+    i32 = lambda a: np.asarray(a, np.int32)  # noqa: E731
+    return (i32(seq), i32(held), i32(tables), i32(shares), i32([0, shared, -1]), _padded(pairs, s["max_moves"]), i32([0, len(pairs), at, -1]),
+            _exact_moved(s, pairs))
+
+
+def _exact_free(s):
+    seq, held, tables, shares, free, head = _arrays(s, "seq_lens", "held", "tables", "shares", "free_pages", "free_head")
+    holders, order = shares + 1, []
+    for i in range(len(seq)):
+        for place in range(-(-seq[i] // PAGE), held[i]):
+            holders[tables[i, place]] -= 1
+            order.append(int(tables[i, place]))
+        held[i] = min(held[i], -(-seq[i] // PAGE))
+    gone = [page for page in dict.fromkeys(order) if holders[page] == 0]
+    at = int(head[0]) - len(gone)
+    free[at:at + len(gone)] = gone
+    i32 = lambda a: np.asarray(a, np.int32)  # noqa: E731
+    return i32(held), i32(np.maximum(holders - 1, 0)), i32(free), i32([0, len(gone), at, -1])
+
+
+def _exact_compact(s):
+    held, tables, shares, free = _arrays(s, "held", "tables", "shares", "free_pages")
+    live = sorted({int(page) for i in range(len(held)) for page in tables[i, :held[i]]})
+    n, total = len(live), s["n_pages"]
+    holes = [p for p in range(n) if p not in set(live)]
+    pairs = list(zip([p for p in live if p >= n], holes))
+    to = dict(pairs)
+    for i in range(len(held)):
+        tables[i, :held[i]] = [to.get(int(p), p) for p in tables[i, :held[i]]]
+    moved = np.zeros_like(shares)
+    for p in live:
+        moved[to.get(p, p)] = shares[p]
+    head = len(free) - (total - n)
+    free[head:] = np.arange(n, total)
+    i32 = lambda a: np.asarray(a, np.int32)  # noqa: E731
+    return i32(tables), i32(moved), i32(free), _padded(pairs, s["max_moves"]), i32([0, len(pairs), head, n]), _exact_moved(s, pairs)
+
+
+def _exact_linear(s):
+    case = s["case"]
+    out = torch.zeros(case["rows"], case["n"], dtype=torch.float64, device="cuda")
+    x, value = s["x"].double(), torch.tensor(E2M1, dtype=torch.float64, device="cuda")
+    for g in range(s["scales"].shape[1]):        # group by group
+        k0, k1 = g * case["group"], min((g + 1) * case["group"], case["k"])
+        half = s["codes"][:, k0 // 2:(k1 + 1) // 2].long()
+        part = torch.zeros(case["rows"], case["n"], dtype=torch.float64, device="cuda")
+        part += torch.mm(x[:, k0:k1:2], value[half & 15].t().contiguous())
+        if k1 - k0 > 1:
+            part += torch.mm(x[:, k0 + 1:k1:2], value[half >> 4][:, :(k1 - k0) // 2].t().contiguous())
+        out += part * s["scales"][:, g].double()
+    return out
+
+
+def _exact_loss(s):
+    case, t = s["case"], s["targets"].long()
+    h, rows, V = s["hidden"].double(), case["rows"], case["vocab"]
+    loss, lse = torch.zeros(rows, dtype=torch.float64, device="cuda"), torch.zeros(rows, dtype=torch.float64, device="cuda")
+    dh, dw = torch.zeros_like(h), torch.zeros(V, case["d"], dtype=torch.float64, device="cuda") if case["grad"] else None
+    w = s["head"].double()
+    wt = w.t().contiguous()
+    trained = (t >= 0) & (t < V)
+    for r in range(0, rows, 512):
+        z = torch.mm(h[r:r + 512], wt)
+        lp = torch.log_softmax(z, 1)
+        on = trained[r:r + 512]
+        pick = torch.where(on, t[r:r + 512], 0)[:, None]
+        loss[r:r + 512] = torch.where(on, -lp.gather(1, pick)[:, 0], 0.0)
+        lse[r:r + 512] = (z - lp)[:, 0]
+        if case["grad"]:
+            q = torch.exp(lp) - torch.zeros_like(lp).scatter_(1, pick, 1.0)
+            q *= torch.where(on, s["weights"][r:r + 512].double(), 0.0)[:, None]
+            dh[r:r + 512] = torch.mm(q, w)
+            dw += torch.mm(q.t().contiguous(), h[r:r + 512])
+    return (loss, lse, dh, dw) if case["grad"] else (loss, lse)
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"fork": _exact_fork, "free": _exact_free, "compact": _exact_compact, "linear": _exact_linear, "loss": _exact_loss}[case["kind"]](s)
