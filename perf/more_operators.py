@@ -5,7 +5,7 @@ A case is a dict of plain values.  Five kinds, each one pass through calls of pa
 
   fork     op_cache_fork, op_cache_own and op_cache_copy: sequences that share the pages of others, and the pages that
            their next tokens fall into made their own
-  free     op_cache_free: pages that their sequences no longer need go back to the pool
+  free     op_cache_free: pages that their sequences no longer need go back to the pool, in ascending order
   compact  op_cache_compact and op_cache_copy: live pages moved to the pool's front
   linear   op_quant_linear: rows times a matrix of 4-bit codes with a scale for each group of columns
   loss     op_head_loss, and op_head_loss_grad where the case has a gradient: -log softmax(hidden head^T)[target] of
@@ -305,14 +305,14 @@ def _plain_free(s):
     col = torch.arange(tables.shape[1], device="cuda")
     keep, held, head, page = _pages(s["seq_lens"].long()), s["held"].long(), s["free_head"].long()[0], tables.long()
     drops = (col >= keep[:, None]) & (col < held[:, None])
-    left = shares.long() - _count(page, drops, n_pages)
-    frees = _first(page, drops, n_pages) & (left[page.clamp(min=0)] < 0)
+    dropped = _count(page, drops, n_pages)
+    left = shares.long() - dropped
+    frees = (dropped > 0) & (left < 0)
     shares.copy_(left.clamp(min=0))
     total = frees.sum()
-    rank = torch.cumsum(frees.reshape(-1).long(), 0) - 1
     size = s["free_pages"].numel()
     room = torch.cat([s["free_pages"].long(), torch.zeros(1, dtype=torch.long, device="cuda")])
-    room[torch.where(frees.reshape(-1), head - total + rank, size)] = page.reshape(-1)
+    room[torch.where(frees, head - total + torch.cumsum(frees.long(), 0) - 1, size)] = torch.arange(n_pages, device="cuda")
     s["free_pages"].copy_(room[:size])
     s["held"].copy_(torch.minimum(held, keep))
     return s["held"], shares, s["free_pages"], _status(0, total, head - total, -1)
@@ -493,13 +493,14 @@ def _exact_fork(s):
 
 def _exact_free(s):
     seq, held, tables, shares, free, head = _arrays(s, "seq_lens", "held", "tables", "shares", "free_pages", "free_head")
-    holders, order = shares + 1, []
+    holders, gone = shares + 1, []
     for i in range(len(seq)):
         for place in range(-(-seq[i] // PAGE), held[i]):
             holders[tables[i, place]] -= 1
-            order.append(int(tables[i, place]))
+            if holders[tables[i, place]] == 0:
+                gone.append(int(tables[i, place]))
         held[i] = min(held[i], -(-seq[i] // PAGE))
-    gone = [page for page in dict.fromkeys(order) if holders[page] == 0]
+    gone.sort()
     at = int(head[0]) - len(gone)
     free[at:at + len(gone)] = gone
     i32 = lambda a: np.asarray(a, np.int32)  # noqa: E731
