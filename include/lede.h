@@ -611,6 +611,77 @@ int lede_op_cache_plan(const int32_t* seq_lens, const int32_t* new_lens, const i
                        int32_t table_ld, int32_t max_rows, int32_t* kv_lens, int32_t* held_out, int32_t* row_start,
                        int64_t* slots, int32_t* status, void* stream);
 
+/* Pages that sequences share.  shares[page] (n_pages entries, cleared to zero
+ * by the caller with the pool) counts the holders of a page besides one: 0 for
+ * a free page and for one that a plan has just taken, so that plans need not
+ * know of it.  The five calls that follow keep it.  An entry of a table
+ * outside the pool is passed on by a fork and otherwise left alone.  Errors of
+ * the lengths are found on the device, as in a plan, and change nothing but
+ * the status (and the pairs, which are then all -1).  They return
+ * LEDE_E_ARG on null pointers and sizes below 1 (below 0: n_free, max_moves),
+ * LEDE_E_UNSUPPORTED from 2^24 sequences, table entries a row or moves on.
+ *
+ * Fork: sequence s with source[s] = r >= 0 becomes the first lens[s] tokens of
+ * sequence r (all of them where lens is null): its table row gets r's pages
+ * of these, seq_lens[s] and held[s] follow, and each page has a holder more.
+ * source[s] = -1 leaves s as it is.  r itself is no fork of the same call.
+ * status [3]: 0 or an error, the number of entries shared, the first sequence
+ * that failed or -1.  LEDE_E_ARG: source[s] neither -1 nor another sequence
+ * with source -1, lengths of r that its row does not hold, lens[s] outside [0,
+ * seq_lens[r]]; LEDE_E_STATE: s holds pages (held[s] != 0). */
+int lede_op_cache_fork(const int32_t* source, const int32_t* lens, int32_t* seq_lens, int32_t* held, int32_t n_seqs,
+                       int32_t* tables, int32_t table_ld, int32_t* shares, int32_t n_pages, int32_t* status, void* stream);
+
+/* Own: before a plan and an append write new_lens[s] tokens behind the
+ * seq_lens[s] cached ones, the pages among the held[s] that they fall into
+ * become the sequence's alone.  A page with other holders is replaced by one
+ * of free_pages[*free_head ..], in sequence order, then in table order; where
+ * all of its holders write, the first of them keeps it.  Where the page holds
+ * tokens already, (old page, new page) is listed in pairs [max_moves][2] for
+ * lede_op_cache_copy, at most one a sequence; -1 behind the last.  status [4]:
+ * 0 or an error, the number of pairs, the position in free_pages after the
+ * call, the first sequence that failed or -1.  free_head may be status + 2.
+ * LEDE_E_ARG: a negative length, held outside [pages of seq_lens, table_ld],
+ * free_head outside [0, n_free], more pairs than max_moves; LEDE_E_KV_FULL. */
+int lede_op_cache_own(const int32_t* seq_lens, const int32_t* new_lens, const int32_t* held, int32_t n_seqs,
+                      const int32_t* free_pages, int32_t n_free, const int32_t* free_head, int32_t* tables, int32_t table_ld,
+                      int32_t* shares, int32_t n_pages, int32_t* pairs, int32_t max_moves, int32_t* status, void* stream);
+
+/* Copy: of one layer's cache, page pairs[i][0] to page pairs[i][1], codes and
+ * scales, for i < min(*count, max_moves) (pairs and count on the device: the
+ * result of own or compact, whose status + 1 is the count).  A pair with a
+ * page outside the pool is skipped.  No page is written twice, or written and
+ * read (else what it holds is undefined).  LEDE_E_ARG also for a cache that
+ * is not 16-byte aligned; the cache's other errors as lede_op_cache_append. */
+int lede_op_cache_copy(const int32_t* pairs, const int32_t* count, int32_t max_moves, void* cache, int32_t n_pages,
+                       int32_t n_kv_heads, int32_t head_dim, void* stream);
+
+/* Free: each sequence gives back the pages that its seq_lens[s] tokens do not
+ * need, the entries from ceil(seq_lens[s] / 64) on of the held[s] (all with
+ * seq_lens[s] = 0), and held[s] follows.  Pages without a holder left are put
+ * before *free_head in free_pages, in ascending order (pools stay dense).  status [4]: 0 or an
+ * error, the number of pages freed, the position in free_pages after the
+ * call, the first sequence that failed or -1.  free_head may be status + 2.
+ * LEDE_E_ARG: a negative length, held outside [0, table_ld], free_head outside
+ * [0, n_free], fewer than that many entries before it.  Returns
+ * LEDE_E_UNSUPPORTED above 2^18 pages. */
+int lede_op_cache_free(const int32_t* seq_lens, int32_t* held, int32_t n_seqs, int32_t* free_pages, int32_t n_free,
+                       const int32_t* free_head, const int32_t* tables, int32_t table_ld, int32_t* shares, int32_t n_pages,
+                       int32_t* status, void* stream);
+
+/* Compact: the L pages that the tables' held entries name move to the pages
+ * 0 .. L - 1: in ascending order, those from L on to the pages before L that
+ * no entry names.  Listed in pairs [max_moves][2] (-1 behind the last) for
+ * lede_op_cache_copy; tables and shares follow.  All other pages are free
+ * then, L .. n_pages - 1, as the last entries of free_pages.  status [4]: 0 or
+ * an error, the number of moves, the position in free_pages after the call, L
+ * (of an error the first sequence that failed or -1).  free_head may be status
+ * + 2.  LEDE_E_ARG: held outside [0, table_ld], more moves than max_moves,
+ * n_free < n_pages - L.  Returns LEDE_E_UNSUPPORTED above 2^18 pages. */
+int lede_op_cache_compact(const int32_t* held, int32_t n_seqs, int32_t* free_pages, int32_t n_free, const int32_t* free_head,
+                          int32_t* tables, int32_t table_ld, int32_t* shares, int32_t n_pages, int32_t* pairs, int32_t max_moves,
+                          int32_t* status, void* stream);
+
 /* K/V rows into the cache: row r (k + r * ldk and v + r * ldv elements of
  * `dtype`, n_kv heads of head_dim) goes to slots[r]; a slot outside the pool
  * skips its row.  Rows of one page stand next to each other with no skipped

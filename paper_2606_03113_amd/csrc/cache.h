@@ -75,6 +75,37 @@ struct CacheAttnArgs {
   void* out; int64_t ldo;
 };
 
+// The pages' life (cache_pages.hip).  The calls take what they need of these.
+constexpr int CACHE_MOST_PAGES = 1 << 18;   // of a pool that is freed into or compacted: a bit a page in LDS
+struct CachePagesArgs {
+  const int32_t *source, *lens;               // [n_seqs]; lens may be null
+  const int32_t* new_lens;                    // [n_seqs]
+  int32_t *seq_lens, *held;                   // [n_seqs]
+  int n_seqs;
+  int32_t* tables;
+  int table_ld;
+  int32_t* shares;                            // [n_pages]
+  int n_pages;
+  int32_t* free_pages;
+  int n_free;
+  const int32_t* free_head;                   // [1]; may be status + 2
+  int32_t* pairs;                             // [max_moves][2]: source page, destination page
+  int max_moves;
+  int32_t* status;
+};
+struct CacheCopyArgs {
+  CacheView c;
+  const int32_t* pairs;
+  const int32_t* count;                       // [1]
+  int max_moves;
+};
+
+hipError_t launch_cache_fork(const CachePagesArgs& a, hipStream_t s);
+hipError_t launch_cache_own(const CachePagesArgs& a, hipStream_t s);
+hipError_t launch_cache_free(const CachePagesArgs& a, hipStream_t s);
+hipError_t launch_cache_compact(const CachePagesArgs& a, hipStream_t s);
+hipError_t launch_cache_copy(const CacheCopyArgs& a, hipStream_t s);
+
 hipError_t launch_cache_plan(const CachePlanArgs& a, hipStream_t s);
 hipError_t launch_cache_append(int dtype, const CacheRowsArgs& a, hipStream_t s);
 hipError_t launch_cache_read(int dtype, const CacheRowsArgs& a, hipStream_t s);

@@ -85,7 +85,8 @@ EXPORTED = ["lede_region_bytes", "lede_create", "lede_destroy", "lede_last_error
             "lede_dqn_update", "lede_dqn_sync_target", "lede_dqn_act", "lede_dqn_read", "lede_step_submit",
             "lede_step_collect", "lede_load_weights", "lede_debug_logits", "lede_debug_inject_failure", "lede_op_sample_noalloc",
             "lede_op_cache_bytes", "lede_op_cache_plan", "lede_op_cache_append", "lede_op_cache_read",
-            "lede_op_cache_attention_bytes", "lede_op_cache_attention", "lede_op_logprobs_bytes", "lede_op_logprobs"]
+            "lede_op_cache_attention_bytes", "lede_op_cache_attention", "lede_op_logprobs_bytes", "lede_op_logprobs",
+            "lede_op_cache_fork", "lede_op_cache_own", "lede_op_cache_copy", "lede_op_cache_free", "lede_op_cache_compact"]
 MAX_IN_FLIGHT = 2
 SAMPLE_SLOTS = 16
 SAMPLE_STRIDE = 33
@@ -159,6 +160,11 @@ def load(path: str = LIB_PATH):
     L.lede_dqn_read.argtypes = [vp, i32, fp, sz, P(i32), vp]
     i64, f32 = ctypes.c_int64, ctypes.c_float
     L.lede_op_cache_bytes.argtypes = [i32] * 3
+    L.lede_op_cache_fork.argtypes = [vp, vp, vp, vp, i32, vp, i32, vp, i32, vp, vp]
+    L.lede_op_cache_own.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, i32, vp, i32, vp, i32, vp, vp]
+    L.lede_op_cache_copy.argtypes = [vp, vp, i32, vp, i32, i32, i32, vp]
+    L.lede_op_cache_free.argtypes = [vp, vp, i32, vp, i32, vp, vp, i32, vp, i32, vp, vp]
+    L.lede_op_cache_compact.argtypes = [vp, i32, vp, i32, vp, vp, i32, vp, i32, vp, i32, vp, vp]
     L.lede_op_cache_plan.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]
     L.lede_op_cache_append.argtypes = [i32, vp, i64, vp, i64, vp, i32, vp, i32, i32, i32, vp]
     L.lede_op_cache_read.argtypes = [i32, vp, i32, i32, i32, vp, i32, vp, i64, vp, i64, vp]
@@ -686,6 +692,106 @@ def op_cache_plan(seq_lens, new_lens, held, free_pages, free_head, tables, max_r
     _call(dev, "op_cache_plan", load().lede_op_cache_plan, seq_lens.data_ptr(), new_lens.data_ptr(), held.data_ptr(), n,
           free_pages.data_ptr(), free_pages.numel(), free_head.data_ptr(), tables.data_ptr(), tables.shape[1], max_rows,
           out.kv_lens.data_ptr(), out.held.data_ptr(), out.row_start.data_ptr(), out.slots.data_ptr(), out.status.data_ptr())
+    return out
+
+
+def _status(torch, status, n: int, device, what: str):
+    if status is None:
+        return torch.empty(n, dtype=torch.int32, device=device)
+    _need(_dense(device, torch.int32, status) and status.numel() == n, what + ": status")
+    return status
+
+
+def op_cache_fork(source, seq_lens, held, tables, shares, lens=None, status=None):
+    """Sequence s with source[s] = r >= 0 becomes the first lens[s] tokens of
+    sequence r (all of them without `lens`) and shares its pages; -1 leaves it.
+    int32 GPU tensors; seq_lens, held, tables [n_seqs][width] and shares
+    [n_pages] are updated.  Returns status [3]: code, entries shared, first
+    failing sequence."""
+    import torch
+    dev, n = seq_lens.device, seq_lens.numel()
+    _need(_dense(dev, torch.int32, source, seq_lens, held, tables, shares) and tables.dim() == 2 and source.numel() == n
+          and held.numel() == n and tables.shape[0] == n
+          and (lens is None or (_dense(dev, torch.int32, lens) and lens.numel() == n)), "op_cache_fork")
+    status = _status(torch, status, 3, dev, "op_cache_fork")
+    _call(dev, "op_cache_fork", load().lede_op_cache_fork, source.data_ptr(), None if lens is None else lens.data_ptr(),
+          seq_lens.data_ptr(), held.data_ptr(), n, tables.data_ptr(), tables.shape[1], shares.data_ptr(), shares.numel(),
+          status.data_ptr())
+    return status
+
+
+@dataclass
+class CacheMoves:
+    pairs: object    # [max_moves][2]: page, page that gets its content; -1 behind the last
+    status: object   # code, moves, place in the free list after the call, first failing sequence (compact: live pages)
+
+
+def _moves(torch, out, max_moves: int, device, what: str) -> CacheMoves:
+    if out is None:
+        buf = torch.empty(2 * max_moves + 4, dtype=torch.int32, device=device)
+        return CacheMoves(buf[4:].view(max_moves, 2), buf[:4])
+    _need(_dense(device, torch.int32, out.pairs, out.status) and out.pairs.numel() == 2 * max_moves and out.status.numel() == 4,
+          what + ": out")
+    return out
+
+
+def op_cache_own(seq_lens, new_lens, held, free_pages, free_head, tables, shares, max_moves: int,
+                 out: Optional[CacheMoves] = None) -> CacheMoves:
+    """Before new_lens[s] tokens are appended behind seq_lens[s]: the held pages
+    that they fall into become the sequence's alone (tables and shares are
+    updated).  Pages whose content has to follow are listed for op_cache_copy;
+    max_moves = n_seqs always suffices."""
+    import torch
+    dev, n, max_moves = seq_lens.device, seq_lens.numel(), int(max_moves)
+    _need(_dense(dev, torch.int32, seq_lens, new_lens, held, free_pages, free_head, tables, shares) and tables.dim() == 2
+          and new_lens.numel() == n and held.numel() == n and tables.shape[0] == n and free_head.numel() == 1 and max_moves >= 0,
+          "op_cache_own")
+    out = _moves(torch, out, max_moves, dev, "op_cache_own")
+    _call(dev, "op_cache_own", load().lede_op_cache_own, seq_lens.data_ptr(), new_lens.data_ptr(), held.data_ptr(), n,
+          free_pages.data_ptr(), free_pages.numel(), free_head.data_ptr(), tables.data_ptr(), tables.shape[1], shares.data_ptr(),
+          shares.numel(), out.pairs.data_ptr(), max_moves, out.status.data_ptr())
+    return out
+
+
+def op_cache_copy(cache: Cache, pairs, count):
+    """Page pairs[i][0] of the cache to page pairs[i][1], for the first
+    count[0] of the pairs [max_moves][2] (int32; moves.pairs and
+    moves.status[1:2] of op_cache_own and op_cache_compact); once a layer."""
+    import torch
+    dev = cache.device
+    _need(_dense(dev, torch.int32, pairs, count) and pairs.dim() == 2 and pairs.shape[1] == 2 and count.numel() == 1, "op_cache_copy")
+    _call(dev, "op_cache_copy", load().lede_op_cache_copy, pairs.data_ptr(), count.data_ptr(), pairs.shape[0], cache.region.data_ptr(),
+          cache.n_pages, cache.n_kv, cache.head_dim)
+
+
+def op_cache_free(seq_lens, held, free_pages, free_head, tables, shares, status=None):
+    """Pages that the sequences' seq_lens[s] tokens do not need (all of them
+    where that is 0) are given back; held, shares and free_pages are updated.
+    Returns status [4]: code, pages freed, place in the free list after the
+    call, first failing sequence (free_head may be its [2:3])."""
+    import torch
+    dev, n = seq_lens.device, seq_lens.numel()
+    _need(_dense(dev, torch.int32, seq_lens, held, free_pages, free_head, tables, shares) and tables.dim() == 2 and held.numel() == n
+          and tables.shape[0] == n and free_head.numel() == 1, "op_cache_free")
+    status = _status(torch, status, 4, dev, "op_cache_free")
+    _call(dev, "op_cache_free", load().lede_op_cache_free, seq_lens.data_ptr(), held.data_ptr(), n, free_pages.data_ptr(),
+          free_pages.numel(), free_head.data_ptr(), tables.data_ptr(), tables.shape[1], shares.data_ptr(), shares.numel(),
+          status.data_ptr())
+    return status
+
+
+def op_cache_compact(held, free_pages, free_head, tables, shares, max_moves: int, out: Optional[CacheMoves] = None) -> CacheMoves:
+    """The pages that the tables' held entries name become the pool's first
+    ones (tables, shares and free_pages are updated); the moves are listed for
+    op_cache_copy; max_moves = n_pages // 2 always suffices."""
+    import torch
+    dev, n, max_moves = held.device, held.numel(), int(max_moves)
+    _need(_dense(dev, torch.int32, held, free_pages, free_head, tables, shares) and tables.dim() == 2 and tables.shape[0] == n
+          and free_head.numel() == 1 and max_moves >= 0, "op_cache_compact")
+    out = _moves(torch, out, max_moves, dev, "op_cache_compact")
+    _call(dev, "op_cache_compact", load().lede_op_cache_compact, held.data_ptr(), n, free_pages.data_ptr(), free_pages.numel(),
+          free_head.data_ptr(), tables.data_ptr(), tables.shape[1], shares.data_ptr(), shares.numel(), out.pairs.data_ptr(), max_moves,
+          out.status.data_ptr())
     return out
 
 
