@@ -761,6 +761,40 @@ int lede_op_logprobs(int32_t dtype, const void* logits, int64_t ld, int32_t n_ro
                      const int32_t* tokens, int32_t n_top, float* logprobs, int32_t* ranks, float* entropy,
                      int32_t* top_ids, float* top_logprobs, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- linear products with 4-bit weights -------------------------------------
+ * A matrix W [N][K] of e2m1 codes (OCP: 0, 0.5, 1, 1.5, 2, 3, 4, 6; the fourth
+ * bit is the sign) with a bf16 scale for every `group` (32, 64 or 128) columns
+ * of a row: W[n][k] = scale * value(code).  As rows: codes [N][ceil(K / 2)]
+ * bytes, the lower column in the low four bits, and scales [N][ceil(K /
+ * group)], any bf16 numbers (NaN and infinities, too, stay with their row).
+ * Packed: what the products read, lede_op_quant_bytes, 16-byte aligned.  The
+ * calls follow the conventions of the batch operators above.  LEDE_E_ARG: null
+ * pointers, bad dtypes, sizes below 1, row strides below the row's length,
+ * pointers that are not aligned to their elements; LEDE_E_UNSUPPORTED
+ * (lede_op_quant_bytes returns 0): another group, sides of 2^24 or more, more
+ * than 2^24 tiles of 16 x 128. */
+size_t lede_op_quant_bytes(int32_t N, int32_t K, int32_t group);
+
+/* Weights w [N][K] (row stride ldw, `dtype`) to codes and scales: the scale is
+ * max |w| of its group / 6, rounded to bf16, a code the nearest to w / scale,
+ * ties to the even one (the quotient itself is not rounded).  A group with an
+ * entry that is not finite has a NaN scale, one whose scale rounds to 0 zeros. */
+int lede_op_quantize(int32_t dtype, const void* w, int64_t ldw, int32_t N, int32_t K, int32_t group, uint8_t* codes,
+                     uint16_t* scales, void* stream);
+
+/* Codes and scales as rows to the packed layout. */
+int lede_op_quant_pack(const uint8_t* codes, const uint16_t* scales, int32_t N, int32_t K, int32_t group, void* packed, void* stream);
+
+/* y[m][n] = sum_k W[n][k] x[m][k] for m < M rows of x (`dtype`, row stride
+ * ldx, any element alignment; faster where x and its rows are 16-byte
+ * aligned), rounded to y_dtype.  Codes and x enter exactly; sums over a
+ * group, and of the groups' scaled sums, are fp32 (terms below 2^-110 may
+ * count as 0).  What is not finite in a row of x stays with that row of y.  y
+ * overlaps nothing else.  M = 0 is no work; LEDE_E_UNSUPPORTED: M of 2^20 or
+ * more. */
+int lede_op_quant_linear(int32_t dtype, const void* packed, int32_t N, int32_t K, int32_t group, const void* x, int64_t ldx,
+                         int32_t M, int32_t y_dtype, void* y, int64_t ldy, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -86,7 +86,8 @@ EXPORTED = ["lede_region_bytes", "lede_create", "lede_destroy", "lede_last_error
             "lede_step_collect", "lede_load_weights", "lede_debug_logits", "lede_debug_inject_failure", "lede_op_sample_noalloc",
             "lede_op_cache_bytes", "lede_op_cache_plan", "lede_op_cache_append", "lede_op_cache_read",
             "lede_op_cache_attention_bytes", "lede_op_cache_attention", "lede_op_logprobs_bytes", "lede_op_logprobs",
-            "lede_op_cache_fork", "lede_op_cache_own", "lede_op_cache_copy", "lede_op_cache_free", "lede_op_cache_compact"]
+            "lede_op_cache_fork", "lede_op_cache_own", "lede_op_cache_copy", "lede_op_cache_free", "lede_op_cache_compact",
+            "lede_op_quant_bytes", "lede_op_quantize", "lede_op_quant_pack", "lede_op_quant_linear"]
 MAX_IN_FLIGHT = 2
 SAMPLE_SLOTS = 16
 SAMPLE_STRIDE = 33
@@ -160,6 +161,12 @@ def load(path: str = LIB_PATH):
     L.lede_dqn_read.argtypes = [vp, i32, fp, sz, P(i32), vp]
     i64, f32 = ctypes.c_int64, ctypes.c_float
     L.lede_op_cache_bytes.argtypes = [i32] * 3
+    i64 = ctypes.c_int64
+    L.lede_op_quant_bytes.argtypes = [i32, i32, i32]
+    L.lede_op_quant_bytes.restype = sz
+    L.lede_op_quantize.argtypes = [i32, vp, i64, i32, i32, i32, vp, vp, vp]
+    L.lede_op_quant_pack.argtypes = [vp, vp, i32, i32, i32, vp, vp]
+    L.lede_op_quant_linear.argtypes = [i32, vp, i32, i32, i32, vp, i64, i32, i32, vp, i64, vp]
     L.lede_op_cache_fork.argtypes = [vp, vp, vp, vp, i32, vp, i32, vp, i32, vp, vp]
     L.lede_op_cache_own.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, i32, vp, i32, vp, i32, vp, vp]
     L.lede_op_cache_copy.argtypes = [vp, vp, i32, vp, i32, i32, i32, vp]
@@ -898,6 +905,69 @@ def op_logprobs(logits, tokens, n_top: int = 0, temperature: float = 1.0, worksp
           at if given else None, at_ranks if given else None, at + 4 * rows, at_ranks + 4 * rows, at + 8 * rows, ws_at, ws_bytes)
     return Logprobs(logprobs.view(f32) if given else None, ranks if given else None, entropy.view(f32), ids.view(rows, n_top),
                     top.view(f32).view(rows, n_top))
+
+
+# ---- linear products with 4-bit weights ---------------------------------------------
+
+def _matrix_stride(x, what: str) -> int:
+    """Elements between the rows of x [rows][columns], whose columns are dense."""
+    rows, cols = x.shape
+    r, c = x.stride()
+    _need(c == 1 or cols == 1, what)
+    return r if rows > 1 else max(r, cols)
+
+
+def op_quantize(w, group: int = 64):
+    """(codes, scales) of weights w [N][K] (float32 or bfloat16, any row
+    stride): e2m1 codes, two a byte, uint8 [N][ceil(K / 2)], and a bfloat16
+    scale for every `group` (32, 64 or 128) columns, [N][ceil(K / group)]."""
+    import torch
+    _need(w.dim() == 2, "op_quantize")
+    (N, K), dev = w.shape, w.device
+    ld = _matrix_stride(w, "op_quantize")
+    if load().lede_op_quant_bytes(N, K, group) == 0:
+        raise LedeError(LEDE_E_UNSUPPORTED, "op_quantize: %d x %d, group %d" % (N, K, group))
+    codes = torch.empty(N, (K + 1) // 2, dtype=torch.uint8, device=dev)
+    scales = torch.empty(N, -(-K // group), dtype=torch.bfloat16, device=dev)
+    _call(dev, "op_quantize", load().lede_op_quantize, _dtype_code(torch, w.dtype), w.data_ptr(), ld, N, K, group, codes.data_ptr(),
+          scales.data_ptr())
+    return codes, scales
+
+
+class QuantMatrix:
+    """A matrix [N][K] of 4-bit weights, packed for op_quant_linear from codes
+    and scales as op_quantize gives them (which may go afterwards)."""
+
+    def __init__(self, codes, scales, K: int, group: int):
+        import torch
+        N, dev = codes.shape[0], codes.device
+        nbytes = load().lede_op_quant_bytes(N, K, group)
+        if nbytes == 0:
+            raise LedeError(LEDE_E_UNSUPPORTED, "4-bit matrix of %d x %d, group %d" % (N, K, group))
+        _need(_dense(dev, torch.uint8, codes) and _dense(dev, torch.bfloat16, scales) and codes.shape == (N, (K + 1) // 2)
+              and scales.shape == (N, -(-K // group)), "QuantMatrix")
+        self.packed = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        self.N, self.K, self.group, self.device = N, K, group, dev
+        _call(dev, "QuantMatrix", load().lede_op_quant_pack, codes.data_ptr(), scales.data_ptr(), N, K, group, self.packed.data_ptr())
+
+
+def op_quant_linear(matrix: QuantMatrix, x, dtype=None, out=None):
+    """x W^T for rows x [M][K] (float32 or bfloat16, any row stride) and a
+    matrix of 4-bit weights: [M][N] of `dtype` (x's when not given); `out`
+    gives the tensor, of any row stride."""
+    import torch
+    dev, N, K = matrix.device, matrix.N, matrix.K
+    _need(x.dim() == 2 and x.shape[1] == K and x.device == dev, "op_quant_linear")
+    M, ldx = x.shape[0], _matrix_stride(x, "op_quant_linear: x")
+    if out is None:
+        out = torch.empty(M, N, dtype=dtype or x.dtype, device=dev)
+        ldy = N
+    else:
+        _need(out.shape == (M, N) and out.device == dev and (dtype is None or out.dtype == dtype), "op_quant_linear: out")
+        ldy = _matrix_stride(out, "op_quant_linear: out")
+    _call(dev, "op_quant_linear", load().lede_op_quant_linear, _dtype_code(torch, x.dtype), matrix.packed.data_ptr(), N, K, matrix.group,
+          x.data_ptr(), ldx, M, _dtype_code(torch, out.dtype), out.data_ptr(), ldy)
+    return out
 
 
 def dqn_noise_count(hidden: int) -> int:
