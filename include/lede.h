@@ -795,6 +795,45 @@ int lede_op_quant_pack(const uint8_t* codes, const uint16_t* scales, int32_t N, 
 int lede_op_quant_linear(int32_t dtype, const void* packed, int32_t N, int32_t K, int32_t group, const void* x, int64_t ldx,
                          int32_t M, int32_t y_dtype, void* y, int64_t ldy, void* stream);
 
+/* ---- the vocabulary head's loss, without the logits --------------------------
+ * Of M rows hidden [M][K] (row stride ldh) and a head [V][K] (row stride ldw),
+ * both of `dtype`, and a target for each row: the logits z = hidden head^T are
+ * formed tile by tile and never written.  (What trains a head that the exit
+ * layers share, Section 2.2, or scores given tokens without their logits.)  A
+ * target outside [0, V) leaves its row out: its loss is 0 and it takes no part
+ * in a gradient, whatever the row holds.  The calls follow the conventions of
+ * the batch operators above.
+ *
+ *   lse[m]   log sum_v exp z[m][v]  (fp32; required)
+ *   loss[m]  lse[m] - z[m][targets[m]]  (fp32; may be null)
+ * Products are exact and sums fp32 (fp32 inputs enter as three bf16 numbers
+ * each, of whose nine products the six largest count: 2^-22 of the largest).
+ * A row whose logits are all -infinity or include a NaN or +infinity has NaN.
+ * LEDE_E_ARG: null pointers, bad dtypes, M < 0, V or K < 1, row strides below
+ * K; hidden, head, the gradients, workspace or row strides not multiples of 16
+ * bytes; a workspace smaller than lede_op_head_loss_bytes (of the same sizes).
+ * LEDE_E_UNSUPPORTED (the sizes are 0): K not a multiple of 8 or above 2^15, M
+ * above 2^18, V above 2^20. */
+size_t lede_op_head_loss_bytes(int32_t dtype, int32_t M, int32_t V, int32_t K);
+int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M, const void* head, int64_t ldw, int32_t V,
+                      int32_t K, const int32_t* targets, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/* The gradient of sum_m weights[m] loss[m] (weights null: 1) with the lse that
+ * lede_op_head_loss gave:
+ *   d_hidden [M][K]  dz head,      dz[m][v] = weights[m] (exp(z[m][v] - lse[m]) - [v = targets[m]])
+ *   d_head   [V][K]  dz^T hidden
+ * of `dtype`, either of them null where it is not asked for.  A row whose
+ * weight is 0 is left out, too.  dz enters the two products with bf16's 8 bits
+ * where the inputs are bf16 (its rounding and the result's are alike) and
+ * with 24 where they are fp32.  d_hidden and d_head overlap nothing else.
+ * Sums have a fixed order: the same call gives the same bits.  M = 0 clears
+ * d_head.  Errors as above, with lede_op_head_loss_grad_bytes. */
+size_t lede_op_head_loss_grad_bytes(int32_t dtype, int32_t M, int32_t V, int32_t K);
+int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32_t M, const void* head, int64_t ldw, int32_t V,
+                           int32_t K, const int32_t* targets, const float* lse, const float* weights, void* d_hidden, int64_t ld_dh,
+                           void* d_head, int64_t ld_dw, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

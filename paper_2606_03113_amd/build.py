@@ -7,7 +7,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 SO = os.path.join(HERE, "liblede.so")
 SOURCES = ["linear.hip", "wide.hip", "norm.hip", "attention.hip", "accept.hip", "policy.hip", "dqn.hip", "misc.hip", "noalloc.hip",
-           "cache.hip", "cache_pages.hip", "cache_attention.hip", "logprobs.hip", "quant.hip", "runtime.cpp", "dqn.cpp", "cache.cpp",
+           "cache.hip", "cache_pages.hip", "cache_attention.hip", "logprobs.hip", "quant.hip", "loss.hip", "runtime.cpp", "dqn.cpp", "cache.cpp",
            "products.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -1,0 +1,58 @@
+// The vocabulary head's loss and its gradient (loss.hip; entry points in
+// products.cpp): the kernels' arguments.  Not part of the public C ABI.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace lede {
+
+// What a product's tile becomes.
+enum HeadEpi : int {
+  HEAD_SUMS = 0,   // i = v, j = m: each row's maximum and sum of exponentials over the tile, and the target's logit
+  HEAD_DZ = 1,     // i = v, j = m: dz, rounded to bf16 or in three parts
+  HEAD_PART = 2,   // i = k, j = m: fp32 sums of a part of the contraction over v
+  HEAD_OUT = 3,    // i = k, j = v: dW
+};
+
+constexpr int HEAD_TILE = 256;   // entries of the vocabulary of a tile
+
+struct HeadArgs {
+  const uint8_t *A, *B;            // bf16 numbers, `planes` planes of them
+  int64_t lda, ldb, plane_a, plane_b;   // elements, bytes
+  int n_i, n_j, C;                 // rows of A and B, length of the contraction
+  int passes;                      // over the contraction: 1, or the six products of parts
+  int chunk;                       // entries of the contraction that a block takes
+  int i_tiles, j_tiles;
+  int planes;                      // 1 (bf16) or 3 (fp32)
+  const int32_t* targets; const float *weights, *lse;
+  int V, v0;                       // the vocabulary, the piece's first entry
+  float2* sums; int ld_sums, tile0;   // HEAD_SUMS: [row][tile of the vocabulary]
+  float* target_z;
+  uint8_t* dz; int64_t plane_dz; int ldz;   // HEAD_DZ: [row][ldz], zeros past the piece
+  float* part; bool add;           // HEAD_PART: [split][row][K]
+  void* out; int64_t ldo;          // HEAD_OUT
+};
+struct HeadCopyArgs {
+  const void* src; int64_t ld;
+  int64_t n; int K;
+  uint8_t* dst; int64_t plane;     // [n][K]; bytes between planes
+  const int32_t* targets; const float* weights; int V;   // null: every row is kept
+};
+struct HeadJoinArgs {
+  const float2* sums; const float* target_z;
+  int n, tiles, V;
+  const int32_t* targets;
+  float *loss, *lse;
+};
+struct HeadOutArgs {
+  const float* part;
+  int split; int64_t n; int K;
+  void* out; int64_t ldo;
+};
+hipError_t launch_head(int epi, const HeadArgs& a, int split, int tile, hipStream_t s);
+hipError_t launch_head_copy(int dtype, const HeadCopyArgs& a, hipStream_t s);
+hipError_t launch_head_join(const HeadJoinArgs& a, hipStream_t s);
+hipError_t launch_head_out(int dtype, const HeadOutArgs& a, hipStream_t s);
+
+}  // namespace lede

@@ -1,0 +1,396 @@
+// The vocabulary head's loss and its gradient without the logits (gfx950).
+//
+// For rows h_m, the head's rows w_v and targets t_m:
+//   z_mv = h_m . w_v,  lse_m = log sum_v exp z_mv,  loss_m = lse_m - z_m,t
+//   dz_mv = g_m (exp(z_mv - lse_m) - [v = t_m]),  dh = dz W,  dW = dz^T h
+// Three products of 2 M V K operations, and the logits' once more in the
+// backward pass: cheaper than to write and read them (M V against K operations
+// an entry).  The forward pass keeps a maximum and a sum for each row and tile
+// of the vocabulary; the backward pass holds dz for a piece of the vocabulary
+// at a time.  Compute-bound for many rows, bound by the head's bytes for few.
+#include "device.h"
+#include "loss.h"
+
+namespace lede {
+
+__device__ uint4 head_zeros[1];   // what is read in place of a contraction's entries past its end
+
+// Four 16-bit entries of a column: of the 16 lanes of a group, lane i gives the
+// address of entries 4 (i & 3) .. + 3 of row i >> 2 (of four rows) and gets
+// column i's four.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint2 lds_column4(const uint8_t* p) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+}
+
+// An operand's tile in LDS: T rows (of the product's output) by 64 entries of
+// the contraction, in one of two layouts, as it lies in memory:
+//   rows  [T][64]: 128 bytes a row, 16-byte chunk c of row r at c ^ (r & 7)
+//   columns  [64][T]: 2 T bytes an entry k of the contraction, its 32-byte unit u
+//            at u ^ f(k), f such that the 16 entries k that a wave reads of a
+//            unit at once (4 of each group of 8) lie in different banks
+// Copies go from memory to LDS directly, 1 KiB a wave instruction in lane order;
+// the permutation is in the lanes' source addresses.
+constexpr int HD_K = 64;
+template <bool COLUMNS, int T, int NW> struct Operand {
+  static constexpr int BYTES = T * HD_K * 2, PER = T / (8 * NW);   // copies of a wave
+  static constexpr int CH = T / 8, RPI = 512 / T;                  // (columns) chunks of a row, rows of a copy
+  const uint8_t* src[PER];
+  int last;   // (rows) the first entry of the contraction that the lane's chunk reads, in its step; (columns) its row
+  int64_t step;
+
+  // f(k) of a lane that reads entries 8 lg + 4 j + (lr >> 2); k & 3 and (k >> 3) & 3 stand for these bits.
+  static __device__ __forceinline__ int perm(int k) {
+    return T == 256 ? (k & 3) | (k >> 3 & 3) << 2 : T == 128 ? (k & 3) | (k >> 3 & 1) << 2 : (k >> 1 & 1) | (k >> 3 & 1) << 1;
+  }
+  // From row r0 of n (clamped: what lies past the end is computed and not
+  // kept; columns are read eight at a time), entry c0 of the contraction.
+  __device__ __forceinline__ void begin(const uint8_t* base, int64_t ld, int r0, int n, int c0, int wave) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int at = wave * PER + i;
+      if (!COLUMNS) {
+        const int r = at * 8 + (lane >> 3), c = (lane & 7) ^ (lane >> 3);
+        src[i] = base + ((int64_t)min(r0 + r, n - 1) * ld + c0 + 8 * c) * 2;
+        last = 8 * c;
+      } else {
+        const int k = at * RPI + lane / CH, c = (lane % CH) ^ (perm(k) << 1);
+        src[i] = base + ((int64_t)(c0 + k) * ld + min(r0 + 8 * c, ((n + 7) & ~7) - 8)) * 2;
+        last = lane / CH;
+      }
+    }
+    step = COLUMNS ? HD_K * ld * 2 : HD_K * 2;
+  }
+  // The next step's copies; `left` entries of the contraction are left.
+  __device__ __forceinline__ void copy(uint8_t* tile, int left, int wave) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint8_t* p = src[i];
+      if (left < HD_K && last + (COLUMNS ? (wave * PER + i) * RPI : 0) >= left) p = (const uint8_t*)head_zeros;
+      __builtin_amdgcn_global_load_lds((const void*)p, (__attribute__((address_space(3))) void*)(tile + (wave * PER + i) * 1024), 16, 0, 0);
+      src[i] += step;
+    }
+  }
+  // The matrix operand of rows r0 .. r0 + 15, entries 32 h .. + 31.
+  static __device__ __forceinline__ bf16x8 read(const uint8_t* tile, int r0, int h) {
+    const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+    if (!COLUMNS) {
+      const int r = r0 + lr;
+      return __builtin_bit_cast(bf16x8, lds_ld16(tile + r * 128 + (((4 * h + lg) ^ (r & 7)) << 4)));
+    }
+    const int k = 32 * h + 8 * lg + (lr >> 2);
+    const uint8_t* p = tile + k * (2 * T) + (((r0 >> 4) ^ perm(8 * lg + (lr >> 2))) << 5) + ((lr & 3) << 3);
+    const uint2 a = lds_column4(p), b = lds_column4(p + 4 * 2 * T);
+    return __builtin_bit_cast(bf16x8, make_uint4(a.x, a.y, b.x, b.y));
+  }
+};
+
+template <int N> __device__ __forceinline__ void copies_barrier() {   // this wave's copies but the last N, and its LDS reads; then all
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// The parts of an fp32 number: three bf16 numbers that sum to it, cut off
+// rather than rounded, so that the first does not overflow.
+__device__ __forceinline__ void split3(float x, uint16_t (&q)[3]) {
+  const uint32_t u = __float_as_uint(x);
+  const bool finite = (u & 0x7F800000u) != 0x7F800000u;
+  const float r1 = x - __uint_as_float(u & 0xFFFF0000u);
+  const uint32_t u1 = __float_as_uint(r1);
+  const float r2 = r1 - __uint_as_float(u1 & 0xFFFF0000u);
+  q[0] = (uint16_t)((finite || !(u & 0x7FFFFFu) ? u : u | 0x400000u) >> 16);
+  q[1] = finite ? (uint16_t)(u1 >> 16) : 0;
+  q[2] = finite ? (uint16_t)(__float_as_uint(r2) >> 16) : 0;
+}
+
+// Which parts of the operands a pass over the contraction multiplies: all of
+// the products down to 2^-16 of the largest, the smallest first.
+__device__ __forceinline__ int pass_a(int passes, int p) { return passes == 1 ? 0 : (0x201100 >> (20 - 4 * p)) & 15; }
+__device__ __forceinline__ int pass_b(int passes, int p) { return passes == 1 ? 0 : (0x021010 >> (20 - 4 * p)) & 15; }
+
+// out[j][i] = sum_c A[i][c] B[j][c], TI x TJ of them a block, WI x WJ waves.  Lane
+// (lr, lg) of a wave holds, of each of its 16 x 16 tiles, i = 4 lg + 0..3 of j =
+// lr.  A ring of S steps of the contraction in LDS: one is multiplied while the
+// next ones are on their way; one barrier a step.
+template <bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
+__global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
+  constexpr int NW = WI * WJ, NI = TI / WI / 16, NJ = TJ / WJ / 16;
+  typedef Operand<CA, TI, NW> OA;
+  typedef Operand<CB, TJ, NW> OB;
+  constexpr int PER = OA::PER + OB::PER, STAGE = OA::BYTES + OB::BYTES;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave % WI, wj = wave / WI;
+  // blocks b, b + 8, .. run on one XCD, which takes every eighth tile of i with
+  // all tiles of j, so that A's tile stays in its L2
+  const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
+  const int it = local / a.j_tiles * 8 + xcd, jt = local % a.j_tiles;
+  if (it >= a.i_tiles) return;
+  const int i0 = it * TI, j0 = jt * TJ;
+  const int c_begin = blockIdx.y * a.chunk, c_end = min(c_begin + a.chunk, a.C);
+
+  f32x4 acc[NI][NJ];
+#pragma unroll
+  for (int x = 0; x < NI; ++x)
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const int steps = (c_end - c_begin + HD_K - 1) / HD_K, total = steps * a.passes;
+  OA oa;
+  OB ob;
+  int copied = 0, pass = 0, in_pass = 0;
+  auto copy = [&]() {   // one step's copies
+    if (in_pass == 0) {
+      oa.begin(a.A + pass_a(a.passes, pass) * a.plane_a, a.lda, i0, a.n_i, c_begin, wave);
+      ob.begin(a.B + pass_b(a.passes, pass) * a.plane_b, a.ldb, j0, a.n_j, c_begin, wave);
+    }
+    uint8_t* tile = smem + (copied % S) * STAGE;
+    const int left = c_end - c_begin - in_pass * HD_K;
+    oa.copy(tile, left, wave);
+    ob.copy(tile + OA::BYTES, left, wave);
+    ++copied;
+    if (++in_pass == steps) {
+      in_pass = 0;
+      ++pass;
+    }
+  };
+  for (int i = 0; i < S - 1 && i < total; ++i) copy();
+  for (int s = 0; s < total; ++s) {
+    if (copied - s == S - 1) copies_barrier<(S - 2) * PER>();
+    else copies_barrier<0>();
+    if (copied < total) copy();
+    const uint8_t* ta = smem + (s % S) * STAGE;
+    const uint8_t* tb = ta + OA::BYTES;
+#pragma unroll
+    for (int h = 0; h < HD_K / 32; ++h) {
+      bf16x8 fa[NI], fb[NJ];
+#pragma unroll
+      for (int x = 0; x < NI; ++x) fa[x] = OA::read(ta, (wi * NI + x) * 16, h);
+#pragma unroll
+      for (int y = 0; y < NJ; ++y) fb[y] = OB::read(tb, (wj * NJ + y) * 16, h);
+#pragma unroll
+      for (int x = 0; x < NI; ++x)
+#pragma unroll
+        for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[x], fb[y], acc[x][y], 0, 0, 0);
+    }
+  }
+
+  if (EPI == HEAD_SUMS) {
+    // of each row the maximum and the sum of exponentials of the tile's entries
+    float2* red = (float2*)smem;   // [TJ][WI]
+    copies_barrier<0>();
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) {
+      const int jl = (wj * NJ + y) * 16 + lr, j = j0 + jl;
+      const int t = j < a.n_j ? a.targets[j] - a.v0 : -1;
+      float m = -INFINITY;
+      bool nan = false;
+#pragma unroll
+      for (int x = 0; x < NI; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = i0 + (wi * NI + x) * 16 + 4 * lg + e;
+          if (i >= a.n_i) acc[x][y][e] = -INFINITY;
+          const float z = acc[x][y][e];
+          nan |= !(z == z);
+          m = fmaxf(m, z);
+          if (i == t && t < a.n_i) a.target_z[j] = z;
+        }
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      float sum = 0.f;
+      const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int x = 0; x < NI; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += __expf(acc[x][y][e] - base);
+      if (nan) sum = __builtin_nanf("");
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (lg == 0) red[jl * WI + wi] = make_float2(m, sum);
+    }
+    __syncthreads();
+    for (int jl = threadIdx.x; jl < TJ; jl += NW * 64) {
+      if (j0 + jl >= a.n_j) break;
+      float m = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < WI; ++w) m = fmaxf(m, red[jl * WI + w].x);
+      const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int w = 0; w < WI; ++w) sum += red[jl * WI + w].y * __expf(red[jl * WI + w].x - base);
+      a.sums[(int64_t)(j0 + jl) * a.ld_sums + a.tile0 + it] = make_float2(m, sum);
+    }
+  } else if (EPI == HEAD_DZ) {
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) {
+      const int j = j0 + (wj * NJ + y) * 16 + lr;
+      if (j >= a.n_j) continue;
+      const int t = a.targets[j];
+      const float g = a.weights ? a.weights[j] : 1.f, lse = a.lse[j];
+      const bool out = t < 0 || t >= a.V || g == 0.f;
+#pragma unroll
+      for (int x = 0; x < NI; ++x) {
+        const int i = i0 + (wi * NI + x) * 16 + 4 * lg;
+        if (i >= a.ldz) continue;
+        float d[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float q = acc[x][y][e] - lse;
+          d[e] = a.planes == 1 ? __expf(q) : expf(q);
+          if (i + e + a.v0 == t) d[e] = expm1f(q);   // (p - 1 keeps its bits where p is near 1)
+          d[e] = out || i + e >= a.n_i ? 0.f : d[e] * g;
+        }
+        uint8_t* to = a.dz + ((int64_t)j * a.ldz + i) * 2;
+        if (a.planes == 1) {
+          *(uint2*)to = make_uint2(f32_to_bf16x2(d[0], d[1]), f32_to_bf16x2(d[2], d[3]));
+        } else {
+          uint16_t q[4][3];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) split3(d[e], q[e]);
+#pragma unroll
+          for (int p = 0; p < 3; ++p)
+            *(uint2*)(to + p * a.plane_dz) = make_uint2(q[0][p] | (uint32_t)q[1][p] << 16, q[2][p] | (uint32_t)q[3][p] << 16);
+        }
+      }
+    }
+  } else {
+    // sums of a part of the contraction (HEAD_PART, added to what is there in
+    // later pieces), or the result
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) {
+      const int j = j0 + (wj * NJ + y) * 16 + lr;
+      if (j >= a.n_j) continue;
+#pragma unroll
+      for (int x = 0; x < NI; ++x) {
+        const int i = i0 + (wi * NI + x) * 16 + 4 * lg;
+        if (i >= a.n_i) continue;
+        float4 v = make_float4(acc[x][y][0], acc[x][y][1], acc[x][y][2], acc[x][y][3]);
+        if (EPI == HEAD_PART) {
+          float4* at = (float4*)(a.part + ((int64_t)blockIdx.y * a.n_j + j) * a.n_i + i);
+          if (a.add) {
+            const float4 o = *at;
+            v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+          }
+          *at = v;
+        } else if (a.planes == 1) {
+          *(uint2*)((uint8_t*)a.out + ((int64_t)j * a.ldo + i) * 2) = make_uint2(f32_to_bf16x2(v.x, v.y), f32_to_bf16x2(v.z, v.w));
+        } else {
+          *(float4*)((uint8_t*)a.out + ((int64_t)j * a.ldo + i) * 4) = v;
+        }
+      }
+    }
+  }
+}
+
+// ---- rows before and after ----------------------------------------------------------
+
+// Rows of a matrix as the products read them: bf16 numbers, or the three parts
+// of fp32 ones.  Rows that are left out become zeros: what they hold (a padded
+// place may hold anything) must not reach dW as 0 x NaN.
+template <int DT>
+__global__ __launch_bounds__(256) void k_head_copy(HeadCopyArgs a) {
+  const int64_t per = a.K / 8, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= a.n * per) return;
+  const int r = (int)(at / per), k = (int)(at % per) * 8;
+  bool out = false;
+  if (a.targets) {
+    const int t = a.targets[r];
+    out = t < 0 || t >= a.V || (a.weights && a.weights[r] == 0.f);
+  }
+  const uint8_t* p = (const uint8_t*)a.src + (r * a.ld + k) * Elem<DT>::ES_;
+  uint8_t* to = a.dst + ((int64_t)r * a.K + k) * 2;
+  if (DT == 1) {
+    *(uint4*)to = out ? make_uint4(0, 0, 0, 0) : ld16(p);
+    return;
+  }
+  uint16_t q[8][3];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) split3(out ? 0.f : ((const float*)p)[e], q[e]);
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+    *(uint4*)(to + i * a.plane) = make_uint4(q[0][i] | (uint32_t)q[1][i] << 16, q[2][i] | (uint32_t)q[3][i] << 16,
+                                             q[4][i] | (uint32_t)q[5][i] << 16, q[6][i] | (uint32_t)q[7][i] << 16);
+}
+
+// A wave joins a row's tiles.
+__global__ __launch_bounds__(256) void k_head_join(HeadJoinArgs a) {
+  const int lane = threadIdx.x & 63, j = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (j >= a.n) return;
+  const float2* p = a.sums + (int64_t)j * a.tiles;
+  float m = -INFINITY;
+  for (int i = lane; i < a.tiles; i += 64) m = fmaxf(m, p[i].x);
+  m = wave_max(m);
+  const float base = m == -INFINITY ? 0.f : m;
+  float s = 0.f;
+  for (int i = lane; i < a.tiles; i += 64) s += p[i].y * __expf(p[i].x - base);
+  s = wave_sum(s);
+  if (lane) return;
+  const double lse = m == -INFINITY ? (double)__builtin_nanf("") : (double)m + log((double)s);
+  const int t = a.targets[j];
+  const bool in = t >= 0 && t < a.V;
+  if (a.loss) a.loss[j] = in ? (float)(lse - (double)a.target_z[j]) : 0.f;
+  a.lse[j] = (float)lse;
+}
+
+// The parts of dh, summed in order and rounded.
+template <int DT>
+__global__ __launch_bounds__(256) void k_head_out(HeadOutArgs a) {
+  const int64_t per = a.K / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= a.n * per) return;
+  const int64_t r = at / per;
+  const int k = (int)(at % per) * 4;
+  float4 v = *(const float4*)(a.part + r * a.K + k);
+  for (int s = 1; s < a.split; ++s) {
+    const float4 o = *(const float4*)(a.part + ((int64_t)s * a.n + r) * a.K + k);
+    v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
+  }
+  store4<DT>((uint8_t*)a.out + r * a.ldo * Elem<DT>::ES_, k, v);
+}
+
+// ---- launchers ----------------------------------------------------------------------
+
+template <bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
+static hipError_t launch(HeadArgs a, int split, hipStream_t s) {
+  const void* f = (const void*)k_head<CA, CB, TI, TJ, WI, WJ, S, EPI>;
+  constexpr int lds = S * (TI + TJ) * HD_K * 2;
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  a.i_tiles = (a.n_i + TI - 1) / TI;
+  a.j_tiles = (a.n_j + TJ - 1) / TJ;
+  const dim3 grid((unsigned)((int64_t)(a.i_tiles + 7) / 8 * 8 * a.j_tiles), split);
+  void* args[] = {(void*)&a};
+  return hipLaunchKernel(f, grid, dim3(WI * WJ * 64), args, lds, s);
+}
+template <bool CA, bool CB, int EPI>
+static hipError_t launch_tile(const HeadArgs& a, int split, int tile, hipStream_t s) {
+  if (tile == 64) return launch<CA, CB, 256, 64, 8, 1, 3, EPI>(a, split, s);
+  if (tile == 128) return launch<CA, CB, 256, 128, 4, 2, 3, EPI>(a, split, s);
+  return launch<CA, CB, 256, 256, 2, 4, 2, EPI>(a, split, s);
+}
+hipError_t launch_head(int epi, const HeadArgs& a, int split, int tile, hipStream_t s) {
+  if (epi == HEAD_SUMS) return launch_tile<false, false, HEAD_SUMS>(a, split, tile, s);
+  if (epi == HEAD_DZ) return launch_tile<false, false, HEAD_DZ>(a, split, tile, s);
+  if (epi == HEAD_PART) return launch_tile<true, false, HEAD_PART>(a, split, tile, s);
+  return launch<true, true, 256, 256, 2, 4, 2, HEAD_OUT>(a, split, s);
+}
+
+hipError_t launch_head_copy(int dtype, const HeadCopyArgs& a, hipStream_t s) {
+  const unsigned blocks = (unsigned)((a.n * (a.K / 8) + 255) / 256);
+  if (dtype) k_head_copy<1><<<blocks, 256, 0, s>>>(a);
+  else k_head_copy<0><<<blocks, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_head_join(const HeadJoinArgs& a, hipStream_t s) {
+  k_head_join<<<(a.n + 3) / 4, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_head_out(int dtype, const HeadOutArgs& a, hipStream_t s) {
+  const unsigned blocks = (unsigned)((a.n * (a.K / 4) + 255) / 256);
+  if (dtype) k_head_out<1><<<blocks, 256, 0, s>>>(a);
+  else k_head_out<0><<<blocks, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace lede

@@ -1,8 +1,12 @@
-// Entry points of the products of a batch's rows with 4-bit weights.  No call
-// allocates, synchronises or keeps anything between calls.
+// Entry points of the products of a batch's rows with 4-bit weights, and of the
+// vocabulary head's loss with its gradient.  No call allocates, synchronises
+// or keeps anything between calls.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "../../include/lede.h"
+#include "loss.h"
 #include "products.h"
 
 using namespace lede;
@@ -25,9 +29,188 @@ int check_quant(int32_t N, int32_t K, int32_t group) {
   return LEDE_OK;
 }
 
+// ---- the vocabulary head's loss ----
+
+constexpr int32_t MOST_ROWS = 1 << 18, MOST_VOCAB = 1 << 20, MOST_WIDTH = 1 << 15;
+int check_head(int32_t dtype, int32_t M, int32_t V, int32_t K) {
+  if (!dtype_ok(dtype) || M < 0 || V < 1 || K < 1) return LEDE_E_ARG;
+  return K % 8 || M > MOST_ROWS || V > MOST_VOCAB || K > MOST_WIDTH ? LEDE_E_UNSUPPORTED : LEDE_OK;
+}
+// Rows that the kernels read or write in 16-byte pieces.
+bool rows_ok(const void* p, int64_t ld, int64_t width, int32_t dt) {
+  return p && aligned(p, 16) && ld >= width && ld * es_of(dt) % 16 == 0;
+}
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Rows of a tile of the products whose second operand is rows of `hidden`.
+int row_tile(int32_t M) { return M <= 64 ? 64 : M <= 128 ? 128 : 256; }
+
+// Entries of the vocabulary at a time: what is kept of a piece, `row_bytes` for
+// each of its entries, takes at most PIECE_BYTES (or is one tile wide).
+constexpr int64_t PIECE_BYTES = 128 << 20;
+int piece_size(int32_t V, int64_t row_bytes) {
+  const int64_t most = std::max<int64_t>(HEAD_TILE, PIECE_BYTES / std::max<int64_t>(row_bytes, 1) / HEAD_TILE * HEAD_TILE);
+  const int64_t n = (V + most - 1) / most, each = (V + n - 1) / n;
+  return (int)((each + HEAD_TILE - 1) / HEAD_TILE * HEAD_TILE);
+}
+
+// Bytes of the workspaces' parts, in their order.
+struct LossPlan {
+  int planes, tiles, piece;
+  int64_t plane_h, plane_w;
+  size_t sums, target, h, w, total;
+  LossPlan(int32_t dtype, int32_t M, int32_t V, int32_t K) {
+    planes = dtype == LEDE_DTYPE_F32 ? 3 : 1;
+    tiles = (V + HEAD_TILE - 1) / HEAD_TILE;
+    piece = planes == 1 ? V : piece_size(V, (int64_t)K * 6);
+    plane_h = (int64_t)M * K * 2;
+    plane_w = (int64_t)std::min(piece, V) * K * 2;
+    sums = up256((size_t)M * tiles * 8);
+    target = up256((size_t)M * 4);
+    h = planes == 1 ? 0 : up256(3 * plane_h);
+    w = planes == 1 ? 0 : up256(3 * plane_w);
+    total = sums + target + h + w;
+  }
+};
+struct GradPlan {
+  int planes, piece, ldz, tile, split, chunk;
+  int64_t plane_h, plane_w, plane_dz;
+  size_t h, w, dz, part, total;
+  GradPlan(int32_t dtype, int32_t M, int32_t V, int32_t K) {
+    planes = dtype == LEDE_DTYPE_F32 ? 3 : 1;
+    piece = piece_size(V, planes == 1 ? (int64_t)M * 2 : 6 * (int64_t)std::max(M, K));
+    ldz = (std::min(piece, V) + 7) & ~7;
+    tile = row_tile(M);
+    // dh has few tiles: its contraction over the vocabulary is split so that
+    // about a block is there for each CU
+    const int64_t blocks = (int64_t)((K + HEAD_TILE - 1) / HEAD_TILE) * std::max(1, (M + tile - 1) / tile);
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(256 / blocks, ldz / 256));
+    chunk = (int)((ldz + want - 1) / want + 63) & ~63;
+    split = (ldz + chunk - 1) / chunk;
+    plane_h = (int64_t)M * K * 2;
+    plane_w = (int64_t)std::min(piece, V) * K * 2;
+    plane_dz = (int64_t)M * ldz * 2;
+    h = up256(planes * plane_h);
+    w = planes == 1 ? 0 : up256(3 * plane_w);
+    dz = up256(planes * plane_dz);
+    part = up256((size_t)split * M * K * 4);
+    total = h + w + dz + part;
+  }
+};
+
 }  // namespace
 
 extern "C" {
+
+size_t lede_op_head_loss_bytes(int32_t dtype, int32_t M, int32_t V, int32_t K) {
+  return check_head(dtype, M, V, K) ? 0 : LossPlan(dtype, M, V, K).total;
+}
+size_t lede_op_head_loss_grad_bytes(int32_t dtype, int32_t M, int32_t V, int32_t K) {
+  return check_head(dtype, M, V, K) ? 0 : GradPlan(dtype, M, V, K).total;
+}
+
+int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M, const void* head, int64_t ldw, int32_t V,
+                      int32_t K, const int32_t* targets, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                      void* stream) {
+  if (int rc = check_head(dtype, M, V, K)) return rc;
+  if (M == 0) return LEDE_OK;
+  if (!targets || !lse || !rows_ok(hidden, ldh, K, dtype) || !rows_ok(head, ldw, K, dtype)) return LEDE_E_ARG;
+  const LossPlan p(dtype, M, V, K);
+  if (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total) return LEDE_E_ARG;
+  hipStream_t s = S_(stream);
+  uint8_t* ws = (uint8_t*)workspace;
+  HeadArgs a{};
+  a.sums = (float2*)ws; a.ld_sums = p.tiles;
+  a.target_z = (float*)(ws + p.sums);
+  uint8_t *wh = ws + p.sums + p.target, *ww = wh + p.h;
+  a.planes = p.planes; a.passes = p.planes == 1 ? 1 : 6;
+  a.n_j = M; a.C = a.chunk = K;
+  a.targets = targets; a.V = V;
+  if (p.planes == 1) {
+    a.A = (const uint8_t*)head; a.lda = ldw; a.B = (const uint8_t*)hidden; a.ldb = ldh; a.n_i = V;
+    if (hipError_t e = launch_head(HEAD_SUMS, a, 1, row_tile(M), s)) return done(e);
+  } else {
+    HeadCopyArgs c{};
+    c.src = hidden; c.ld = ldh; c.n = M; c.K = K; c.dst = wh; c.plane = p.plane_h;
+    if (hipError_t e = launch_head_copy(dtype, c, s)) return done(e);
+    a.A = ww; a.lda = K; a.plane_a = p.plane_w; a.B = wh; a.ldb = K; a.plane_b = p.plane_h;
+    for (int v0 = 0; v0 < V; v0 += p.piece) {
+      a.v0 = v0; a.n_i = std::min(p.piece, V - v0); a.tile0 = v0 / HEAD_TILE;
+      c.src = (const float*)head + v0 * ldw; c.ld = ldw; c.n = a.n_i; c.dst = ww; c.plane = p.plane_w;
+      if (hipError_t e = launch_head_copy(dtype, c, s)) return done(e);
+      if (hipError_t e = launch_head(HEAD_SUMS, a, 1, row_tile(M), s)) return done(e);
+    }
+  }
+  HeadJoinArgs j{};
+  j.sums = a.sums; j.target_z = a.target_z; j.n = M; j.tiles = p.tiles; j.V = V; j.targets = targets; j.loss = loss; j.lse = lse;
+  return done(launch_head_join(j, s));
+}
+
+int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32_t M, const void* head, int64_t ldw, int32_t V,
+                           int32_t K, const int32_t* targets, const float* lse, const float* weights, void* d_hidden, int64_t ld_dh,
+                           void* d_head, int64_t ld_dw, void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = check_head(dtype, M, V, K)) return rc;
+  if (!d_head && (!d_hidden || M == 0)) return LEDE_OK;
+  if (d_head && !rows_ok(d_head, ld_dw, K, dtype)) return LEDE_E_ARG;
+  if (M && (!targets || !lse || !rows_ok(hidden, ldh, K, dtype) || !rows_ok(head, ldw, K, dtype))) return LEDE_E_ARG;
+  if (M && d_hidden && !rows_ok(d_hidden, ld_dh, K, dtype)) return LEDE_E_ARG;
+  const GradPlan p(dtype, M, V, K);
+  if (p.total && (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total)) return LEDE_E_ARG;
+  hipStream_t s = S_(stream);
+  uint8_t *wh = (uint8_t*)workspace, *ww = wh + p.h, *wz = ww + p.w, *wp = wz + p.dz;
+  if (M) {
+    HeadCopyArgs c{};
+    c.src = hidden; c.ld = ldh; c.n = M; c.K = K; c.dst = wh; c.plane = p.plane_h;
+    c.targets = targets; c.weights = weights; c.V = V;
+    if (hipError_t e = launch_head_copy(dtype, c, s)) return done(e);
+  }
+  for (int v0 = 0; v0 < V; v0 += p.piece) {
+    const int n = std::min(p.piece, V - v0);
+    const uint8_t* w = (const uint8_t*)head + v0 * ldw * es_of(dtype);
+    int64_t lw = ldw;
+    if (M && p.planes == 3) {
+      HeadCopyArgs c{};
+      c.src = w; c.ld = ldw; c.n = n; c.K = K; c.dst = ww; c.plane = p.plane_w;
+      if (hipError_t e = launch_head_copy(dtype, c, s)) return done(e);
+      w = ww;
+      lw = K;
+    }
+    HeadArgs a{};
+    a.planes = p.planes; a.passes = p.planes == 1 ? 1 : 6;
+    a.V = V; a.v0 = v0;
+    if (M) {
+      HeadArgs z = a;
+      z.A = w; z.lda = lw; z.plane_a = p.plane_w; z.n_i = n;
+      z.B = wh; z.ldb = K; z.plane_b = p.plane_h; z.n_j = M;
+      z.C = z.chunk = K;
+      z.targets = targets; z.weights = weights; z.lse = lse;
+      z.dz = wz; z.plane_dz = p.plane_dz; z.ldz = p.ldz;
+      if (hipError_t e = launch_head(HEAD_DZ, z, 1, p.tile, s)) return done(e);
+    }
+    if (M && d_hidden) {
+      HeadArgs h = a;
+      h.A = w; h.lda = lw; h.plane_a = p.plane_w; h.n_i = K;
+      h.B = wz; h.ldb = p.ldz; h.plane_b = p.plane_dz; h.n_j = M;
+      h.C = n; h.chunk = p.chunk;
+      h.part = (float*)wp; h.add = v0 > 0;
+      if (hipError_t e = launch_head(HEAD_PART, h, p.split, p.tile, s)) return done(e);
+    }
+    if (d_head) {
+      HeadArgs d = a;
+      d.A = wh; d.lda = K; d.plane_a = p.plane_h; d.n_i = K;
+      d.B = wz; d.ldb = p.ldz; d.plane_b = p.plane_dz; d.n_j = n;
+      d.C = d.chunk = M;
+      d.out = (uint8_t*)d_head + v0 * ld_dw * es_of(dtype); d.ldo = ld_dw;
+      if (hipError_t e = launch_head(HEAD_OUT, d, 1, 256, s)) return done(e);
+    }
+  }
+  if (M && d_hidden) {
+    HeadOutArgs o{};
+    o.part = (const float*)wp; o.split = p.split; o.n = M; o.K = K; o.out = d_hidden; o.ldo = ld_dh;
+    return done(launch_head_out(dtype, o, s));
+  }
+  return LEDE_OK;
+}
 
 size_t lede_op_quant_bytes(int32_t N, int32_t K, int32_t group) { return check_quant(N, K, group) ? 0 : q_bytes(N, K, group); }
 

@@ -87,7 +87,8 @@ EXPORTED = ["lede_region_bytes", "lede_create", "lede_destroy", "lede_last_error
             "lede_op_cache_bytes", "lede_op_cache_plan", "lede_op_cache_append", "lede_op_cache_read",
             "lede_op_cache_attention_bytes", "lede_op_cache_attention", "lede_op_logprobs_bytes", "lede_op_logprobs",
             "lede_op_cache_fork", "lede_op_cache_own", "lede_op_cache_copy", "lede_op_cache_free", "lede_op_cache_compact",
-            "lede_op_quant_bytes", "lede_op_quantize", "lede_op_quant_pack", "lede_op_quant_linear"]
+            "lede_op_quant_bytes", "lede_op_quantize", "lede_op_quant_pack", "lede_op_quant_linear",
+            "lede_op_head_loss_bytes", "lede_op_head_loss", "lede_op_head_loss_grad_bytes", "lede_op_head_loss_grad"]
 MAX_IN_FLIGHT = 2
 SAMPLE_SLOTS = 16
 SAMPLE_STRIDE = 33
@@ -162,6 +163,10 @@ def load(path: str = LIB_PATH):
     i64, f32 = ctypes.c_int64, ctypes.c_float
     L.lede_op_cache_bytes.argtypes = [i32] * 3
     i64 = ctypes.c_int64
+    L.lede_op_head_loss_bytes.argtypes = L.lede_op_head_loss_grad_bytes.argtypes = [i32, i32, i32, i32]
+    L.lede_op_head_loss_bytes.restype = L.lede_op_head_loss_grad_bytes.restype = sz
+    L.lede_op_head_loss.argtypes = [i32, vp, i64, i32, vp, i64, i32, i32, vp, vp, vp, vp, sz, vp]
+    L.lede_op_head_loss_grad.argtypes = [i32, vp, i64, i32, vp, i64, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp, sz, vp]
     L.lede_op_quant_bytes.argtypes = [i32, i32, i32]
     L.lede_op_quant_bytes.restype = sz
     L.lede_op_quantize.argtypes = [i32, vp, i64, i32, i32, i32, vp, vp, vp]
@@ -968,6 +973,72 @@ def op_quant_linear(matrix: QuantMatrix, x, dtype=None, out=None):
     _call(dev, "op_quant_linear", load().lede_op_quant_linear, _dtype_code(torch, x.dtype), matrix.packed.data_ptr(), N, K, matrix.group,
           x.data_ptr(), ldx, M, _dtype_code(torch, out.dtype), out.data_ptr(), ldy)
     return out
+
+
+# ---- the vocabulary head's loss, without the logits -----------------------------------
+
+@dataclass
+class HeadLoss:
+    loss: object   # float32 [rows]; 0 where the target lies outside the vocabulary
+    lse: object    # float32 [rows]
+
+
+def _head_inputs(torch, hidden, head, targets, what: str):
+    dev = hidden.device
+    _need(hidden.dim() == 2 and head.dim() == 2 and hidden.shape[1] == head.shape[1] and head.device == dev and head.dtype == hidden.dtype
+          and _dense(dev, torch.int32, targets) and targets.numel() == hidden.shape[0], what)
+    return (_dtype_code(torch, hidden.dtype), hidden.shape[0], head.shape[0], hidden.shape[1], _matrix_stride(hidden, what),
+            _matrix_stride(head, what))
+
+
+def _head_supported(nbytes: int, M: int, V: int, K: int, what: str):
+    if nbytes == 0 and M > 0:
+        raise LedeError(LEDE_E_UNSUPPORTED, "%s: %d rows, %d x %d" % (what, M, V, K))
+
+
+def op_head_loss(hidden, head, targets, workspace=None) -> HeadLoss:
+    """-log softmax(hidden head^T)[target] of every row of hidden [M][K], and
+    its log of the sum, without the logits; head [V][K] of the same dtype
+    (float32 or bfloat16), targets int32 [M] (outside [0, V): the row is left
+    out).  Rows lie at multiples of 16 bytes; K is a multiple of 8."""
+    import torch
+    dev = hidden.device
+    code, M, V, K, ldh, ldw = _head_inputs(torch, hidden, head, targets, "op_head_loss")
+    L = load()
+    need = L.lede_op_head_loss_bytes(code, M, V, K)
+    _head_supported(need, M, V, K, "op_head_loss")
+    loss, lse = torch.empty(2, M, dtype=torch.float32, device=dev).unbind(0)
+    ws, ws_at, ws_bytes = _workspace(torch, need, workspace, dev, "op_head_loss: workspace")
+    _call(dev, "op_head_loss", L.lede_op_head_loss, code, hidden.data_ptr(), ldh, M, head.data_ptr(), ldw, V, K, targets.data_ptr(),
+          loss.data_ptr(), lse.data_ptr(), ws_at, ws_bytes)
+    return HeadLoss(loss, lse)
+
+
+def op_head_loss_grad(hidden, head, targets, lse, weights=None, want_hidden: bool = True, want_head: bool = True, out=None,
+                      workspace=None):
+    """(d_hidden, d_head): the gradient of sum(weights * loss) (float32 [M],
+    all 1 when not given) with the lse of op_head_loss; None for one that is
+    not wanted.  `out` gives the two tensors (or None in a place)."""
+    import torch
+    dev = hidden.device
+    code, M, V, K, ldh, ldw = _head_inputs(torch, hidden, head, targets, "op_head_loss_grad")
+    _need(_dense(dev, torch.float32, lse) and lse.numel() == M
+          and (weights is None or (_dense(dev, torch.float32, weights) and weights.numel() == M)), "op_head_loss_grad")
+    L = load()
+    need = L.lede_op_head_loss_grad_bytes(code, M, V, K)
+    _head_supported(need, M, V, K, "op_head_loss_grad")
+    if out is None:
+        out = (torch.empty(M, K, dtype=hidden.dtype, device=dev) if want_hidden else None,
+               torch.empty(V, K, dtype=hidden.dtype, device=dev) if want_head else None)
+    dh, dw = out
+    for t, n in ((dh, M), (dw, V)):
+        _need(t is None or (t.shape == (n, K) and t.dtype == hidden.dtype and t.device == dev), "op_head_loss_grad: out")
+    ws, ws_at, ws_bytes = _workspace(torch, need, workspace, dev, "op_head_loss_grad: workspace")
+    _call(dev, "op_head_loss_grad", L.lede_op_head_loss_grad, code, hidden.data_ptr(), ldh, M, head.data_ptr(), ldw, V, K,
+          targets.data_ptr(), lse.data_ptr(), None if weights is None else weights.data_ptr(),
+          None if dh is None else dh.data_ptr(), 0 if dh is None else _matrix_stride(dh, "op_head_loss_grad: out"),
+          None if dw is None else dw.data_ptr(), 0 if dw is None else _matrix_stride(dw, "op_head_loss_grad: out"), ws_at, ws_bytes)
+    return dh, dw
 
 
 def dqn_noise_count(hidden: int) -> int:
