@@ -248,7 +248,7 @@ int lede_op_quant_linear(int32_t dtype, const void* packed, int32_t N, int32_t K
   a.scales = (const uint16_t*)(a.codes + q_code_bytes(N, K));
   a.N = N; a.K = K; a.group = group; a.n_groups = q_groups(N); a.tiles = q_tiles(K);
   a.x = x; a.ldx = ldx; a.M = M;
-  a.vec = aligned(x, 16) && (M == 1 || ldx * es_of(dtype) % 16 == 0);
+  a.vec = K % 8 == 0 && aligned(x, 16) && (M == 1 || ldx * es_of(dtype) % 16 == 0);
   a.y_dtype = y_dtype; a.y = y; a.ldy = ldy;
   return done(launch_quant_linear(dtype, a, S_(stream)));
 }

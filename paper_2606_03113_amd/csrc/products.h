@@ -43,7 +43,7 @@ struct QuantLinearArgs {
   int N, K, group, n_groups, tiles;
   const void* x; int64_t ldx;
   int M;
-  bool vec;           // rows of x can be read in 16-byte pieces
+  bool vec;           // x can be read in pieces of eight columns, 16-byte aligned
   int y_dtype;
   void* y; int64_t ldy;
 };

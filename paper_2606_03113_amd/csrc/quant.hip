@@ -111,15 +111,20 @@ template <int I> __device__ __forceinline__ bf16x8 codes8(uint4 w) {
   return bf16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
 }
 
+__device__ uint4 q_zeros[2];   // what is read in place of columns past the last
+
 // Eight elements of a row of x as they came, and as matrix operands: one, or
 // (fp32) three that sum to them exactly, cut off rather than rounded so that
 // the first cannot overflow.  What is not finite is in the first part alone.
 template <int DT> struct X8 {
   uint4 u[DT ? 1 : 2];
-  __device__ __forceinline__ void load(const uint8_t* row, int k, int K, bool vec) {
-    if (vec && k + 8 <= K) {
-      u[0] = ld16(row + (int64_t)k * Elem<DT>::ES_);
-      if (DT == 0) u[DT ? 0 : 1] = ld16(row + (int64_t)k * Elem<DT>::ES_ + 16);
+  __device__ __forceinline__ void zero() { u[0] = u[DT ? 0 : 1] = make_uint4(0, 0, 0, 0); }
+  // VEC: rows in 16-byte pieces, K a multiple of 8
+  template <bool VEC> __device__ __forceinline__ void load(const uint8_t* row, int k, int K) {
+    if (VEC) {
+      const uint8_t* p = k < K ? row + (int64_t)k * Elem<DT>::ES_ : (const uint8_t*)q_zeros;
+      u[0] = ld16(p);
+      if (DT == 0) u[DT ? 0 : 1] = ld16(p + 16);
       return;
     }
     uint32_t e[8];
@@ -163,82 +168,324 @@ template <int DT> struct X8 {
 
 __device__ __forceinline__ f32x4 mfma_bf16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// Few rows: a block has 16 rows of W and 16 of x; its eight waves take the
-// tiles of K in turn, straight from memory into the operands' registers, D
-// tiles ahead, and meet in LDS once.  Lane l has x row l & 15 (rows past the
-// last: the last) and the results of W row l & 15 for x rows 4 (l >> 4) + i.
-// MR: how many of these i can be rows at all.
-constexpr int QL_WAVES = 8;
-template <int DT, int GROUP, int MR, int D>
-__global__ __launch_bounds__(QL_WAVES * 64) void k_quant_thin(QuantLinearArgs a) {
-  constexpr int PER = QT_K / GROUP, PARTS = X8<DT>::PARTS;
-  typedef typename std::conditional<PER == 4, uint2, typename std::conditional<PER == 2, uint32_t, uint16_t>::type>::type Scales;
-  __shared__ float part[QL_WAVES][MR][64];
-  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int g = blockIdx.x, m0 = blockIdx.y * 16, T = a.tiles;
-  const uint8_t* wp = a.codes + (int64_t)g * T * 1024 + lane * 16;
-  const Scales* sp = (const Scales*)a.scales + (int64_t)g * T * 16 + lr;
-  const uint8_t* xr = (const uint8_t*)a.x + min(m0 + lr, a.M - 1) * a.ldx * Elem<DT>::ES_;
-  uint4 w[D];
-  Scales sc[D];
-  X8<DT> x[D][4];
-  auto load = [&](int u, int t) {   // (a step past the end reads the last tile again)
-    t = min(t, T - 1);
-    w[u] = ld16_stream(wp + (int64_t)t * 1024);
-    sc[u] = sp[t * 16];
+// What a tile of W takes besides its codes: the scales of a lane's row.
+template <int GROUP> struct Scales {
+  static constexpr int PER = QT_K / GROUP;
+  typedef typename std::conditional<PER == 4, uint2, typename std::conditional<PER == 2, uint32_t, uint16_t>::type>::type T;
+  static __device__ __forceinline__ float get(const T& s, int p) { return __uint_as_float((uint32_t)((const uint16_t*)&s)[p] << 16); }
+};
+
+// acc[n][mt] += the products of TN tiles of 16 rows of W (codes w, scales s) with
+// 16 MT rows of x, whose operands x(j, mt, part) gives for columns 32 j .. + 31.
+// Results of lane l: W row l & 15, x rows 4 (l >> 4) + i, of which MR can be rows
+// at all.  The next group's operands are read, and its products started,
+// before a group is scaled.
+template <int GROUP, int TN, int MT, int MR, int PARTS, class X>
+__device__ __forceinline__ void tile_products(const uint4 (&w)[TN], const typename Scales<GROUP>::T (&s)[TN], f32x4 (&acc)[TN][MT], X x) {
+  constexpr int PER = Scales<GROUP>::PER, J = 4 / PER, UNITS = PER * TN;
+  f32x4 c[2][MT];
+  bf16x8 xf[2][J][MT][PARTS];
+  auto read = [&](int p) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[u][j].load(xr, t * QT_K + 32 * j + 8 * lg, a.K, a.vec);
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) xf[p & 1][j][m][q] = x(p * J + j, m, q);
   };
-  f32x4 acc{0.f, 0.f, 0.f, 0.f};
-  auto step = [&](int u) {
-    f32x4 c[PER];
+  auto scale = [&](int u) {
+    const int p = u / TN, n = u % TN;
+    const float f = Scales<GROUP>::get(s[n], p);
 #pragma unroll
-    for (int p = 0; p < PER; ++p) c[p] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bf16x8 b = j == 0 ? codes8<0>(w[u]) : j == 1 ? codes8<1>(w[u]) : j == 2 ? codes8<2>(w[u]) : codes8<3>(w[u]);
-      bf16x8 p[PARTS];
-      x[u][j].parts(p);
-#pragma unroll
-      for (int q = PARTS - 1; q >= 0; --q) c[j * PER / 4] = mfma_bf16(p[q], b, c[j * PER / 4]);   // (the smallest part first)
-    }
-#pragma unroll
-    for (int p = 0; p < PER; ++p) {
-      const uint32_t word = ((const uint16_t*)&sc[u])[p];
-      const float s = __uint_as_float(word << 16);
-#pragma unroll
-      for (int i = 0; i < MR; ++i) acc[i] = fmaf(s, c[p][i], acc[i]);
-    }
+      for (int i = 0; i < MR; ++i) acc[n][m][i] = fmaf(f, c[u & 1][m][i], acc[n][m][i]);
   };
+  read(0);
 #pragma unroll
-  for (int u = 0; u < D; ++u) load(u, wave + QL_WAVES * u);
-  for (int t = wave; t < T; t += QL_WAVES * D) {
+  for (int u = 0; u < UNITS; ++u) {
+    const int p = u / TN, n = u % TN;
+    if (n == 0 && p + 1 < PER) read(p + 1);
 #pragma unroll
-    for (int u = 0; u < D; ++u) {
-      if (t + QL_WAVES * u < T) step(u);
-      if (t + QL_WAVES * (u + D) < T) load(u, t + QL_WAVES * (u + D));
+    for (int m = 0; m < MT; ++m) c[u & 1][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int jj = p * J + j;
+      const bf16x8 b = jj == 0 ? codes8<0>(w[n]) : jj == 1 ? codes8<1>(w[n]) : jj == 2 ? codes8<2>(w[n]) : codes8<3>(w[n]);
+#pragma unroll
+      for (int q = PARTS - 1; q >= 0; --q)   // (the smallest part first)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) c[u & 1][m] = mfma_bf16(xf[p & 1][j][m][q], b, c[u & 1][m]);
     }
+    if (u) scale(u - 1);
   }
-#pragma unroll
-  for (int i = 0; i < MR; ++i) part[wave][i][lane] = acc[i];
-  __syncthreads();
-  // thread (i, lane) sums one result
-  const int i = threadIdx.x >> 6, m = m0 + 4 * lg + i, n = g * 16 + lr;
-  if (i >= MR || m >= a.M || n >= a.N) return;
-  float v = 0.f;
-#pragma unroll
-  for (int q = 0; q < QL_WAVES; ++q) v += part[q][i][lane];
+  scale(UNITS - 1);
+}
+
+__device__ __forceinline__ void store_y(const QuantLinearArgs& a, int m, int n, float v) {
+  if (m >= a.M || n >= a.N) return;
   v *= Q_UP;
   if (a.y_dtype) Elem<1>::store(a.y, m * a.ldy + n, v);
   else Elem<0>::store(a.y, m * a.ldy + n, v);
 }
 
+// Few rows, all of x in LDS: a block has 16 rows of W; its waves take the tiles
+// of K in turn, straight from memory into registers, D tiles ahead, and meet in
+// LDS once.  The first tiles are on their way while x is brought to LDS as
+// matrix operands ([part][row][column], rows 16 bytes apart besides).
+template <int DT, int GROUP, bool VEC, int MR, int D, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void k_quant_thin(QuantLinearArgs a) {
+  constexpr int PARTS = X8<DT>::PARTS;
+  typedef typename Scales<GROUP>::T S;
+  __shared__ float part[WAVES][MR][64];
+  extern __shared__ __align__(16) uint8_t xs[];
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = blockIdx.x, T = a.tiles;
+  const uint8_t* wp = a.codes + (int64_t)g * T * 1024 + lane * 16;
+  const S* sp = (const S*)a.scales + (int64_t)g * T * 16 + lr;
+  uint4 w[D][1];
+  S sc[D][1];
+  auto load = [&](int u, int t) {
+    w[u][0] = ld16_stream(wp + (int64_t)t * 1024);
+    sc[u][0] = sp[t * 16];
+  };
+#pragma unroll
+  for (int u = 0; u < D; ++u)
+    if (wave + WAVES * u < T) load(u, wave + WAVES * u);
+  const int pitch = T * QT_K * 2 + 16, plane = a.M * pitch, chunks = T * (QT_K / 8);
+  for (int i = threadIdx.x; i < a.M * chunks; i += WAVES * 64) {
+    const int m = i / chunks, k = (i - m * chunks) * 8;
+    X8<DT> x;
+    x.template load<VEC>((const uint8_t*)a.x + m * a.ldx * Elem<DT>::ES_, k, a.K);
+    bf16x8 p[PARTS];
+    x.parts(p);
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q) *(uint4*)(xs + q * plane + m * pitch + k * 2) = __builtin_bit_cast(uint4, p[q]);
+  }
+  __syncthreads();
+  const uint8_t* xl = xs + min(lr, a.M - 1) * pitch + lg * 16;   // (rows past the last: the last)
+  f32x4 acc[1][1] = {{f32x4{0.f, 0.f, 0.f, 0.f}}};
+  for (int t0 = wave; t0 < T; t0 += WAVES * D) {
+#pragma unroll
+    for (int u = 0; u < D; ++u) {
+      const int t = t0 + WAVES * u;
+      if (t < T) {
+        tile_products<GROUP, 1, 1, MR, PARTS>(w[u], sc[u], acc, [&](int j, int, int q) {
+          return __builtin_bit_cast(bf16x8, lds_ld16(xl + q * plane + (t * QT_K + 32 * j) * 2));
+        });
+        if (t + WAVES * D < T) load(u, t + WAVES * D);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MR; ++i) part[wave][i][lane] = acc[0][0][i];
+  __syncthreads();
+  const int i = threadIdx.x >> 6;   // thread (i, lane) sums one result
+  if (i >= MR) return;
+  float v = 0.f;
+#pragma unroll
+  for (int q = 0; q < WAVES; ++q) v += part[q][i][lane];
+  store_y(a, 4 * lg + i, g * 16 + lr, v);
+}
+
+// More rows: a block has 16 MT rows of x and WN x TN row groups of W.  WK tiles
+// of K are a step: waves take them and the row groups; x's part of a step is in
+// LDS for all waves, the next one's on its way in registers (where it becomes
+// matrix operands), W's tiles straight in registers D steps ahead.
+template <int DT, int GROUP, bool VEC, int MT, int TN, int WN, int WK, int D>
+__global__ __launch_bounds__(WN * WK * 64) void k_quant_wide(QuantLinearArgs a) {
+  constexpr int PARTS = X8<DT>::PARTS, THREADS = WN * WK * 64, ROWS = 16 * MT;
+  constexpr int CH = ROWS * WK * 16, PER = CH / THREADS;              // 8-column chunks of x a step, of a thread
+  constexpr int STAGE = PARTS * CH * 16;
+  static_assert(CH % THREADS == 0, "");
+  typedef typename Scales<GROUP>::T S;
+  extern __shared__ __align__(16) uint8_t smem[];   // [2][part][tile of K][row][16 chunks, permuted by the row]
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wn = wave % WN, wk = wave / WN, T = a.tiles;
+  const int g0 = (blockIdx.x * WN + wn) * TN, m0 = blockIdx.y * ROWS;
+  const uint8_t* wp[TN];
+  const S* sp[TN];
+#pragma unroll
+  for (int n = 0; n < TN; ++n) {
+    const int64_t g = min(g0 + n, a.n_groups - 1);
+    wp[n] = a.codes + g * T * 1024 + lane * 16;
+    sp[n] = (const S*)a.scales + g * T * 16 + lr;
+  }
+  uint4 w[D][TN];
+  S sc[D][TN];
+  auto load_w = [&](int u, int t) {
+    t = min(t, T - 1);
+#pragma unroll
+    for (int n = 0; n < TN; ++n) {
+      w[u][n] = ld16(wp[n] + (int64_t)t * 1024);
+      sc[u][n] = sp[n][t * 16];
+    }
+  };
+  X8<DT> x[D][PER];
+  const uint8_t* xp[PER];
+  int xk[PER];   // the column of a thread's chunk in a step
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int c = threadIdx.x + i * THREADS, row = c / (WK * 16);
+    xk[i] = c % (WK * 16) * 8;
+    xp[i] = (const uint8_t*)a.x + min(m0 + row, a.M - 1) * a.ldx * Elem<DT>::ES_;
+  }
+  auto load_x = [&](int u, int s) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) x[u][i].template load<VEC>(xp[i], s * WK * QT_K + xk[i], a.K);
+  };
+  auto store_x = [&](int u, int s) {
+    uint8_t* stage = smem + (s & 1) * STAGE;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int c = threadIdx.x + i * THREADS, row = c / (WK * 16), kc = c % (WK * 16);
+      bf16x8 p[PARTS];
+      x[u][i].parts(p);
+#pragma unroll
+      for (int q = 0; q < PARTS; ++q)
+        *(uint4*)(stage + (((q * WK + kc / 16) * ROWS + row) * 16 + ((kc ^ row) & 15)) * 16) = __builtin_bit_cast(uint4, p[q]);
+    }
+  };
+  f32x4 acc[TN][MT];
+#pragma unroll
+  for (int n = 0; n < TN; ++n)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int steps = (T + WK - 1) / WK;
+  // Loads return in order: those of x wait for W's that were asked for before
+  // them, so both are asked for equally far ahead; and no branch stands around
+  // them (past the end they read the last tile and zeros), or the wait at the
+  // place where its ways meet would be for all of them.
+#pragma unroll
+  for (int u = 0; u < D; ++u) {
+    load_x(u, u);
+    load_w(u, u * WK + wk);
+  }
+  for (int s0 = 0; s0 < steps; s0 += D) {
+#pragma unroll
+    for (int u = 0; u < D; ++u) {
+      const int s = s0 + u, t = s * WK + wk;
+      store_x(u, s);
+      load_x(u, s + D);
+      __syncthreads();
+      if (t < T) {
+        const uint8_t* xt = smem + (s & 1) * STAGE + wk * ROWS * 256;
+        tile_products<GROUP, TN, MT, 4, PARTS>(w[u], sc[u], acc, [&](int j, int m, int q) {
+          return __builtin_bit_cast(bf16x8, lds_ld16(xt + (q * WK * ROWS + 16 * m + lr) * 256 + (((4 * j + lg) ^ lr) << 4)));
+        });
+      }
+      load_w(u, t + D * WK);
+    }
+  }
+  if (WK == 1) {
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store_y(a, m0 + 16 * m + 4 * lg + i, (g0 + n) * 16 + lr, acc[n][m][i]);
+    return;
+  }
+  // the waves that share row groups meet: [wk][wn][n][m][lane]
+  __syncthreads();
+  float4* part = (float4*)smem;
+#pragma unroll
+  for (int n = 0; n < TN; ++n)
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+      part[(((wk * WN + wn) * TN + n) * MT + m) * 64 + lane] = make_float4(acc[n][m][0], acc[n][m][1], acc[n][m][2], acc[n][m][3]);
+  __syncthreads();
+  for (int o = wave; o < WN * TN * MT; o += WN * WK) {
+    float4 v = part[o * 64 + lane];
+#pragma unroll
+    for (int q = 1; q < WK; ++q) {
+      const float4 p = part[(q * WN * TN * MT + o) * 64 + lane];
+      v = make_float4(v.x + p.x, v.y + p.y, v.z + p.z, v.w + p.w);
+    }
+    const int m = m0 + 16 * (o % MT) + 4 * lg, n = (blockIdx.x * WN * TN + o / MT) * 16 + lr;
+    store_y(a, m, n, v.x);
+    store_y(a, m + 1, n, v.y);
+    store_y(a, m + 2, n, v.z);
+    store_y(a, m + 3, n, v.w);
+  }
+}
+
+constexpr size_t THIN_LDS = 64 * 1024;
+static size_t thin_lds(int dtype, const QuantLinearArgs& a) { return (size_t)(dtype ? 1 : 3) * a.M * (a.tiles * QT_K * 2 + 16); }
+
+template <int DT, int GROUP, bool VEC, int MR, int D, int WAVES>
+static hipError_t launch_thin(const QuantLinearArgs& a, hipStream_t s) {
+  const size_t lds = thin_lds(DT, a);
+  const void* f = (const void*)k_quant_thin<DT, GROUP, VEC, MR, D, WAVES>;
+  if (lds + WAVES * MR * 256 > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  void* args[] = {(void*)&a};
+  return hipLaunchKernel(f, dim3(a.n_groups), dim3(WAVES * 64), args, lds, s);
+}
+template <int DT, int GROUP, bool VEC, int MT, int TN, int WN, int WK, int D>
+static hipError_t launch_wide(const QuantLinearArgs& a, hipStream_t s) {
+  constexpr size_t stage = (size_t)X8<DT>::PARTS * 16 * MT * WK * 256, meet = WK == 1 ? 0 : (size_t)WK * WN * TN * MT * 1024;
+  constexpr size_t lds = 2 * stage > meet ? 2 * stage : meet;
+  static_assert(lds <= 160 * 1024, "");
+  const void* f = (const void*)k_quant_wide<DT, GROUP, VEC, MT, TN, WN, WK, D>;
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  void* args[] = {(void*)&a};
+  return hipLaunchKernel(f, dim3((a.n_groups + WN * TN - 1) / (WN * TN), (a.M + 16 * MT - 1) / (16 * MT)), dim3(WN * WK * 64), args, lds, s);
+}
+
+// Which kernel, by sizes alone (us; all matrices 4096 wide but where another K is
+// given, bf16 with groups of 64, fp32 likewise; weights from memory):
+//  - x in LDS (k_quant_thin) where its rows take at most 64 KiB; of large
+//    matrices for up to two rows (28672 outputs: 2 rows 14.1, 15.4 in
+//    k_quant_wide; 4 rows 16.9, 13.8), for fp32 always (2 rows 23, 32).
+//    16 waves share a K of few row groups (4096 outputs of 11008, one row: 6.7,
+//    8.4 with 8), 8 of many (28672: 12.2, 15.1 with 16);
+//  - k_quant_wide's blocks cover 32 or 64 rows of W by 16 of x, or 128 by 32 or
+//    64.  The smaller ones while they are about a block a CU, the larger ones
+//    read x and W less often:
+//      outputs x rows       32 x 16  64 x 16  128 x 32  128 x 64
+//      4096 x 16                6.3      7.3       12        20
+//      5120 x 16                7.4      8.2
+//      4096 x 64                9.3      7.3       13        20
+//      28672 x 16                22       17       20        27
+//      10000 x 40, K 5000        22       17       17        26
+//      16384 x 64                32       23       17        23
+//      22016 x 64                40       31       30        24
+//      28672 x 256              206      145      105        90
+//    fp32 (three parts of x, so less of it in LDS)  32 x 16  64 x 16  128 x 32
+//      4096 x 32                                        15       16        34
+//      4096 x 64                                        28       18        35
+//      12288 x 24                                       40       31        36
+//      12288 x 64                                       79       51        38
+constexpr int MANY_GROUPS = 512;   // 8192 outputs
+template <int DT, int GROUP, bool VEC>
+static hipError_t linear_vec(const QuantLinearArgs& a, hipStream_t s) {
+  const bool many = a.n_groups >= MANY_GROUPS;
+  if (thin_lds(DT, a) <= THIN_LDS && a.M <= (DT && many ? 2 : 16)) {
+    if (a.M == 1) return many ? launch_thin<DT, GROUP, VEC, 1, 4, 8>(a, s) : launch_thin<DT, GROUP, VEC, 1, 2, 16>(a, s);
+    return many ? launch_thin<DT, GROUP, VEC, 4, 4, 8>(a, s) : launch_thin<DT, GROUP, VEC, 4, 2, 16>(a, s);
+  }
+  const int64_t m = (a.M + 15) / 16, b32 = (a.n_groups + 1) / 2 * m, b64 = (a.n_groups + 3) / 4 * m, b128 = (a.n_groups + 7) / 8 * ((m + 1) / 2);
+  if constexpr (DT == 1) {
+    if (b32 <= 256) return launch_wide<1, GROUP, VEC, 1, 2, 1, 8, 2>(a, s);
+    if (m == 1 || b64 <= 512) return launch_wide<1, GROUP, VEC, 1, 2, 2, 4, 2>(a, s);
+    if (b128 <= 256) return launch_wide<1, GROUP, VEC, 2, 2, 4, 4, 2>(a, s);
+    return launch_wide<1, GROUP, VEC, 4, 2, 4, 2, 2>(a, s);
+  } else {
+    if (b32 <= 256) return launch_wide<0, GROUP, VEC, 1, 1, 2, 4, 2>(a, s);
+    if (m == 1 || b64 <= 512) return launch_wide<0, GROUP, VEC, 1, 2, 2, 4, 2>(a, s);
+    return launch_wide<0, GROUP, VEC, 2, 2, 4, 2, 2>(a, s);
+  }
+}
+// Rows of x that cannot be read in 16-byte pieces go element by element.
 template <int DT, int GROUP>
 static hipError_t linear_group(const QuantLinearArgs& a, hipStream_t s) {
-  const dim3 grid(a.n_groups, (a.M + 15) / 16);
-  if (a.M == 1) k_quant_thin<DT, GROUP, 1, 4><<<grid, QL_WAVES * 64, 0, s>>>(a);
-  else k_quant_thin<DT, GROUP, 4, 2><<<grid, QL_WAVES * 64, 0, s>>>(a);
-  return hipGetLastError();
+  return a.vec ? linear_vec<DT, GROUP, true>(a, s) : linear_vec<DT, GROUP, false>(a, s);
 }
 template <int DT>
 static hipError_t linear_dt(const QuantLinearArgs& a, hipStream_t s) {

@@ -633,8 +633,9 @@ def _need(ok: bool, what: str):
 
 
 def _dense(device, dtype, *tensors) -> bool:
+    index = -1 if device.index is None else device.index
     for t in tensors:
-        if t.dtype != dtype or t.device != device or not t.is_contiguous():
+        if t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
             return False
     return True
 
@@ -740,8 +741,7 @@ class CacheMoves:
 
 def _moves(torch, out, max_moves: int, device, what: str) -> CacheMoves:
     if out is None:
-        buf = torch.empty(2 * max_moves + 4, dtype=torch.int32, device=device)
-        return CacheMoves(buf[4:].view(max_moves, 2), buf[:4])
+        return CacheMoves(torch.empty(max_moves, 2, dtype=torch.int32, device=device), torch.empty(4, dtype=torch.int32, device=device))
     _need(_dense(device, torch.int32, out.pairs, out.status) and out.pairs.numel() == 2 * max_moves and out.status.numel() == 4,
           what + ": out")
     return out
