@@ -35,42 +35,44 @@ constexpr int HD_K = 64;
 template <bool COLUMNS, int T, int NW> struct Operand {
   static constexpr int BYTES = T * HD_K * 2, PER = T / (8 * NW);   // copies of a wave
   static constexpr int CH = T / 8, RPI = 512 / T;                  // (columns) chunks of a row, rows of a copy
-  const uint8_t* src[PER];
-  int last;   // (rows) the first entry of the contraction that the lane's chunk reads, in its step; (columns) its row
+  const uint8_t* base;   // of the next step's copies: the same in all lanes
+  uint32_t off[PER];
   int64_t step;
 
   // f(k) of a lane that reads entries 8 lg + 4 j + (lr >> 2); k & 3 and (k >> 3) & 3 stand for these bits.
   static __device__ __forceinline__ int perm(int k) {
     return T == 256 ? (k & 3) | (k >> 3 & 3) << 2 : T == 128 ? (k & 3) | (k >> 3 & 1) << 2 : (k >> 1 & 1) | (k >> 3 & 1) << 1;
   }
+  // The first entry of the contraction that copy i of a lane reads, in its step.
+  static __device__ __forceinline__ int entry(int i, int wave) {
+    const int lane = threadIdx.x & 63;
+    return COLUMNS ? (wave * PER + i) * RPI + lane / CH : 8 * ((lane & 7) ^ (lane >> 3));
+  }
   // From row r0 of n (clamped: what lies past the end is computed and not
   // kept; columns are read eight at a time), entry c0 of the contraction.
-  __device__ __forceinline__ void begin(const uint8_t* base, int64_t ld, int r0, int n, int c0, int wave) {
+  __device__ __forceinline__ void begin(const uint8_t* p, int64_t ld, int r0, int n, int c0, int wave) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int at = wave * PER + i;
       if (!COLUMNS) {
-        const int r = at * 8 + (lane >> 3), c = (lane & 7) ^ (lane >> 3);
-        src[i] = base + ((int64_t)min(r0 + r, n - 1) * ld + c0 + 8 * c) * 2;
-        last = 8 * c;
+        off[i] = ((uint32_t)min((wave * PER + i) * 8 + (lane >> 3), n - 1 - r0) * (uint32_t)ld + entry(i, wave)) * 2;
       } else {
-        const int k = at * RPI + lane / CH, c = (lane % CH) ^ (perm(k) << 1);
-        src[i] = base + ((int64_t)(c0 + k) * ld + min(r0 + 8 * c, ((n + 7) & ~7) - 8)) * 2;
-        last = lane / CH;
+        const int k = entry(i, wave), c = (lane % CH) ^ (perm(k) << 1);
+        off[i] = ((uint32_t)k * (uint32_t)ld + min(8 * c, ((n + 7) & ~7) - 8 - r0)) * 2;
       }
     }
+    base = p + (COLUMNS ? (int64_t)c0 * ld + r0 : (int64_t)r0 * ld + c0) * 2;
     step = COLUMNS ? HD_K * ld * 2 : HD_K * 2;
   }
   // The next step's copies; `left` entries of the contraction are left.
   __device__ __forceinline__ void copy(uint8_t* tile, int left, int wave) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const uint8_t* p = src[i];
-      if (left < HD_K && last + (COLUMNS ? (wave * PER + i) * RPI : 0) >= left) p = (const uint8_t*)head_zeros;
+      const uint8_t* p = base + off[i];
+      if (left < HD_K && entry(i, wave) >= left) p = (const uint8_t*)head_zeros;
       __builtin_amdgcn_global_load_lds((const void*)p, (__attribute__((address_space(3))) void*)(tile + (wave * PER + i) * 1024), 16, 0, 0);
-      src[i] += step;
     }
+    base += step;
   }
   // The matrix operand of rows r0 .. r0 + 15, entries 32 h .. + 31.
   static __device__ __forceinline__ bf16x8 read(const uint8_t* tile, int r0, int h) {
@@ -154,24 +156,51 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
       ++pass;
     }
   };
-  for (int i = 0; i < S - 1 && i < total; ++i) copy();
-  for (int s = 0; s < total; ++s) {
-    if (copied - s == S - 1) copies_barrier<(S - 2) * PER>();
+  // The operands of half a step are read while the other half is multiplied:
+  // those of A into the registers that its products have just left, those of
+  // B into a second set.  Early in a step's second half all waves have read all
+  // of it, and the next one has arrived: a barrier, and the copies of the step
+  // that takes this one's place.
+  bf16x8 fa[NI], fb[2][NJ];
+  constexpr int EARLY = NI > 2 ? 2 : 1;   // rows of tiles before the barrier
+  auto read_a = [&](int s, int h, int x) { fa[x] = OA::read(smem + (s % S) * STAGE, (wi * NI + x) * 16, h); };
+  auto read_b = [&](int s, int h) {
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) fb[h][y] = OB::read(smem + (s % S) * STAGE + OA::BYTES, (wj * NJ + y) * 16, h);
+  };
+  auto multiply = [&](int h, int x) {
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[x], fb[h][y], acc[x][y], 0, 0, 0);
+  };
+  if (total > 0) {
+    for (int i = 0; i < S && i < total; ++i) copy();
+    if (total >= S) copies_barrier<(S - 1) * PER>();
     else copies_barrier<0>();
-    if (copied < total) copy();
-    const uint8_t* ta = smem + (s % S) * STAGE;
-    const uint8_t* tb = ta + OA::BYTES;
+    read_b(0, 0);
 #pragma unroll
-    for (int h = 0; h < HD_K / 32; ++h) {
-      bf16x8 fa[NI], fb[NJ];
+    for (int x = 0; x < NI; ++x) read_a(0, 0, x);
+    for (int s = 0; s < total; ++s) {
+      const bool more = s + 1 < total;
+      read_b(s, 1);
 #pragma unroll
-      for (int x = 0; x < NI; ++x) fa[x] = OA::read(ta, (wi * NI + x) * 16, h);
+      for (int x = 0; x < NI; ++x) {
+        multiply(0, x);
+        read_a(s, 1, x);
+      }
 #pragma unroll
-      for (int y = 0; y < NJ; ++y) fb[y] = OB::read(tb, (wj * NJ + y) * 16, h);
+      for (int x = 0; x < EARLY; ++x) multiply(1, x);
+      if (s + S <= total) copies_barrier<(S - 2) * PER>();
+      else copies_barrier<0>();
+      if (copied < total) copy();
+      const int n = more ? s + 1 : s;   // (past the end: this step's once more, which nothing uses)
+      read_b(n, 0);
 #pragma unroll
-      for (int x = 0; x < NI; ++x)
+      for (int x = 0; x < EARLY; ++x) read_a(n, 0, x);
 #pragma unroll
-        for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[x], fb[y], acc[x][y], 0, 0, 0);
+      for (int x = EARLY; x < NI; ++x) {
+        multiply(1, x);
+        read_a(n, 0, x);
+      }
     }
   }
 

@@ -36,6 +36,8 @@ int check_head(int32_t dtype, int32_t M, int32_t V, int32_t K) {
   if (!dtype_ok(dtype) || M < 0 || V < 1 || K < 1) return LEDE_E_ARG;
   return K % 8 || M > MOST_ROWS || V > MOST_VOCAB || K > MOST_WIDTH ? LEDE_E_UNSUPPORTED : LEDE_OK;
 }
+// Row strides: a tile's rows are addressed with 32 bits.
+bool stride_ok(int64_t ld) { return ld < 1 << 22; }
 // Rows that the kernels read or write in 16-byte pieces.
 bool rows_ok(const void* p, int64_t ld, int64_t width, int32_t dt) {
   return p && aligned(p, 16) && ld >= width && ld * es_of(dt) % 16 == 0;
@@ -115,6 +117,7 @@ int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M,
   if (int rc = check_head(dtype, M, V, K)) return rc;
   if (M == 0) return LEDE_OK;
   if (!targets || !lse || !rows_ok(hidden, ldh, K, dtype) || !rows_ok(head, ldw, K, dtype)) return LEDE_E_ARG;
+  if (!stride_ok(ldh) || !stride_ok(ldw)) return LEDE_E_UNSUPPORTED;
   const LossPlan p(dtype, M, V, K);
   if (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total) return LEDE_E_ARG;
   hipStream_t s = S_(stream);
@@ -154,6 +157,7 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
   if (d_head && !rows_ok(d_head, ld_dw, K, dtype)) return LEDE_E_ARG;
   if (M && (!targets || !lse || !rows_ok(hidden, ldh, K, dtype) || !rows_ok(head, ldw, K, dtype))) return LEDE_E_ARG;
   if (M && d_hidden && !rows_ok(d_hidden, ld_dh, K, dtype)) return LEDE_E_ARG;
+  if (M && !stride_ok(ldw)) return LEDE_E_UNSUPPORTED;
   const GradPlan p(dtype, M, V, K);
   if (p.total && (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total)) return LEDE_E_ARG;
   hipStream_t s = S_(stream);

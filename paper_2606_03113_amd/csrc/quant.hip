@@ -474,7 +474,8 @@ static hipError_t linear_vec(const QuantLinearArgs& a, hipStream_t s) {
   if constexpr (DT == 1) {
     if (b32 <= 256) return launch_wide<1, GROUP, VEC, 1, 2, 1, 8, 2>(a, s);
     if (m == 1 || b64 <= 512) return launch_wide<1, GROUP, VEC, 1, 2, 2, 4, 2>(a, s);
-    if (b128 <= 256) return launch_wide<1, GROUP, VEC, 2, 2, 4, 4, 2>(a, s);
+    if constexpr (VEC)   // (element by element it does not fit the registers)
+      if (b128 <= 256) return launch_wide<1, GROUP, VEC, 2, 2, 4, 4, 2>(a, s);
     return launch_wide<1, GROUP, VEC, 4, 2, 4, 2, 2>(a, s);
   } else {
     if (b32 <= 256) return launch_wide<0, GROUP, VEC, 1, 1, 2, 4, 2>(a, s);
