@@ -21,10 +21,9 @@ struct HeadArgs {
   const uint8_t *A, *B;            // bf16 numbers, `planes` planes of them
   int64_t lda, ldb, plane_a, plane_b;   // elements, bytes
   int n_i, n_j, C;                 // rows of A and B, length of the contraction
-  int passes;                      // over the contraction: 1, or the six products of parts
   int chunk;                       // entries of the contraction that a block takes
   int i_tiles, j_tiles;
-  int planes;                      // 1 (bf16) or 3 (fp32)
+  int planes;                      // 1 (bf16), or the 3 parts of fp32 numbers
   const int32_t* targets; const float *weights, *lse;
   int V, v0;                       // the vocabulary, the piece's first entry
   float2* sums; int ld_sums, tile0;   // HEAD_SUMS: [row][tile of the vocabulary]

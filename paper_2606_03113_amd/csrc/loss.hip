@@ -19,9 +19,11 @@ __device__ uint4 head_zeros[1];   // what is read in place of a contraction's en
 // address of entries 4 (i & 3) .. + 3 of row i >> 2 (of four rows) and gets
 // column i's four.
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ uint2 lds_column4(const uint8_t* p) {
+typedef __attribute__((address_space(3))) uint8_t lds8;
+__device__ __forceinline__ uint2 lds_column4(const lds8* p) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
 }
+__device__ __forceinline__ bf16x8 lds_row8(const lds8* p) { return __builtin_bit_cast(bf16x8, *(const __attribute__((address_space(3))) u32x4*)p); }
 
 // An operand's tile in LDS: T rows (of the product's output) by 64 entries of
 // the contraction, in one of two layouts, as it lies in memory:
@@ -65,7 +67,7 @@ template <bool COLUMNS, int T, int NW> struct Operand {
     step = COLUMNS ? HD_K * ld * 2 : HD_K * 2;
   }
   // The next step's copies; `left` entries of the contraction are left.
-  __device__ __forceinline__ void copy(uint8_t* tile, int left, int wave) {
+  __device__ __forceinline__ void copy(lds8* tile, int left, int wave) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const uint8_t* p = base + off[i];
@@ -75,14 +77,14 @@ template <bool COLUMNS, int T, int NW> struct Operand {
     base += step;
   }
   // The matrix operand of rows r0 .. r0 + 15, entries 32 h .. + 31.
-  static __device__ __forceinline__ bf16x8 read(const uint8_t* tile, int r0, int h) {
+  static __device__ __forceinline__ bf16x8 read(const lds8* tile, int r0, int h) {
     const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
     if (!COLUMNS) {
       const int r = r0 + lr;
-      return __builtin_bit_cast(bf16x8, lds_ld16(tile + r * 128 + (((4 * h + lg) ^ (r & 7)) << 4)));
+      return lds_row8(tile + r * 128 + (((4 * h + lg) ^ (r & 7)) << 4));
     }
     const int k = 32 * h + 8 * lg + (lr >> 2);
-    const uint8_t* p = tile + k * (2 * T) + (((r0 >> 4) ^ perm(8 * lg + (lr >> 2))) << 5) + ((lr & 3) << 3);
+    const lds8* p = tile + k * (2 * T) + (((r0 >> 4) ^ perm(8 * lg + (lr >> 2))) << 5) + ((lr & 3) << 3);
     const uint2 a = lds_column4(p), b = lds_column4(p + 4 * 2 * T);
     return __builtin_bit_cast(bf16x8, make_uint4(a.x, a.y, b.x, b.y));
   }
@@ -107,14 +109,96 @@ __device__ __forceinline__ void split3(float x, uint16_t (&q)[3]) {
 
 // Which parts of the operands a pass over the contraction multiplies: all of
 // the products down to 2^-16 of the largest, the smallest first.
-__device__ __forceinline__ int pass_a(int passes, int p) { return passes == 1 ? 0 : (0x201100 >> (20 - 4 * p)) & 15; }
-__device__ __forceinline__ int pass_b(int passes, int p) { return passes == 1 ? 0 : (0x021010 >> (20 - 4 * p)) & 15; }
+constexpr int PASSES = 6;
+__device__ __forceinline__ int pass_a(int p) { return (0x201100 >> (20 - 4 * p)) & 15; }
+__device__ __forceinline__ int pass_b(int p) { return (0x021010 >> (20 - 4 * p)) & 15; }
+
+// The copies of the two operands, step after step of passes over the contraction.
+template <class OA, class OB, bool PARTS> struct Copies {
+  OA oa;
+  OB ob;
+  const HeadArgs& a;
+  int i0, j0, c_begin, length, steps, wave;   // length of the contraction, in steps
+  int done = 0, pass = 0, in_pass = 0;
+  __device__ __forceinline__ Copies(const HeadArgs& a_, int i0_, int j0_, int c_begin_, int length_, int wave_)
+      : a(a_), i0(i0_), j0(j0_), c_begin(c_begin_), length(length_), steps((length_ + HD_K - 1) / HD_K), wave(wave_) {
+    if (!PARTS) begin(0, 0);
+  }
+  __device__ __forceinline__ void begin(int pa, int pb) {
+    oa.begin(a.A + pa * a.plane_a, a.lda, i0, a.n_i, c_begin, wave);
+    ob.begin(a.B + pb * a.plane_b, a.ldb, j0, a.n_j, c_begin, wave);
+  }
+  __device__ __forceinline__ void next(lds8* tile) {
+    if (PARTS && in_pass == 0) begin(pass_a(pass), pass_b(pass));
+    const int left = length - in_pass * HD_K;
+    oa.copy(tile, left, wave);
+    ob.copy(tile + OA::BYTES, left, wave);
+    ++done;
+    ++in_pass;
+    if (PARTS && in_pass == steps) {
+      in_pass = 0;
+      ++pass;
+    }
+  }
+};
+
+// One step of the contraction, in `cur`.  The operands of half a step are read
+// while the other half is multiplied: those of A into the registers that its
+// products have just left, those of B into a second set.  Early in the second
+// half all waves have read all of cur and `next` has arrived: a barrier, and the
+// copies of a later step to cur's place (`to`).  The pointers are said to be
+// apart although `to` is cur: the barrier stands between their uses, and
+// without it the compiler waits for all copies on their way before it reads
+// columns.
+template <class OA, class OB, bool ORDER, bool COPY, int WAIT, int NI, int NJ, class Copies_>
+__device__ __forceinline__ void head_step(const lds8* __restrict__ cur, const lds8* __restrict__ next, lds8* __restrict__ to, Copies_& copies,
+                                          int wi, int wj, bf16x8 (&fa)[NI], bf16x8 (&fb)[2][NJ], f32x4 (&acc)[NI][NJ]) {
+  auto keep_order = []() {
+    if (ORDER) __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr int EARLY = NI > 2 ? 2 : 1;   // rows of tiles before the barrier
+  auto read_a = [&](const lds8* t, int h, int x) { fa[x] = OA::read(t, (wi * NI + x) * 16, h); };
+  auto read_b = [&](const lds8* t, int h) {
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) fb[h][y] = OB::read(t + OA::BYTES, (wj * NJ + y) * 16, h);
+  };
+  auto multiply = [&](int h, int x) {
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[x], fb[h][y], acc[x][y], 0, 0, 0);
+  };
+#pragma unroll
+  for (int x = 0; x < NI; ++x) {
+    multiply(0, x);
+    if (x == 0) {   // (not before it: the count of reads on their way ends at 15)
+      keep_order();
+      read_b(cur, 1);
+    }
+    read_a(cur, 1, x);
+    keep_order();   // (left alone, reads stand right before what waits for them)
+  }
+#pragma unroll
+  for (int x = 0; x < EARLY; ++x) {
+    multiply(1, x);
+    keep_order();
+  }
+  copies_barrier<WAIT>();
+  if (COPY) copies.next(to);
+  read_b(next, 0);
+#pragma unroll
+  for (int x = 0; x < EARLY; ++x) read_a(next, 0, x);
+#pragma unroll
+  for (int x = EARLY; x < NI; ++x) {
+    multiply(1, x);
+    read_a(next, 0, x);
+    keep_order();
+  }
+}
 
 // out[j][i] = sum_c A[i][c] B[j][c], TI x TJ of them a block, WI x WJ waves.  Lane
 // (lr, lg) of a wave holds, of each of its 16 x 16 tiles, i = 4 lg + 0..3 of j =
 // lr.  A ring of S steps of the contraction in LDS: one is multiplied while the
 // next ones are on their way; one barrier a step.
-template <bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
+template <bool PARTS, bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
 __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
   constexpr int NW = WI * WJ, NI = TI / WI / 16, NJ = TJ / WJ / 16;
   typedef Operand<CA, TI, NW> OA;
@@ -137,70 +221,30 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
 #pragma unroll
     for (int y = 0; y < NJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const int steps = (c_end - c_begin + HD_K - 1) / HD_K, total = steps * a.passes;
-  OA oa;
-  OB ob;
-  int copied = 0, pass = 0, in_pass = 0;
-  auto copy = [&]() {   // one step's copies
-    if (in_pass == 0) {
-      oa.begin(a.A + pass_a(a.passes, pass) * a.plane_a, a.lda, i0, a.n_i, c_begin, wave);
-      ob.begin(a.B + pass_b(a.passes, pass) * a.plane_b, a.ldb, j0, a.n_j, c_begin, wave);
-    }
-    uint8_t* tile = smem + (copied % S) * STAGE;
-    const int left = c_end - c_begin - in_pass * HD_K;
-    oa.copy(tile, left, wave);
-    ob.copy(tile + OA::BYTES, left, wave);
-    ++copied;
-    if (++in_pass == steps) {
-      in_pass = 0;
-      ++pass;
-    }
-  };
-  // The operands of half a step are read while the other half is multiplied:
-  // those of A into the registers that its products have just left, those of
-  // B into a second set.  Early in a step's second half all waves have read all
-  // of it, and the next one has arrived: a barrier, and the copies of the step
-  // that takes this one's place.
-  bf16x8 fa[NI], fb[2][NJ];
-  constexpr int EARLY = NI > 2 ? 2 : 1;   // rows of tiles before the barrier
-  auto read_a = [&](int s, int h, int x) { fa[x] = OA::read(smem + (s % S) * STAGE, (wi * NI + x) * 16, h); };
-  auto read_b = [&](int s, int h) {
-#pragma unroll
-    for (int y = 0; y < NJ; ++y) fb[h][y] = OB::read(smem + (s % S) * STAGE + OA::BYTES, (wj * NJ + y) * 16, h);
-  };
-  auto multiply = [&](int h, int x) {
-#pragma unroll
-    for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[x], fb[h][y], acc[x][y], 0, 0, 0);
-  };
+  Copies<OA, OB, PARTS> copies(a, i0, j0, c_begin, c_end - c_begin, wave);
+  const int total = copies.steps * (PARTS ? PASSES : 1);
   if (total > 0) {
-    for (int i = 0; i < S && i < total; ++i) copy();
+    lds8* ring = (lds8*)smem;
+    for (int i = 0; i < S && i < total; ++i) copies.next(ring + i * STAGE);
     if (total >= S) copies_barrier<(S - 1) * PER>();
     else copies_barrier<0>();
-    read_b(0, 0);
+    bf16x8 fa[NI], fb[2][NJ];
 #pragma unroll
-    for (int x = 0; x < NI; ++x) read_a(0, 0, x);
-    for (int s = 0; s < total; ++s) {
-      const bool more = s + 1 < total;
-      read_b(s, 1);
+    for (int y = 0; y < NJ; ++y) fb[0][y] = OB::read(ring + OA::BYTES, (wj * NJ + y) * 16, 0);
 #pragma unroll
-      for (int x = 0; x < NI; ++x) {
-        multiply(0, x);
-        read_a(s, 1, x);
-      }
-#pragma unroll
-      for (int x = 0; x < EARLY; ++x) multiply(1, x);
-      if (s + S <= total) copies_barrier<(S - 2) * PER>();
-      else copies_barrier<0>();
-      if (copied < total) copy();
-      const int n = more ? s + 1 : s;   // (past the end: this step's once more, which nothing uses)
-      read_b(n, 0);
-#pragma unroll
-      for (int x = 0; x < EARLY; ++x) read_a(n, 0, x);
-#pragma unroll
-      for (int x = EARLY; x < NI; ++x) {
-        multiply(1, x);
-        read_a(n, 0, x);
-      }
+    for (int x = 0; x < NI; ++x) fa[x] = OA::read(ring, (wi * NI + x) * 16, 0);
+    int slot = 0;
+    auto after = [&](int x) { return x + 1 == S ? 0 : x + 1; };
+    for (int s = S; s < total; ++s) {
+      lds8* cur = ring + slot * STAGE;
+      slot = after(slot);
+      head_step<OA, OB, !CA, true, (S - 2) * PER>(cur, ring + slot * STAGE, cur, copies, wi, wj, fa, fb, acc);
+    }
+#pragma unroll 1
+    for (int s = max(total - S, 0); s < total; ++s) {   // (behind the last step: what an earlier one left, which nothing uses)
+      lds8* cur = ring + slot * STAGE;
+      slot = after(slot);
+      head_step<OA, OB, !CA, false, 0>(cur, ring + slot * STAGE, cur, copies, wi, wj, fa, fb, acc);
     }
   }
 
@@ -265,12 +309,12 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float q = acc[x][y][e] - lse;
-          d[e] = a.planes == 1 ? __expf(q) : expf(q);
+          d[e] = PARTS ? expf(q) : __expf(q);
           if (i + e + a.v0 == t) d[e] = expm1f(q);   // (p - 1 keeps its bits where p is near 1)
           d[e] = out || i + e >= a.n_i ? 0.f : d[e] * g;
         }
         uint8_t* to = a.dz + ((int64_t)j * a.ldz + i) * 2;
-        if (a.planes == 1) {
+        if (!PARTS) {
           *(uint2*)to = make_uint2(f32_to_bf16x2(d[0], d[1]), f32_to_bf16x2(d[2], d[3]));
         } else {
           uint16_t q[4][3];
@@ -301,7 +345,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
             v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
           }
           *at = v;
-        } else if (a.planes == 1) {
+        } else if (!PARTS) {
           *(uint2*)((uint8_t*)a.out + ((int64_t)j * a.ldo + i) * 2) = make_uint2(f32_to_bf16x2(v.x, v.y), f32_to_bf16x2(v.z, v.w));
         } else {
           *(float4*)((uint8_t*)a.out + ((int64_t)j * a.ldo + i) * 4) = v;
@@ -378,9 +422,9 @@ __global__ __launch_bounds__(256) void k_head_out(HeadOutArgs a) {
 
 // ---- launchers ----------------------------------------------------------------------
 
-template <bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
+template <bool PARTS, bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
 static hipError_t launch(HeadArgs a, int split, hipStream_t s) {
-  const void* f = (const void*)k_head<CA, CB, TI, TJ, WI, WJ, S, EPI>;
+  const void* f = (const void*)k_head<PARTS, CA, CB, TI, TJ, WI, WJ, S, EPI>;
   constexpr int lds = S * (TI + TJ) * HD_K * 2;
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -392,17 +436,21 @@ static hipError_t launch(HeadArgs a, int split, hipStream_t s) {
   void* args[] = {(void*)&a};
   return hipLaunchKernel(f, grid, dim3(WI * WJ * 64), args, lds, s);
 }
-template <bool CA, bool CB, int EPI>
+template <bool PARTS, bool CA, bool CB, int EPI>
 static hipError_t launch_tile(const HeadArgs& a, int split, int tile, hipStream_t s) {
-  if (tile == 64) return launch<CA, CB, 256, 64, 8, 1, 3, EPI>(a, split, s);
-  if (tile == 128) return launch<CA, CB, 256, 128, 4, 2, 3, EPI>(a, split, s);
-  return launch<CA, CB, 256, 256, 2, 4, 2, EPI>(a, split, s);
+  if (tile == 64) return launch<PARTS, CA, CB, 256, 64, 8, 1, 3, EPI>(a, split, s);
+  if (tile == 128) return launch<PARTS, CA, CB, 256, 128, 4, 2, 3, EPI>(a, split, s);
+  return launch<PARTS, CA, CB, 256, 256, 2, 4, 2, EPI>(a, split, s);
+}
+template <bool PARTS>
+static hipError_t launch_epi(int epi, const HeadArgs& a, int split, int tile, hipStream_t s) {
+  if (epi == HEAD_SUMS) return launch_tile<PARTS, false, false, HEAD_SUMS>(a, split, tile, s);
+  if (epi == HEAD_DZ) return launch_tile<PARTS, false, false, HEAD_DZ>(a, split, tile, s);
+  if (epi == HEAD_PART) return launch_tile<PARTS, true, false, HEAD_PART>(a, split, tile, s);
+  return launch<PARTS, true, true, 256, 256, 2, 4, 2, HEAD_OUT>(a, split, s);
 }
 hipError_t launch_head(int epi, const HeadArgs& a, int split, int tile, hipStream_t s) {
-  if (epi == HEAD_SUMS) return launch_tile<false, false, HEAD_SUMS>(a, split, tile, s);
-  if (epi == HEAD_DZ) return launch_tile<false, false, HEAD_DZ>(a, split, tile, s);
-  if (epi == HEAD_PART) return launch_tile<true, false, HEAD_PART>(a, split, tile, s);
-  return launch<true, true, 256, 256, 2, 4, 2, HEAD_OUT>(a, split, s);
+  return a.planes == 3 ? launch_epi<true>(epi, a, split, tile, s) : launch_epi<false>(epi, a, split, tile, s);
 }
 
 hipError_t launch_head_copy(int dtype, const HeadCopyArgs& a, hipStream_t s) {

@@ -126,7 +126,7 @@ int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M,
   a.sums = (float2*)ws; a.ld_sums = p.tiles;
   a.target_z = (float*)(ws + p.sums);
   uint8_t *wh = ws + p.sums + p.target, *ww = wh + p.h;
-  a.planes = p.planes; a.passes = p.planes == 1 ? 1 : 6;
+  a.planes = p.planes;
   a.n_j = M; a.C = a.chunk = K;
   a.targets = targets; a.V = V;
   if (p.planes == 1) {
@@ -180,7 +180,7 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
       lw = K;
     }
     HeadArgs a{};
-    a.planes = p.planes; a.passes = p.planes == 1 ? 1 : 6;
+    a.planes = p.planes;
     a.V = V; a.v0 = v0;
     if (M) {
       HeadArgs z = a;
