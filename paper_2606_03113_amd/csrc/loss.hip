@@ -13,8 +13,6 @@
 
 namespace lede {
 
-__device__ uint4 head_zeros[1];   // what is read in place of a contraction's entries past its end
-
 // Four 16-bit entries of a column: of the 16 lanes of a group, lane i gives the
 // address of entries 4 (i & 3) .. + 3 of row i >> 2 (of four rows) and gets
 // column i's four.
@@ -34,6 +32,7 @@ __device__ __forceinline__ bf16x8 lds_row8(const lds8* p) { return __builtin_bit
 // Copies go from memory to LDS directly, 1 KiB a wave instruction in lane order;
 // the permutation is in the lanes' source addresses.
 constexpr int HD_K = 64;
+constexpr uint32_t BUFFER_RANGE = 0xFFFFFFF0u;   // (a tile's rows span less than 2^31 bytes)
 template <bool COLUMNS, int T, int NW> struct Operand {
   static constexpr int BYTES = T * HD_K * 2, PER = T / (8 * NW);   // copies of a wave
   static constexpr int CH = T / 8, RPI = 512 / T;                  // (columns) chunks of a row, rows of a copy
@@ -66,13 +65,16 @@ template <bool COLUMNS, int T, int NW> struct Operand {
     base = p + (COLUMNS ? (int64_t)c0 * ld + r0 : (int64_t)r0 * ld + c0) * 2;
     step = COLUMNS ? HD_K * ld * 2 : HD_K * 2;
   }
-  // The next step's copies; `left` entries of the contraction are left.
+  // The next step's copies; `left` entries of the contraction are left: what
+  // lies behind them is out of the buffer's range and read as zeros.  (Buffer
+  // loads: behind global ones, which are flat instructions, the compiler waits
+  // for all LDS reads on their way instead of the oldest.)
   __device__ __forceinline__ void copy(lds8* tile, int left, int wave) {
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)BUFFER_RANGE, 0x00020000);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const uint8_t* p = base + off[i];
-      if (left < HD_K && entry(i, wave) >= left) p = (const uint8_t*)head_zeros;
-      __builtin_amdgcn_global_load_lds((const void*)p, (__attribute__((address_space(3))) void*)(tile + (wave * PER + i) * 1024), 16, 0, 0);
+      const uint32_t o = left < HD_K && entry(i, wave) >= left ? BUFFER_RANGE : off[i];
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(tile + (wave * PER + i) * 1024), 16, (int)o, 0, 0, 0);
     }
     base += step;
   }
