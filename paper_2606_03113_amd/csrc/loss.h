@@ -15,20 +15,22 @@ enum HeadEpi : int {
   HEAD_OUT = 3,    // i = k, j = v: dW
 };
 
-constexpr int HEAD_TILE = 256;   // entries of the vocabulary of a tile
+// A block's tile of a product: 256 x 64, 128 or 256, or 128 x 64.
+struct HeadTile { int i, j; };
 
 struct HeadArgs {
   const uint8_t *A, *B;            // bf16 numbers, `planes` planes of them
   int64_t lda, ldb, plane_a, plane_b;   // elements, bytes
   int n_i, n_j, C;                 // rows of A and B, length of the contraction
   int chunk;                       // entries of the contraction that a block takes
-  int i_tiles, j_tiles;
+  int i_tiles, j_tiles, split;     // of the grid
   int planes;                      // 1 (bf16), or the 3 parts of fp32 numbers
   const int32_t* targets; const float *weights, *lse;
   int V, v0;                       // the vocabulary, the piece's first entry
   float2* sums; int ld_sums, tile0;   // HEAD_SUMS: [row][tile of the vocabulary]
   float* target_z;
   uint8_t* dz; int64_t plane_dz; int ldz;   // HEAD_DZ: [row][ldz], zeros past the piece
+  float* rest;                     // (bf16) [row]: what rounding took from the target's dz
   float* part; bool add;           // HEAD_PART: [split][row][K]
   void* out; int64_t ldo;          // HEAD_OUT
 };
@@ -47,9 +49,11 @@ struct HeadJoinArgs {
 struct HeadOutArgs {
   const float* part;
   int split; int64_t n; int K;
+  const int32_t* targets; const float* rest; int V;   // (bf16)
+  const void* head; int64_t ldw;
   void* out; int64_t ldo;
 };
-hipError_t launch_head(int epi, const HeadArgs& a, int split, int tile, hipStream_t s);
+hipError_t launch_head(int epi, const HeadArgs& a, int split, HeadTile tile, hipStream_t s);
 hipError_t launch_head_copy(int dtype, const HeadCopyArgs& a, hipStream_t s);
 hipError_t launch_head_join(const HeadJoinArgs& a, hipStream_t s);
 hipError_t launch_head_out(int dtype, const HeadOutArgs& a, hipStream_t s);

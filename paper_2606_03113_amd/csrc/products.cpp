@@ -44,26 +44,36 @@ bool rows_ok(const void* p, int64_t ld, int64_t width, int32_t dt) {
 }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Rows of a tile of the products whose second operand is rows of `hidden`.
-int row_tile(int32_t M) { return M <= 64 ? 64 : M <= 128 ? 128 : 256; }
+// The tile of a product's blocks, n_i x n_j outputs: wide ones read each operand
+// less often; where they would be few, small ones of which more are on the card
+// and more steps on their way.
+HeadTile head_tile(int64_t n_i, int64_t n_j) {
+  const int j = n_j <= 64 ? 64 : n_j <= 128 ? 128 : 256;
+  if ((n_i + 255) / 256 * ((n_j + j - 1) / j) < 64) return {128, 64};
+  return {256, j};
+}
+int64_t head_blocks(HeadTile t, int64_t n_i, int64_t n_j) { return (n_i + t.i - 1) / t.i * ((n_j + t.j - 1) / t.j); }
 
 // Entries of the vocabulary at a time: what is kept of a piece, `row_bytes` for
 // each of its entries, takes at most PIECE_BYTES (or is one tile wide).
+// A multiple of 256, so that tiles of the pieces are tiles of the whole.
 constexpr int64_t PIECE_BYTES = 128 << 20;
 int piece_size(int32_t V, int64_t row_bytes) {
-  const int64_t most = std::max<int64_t>(HEAD_TILE, PIECE_BYTES / std::max<int64_t>(row_bytes, 1) / HEAD_TILE * HEAD_TILE);
+  const int64_t most = std::max<int64_t>(256, PIECE_BYTES / std::max<int64_t>(row_bytes, 1) / 256 * 256);
   const int64_t n = (V + most - 1) / most, each = (V + n - 1) / n;
-  return (int)((each + HEAD_TILE - 1) / HEAD_TILE * HEAD_TILE);
+  return (int)((each + 256 - 1) / 256 * 256);
 }
 
 // Bytes of the workspaces' parts, in their order.
 struct LossPlan {
   int planes, tiles, piece;
+  HeadTile tile;
   int64_t plane_h, plane_w;
   size_t sums, target, h, w, total;
   LossPlan(int32_t dtype, int32_t M, int32_t V, int32_t K) {
     planes = dtype == LEDE_DTYPE_F32 ? 3 : 1;
-    tiles = (V + HEAD_TILE - 1) / HEAD_TILE;
+    tile = head_tile(V, M);
+    tiles = (V + tile.i - 1) / tile.i;
     piece = planes == 1 ? V : piece_size(V, (int64_t)K * 6);
     plane_h = (int64_t)M * K * 2;
     plane_w = (int64_t)std::min(piece, V) * K * 2;
@@ -75,18 +85,23 @@ struct LossPlan {
   }
 };
 struct GradPlan {
-  int planes, piece, ldz, tile, split, chunk;
+  int planes, piece, ldz, split, chunk;
+  HeadTile tile_z, tile_h, tile_w;   // of dz, dh and dW
   int64_t plane_h, plane_w, plane_dz;
-  size_t h, w, dz, part, total;
+  size_t h, w, dz, rest, part, total;
   GradPlan(int32_t dtype, int32_t M, int32_t V, int32_t K) {
     planes = dtype == LEDE_DTYPE_F32 ? 3 : 1;
     piece = piece_size(V, planes == 1 ? (int64_t)M * 2 : 6 * (int64_t)std::max(M, K));
-    ldz = (std::min(piece, V) + 7) & ~7;
-    tile = row_tile(M);
+    const int n = std::min(piece, V);
+    ldz = (n + 7) & ~7;
+    tile_z = head_tile(n, M);
+    tile_w = head_tile(K, n);
     // dh has few tiles: its contraction over the vocabulary is split so that
     // about a block is there for each CU
-    const int64_t blocks = (int64_t)((K + HEAD_TILE - 1) / HEAD_TILE) * std::max(1, (M + tile - 1) / tile);
+    tile_h = {256, M <= 64 ? 64 : M <= 128 ? 128 : 256};
+    const int64_t blocks = std::max<int64_t>(1, head_blocks(tile_h, K, M));
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>(256 / blocks, ldz / 256));
+    if (blocks * want < 64) tile_h = {128, 64};
     chunk = (int)((ldz + want - 1) / want + 63) & ~63;
     split = (ldz + chunk - 1) / chunk;
     plane_h = (int64_t)M * K * 2;
@@ -95,8 +110,9 @@ struct GradPlan {
     h = up256(planes * plane_h);
     w = planes == 1 ? 0 : up256(3 * plane_w);
     dz = up256(planes * plane_dz);
+    rest = up256((size_t)M * 4);
     part = up256((size_t)split * M * K * 4);
-    total = h + w + dz + part;
+    total = h + w + dz + rest + part;
   }
 };
 
@@ -131,17 +147,17 @@ int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M,
   a.targets = targets; a.V = V;
   if (p.planes == 1) {
     a.A = (const uint8_t*)head; a.lda = ldw; a.B = (const uint8_t*)hidden; a.ldb = ldh; a.n_i = V;
-    if (hipError_t e = launch_head(HEAD_SUMS, a, 1, row_tile(M), s)) return done(e);
+    if (hipError_t e = launch_head(HEAD_SUMS, a, 1, p.tile, s)) return done(e);
   } else {
     HeadCopyArgs c{};
     c.src = hidden; c.ld = ldh; c.n = M; c.K = K; c.dst = wh; c.plane = p.plane_h;
     if (hipError_t e = launch_head_copy(dtype, c, s)) return done(e);
     a.A = ww; a.lda = K; a.plane_a = p.plane_w; a.B = wh; a.ldb = K; a.plane_b = p.plane_h;
     for (int v0 = 0; v0 < V; v0 += p.piece) {
-      a.v0 = v0; a.n_i = std::min(p.piece, V - v0); a.tile0 = v0 / HEAD_TILE;
+      a.v0 = v0; a.n_i = std::min(p.piece, V - v0); a.tile0 = v0 / p.tile.i;
       c.src = (const float*)head + v0 * ldw; c.ld = ldw; c.n = a.n_i; c.dst = ww; c.plane = p.plane_w;
       if (hipError_t e = launch_head_copy(dtype, c, s)) return done(e);
-      if (hipError_t e = launch_head(HEAD_SUMS, a, 1, row_tile(M), s)) return done(e);
+      if (hipError_t e = launch_head(HEAD_SUMS, a, 1, p.tile, s)) return done(e);
     }
   }
   HeadJoinArgs j{};
@@ -161,7 +177,7 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
   const GradPlan p(dtype, M, V, K);
   if (p.total && (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total)) return LEDE_E_ARG;
   hipStream_t s = S_(stream);
-  uint8_t *wh = (uint8_t*)workspace, *ww = wh + p.h, *wz = ww + p.w, *wp = wz + p.dz;
+  uint8_t *wh = (uint8_t*)workspace, *ww = wh + p.h, *wz = ww + p.w, *wr = wz + p.dz, *wp = wr + p.rest;
   if (M) {
     HeadCopyArgs c{};
     c.src = hidden; c.ld = ldh; c.n = M; c.K = K; c.dst = wh; c.plane = p.plane_h;
@@ -188,8 +204,8 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
       z.B = wh; z.ldb = K; z.plane_b = p.plane_h; z.n_j = M;
       z.C = z.chunk = K;
       z.targets = targets; z.weights = weights; z.lse = lse;
-      z.dz = wz; z.plane_dz = p.plane_dz; z.ldz = p.ldz;
-      if (hipError_t e = launch_head(HEAD_DZ, z, 1, p.tile, s)) return done(e);
+      z.dz = wz; z.plane_dz = p.plane_dz; z.ldz = p.ldz; z.rest = (float*)wr;
+      if (hipError_t e = launch_head(HEAD_DZ, z, 1, p.tile_z, s)) return done(e);
     }
     if (M && d_hidden) {
       HeadArgs h = a;
@@ -197,7 +213,7 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
       h.B = wz; h.ldb = p.ldz; h.plane_b = p.plane_dz; h.n_j = M;
       h.C = n; h.chunk = p.chunk;
       h.part = (float*)wp; h.add = v0 > 0;
-      if (hipError_t e = launch_head(HEAD_PART, h, p.split, p.tile, s)) return done(e);
+      if (hipError_t e = launch_head(HEAD_PART, h, p.split, p.tile_h, s)) return done(e);
     }
     if (d_head) {
       HeadArgs d = a;
@@ -205,12 +221,13 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
       d.B = wz; d.ldb = p.ldz; d.plane_b = p.plane_dz; d.n_j = n;
       d.C = d.chunk = M;
       d.out = (uint8_t*)d_head + v0 * ld_dw * es_of(dtype); d.ldo = ld_dw;
-      if (hipError_t e = launch_head(HEAD_OUT, d, 1, 256, s)) return done(e);
+      if (hipError_t e = launch_head(HEAD_OUT, d, 1, p.tile_w, s)) return done(e);
     }
   }
   if (M && d_hidden) {
     HeadOutArgs o{};
     o.part = (const float*)wp; o.split = p.split; o.n = M; o.K = K; o.out = d_hidden; o.ldo = ld_dh;
+    o.targets = targets; o.rest = (const float*)wr; o.V = V; o.head = head; o.ldw = ldw;
     return done(launch_head_out(dtype, o, s));
   }
   return LEDE_OK;
