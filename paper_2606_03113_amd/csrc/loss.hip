@@ -111,6 +111,18 @@ __device__ __forceinline__ void split3(float x, uint16_t (&q)[3]) {
   q[2] = finite ? (uint16_t)(__float_as_uint(r2) >> 16) : 0;
 }
 
+// Two tiles' four entries of a lane (i = 4 lg ..), rounded: neighbouring lanes
+// exchange them, so that each has eight in a row, from place i on of the two
+// tiles' 32 (stores of 64 bytes a row: STORE_NEW, with 32 STORE_OLD).
+__device__ __forceinline__ uint4 eight(const float (&d0)[4], const float (&d1)[4], int& i) {
+  const int lg = (threadIdx.x & 63) >> 4;
+  const bool odd = lg & 1;
+  const uint32_t a0 = f32_to_bf16x2(d0[0], d0[1]), a1 = f32_to_bf16x2(d0[2], d0[3]), b0 = f32_to_bf16x2(d1[0], d1[1]), b1 = f32_to_bf16x2(d1[2], d1[3]);
+  const uint32_t r0 = __shfl_xor((int)(odd ? a0 : b0), 16), r1 = __shfl_xor((int)(odd ? a1 : b1), 16);
+  i = 16 * (lg & 1) + 4 * (lg & 2);
+  return odd ? make_uint4(r0, r1, b0, b1) : make_uint4(a0, a1, r0, r1);
+}
+
 // Which parts of the operands a pass over the contraction multiplies: all of
 // the products down to 2^-16 of the largest, the smallest first.
 constexpr int PASSES = 6;
@@ -306,38 +318,44 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
   } else if (EPI == HEAD_DZ) {
 #pragma unroll
     for (int y = 0; y < NJ; ++y) {
-      const int j = j0 + (wj * NJ + y) * 16 + lr;
-      if (j >= a.n_j) continue;
-      const int t = a.targets[j];
-      const float g = a.weights ? a.weights[j] : 1.f, lse = a.lse[j];
+      const int j = j0 + (wj * NJ + y) * 16 + lr, jc = min(j, a.n_j - 1);
+      const int t = a.targets[jc];
+      const float g = a.weights ? a.weights[jc] : 1.f, lse = a.lse[jc];
       const bool out = t < 0 || t >= a.V || g == 0.f;
-#pragma unroll
-      for (int x = 0; x < NI; ++x) {
-        const int i = i0 + (wi * NI + x) * 16 + 4 * lg;
-        if (i >= a.ldz) continue;
-        float d[4];
+      uint8_t* row = a.dz + (int64_t)j * a.ldz * 2;
+      auto dz = [&](int x, float (&d)[4]) {
+        const int i = i0 + (wi * NI + x) * 16 + 4 * lg, at = t - a.v0 - i;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float q = acc[x][y][e] - lse;
           d[e] = PARTS ? expf(q) : __expf(q);
-          if (i + e + a.v0 == t) d[e] = expm1f(q);   // (p - 1 keeps its bits where p is near 1)
+          if (e == at) d[e] = expm1f(q);   // (p - 1 keeps its bits where p is near 1)
           d[e] = out || i + e >= a.n_i ? 0.f : d[e] * g;
+          if (!PARTS && e == at && j < a.n_j) a.rest[j] = d[e] - Elem<1>::round(d[e]);
         }
-        uint8_t* to = a.dz + ((int64_t)j * a.ldz + i) * 2;
+      };
+#pragma unroll
+      for (int x = 0; x < NI; x += 2) {
+        float d[2][4];
+        dz(x, d[0]);
+        dz(x + 1, d[1]);
         if (!PARTS) {
-          *(uint2*)to = make_uint2(f32_to_bf16x2(d[0], d[1]), f32_to_bf16x2(d[2], d[3]));
-          const int at = t - a.v0 - i;
-          if (at >= 0 && at < 4) {
-            const float dt = at == 0 ? d[0] : at == 1 ? d[1] : at == 2 ? d[2] : d[3];
-            a.rest[j] = dt - Elem<1>::round(dt);
-          }
+          int i;
+          const uint4 u = eight(d[0], d[1], i);
+          i += i0 + (wi * NI + x) * 16;
+          if (j < a.n_j && i < a.ldz) *(uint4*)(row + i * 2) = u;
         } else {
-          uint16_t q[4][3];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) split3(d[e], q[e]);
+          for (int b = 0; b < 2; ++b) {
+            const int i = i0 + (wi * NI + x + b) * 16 + 4 * lg;
+            uint16_t q[4][3];
 #pragma unroll
-          for (int p = 0; p < 3; ++p)
-            *(uint2*)(to + p * a.plane_dz) = make_uint2(q[0][p] | (uint32_t)q[1][p] << 16, q[2][p] | (uint32_t)q[3][p] << 16);
+            for (int e = 0; e < 4; ++e) split3(d[b][e], q[e]);
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+              if (j < a.n_j && i < a.ldz)
+                *(uint2*)(row + i * 2 + p * a.plane_dz) = make_uint2(q[0][p] | (uint32_t)q[1][p] << 16, q[2][p] | (uint32_t)q[3][p] << 16);
+          }
         }
       }
     }
@@ -347,6 +365,18 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
 #pragma unroll
     for (int y = 0; y < NJ; ++y) {
       const int j = j0 + (wj * NJ + y) * 16 + lr;
+      if (EPI == HEAD_OUT && !PARTS) {
+#pragma unroll
+        for (int x = 0; x < NI; x += 2) {
+          int i;
+          const f32x4 v = acc[x][y], w = acc[x + 1][y];
+          const float d0[4] = {v[0], v[1], v[2], v[3]}, d1[4] = {w[0], w[1], w[2], w[3]};
+          const uint4 u = eight(d0, d1, i);
+          i += i0 + (wi * NI + x) * 16;
+          if (j < a.n_j && i < a.n_i) *(uint4*)((uint8_t*)a.out + ((int64_t)j * a.ldo + i) * 2) = u;
+        }
+        continue;
+      }
       if (j >= a.n_j) continue;
 #pragma unroll
       for (int x = 0; x < NI; ++x) {
@@ -354,14 +384,12 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
         if (i >= a.n_i) continue;
         float4 v = make_float4(acc[x][y][0], acc[x][y][1], acc[x][y][2], acc[x][y][3]);
         if (EPI == HEAD_PART) {
-          float4* at = (float4*)(a.part + ((int64_t)part * a.n_j + j) * a.n_i + i);
+          float4* to = (float4*)(a.part + ((int64_t)part * a.n_j + j) * a.n_i + i);
           if (a.add) {
-            const float4 o = *at;
+            const float4 o = *to;
             v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
           }
-          *at = v;
-        } else if (!PARTS) {
-          *(uint2*)((uint8_t*)a.out + ((int64_t)j * a.ldo + i) * 2) = make_uint2(f32_to_bf16x2(v.x, v.y), f32_to_bf16x2(v.z, v.w));
+          *to = v;
         } else {
           *(float4*)((uint8_t*)a.out + ((int64_t)j * a.ldo + i) * 4) = v;
         }
