@@ -619,7 +619,8 @@ int lede_op_cache_plan(const int32_t* seq_lens, const int32_t* new_lens, const i
  * the lengths are found on the device, as in a plan, and change nothing but
  * the status (and the pairs, which are then all -1).  They return
  * LEDE_E_ARG on null pointers and sizes below 1 (below 0: n_free, max_moves),
- * LEDE_E_UNSUPPORTED from 2^24 sequences, table entries a row or moves on.
+ * LEDE_E_UNSUPPORTED from 2^24 sequences or moves on and above 2^30 table
+ * entries.
  *
  * Fork: sequence s with source[s] = r >= 0 becomes the first lens[s] tokens of
  * sequence r (all of them where lens is null): its table row gets r's pages
@@ -772,7 +773,7 @@ int lede_op_logprobs(int32_t dtype, const void* logits, int64_t ld, int32_t n_ro
  * pointers, bad dtypes, sizes below 1, row strides below the row's length,
  * pointers that are not aligned to their elements; LEDE_E_UNSUPPORTED
  * (lede_op_quant_bytes returns 0): another group, sides of 2^24 or more, more
- * than 2^24 tiles of 16 x 128. */
+ * than 2^23 tiles of 16 x 128. */
 size_t lede_op_quant_bytes(int32_t N, int32_t K, int32_t group);
 
 /* Weights w [N][K] (row stride ldw, `dtype`) to codes and scales: the scale is
@@ -791,7 +792,7 @@ int lede_op_quant_pack(const uint8_t* codes, const uint16_t* scales, int32_t N, 
  * group, and of the groups' scaled sums, are fp32 (terms below 2^-110 may
  * count as 0).  What is not finite in a row of x stays with that row of y.  y
  * overlaps nothing else.  M = 0 is no work; LEDE_E_UNSUPPORTED: M of 2^20 or
- * more. */
+ * more, N x M above 2^34. */
 int lede_op_quant_linear(int32_t dtype, const void* packed, int32_t N, int32_t K, int32_t group, const void* x, int64_t ldx,
                          int32_t M, int32_t y_dtype, void* y, int64_t ldy, void* stream);
 
@@ -813,7 +814,8 @@ int lede_op_quant_linear(int32_t dtype, const void* packed, int32_t N, int32_t K
  * K; hidden, head, the gradients, workspace or row strides not multiples of 16
  * bytes; a workspace smaller than lede_op_head_loss_bytes (of the same sizes).
  * LEDE_E_UNSUPPORTED (the sizes are 0): K not a multiple of 8 or above 2^15, M
- * above 2^18, V above 2^20. */
+ * above 2^18, V above 2^20, a row stride of hidden or head of 2^22 elements or
+ * more. */
 size_t lede_op_head_loss_bytes(int32_t dtype, int32_t M, int32_t V, int32_t K);
 int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M, const void* head, int64_t ldw, int32_t V,
                       int32_t K, const int32_t* targets, float* loss, float* lse, void* workspace, size_t workspace_bytes,

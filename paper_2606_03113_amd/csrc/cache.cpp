@@ -179,11 +179,11 @@ int lede_op_cache_plan(const int32_t* seq_lens, const int32_t* new_lens, const i
   return done(launch_cache_plan(a, S_(stream)));
 }
 
-// Tables and shares that the pages' calls step through: entries are numbered in
-// 31 bits, and sequences and places in 24.
+// Tables and shares that the pages' calls step through: all entries of a table
+// are counted in 32 bits.
 static int pages_check(const int32_t* tables, int32_t table_ld, int32_t n_seqs, const int32_t* shares, int32_t n_pages, const int32_t* status) {
   if (!tables || !shares || !status || table_ld < 1 || n_seqs < 1 || n_pages < 1) return LEDE_E_ARG;
-  return n_seqs > MOST_BLOCKS || table_ld > MOST_BLOCKS ? LEDE_E_UNSUPPORTED : LEDE_OK;
+  return n_seqs > MOST_BLOCKS || (int64_t)n_seqs * table_ld > 1 << 30 ? LEDE_E_UNSUPPORTED : LEDE_OK;
 }
 static CachePagesArgs pages_args(int32_t n_seqs, int32_t* tables, int32_t table_ld, int32_t* shares, int32_t n_pages, int32_t* status) {
   CachePagesArgs a{};

@@ -376,16 +376,19 @@ __device__ __forceinline__ int free_from(const CachePagesArgs& a, int s, int& he
 __device__ __forceinline__ bool leaves(const CachePagesArgs& a, int page, int x) { return x == 0 || atomicSub(a.shares + page, 1) == 0; }
 
 // Many entries: a wave a sequence, over the card.  Pages without a holder are
-// marked with -1.
+// marked with -1.  (Each block checks all sequences, so there are few blocks.)
+constexpr int LEAVE_BLOCKS = 512;
 __global__ __launch_bounds__(256) void k_cache_leave(CachePagesArgs a) {
   __shared__ int bad_seq;
   if (free_bad(a, *a.free_head, &bad_seq) != INT_MAX) return;
-  int held;
-  const int s = blockIdx.x * 4 + (threadIdx.x >> 6), from = free_from(a, s, held);
-  for (int i = from + (threadIdx.x & 63); i < held; i += 64) {
-    const int page = a.tables[(int64_t)s * a.table_ld + i];
-    if (in_pool(a, page) && leaves(a, page, count_of(a.shares + page)))
-      __hip_atomic_store(a.shares + page, -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (int s = blockIdx.x * 4 + (threadIdx.x >> 6); s < a.n_seqs; s += gridDim.x * 4) {
+    int held;
+    const int from = free_from(a, s, held);
+    for (int i = from + (threadIdx.x & 63); i < held; i += 64) {
+      const int page = a.tables[(int64_t)s * a.table_ld + i];
+      if (in_pool(a, page) && leaves(a, page, count_of(a.shares + page)))
+        __hip_atomic_store(a.shares + page, -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
   }
 }
 
@@ -585,7 +588,7 @@ hipError_t launch_cache_free(const CachePagesArgs& a, hipStream_t s) {
   if ((int64_t)a.n_seqs * a.table_ld <= FREE_ALONE) {
     k_cache_free<false><<<1, PG_THREADS, 0, s>>>(a);
   } else {
-    k_cache_leave<<<(a.n_seqs + 3) / 4, 256, 0, s>>>(a);
+    k_cache_leave<<<min((a.n_seqs + 3) / 4, LEAVE_BLOCKS), 256, 0, s>>>(a);
     k_cache_free<true><<<1, PG_THREADS, 0, s>>>(a);
   }
   return hipGetLastError();

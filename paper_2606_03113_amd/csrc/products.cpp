@@ -25,7 +25,7 @@ constexpr int32_t MOST_SIDE = (1 << 24) - 1;
 int check_quant(int32_t N, int32_t K, int32_t group) {
   if (N < 1 || K < 1) return LEDE_E_ARG;
   if (group != 32 && group != 64 && group != 128) return LEDE_E_UNSUPPORTED;
-  if (N > MOST_SIDE || K > MOST_SIDE || (int64_t)q_groups(N) * q_tiles(K) > (1 << 24)) return LEDE_E_UNSUPPORTED;
+  if (N > MOST_SIDE || K > MOST_SIDE || (int64_t)q_groups(N) * q_tiles(K) > (1 << 23)) return LEDE_E_UNSUPPORTED;
   return LEDE_OK;
 }
 
@@ -261,7 +261,7 @@ int lede_op_quant_linear(int32_t dtype, const void* packed, int32_t N, int32_t K
   if (!dtype_ok(dtype) || !dtype_ok(y_dtype) || !packed || M < 0) return LEDE_E_ARG;
   if (int rc = check_quant(N, K, group)) return rc;
   if (!aligned(packed, 16)) return LEDE_E_ARG;
-  if (M > 65535 * 16) return LEDE_E_UNSUPPORTED;
+  if (M >= 1 << 20 || (int64_t)N * M > 1ll << 34) return LEDE_E_UNSUPPORTED;   // (a launch has fewer than 2^32 threads)
   if (M == 0) return LEDE_OK;
   if (!x || !y || ldx < K || ldy < N || !aligned(x, es_of(dtype)) || !aligned(y, es_of(y_dtype))) return LEDE_E_ARG;
   QuantLinearArgs a{};

@@ -195,8 +195,8 @@ def test_own_failures_change_nothing():
         d.check(pool, want, pairs, got)
 
 
-@pytest.mark.parametrize("n,ctx,gone", [(1, 1, 1.0), (1, 64, 0.0), (5, 400, 0.5), (64, 4000, 0.1), (1023, 100, 0.5), (1025, 300, 1.0), (2100, 64, 0.3),
-                                        (2, 60000, 0.5)])
+@pytest.mark.parametrize("n,ctx,gone", [(1, 1, 1.0), (1, 64, 0.0), (5, 400, 0.5), (64, 4000, 0.1), (64, 20000, 0.5), (1023, 100, 0.5), (1025, 300, 1.0),
+                                        (2100, 64, 0.3), (2100, 1500, 0.7), (2, 60000, 0.5), (2, 600000, 1.0)])
 def test_free(n, ctx, gone):
     m = lede()
     for seed in range(2):
@@ -215,17 +215,20 @@ def test_free(n, ctx, gone):
         assert want[1] == 0
 
 
-def test_free_failures_change_nothing():
+@pytest.mark.parametrize("n", [40, 1200])     # in one launch and in two
+def test_free_failures_change_nothing(n):
     m = lede()
     r = np.random.default_rng(8)
-    base = _pool(r, 1200, 300, extra=1)
+    base = _pool(r, n, 300 if n > 100 else 2000, extra=1, empty=0.3)
+    source, lens = _forks(r, base)
+    base.fork(source, lens)
     base.seq[:] = base.seq // 3
     gone = base.copy().release()[1]
     for change in ("seq", "held", "head", "room", "low"):
         say("free failure", change)
         pool = base.copy()
         if change == "seq":
-            pool.seq[77] = -5
+            pool.seq[n // 2] = -5
         elif change == "head":
             pool.head = len(pool.free) + 1
         elif change == "low":
@@ -233,17 +236,18 @@ def test_free_failures_change_nothing():
         elif change == "room":
             pool.head = gone - 1
         if change == "held":
-            held, pool.held[1100] = pool.tables.shape[1] + 1, 0
+            at = n - 3
+            held, pool.held[at] = pool.tables.shape[1] + 1, 0
             d = Device(pool)
-            d.held[1100] = held
-            want = [-1, 0, pool.head, 1100]
+            d.held[at] = held
+            want = [-1, 0, pool.head, at]
         else:
             d = Device(pool)
             want = pool.release()
         assert want[0] != 0
         assert m.op_cache_free(d.seq, d.held, d.free, d.head, d.tables, d.shares).tolist() == want
         if change == "held":
-            d.held[1100] = 0
+            d.held[at] = 0
         d.check(pool)
 
 

@@ -20,7 +20,7 @@ COMPACT_GOOD = [P, 3, P, 9, P, P, 4, P, 9, P, 4, P, NULL]
 COPY = ["pairs", "count", "max_moves", "cache", "n_pages", "kv", "hd", "stream"]
 COPY_GOOD = [P, P, 4, P, 9, 8, 128, NULL]
 
-SIZES = [(dict(n=0), ARG), (dict(ld=0), ARG), (dict(n_pages=0), ARG), (dict(n=1 << 24), UNSUPPORTED), (dict(ld=1 << 24), UNSUPPORTED)]
+SIZES = [(dict(n=0), ARG), (dict(ld=0), ARG), (dict(n_pages=0), ARG), (dict(n=1 << 24), UNSUPPORTED), (dict(ld=1 << 29), UNSUPPORTED), (dict(n=1 << 16, ld=(1 << 14) + 1), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("bad,code", [({k: NULL}, ARG) for k in ("source", "seq", "held", "tables", "shares", "status")] + SIZES, ids=str)

@@ -40,7 +40,7 @@ def test_pack_refuses(lib, bad, code):  # noqa: F811
 
 
 @pytest.mark.parametrize("bad,code", [({k: NULL}, ARG) for k in ("packed", "x", "y")] + SHAPE + [
-    (dict(dtype=-1), ARG), (dict(y_dtype=2), ARG), (dict(M=-1), ARG), (dict(M=1 << 20), UNSUPPORTED), (dict(ldx=299), ARG), (dict(ldy=19), ARG),
+    (dict(dtype=-1), ARG), (dict(y_dtype=2), ARG), (dict(M=-1), ARG), (dict(M=1 << 20), UNSUPPORTED), (dict(N=1 << 15, ldy=1 << 15, M=(1 << 19) + 1), UNSUPPORTED), (dict(ldx=299), ARG), (dict(ldy=19), ARG),
     (dict(packed=P + 4), ARG), (dict(x=P + 1), ARG), (dict(y=P + 2), ARG), (dict(dtype=0, x=P + 2), ARG)], ids=str)
 def test_linear_refuses(lib, bad, code):  # noqa: F811
     assert lib.lede_op_quant_linear(*_change(LINEAR_GOOD, LINEAR, **bad)) == code
