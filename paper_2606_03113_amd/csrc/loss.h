@@ -15,16 +15,20 @@ enum HeadEpi : int {
   HEAD_OUT = 3,    // i = k, j = v: dW
 };
 
-// A block's tile of a product: 256 x 64, 128 or 256, or 128 x 64.
+// What the operands are: bf16 numbers, fp32 ones as three planes of parts, fp32
+// ones as they are (split on their way: few rows).
+enum HeadMode : int { HEAD_BF16 = 0, HEAD_PARTS = 1, HEAD_FP32 = 2 };
+// A block's tile of a product: 256 x 64, 128 or 256, or 128 x 64; with
+// HEAD_FP32 128 x 64 or 128.
 struct HeadTile { int i, j; };
 
 struct HeadArgs {
-  const uint8_t *A, *B;            // bf16 numbers, `planes` planes of them
+  const uint8_t *A, *B;            // numbers as `mode` says
   int64_t lda, ldb, plane_a, plane_b;   // elements, bytes
   int n_i, n_j, C;                 // rows of A and B, length of the contraction
   int chunk;                       // entries of the contraction that a block takes
   int i_tiles, j_tiles, split;     // of the grid
-  int planes;                      // 1 (bf16), or the 3 parts of fp32 numbers
+  int mode;                        // HeadMode
   const int32_t* targets; const float *weights, *lse;
   int V, v0;                       // the vocabulary, the piece's first entry
   float2* sums; int ld_sums, tile0;   // HEAD_SUMS: [row][tile of the vocabulary]
@@ -37,7 +41,7 @@ struct HeadArgs {
 struct HeadCopyArgs {
   const void* src; int64_t ld;
   int64_t n; int K;
-  uint8_t* dst; int64_t plane;     // [n][K]; bytes between planes
+  uint8_t* dst; int64_t plane;     // [n][K]; (HEAD_PARTS) bytes between planes
   const int32_t* targets; const float* weights; int V;   // null: every row is kept
 };
 struct HeadJoinArgs {
@@ -54,7 +58,7 @@ struct HeadOutArgs {
   void* out; int64_t ldo;
 };
 hipError_t launch_head(int epi, const HeadArgs& a, int split, HeadTile tile, hipStream_t s);
-hipError_t launch_head_copy(int dtype, const HeadCopyArgs& a, hipStream_t s);
+hipError_t launch_head_copy(int mode, const HeadCopyArgs& a, hipStream_t s);
 hipError_t launch_head_join(const HeadJoinArgs& a, hipStream_t s);
 hipError_t launch_head_out(int dtype, const HeadOutArgs& a, hipStream_t s);
 

@@ -214,62 +214,29 @@ __device__ __forceinline__ void head_step(const lds8* __restrict__ cur, const ld
 // (lr, lg) of a wave holds, of each of its 16 x 16 tiles, i = 4 lg + 0..3 of j =
 // lr.  A ring of S steps of the contraction in LDS: one is multiplied while the
 // next ones are on their way; one barrier a step.
-template <bool PARTS, bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
-__global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
-  constexpr int NW = WI * WJ, NI = TI / WI / 16, NJ = TJ / WJ / 16;
-  typedef Operand<CA, TI, NW> OA;
-  typedef Operand<CB, TJ, NW> OB;
-  constexpr int PER = OA::PER + OB::PER, STAGE = OA::BYTES + OB::BYTES;
-  extern __shared__ __align__(1024) uint8_t smem[];
-  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave % WI, wj = wave / WI;
-  // Blocks b, b + 8, .. run on one XCD, which takes an eighth of the tiles: one
-  // part of the contraction after the other, bands of four tiles of i with all
-  // tiles of j, so that what runs at a time is about square and shares its
-  // operands in the XCD's L2.
+// A block's place: blocks b, b + 8, .. run on one XCD, which takes an eighth of
+// the tiles: one part of the contraction after the other, bands of four tiles
+// of i with all tiles of j, so that what runs at a time is about square and
+// shares its operands in the XCD's L2.
+struct HeadPlace { int part, it, jt; };
+__device__ __forceinline__ bool head_place(const HeadArgs& a, HeadPlace& p) {
   const int per_part = a.i_tiles * a.j_tiles, per_xcd = (per_part * a.split + 7) / 8;
   const int at = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if (at >= per_part * a.split) return;
-  const int part = at / per_part, rest = at - part * per_part, band = rest / (4 * a.j_tiles);
+  if (at >= per_part * a.split) return false;
+  p.part = at / per_part;
+  const int rest = at - p.part * per_part, band = rest / (4 * a.j_tiles);
   const int in_band = rest - band * 4 * a.j_tiles, rows = min(4, a.i_tiles - 4 * band);
-  const int it = 4 * band + in_band % rows, jt = in_band / rows;
-  const int i0 = it * TI, j0 = jt * TJ;
-  const int c_begin = part * a.chunk, c_end = min(c_begin + a.chunk, a.C);
+  p.it = 4 * band + in_band % rows;
+  p.jt = in_band / rows;
+  return true;
+}
 
-  f32x4 acc[NI][NJ];
-#pragma unroll
-  for (int x = 0; x < NI; ++x)
-#pragma unroll
-    for (int y = 0; y < NJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-  Copies<OA, OB, PARTS> copies(a, i0, j0, c_begin, c_end - c_begin, wave);
-  const int total = copies.steps * (PARTS ? PASSES : 1);
-  if (total > 0) {
-    lds8* ring = (lds8*)smem;
-    for (int i = 0; i < S && i < total; ++i) copies.next(ring + i * STAGE);
-    if (total >= S) copies_barrier<(S - 1) * PER>();
-    else copies_barrier<0>();
-    bf16x8 fa[NI], fb[2][NJ];
-#pragma unroll
-    for (int y = 0; y < NJ; ++y) fb[0][y] = OB::read(ring + OA::BYTES, (wj * NJ + y) * 16, 0);
-#pragma unroll
-    for (int x = 0; x < NI; ++x) fa[x] = OA::read(ring, (wi * NI + x) * 16, 0);
-    int slot = 0;
-    auto after = [&](int x) { return x + 1 == S ? 0 : x + 1; };
-    for (int s = S; s < total; ++s) {
-      lds8* cur = ring + slot * STAGE;
-      slot = after(slot);
-      head_step<OA, OB, !CA, true, (S - 2) * PER>(cur, ring + slot * STAGE, cur, copies, wi, wj, fa, fb, acc);
-    }
-#pragma unroll 1
-    for (int s = max(total - S, 0); s < total; ++s) {
-      lds8* cur = ring + slot * STAGE;
-      slot = after(slot);
-      const lds8* next = s + 1 < total ? ring + slot * STAGE : cur;   // (behind the last step: its own once more, which nothing uses)
-      head_step<OA, OB, !CA, false, 0>(cur, next, cur, copies, wi, wj, fa, fb, acc);
-    }
-  }
-
+// What becomes of a block's tile of sums.  Lane (lr, lg) of a wave holds, of each
+// of its 16 x 16 tiles, i = 4 lg + 0..3 of j = lr.
+template <int MODE, int EPI, int TI, int TJ, int WI, int WJ, int NI, int NJ>
+__device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][NJ], uint8_t* smem, const HeadPlace& place, int wi, int wj) {
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+  const int it = place.it, i0 = it * TI, j0 = place.jt * TJ, part = place.part;
   if (EPI == HEAD_SUMS) {
     // of each row the maximum and the sum of exponentials of the tile's entries
     float2* red = (float2*)smem;   // [TJ][WI]
@@ -305,7 +272,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
       if (lg == 0) red[jl * WI + wi] = make_float2(m, sum);
     }
     __syncthreads();
-    for (int jl = threadIdx.x; jl < TJ; jl += NW * 64) {
+    for (int jl = threadIdx.x; jl < TJ; jl += WI * WJ * 64) {
       if (j0 + jl >= a.n_j) break;
       float m = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -328,10 +295,10 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float q = acc[x][y][e] - lse;
-          d[e] = PARTS ? expf(q) : __expf(q);
+          d[e] = MODE ? expf(q) : __expf(q);
           if (e == at) d[e] = expm1f(q);   // (p - 1 keeps its bits where p is near 1)
           d[e] = out || i + e >= a.n_i ? 0.f : d[e] * g;
-          if (!PARTS && e == at && j < a.n_j) a.rest[j] = d[e] - Elem<1>::round(d[e]);
+          if (MODE == HEAD_BF16 && e == at && j < a.n_j) a.rest[j] = d[e] - Elem<1>::round(d[e]);
         }
       };
 #pragma unroll
@@ -339,11 +306,17 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
         float d[2][4];
         dz(x, d[0]);
         dz(x + 1, d[1]);
-        if (!PARTS) {
+        if (MODE == HEAD_BF16) {
           int i;
           const uint4 u = eight(d[0], d[1], i);
           i += i0 + (wi * NI + x) * 16;
           if (j < a.n_j && i < a.ldz) *(uint4*)(row + i * 2) = u;
+        } else if (MODE == HEAD_FP32) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const int i = i0 + (wi * NI + x + b) * 16 + 4 * lg;
+            if (j < a.n_j && i < a.ldz) *(float4*)((float*)a.dz + (int64_t)j * a.ldz + i) = make_float4(d[b][0], d[b][1], d[b][2], d[b][3]);
+          }
         } else {
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
@@ -365,7 +338,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
 #pragma unroll
     for (int y = 0; y < NJ; ++y) {
       const int j = j0 + (wj * NJ + y) * 16 + lr;
-      if (EPI == HEAD_OUT && !PARTS) {
+      if (EPI == HEAD_OUT && MODE == HEAD_BF16) {
 #pragma unroll
         for (int x = 0; x < NI; x += 2) {
           int i;
@@ -398,13 +371,194 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
   }
 }
 
+template <bool PARTS, bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
+__global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
+  constexpr int NW = WI * WJ, NI = TI / WI / 16, NJ = TJ / WJ / 16;
+  typedef Operand<CA, TI, NW> OA;
+  typedef Operand<CB, TJ, NW> OB;
+  constexpr int PER = OA::PER + OB::PER, STAGE = OA::BYTES + OB::BYTES;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave % WI, wj = wave / WI;
+  HeadPlace place;
+  if (!head_place(a, place)) return;
+  const int i0 = place.it * TI, j0 = place.jt * TJ;
+  const int c_begin = place.part * a.chunk, c_end = min(c_begin + a.chunk, a.C);
+
+  f32x4 acc[NI][NJ];
+#pragma unroll
+  for (int x = 0; x < NI; ++x)
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  Copies<OA, OB, PARTS> copies(a, i0, j0, c_begin, c_end - c_begin, wave);
+  const int total = copies.steps * (PARTS ? PASSES : 1);
+  if (total > 0) {
+    lds8* ring = (lds8*)smem;
+    for (int i = 0; i < S && i < total; ++i) copies.next(ring + i * STAGE);
+    if (total >= S) copies_barrier<(S - 1) * PER>();
+    else copies_barrier<0>();
+    bf16x8 fa[NI], fb[2][NJ];
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) fb[0][y] = OB::read(ring + OA::BYTES, (wj * NJ + y) * 16, 0);
+#pragma unroll
+    for (int x = 0; x < NI; ++x) fa[x] = OA::read(ring, (wi * NI + x) * 16, 0);
+    int slot = 0;
+    auto after = [&](int x) { return x + 1 == S ? 0 : x + 1; };
+    for (int s = S; s < total; ++s) {
+      lds8* cur = ring + slot * STAGE;
+      slot = after(slot);
+      head_step<OA, OB, !CA, true, (S - 2) * PER>(cur, ring + slot * STAGE, cur, copies, wi, wj, fa, fb, acc);
+    }
+#pragma unroll 1
+    for (int s = max(total - S, 0); s < total; ++s) {
+      lds8* cur = ring + slot * STAGE;
+      slot = after(slot);
+      const lds8* next = s + 1 < total ? ring + slot * STAGE : cur;   // (behind the last step: its own once more, which nothing uses)
+      head_step<OA, OB, !CA, false, 0>(cur, next, cur, copies, wi, wj, fa, fb, acc);
+    }
+  }
+
+  head_finish<PARTS ? HEAD_PARTS : HEAD_BF16, EPI, TI, TJ, WI, WJ>(a, acc, smem, place, wi, wj);
+}
+
+// ---- few fp32 rows --------------------------------------------------------------------
+
+// With few rows the head's bytes are what counts, and planes of parts would be
+// read and written many times over: here fp32 operands are split on their way
+// to LDS, once a tile, and all six products of parts are made of them.  A step
+// is 32 entries of the contraction: loaded into registers during the step
+// before, split (5.5 operations an entry), written; two barriers a step, and
+// other blocks on the CU meanwhile.  What is not finite becomes NaN in the
+// second part.
+constexpr int HF_K = 32;
+__device__ float4 head_zeros[2];   // what is read in place of entries past the contraction's end
+template <bool COLUMNS, int T> struct Split {
+  static constexpr int PLANE = T * HF_K * 2, CHUNKS = T * HF_K / 8, PER = CHUNKS / 256;   // chunks of eight entries; of a thread
+  const float* src[PER];
+  int64_t step;
+  float4 x[PER][2];
+  static __device__ __forceinline__ int entry(int i) {   // of the contraction, in a step: a chunk's first
+    const int q = threadIdx.x + 256 * i;
+    return COLUMNS ? q / (T / 8) : q % 4 * 8;
+  }
+  __device__ __forceinline__ void begin(const float* p, int64_t ld, int r0, int n, int c0) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int q = threadIdx.x + 256 * i;
+      src[i] = COLUMNS ? p + (int64_t)(c0 + entry(i)) * ld + min(r0 + q % (T / 8) * 8, ((n + 7) & ~7) - 8)
+                       : p + (int64_t)min(r0 + q / 4, n - 1) * ld + c0 + entry(i);
+    }
+    step = COLUMNS ? HF_K * ld : HF_K;
+  }
+  __device__ __forceinline__ void load(int left) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const float4* p = entry(i) < left ? (const float4*)src[i] : head_zeros;
+      x[i][0] = p[0];
+      x[i][1] = p[1];
+      src[i] += step;
+    }
+  }
+  __device__ __forceinline__ void store(lds8* planes) const {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int q = threadIdx.x + 256 * i;
+      int at;
+      if (COLUMNS) {
+        const int k = q / (T / 8), c = q % (T / 8);
+        at = k * (2 * T) + ((c ^ (Operand<true, T, 4>::perm(k) << 1)) << 4);
+      } else {
+        const int r = q / 4;
+        at = r * 64 + (((q & 3) ^ (r >> 2 & 3)) << 4);
+      }
+      const float v[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
+      uint32_t w[3][4];
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        uint32_t u[3][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u[0][h] = __float_as_uint(v[e + h]);
+          const float r1 = v[e + h] - __uint_as_float(u[0][h] & 0xFFFF0000u);
+          u[1][h] = __float_as_uint(r1);
+          u[2][h] = __float_as_uint(r1 - __uint_as_float(u[1][h] & 0xFFFF0000u));
+        }
+#pragma unroll
+        for (int q3 = 0; q3 < 3; ++q3) w[q3][e / 2] = __builtin_amdgcn_perm(u[q3][1], u[q3][0], 0x07060302);
+      }
+#pragma unroll
+      for (int q3 = 0; q3 < 3; ++q3)
+        *(__attribute__((address_space(3))) u32x4*)(planes + q3 * PLANE + at) = u32x4{w[q3][0], w[q3][1], w[q3][2], w[q3][3]};
+    }
+  }
+  static __device__ __forceinline__ bf16x8 read(const lds8* plane, int r0) {
+    if (COLUMNS) return Operand<true, T, 4>::read(plane, r0, 0);
+    const int lane = threadIdx.x & 63, r = r0 + (lane & 15);
+    return lds_row8(plane + r * 64 + (((lane >> 4) ^ (r >> 2 & 3)) << 4));
+  }
+};
+
+template <bool CA, bool CB, int TJ, int WI, int WJ, int EPI>
+__global__ __launch_bounds__(256) void k_head_few(HeadArgs a) {
+  constexpr int TI = 128, NI = TI / WI / 16, NJ = TJ / WJ / 16;
+  typedef Split<CA, TI> SA;
+  typedef Split<CB, TJ> SB;
+  __shared__ __align__(16) uint8_t smem[3 * (SA::PLANE + SB::PLANE)];
+  static_assert(TJ * WI * 8 <= sizeof(smem), "the sums of the waves");
+  lds8 *la = (lds8*)smem, *lb = la + 3 * SA::PLANE;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave % WI, wj = wave / WI;
+  HeadPlace place;
+  if (!head_place(a, place)) return;
+  const int i0 = place.it * TI, j0 = place.jt * TJ;
+  const int c_begin = place.part * a.chunk, c_end = min(c_begin + a.chunk, a.C);
+  f32x4 acc[NI][NJ];
+#pragma unroll
+  for (int x = 0; x < NI; ++x)
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+  SA sa;
+  SB sb;
+  if (c_begin < c_end) {
+    sa.begin((const float*)a.A, a.lda, i0, a.n_i, c_begin);
+    sb.begin((const float*)a.B, a.ldb, j0, a.n_j, c_begin);
+    sa.load(c_end - c_begin);
+    sb.load(c_end - c_begin);
+  }
+  for (int c = c_begin; c < c_end; c += HF_K) {
+    __syncthreads();
+    sa.store(la);
+    sb.store(lb);
+    sa.load(c_end - c - HF_K);   // (behind the last step: zeros)
+    sb.load(c_end - c - HF_K);
+    __syncthreads();
+    bf16x8 fa[3][NI], fb[3][NJ];
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+#pragma unroll
+      for (int x = 0; x < NI; ++x) fa[q][x] = SA::read(la + q * SA::PLANE, (wi * NI + x) * 16);
+#pragma unroll
+      for (int y = 0; y < NJ; ++y) fb[q][y] = SB::read(lb + q * SB::PLANE, (wj * NJ + y) * 16);
+    }
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      constexpr int PA[PASSES] = {2, 0, 1, 1, 0, 0}, PB[PASSES] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+      for (int x = 0; x < NI; ++x)
+#pragma unroll
+        for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[PA[p]][x], fb[PB[p]][y], acc[x][y], 0, 0, 0);
+    }
+  }
+  head_finish<HEAD_FP32, EPI, TI, TJ, WI, WJ>(a, acc, smem, place, wi, wj);
+}
+
 // ---- rows before and after ----------------------------------------------------------
 
 // Rows of a matrix as the products read them: bf16 numbers, or the three parts
 // of fp32 ones.  Rows that are left out become zeros: what they hold (a padded
 // place may hold anything) must not reach dW as 0 x NaN.
-template <int DT>
+template <int MODE>
 __global__ __launch_bounds__(256) void k_head_copy(HeadCopyArgs a) {
+  constexpr int DT = MODE == HEAD_BF16 ? 1 : 0;
   const int64_t per = a.K / 8, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= a.n * per) return;
   const int r = (int)(at / per), k = (int)(at % per) * 8;
@@ -414,8 +568,14 @@ __global__ __launch_bounds__(256) void k_head_copy(HeadCopyArgs a) {
     out = t < 0 || t >= a.V || (a.weights && a.weights[r] == 0.f);
   }
   const uint8_t* p = (const uint8_t*)a.src + (r * a.ld + k) * Elem<DT>::ES_;
+  if (MODE == HEAD_FP32) {
+    float4* to = (float4*)(a.dst + ((int64_t)r * a.K + k) * 4);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) to[i] = out ? make_float4(0.f, 0.f, 0.f, 0.f) : ((const float4*)p)[i];
+    return;
+  }
   uint8_t* to = a.dst + ((int64_t)r * a.K + k) * 2;
-  if (DT == 1) {
+  if (MODE == HEAD_BF16) {
     *(uint4*)to = out ? make_uint4(0, 0, 0, 0) : ld16(p);
     return;
   }
@@ -512,14 +672,30 @@ static hipError_t launch_epi(int epi, const HeadArgs& a, int split, HeadTile til
   if (epi == HEAD_PART) return launch_tile<PARTS, true, false, HEAD_PART>(a, split, tile, s);
   return launch_tile<PARTS, true, true, HEAD_OUT>(a, split, tile, s);
 }
+template <bool CA, bool CB, int EPI>
+static hipError_t launch_few(HeadArgs a, int split, HeadTile tile, hipStream_t s) {
+  a.i_tiles = (a.n_i + 127) / 128;
+  a.j_tiles = (a.n_j + tile.j - 1) / tile.j;
+  a.split = split;
+  const unsigned grid = (unsigned)(((int64_t)a.i_tiles * a.j_tiles * split + 7) / 8 * 8);
+  if (tile.j == 64) k_head_few<CA, CB, 64, 4, 1, EPI><<<grid, 256, 0, s>>>(a);
+  else k_head_few<CA, CB, 128, 2, 2, EPI><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
 hipError_t launch_head(int epi, const HeadArgs& a, int split, HeadTile tile, hipStream_t s) {
-  return a.planes == 3 ? launch_epi<true>(epi, a, split, tile, s) : launch_epi<false>(epi, a, split, tile, s);
+  if (a.mode == HEAD_PARTS) return launch_epi<true>(epi, a, split, tile, s);
+  if (a.mode == HEAD_BF16) return launch_epi<false>(epi, a, split, tile, s);
+  if (epi == HEAD_SUMS) return launch_few<false, false, HEAD_SUMS>(a, split, tile, s);
+  if (epi == HEAD_DZ) return launch_few<false, false, HEAD_DZ>(a, split, tile, s);
+  if (epi == HEAD_PART) return launch_few<true, false, HEAD_PART>(a, split, tile, s);
+  return launch_few<true, true, HEAD_OUT>(a, split, tile, s);
 }
 
-hipError_t launch_head_copy(int dtype, const HeadCopyArgs& a, hipStream_t s) {
+hipError_t launch_head_copy(int mode, const HeadCopyArgs& a, hipStream_t s) {
   const unsigned blocks = (unsigned)((a.n * (a.K / 8) + 255) / 256);
-  if (dtype) k_head_copy<1><<<blocks, 256, 0, s>>>(a);
-  else k_head_copy<0><<<blocks, 256, 0, s>>>(a);
+  if (mode == HEAD_BF16) k_head_copy<HEAD_BF16><<<blocks, 256, 0, s>>>(a);
+  else if (mode == HEAD_PARTS) k_head_copy<HEAD_PARTS><<<blocks, 256, 0, s>>>(a);
+  else k_head_copy<HEAD_FP32><<<blocks, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 hipError_t launch_head_join(const HeadJoinArgs& a, hipStream_t s) {

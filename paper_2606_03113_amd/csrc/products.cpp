@@ -44,72 +44,86 @@ bool rows_ok(const void* p, int64_t ld, int64_t width, int32_t dt) {
 }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// fp32 rows up to which the operands are split on their way to LDS (us, with the
+// gradient, 32000 x 5120: FEW_TABLE).
+constexpr int32_t FEW_ROWS = 128;
+HeadMode head_mode(int32_t dtype, int32_t M) { return dtype == LEDE_DTYPE_BF16 ? HEAD_BF16 : M <= FEW_ROWS ? HEAD_FP32 : HEAD_PARTS; }
+
 // The tile of a product's blocks, n_i x n_j outputs: wide ones read each operand
 // less often; where they would be few, small ones of which more are on the card
 // and more steps on their way.
-HeadTile head_tile(int64_t n_i, int64_t n_j) {
+HeadTile head_tile(HeadMode mode, int64_t n_i, int64_t n_j) {
+  if (mode == HEAD_FP32) return {128, n_j <= 64 ? 64 : 128};
   const int j = n_j <= 64 ? 64 : n_j <= 128 ? 128 : 256;
   if ((n_i + 255) / 256 * ((n_j + j - 1) / j) < 64) return {128, 64};
   return {256, j};
 }
 int64_t head_blocks(HeadTile t, int64_t n_i, int64_t n_j) { return (n_i + t.i - 1) / t.i * ((n_j + t.j - 1) / t.j); }
 
-// Entries of the vocabulary at a time: what is kept of a piece, `row_bytes` for
-// each of its entries, takes at most PIECE_BYTES (or is one tile wide).
-// A multiple of 256, so that tiles of the pieces are tiles of the whole.
-constexpr int64_t PIECE_BYTES = 128 << 20;
-int piece_size(int32_t V, int64_t row_bytes) {
-  const int64_t most = std::max<int64_t>(256, PIECE_BYTES / std::max<int64_t>(row_bytes, 1) / 256 * 256);
+// Entries of the vocabulary at a time: dz of a piece takes at most DZ_BYTES, the
+// parts of its rows of an fp32 head at most W_BYTES (or it is one tile wide);
+// pieces must be wide enough to fill the card (500 rows over 32000 x 2048 in
+// three pieces 2.7 ms, in one PIECE_ONE).  A multiple of 256, so that tiles of
+// the pieces are tiles of the whole.
+constexpr int64_t DZ_BYTES = 128 << 20, W_BYTES = 1 << 30;
+int piece_size(HeadMode mode, int32_t M, int32_t V, int32_t K, bool grad) {
+  int64_t most = V;
+  if (grad) most = std::min(most, DZ_BYTES / std::max<int64_t>((int64_t)M * (mode == HEAD_BF16 ? 2 : mode == HEAD_PARTS ? 6 : 4), 1));
+  if (mode == HEAD_PARTS) most = std::min(most, W_BYTES / ((int64_t)K * 6));
+  if (most >= V) return V;
+  most = std::max<int64_t>(256, most / 256 * 256);
   const int64_t n = (V + most - 1) / most, each = (V + n - 1) / n;
-  return (int)((each + 256 - 1) / 256 * 256);
+  return (int)((each + 255) / 256 * 256);
 }
 
 // Bytes of the workspaces' parts, in their order.
 struct LossPlan {
-  int planes, tiles, piece;
+  HeadMode mode;
+  int tiles, piece;
   HeadTile tile;
   int64_t plane_h, plane_w;
   size_t sums, target, h, w, total;
   LossPlan(int32_t dtype, int32_t M, int32_t V, int32_t K) {
-    planes = dtype == LEDE_DTYPE_F32 ? 3 : 1;
-    tile = head_tile(V, M);
+    mode = head_mode(dtype, M);
+    piece = piece_size(mode, M, V, K, false);
+    tile = head_tile(mode, piece, M);
     tiles = (V + tile.i - 1) / tile.i;
-    piece = planes == 1 ? V : piece_size(V, (int64_t)K * 6);
     plane_h = (int64_t)M * K * 2;
     plane_w = (int64_t)std::min(piece, V) * K * 2;
     sums = up256((size_t)M * tiles * 8);
     target = up256((size_t)M * 4);
-    h = planes == 1 ? 0 : up256(3 * plane_h);
-    w = planes == 1 ? 0 : up256(3 * plane_w);
+    h = mode == HEAD_PARTS ? up256(3 * plane_h) : 0;
+    w = mode == HEAD_PARTS ? up256(3 * plane_w) : 0;
     total = sums + target + h + w;
   }
 };
 struct GradPlan {
-  int planes, piece, ldz, split, chunk;
+  HeadMode mode;
+  int piece, ldz, split, chunk;
   HeadTile tile_z, tile_h, tile_w;   // of dz, dh and dW
   int64_t plane_h, plane_w, plane_dz;
   size_t h, w, dz, rest, part, total;
   GradPlan(int32_t dtype, int32_t M, int32_t V, int32_t K) {
-    planes = dtype == LEDE_DTYPE_F32 ? 3 : 1;
-    piece = piece_size(V, planes == 1 ? (int64_t)M * 2 : 6 * (int64_t)std::max(M, K));
+    mode = head_mode(dtype, M);
+    piece = piece_size(mode, M, V, K, true);
     const int n = std::min(piece, V);
     ldz = (n + 7) & ~7;
-    tile_z = head_tile(n, M);
-    tile_w = head_tile(K, n);
+    tile_z = head_tile(mode, n, M);
+    tile_w = head_tile(mode, K, n);
     // dh has few tiles: its contraction over the vocabulary is split so that
-    // about a block is there for each CU
-    tile_h = {256, M <= 64 ? 64 : M <= 128 ? 128 : 256};
+    // about a block is there for each CU (of k_head_few's, four)
+    tile_h = mode == HEAD_FP32 ? head_tile(mode, K, M) : HeadTile{256, M <= 64 ? 64 : M <= 128 ? 128 : 256};
     const int64_t blocks = std::max<int64_t>(1, head_blocks(tile_h, K, M));
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(256 / blocks, ldz / 256));
-    if (blocks * want < 64) tile_h = {128, 64};
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((mode == HEAD_FP32 ? 1024 : 256) / blocks, ldz / 256));
+    if (mode != HEAD_FP32 && blocks * want < 64) tile_h = {128, 64};
     chunk = (int)((ldz + want - 1) / want + 63) & ~63;
     split = (ldz + chunk - 1) / chunk;
     plane_h = (int64_t)M * K * 2;
-    plane_w = (int64_t)std::min(piece, V) * K * 2;
+    plane_w = (int64_t)n * K * 2;
     plane_dz = (int64_t)M * ldz * 2;
-    h = up256(planes * plane_h);
-    w = planes == 1 ? 0 : up256(3 * plane_w);
-    dz = up256(planes * plane_dz);
+    h = up256((mode == HEAD_BF16 ? 1 : mode == HEAD_PARTS ? 3 : 2) * plane_h);
+    w = mode == HEAD_PARTS ? up256(3 * plane_w) : 0;
+    dz = up256((mode == HEAD_BF16 ? 1 : mode == HEAD_PARTS ? 3 : 2) * plane_dz);
     rest = up256((size_t)M * 4);
     part = up256((size_t)split * M * K * 4);
     total = h + w + dz + rest + part;
@@ -142,21 +156,21 @@ int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M,
   a.sums = (float2*)ws; a.ld_sums = p.tiles;
   a.target_z = (float*)(ws + p.sums);
   uint8_t *wh = ws + p.sums + p.target, *ww = wh + p.h;
-  a.planes = p.planes;
+  a.mode = p.mode;
   a.n_j = M; a.C = a.chunk = K;
   a.targets = targets; a.V = V;
-  if (p.planes == 1) {
+  if (p.mode != HEAD_PARTS) {
     a.A = (const uint8_t*)head; a.lda = ldw; a.B = (const uint8_t*)hidden; a.ldb = ldh; a.n_i = V;
     if (hipError_t e = launch_head(HEAD_SUMS, a, 1, p.tile, s)) return done(e);
   } else {
     HeadCopyArgs c{};
     c.src = hidden; c.ld = ldh; c.n = M; c.K = K; c.dst = wh; c.plane = p.plane_h;
-    if (hipError_t e = launch_head_copy(dtype, c, s)) return done(e);
+    if (hipError_t e = launch_head_copy(p.mode, c, s)) return done(e);
     a.A = ww; a.lda = K; a.plane_a = p.plane_w; a.B = wh; a.ldb = K; a.plane_b = p.plane_h;
     for (int v0 = 0; v0 < V; v0 += p.piece) {
       a.v0 = v0; a.n_i = std::min(p.piece, V - v0); a.tile0 = v0 / p.tile.i;
       c.src = (const float*)head + v0 * ldw; c.ld = ldw; c.n = a.n_i; c.dst = ww; c.plane = p.plane_w;
-      if (hipError_t e = launch_head_copy(dtype, c, s)) return done(e);
+      if (hipError_t e = launch_head_copy(p.mode, c, s)) return done(e);
       if (hipError_t e = launch_head(HEAD_SUMS, a, 1, p.tile, s)) return done(e);
     }
   }
@@ -182,21 +196,21 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
     HeadCopyArgs c{};
     c.src = hidden; c.ld = ldh; c.n = M; c.K = K; c.dst = wh; c.plane = p.plane_h;
     c.targets = targets; c.weights = weights; c.V = V;
-    if (hipError_t e = launch_head_copy(dtype, c, s)) return done(e);
+    if (hipError_t e = launch_head_copy(p.mode, c, s)) return done(e);
   }
   for (int v0 = 0; v0 < V; v0 += p.piece) {
     const int n = std::min(p.piece, V - v0);
     const uint8_t* w = (const uint8_t*)head + v0 * ldw * es_of(dtype);
     int64_t lw = ldw;
-    if (M && p.planes == 3) {
+    if (M && p.mode == HEAD_PARTS) {
       HeadCopyArgs c{};
       c.src = w; c.ld = ldw; c.n = n; c.K = K; c.dst = ww; c.plane = p.plane_w;
-      if (hipError_t e = launch_head_copy(dtype, c, s)) return done(e);
+      if (hipError_t e = launch_head_copy(p.mode, c, s)) return done(e);
       w = ww;
       lw = K;
     }
     HeadArgs a{};
-    a.planes = p.planes;
+    a.mode = p.mode;
     a.V = V; a.v0 = v0;
     if (M) {
       HeadArgs z = a;
