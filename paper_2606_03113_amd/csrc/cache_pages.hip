@@ -72,7 +72,7 @@ __device__ __forceinline__ int at_most(const int32_t* v, int n, int i) {
 // `from` on.  each(u, sequence, place) is called for up to FLAT entries of a
 // thread, and then done() once, so that their loads can be on their way
 // together (a wave a sequence, one load after the other: 12400 entries of 1001
-// sequences freed in 77 us against 17).
+// sequences freed by one block in 77 us against 36).
 constexpr int FLAT = 4;
 struct FlatEntries {
   int32_t end[PG_THREADS], from[PG_THREADS];
@@ -118,8 +118,8 @@ __device__ __forceinline__ int fork_code(const CachePagesArgs& a, int s) {
 
 // One block checks all sequences, then spreads the shared entries.  A source is
 // no fork itself, so its lengths and row stay as they are.  Bound by the chain
-// of loads (source, lengths, entry): 3 forks of 11 pages FORK_SMALL us, 224 of up
-// to 32 FORK_LARGE.
+// of loads (source, lengths, entry): 3 forks of 11 pages 3.5 us, 224 of up
+// to 32 8.9.
 __global__ __launch_bounds__(PG_THREADS) void k_cache_fork(CachePagesArgs a) {
   __shared__ FlatEntries flat;
   __shared__ Two red[PG_WAVES];
@@ -222,8 +222,7 @@ template <class Each> __device__ __forceinline__ void own_entries(const CachePag
 // (INT_MIN + s stands for that).  The others take pages from the free list in
 // sequence order, then in table order; of a page with tokens before the new
 // ones the content has to follow (a pair for the copy).  A chain of loads,
-// atomics and their loads: 4 sequences OWN_SMALL us, 256 OWN_LARGE, 256 with
-// nothing shared OWN_NONE.
+// atomics and their loads: 4 sequences 6.3 us, 256 7.5.
 __global__ __launch_bounds__(PG_THREADS) void k_cache_own(CachePagesArgs a) {
   __shared__ Two red[PG_WAVES];
   __shared__ int bad_seq, bad_code;
@@ -394,8 +393,8 @@ __global__ __launch_bounds__(256) void k_cache_leave(CachePagesArgs a) {
 
 // The pages without a holder go to the list in ascending order, which does not
 // depend on who came last.  MARKED: k_cache_leave has found them.  Bound by
-// chains of loads: 71 entries of 64 sequences FREE_SMALL us in one launch (FREE_SMALL2 in two),
-// 12400 of 1001 FREE_LARGE in two (FREE_LARGE1 in one).
+// chains of loads: 71 entries of 64 sequences 5.6 us in one launch,
+// 12400 of 1001 16 in two (in one 36).
 template <bool MARKED>
 __global__ __launch_bounds__(PG_THREADS) void k_cache_free(CachePagesArgs a) {
   __shared__ uint32_t words[CACHE_MOST_PAGES / 32];
@@ -478,7 +477,7 @@ __global__ __launch_bounds__(PG_THREADS) void k_cache_free(CachePagesArgs a) {
 // With L live pages, the k-th of those from page L on (in ascending order)
 // moves to the k-th hole before it: as many as there are holes, and no page is
 // both read and written.  Bound by the chains of loads: 3500 entries of 150
-// sequences in a pool of 5000 COMPACT_LARGE us, 120 of 9 COMPACT_SMALL.
+// sequences in a pool of 5000 14.4 us, 120 of 9 7.3.
 __global__ __launch_bounds__(PG_THREADS) void k_cache_compact(CachePagesArgs a) {
   __shared__ uint32_t words[CACHE_MOST_PAGES / 32];
   __shared__ int before[PG_THREADS];

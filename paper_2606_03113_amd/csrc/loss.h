@@ -10,39 +10,35 @@ namespace lede {
 // What a product's tile becomes.
 enum HeadEpi : int {
   HEAD_SUMS = 0,   // i = v, j = m: each row's maximum and sum of exponentials over the tile, and the target's logit
-  HEAD_DZ = 1,     // i = v, j = m: dz, rounded to bf16 or in three parts
+  HEAD_DZ = 1,     // i = v, j = m: dz, in the operands' type
   HEAD_PART = 2,   // i = k, j = m: fp32 sums of a part of the contraction over v
   HEAD_OUT = 3,    // i = k, j = v: dW
 };
 
-// What the operands are: bf16 numbers, fp32 ones as three planes of parts, fp32
-// ones as they are (split on their way: few rows).
-enum HeadMode : int { HEAD_BF16 = 0, HEAD_PARTS = 1, HEAD_FP32 = 2 };
-// A block's tile of a product: 256 x 64, 128 or 256, or 128 x 64; with
-// HEAD_FP32 128 x 64 or 128.
+// A block's tile of a product: bf16 256 x 64, 128 or 256, or 128 x 64; fp32 64 or
+// 128 x 64 or 128.
 struct HeadTile { int i, j; };
 
 struct HeadArgs {
-  const uint8_t *A, *B;            // numbers as `mode` says
-  int64_t lda, ldb, plane_a, plane_b;   // elements, bytes
+  const uint8_t *A, *B;
+  int64_t lda, ldb;                // elements
   int n_i, n_j, C;                 // rows of A and B, length of the contraction
   int chunk;                       // entries of the contraction that a block takes
   int i_tiles, j_tiles, split;     // of the grid
-  int mode;                        // HeadMode
   const int32_t* targets; const float *weights, *lse;
   int V, v0;                       // the vocabulary, the piece's first entry
-  float2* sums; int ld_sums, tile0;   // HEAD_SUMS: [row][tile of the vocabulary]
+  float2* sums; int ld_sums;   // HEAD_SUMS: [row][tile of the vocabulary]
   float* target_z;
-  uint8_t* dz; int64_t plane_dz; int ldz;   // HEAD_DZ: [row][ldz], zeros past the piece
+  uint8_t* dz; int ldz;            // HEAD_DZ: [row][ldz], zeros past the piece
   float* rest;                     // (bf16) [row]: what rounding took from the target's dz
   float* part; bool add;           // HEAD_PART: [split][row][K]
   void* out; int64_t ldo;          // HEAD_OUT
 };
 struct HeadCopyArgs {
-  const void* src; int64_t ld;
-  int64_t n; int K;
-  uint8_t* dst; int64_t plane;     // [n][K]; (HEAD_PARTS) bytes between planes
-  const int32_t* targets; const float* weights; int V;   // null: every row is kept
+  const void* src; int64_t pitch;  // bytes between rows
+  int64_t n; int chunks;           // of 16 bytes, in a row
+  uint8_t* dst;
+  const int32_t* targets; const float* weights; int V;
 };
 struct HeadJoinArgs {
   const float2* sums; const float* target_z;
@@ -57,8 +53,8 @@ struct HeadOutArgs {
   const void* head; int64_t ldw;
   void* out; int64_t ldo;
 };
-hipError_t launch_head(int epi, const HeadArgs& a, int split, HeadTile tile, hipStream_t s);
-hipError_t launch_head_copy(int mode, const HeadCopyArgs& a, hipStream_t s);
+hipError_t launch_head(int dtype, int epi, const HeadArgs& a, HeadTile tile, hipStream_t s);
+hipError_t launch_head_copy(const HeadCopyArgs& a, hipStream_t s);
 hipError_t launch_head_join(const HeadJoinArgs& a, hipStream_t s);
 hipError_t launch_head_out(int dtype, const HeadOutArgs& a, hipStream_t s);
 

@@ -98,22 +98,10 @@ template <int N> __device__ __forceinline__ void copies_barrier() {   // this wa
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// The parts of an fp32 number: three bf16 numbers that sum to it, cut off
-// rather than rounded, so that the first does not overflow.
-__device__ __forceinline__ void split3(float x, uint16_t (&q)[3]) {
-  const uint32_t u = __float_as_uint(x);
-  const bool finite = (u & 0x7F800000u) != 0x7F800000u;
-  const float r1 = x - __uint_as_float(u & 0xFFFF0000u);
-  const uint32_t u1 = __float_as_uint(r1);
-  const float r2 = r1 - __uint_as_float(u1 & 0xFFFF0000u);
-  q[0] = (uint16_t)((finite || !(u & 0x7FFFFFu) ? u : u | 0x400000u) >> 16);
-  q[1] = finite ? (uint16_t)(u1 >> 16) : 0;
-  q[2] = finite ? (uint16_t)(__float_as_uint(r2) >> 16) : 0;
-}
-
 // Two tiles' four entries of a lane (i = 4 lg ..), rounded: neighbouring lanes
 // exchange them, so that each has eight in a row, from place i on of the two
-// tiles' 32 (stores of 64 bytes a row: STORE_NEW, with 32 STORE_OLD).
+// tiles' 32 (dW of 8 rows over 128256 x 5120 366 us, with stores of 8 bytes a
+// lane 455).
 __device__ __forceinline__ uint4 eight(const float (&d0)[4], const float (&d1)[4], int& i) {
   const int lg = (threadIdx.x & 63) >> 4;
   const bool odd = lg & 1;
@@ -123,38 +111,16 @@ __device__ __forceinline__ uint4 eight(const float (&d0)[4], const float (&d1)[4
   return odd ? make_uint4(r0, r1, b0, b1) : make_uint4(a0, a1, r0, r1);
 }
 
-// Which parts of the operands a pass over the contraction multiplies: all of
-// the products down to 2^-16 of the largest, the smallest first.
-constexpr int PASSES = 6;
-__device__ __forceinline__ int pass_a(int p) { return (0x201100 >> (20 - 4 * p)) & 15; }
-__device__ __forceinline__ int pass_b(int p) { return (0x021010 >> (20 - 4 * p)) & 15; }
-
-// The copies of the two operands, step after step of passes over the contraction.
-template <class OA, class OB, bool PARTS> struct Copies {
+// The copies of the two operands, step after step.
+template <class OA, class OB> struct Copies {
   OA oa;
   OB ob;
-  const HeadArgs& a;
-  int i0, j0, c_begin, length, steps, wave;   // length of the contraction, in steps
-  int done = 0, pass = 0, in_pass = 0;
-  __device__ __forceinline__ Copies(const HeadArgs& a_, int i0_, int j0_, int c_begin_, int length_, int wave_)
-      : a(a_), i0(i0_), j0(j0_), c_begin(c_begin_), length(length_), steps((length_ + HD_K - 1) / HD_K), wave(wave_) {
-    if (!PARTS) begin(0, 0);
-  }
-  __device__ __forceinline__ void begin(int pa, int pb) {
-    oa.begin(a.A + pa * a.plane_a, a.lda, i0, a.n_i, c_begin, wave);
-    ob.begin(a.B + pb * a.plane_b, a.ldb, j0, a.n_j, c_begin, wave);
-  }
+  int left, wave, done = 0;   // entries of the contraction that are left
   __device__ __forceinline__ void next(lds8* tile) {
-    if (PARTS && in_pass == 0) begin(pass_a(pass), pass_b(pass));
-    const int left = length - in_pass * HD_K;
     oa.copy(tile, left, wave);
     ob.copy(tile + OA::BYTES, left, wave);
+    left -= HD_K;
     ++done;
-    ++in_pass;
-    if (PARTS && in_pass == steps) {
-      in_pass = 0;
-      ++pass;
-    }
   }
 };
 
@@ -210,10 +176,6 @@ __device__ __forceinline__ void head_step(const lds8* __restrict__ cur, const ld
   }
 }
 
-// out[j][i] = sum_c A[i][c] B[j][c], TI x TJ of them a block, WI x WJ waves.  Lane
-// (lr, lg) of a wave holds, of each of its 16 x 16 tiles, i = 4 lg + 0..3 of j =
-// lr.  A ring of S steps of the contraction in LDS: one is multiplied while the
-// next ones are on their way; one barrier a step.
 // A block's place: blocks b, b + 8, .. run on one XCD, which takes an eighth of
 // the tiles: one part of the contraction after the other, bands of four tiles
 // of i with all tiles of j, so that what runs at a time is about square and
@@ -233,7 +195,7 @@ __device__ __forceinline__ bool head_place(const HeadArgs& a, HeadPlace& p) {
 
 // What becomes of a block's tile of sums.  Lane (lr, lg) of a wave holds, of each
 // of its 16 x 16 tiles, i = 4 lg + 0..3 of j = lr.
-template <int MODE, int EPI, int TI, int TJ, int WI, int WJ, int NI, int NJ>
+template <int DT, int EPI, int TI, int TJ, int WI, int WJ, int NI, int NJ>
 __device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][NJ], uint8_t* smem, const HeadPlace& place, int wi, int wj) {
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int it = place.it, i0 = it * TI, j0 = place.jt * TJ, part = place.part;
@@ -280,7 +242,7 @@ __device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][
       const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
       for (int w = 0; w < WI; ++w) sum += red[jl * WI + w].y * __expf(red[jl * WI + w].x - base);
-      a.sums[(int64_t)(j0 + jl) * a.ld_sums + a.tile0 + it] = make_float2(m, sum);
+      a.sums[(int64_t)(j0 + jl) * a.ld_sums + it] = make_float2(m, sum);
     }
   } else if (EPI == HEAD_DZ) {
 #pragma unroll
@@ -295,10 +257,10 @@ __device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float q = acc[x][y][e] - lse;
-          d[e] = MODE ? expf(q) : __expf(q);
+          d[e] = DT ? __expf(q) : expf(q);
           if (e == at) d[e] = expm1f(q);   // (p - 1 keeps its bits where p is near 1)
           d[e] = out || i + e >= a.n_i ? 0.f : d[e] * g;
-          if (MODE == HEAD_BF16 && e == at && j < a.n_j) a.rest[j] = d[e] - Elem<1>::round(d[e]);
+          if (DT && e == at && j < a.n_j) a.rest[j] = d[e] - Elem<1>::round(d[e]);
         }
       };
 #pragma unroll
@@ -306,28 +268,16 @@ __device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][
         float d[2][4];
         dz(x, d[0]);
         dz(x + 1, d[1]);
-        if (MODE == HEAD_BF16) {
+        if (DT) {
           int i;
           const uint4 u = eight(d[0], d[1], i);
           i += i0 + (wi * NI + x) * 16;
           if (j < a.n_j && i < a.ldz) *(uint4*)(row + i * 2) = u;
-        } else if (MODE == HEAD_FP32) {
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int i = i0 + (wi * NI + x + b) * 16 + 4 * lg;
-            if (j < a.n_j && i < a.ldz) *(float4*)((float*)a.dz + (int64_t)j * a.ldz + i) = make_float4(d[b][0], d[b][1], d[b][2], d[b][3]);
-          }
         } else {
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             const int i = i0 + (wi * NI + x + b) * 16 + 4 * lg;
-            uint16_t q[4][3];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) split3(d[b][e], q[e]);
-#pragma unroll
-            for (int p = 0; p < 3; ++p)
-              if (j < a.n_j && i < a.ldz)
-                *(uint2*)(row + i * 2 + p * a.plane_dz) = make_uint2(q[0][p] | (uint32_t)q[1][p] << 16, q[2][p] | (uint32_t)q[3][p] << 16);
+            if (j < a.n_j && i < a.ldz) *(float4*)((float*)a.dz + (int64_t)j * a.ldz + i) = make_float4(d[b][0], d[b][1], d[b][2], d[b][3]);
           }
         }
       }
@@ -338,7 +288,7 @@ __device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][
 #pragma unroll
     for (int y = 0; y < NJ; ++y) {
       const int j = j0 + (wj * NJ + y) * 16 + lr;
-      if (EPI == HEAD_OUT && MODE == HEAD_BF16) {
+      if (EPI == HEAD_OUT && DT) {
 #pragma unroll
         for (int x = 0; x < NI; x += 2) {
           int i;
@@ -371,7 +321,11 @@ __device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][
   }
 }
 
-template <bool PARTS, bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
+// out[j][i] = sum_c A[i][c] B[j][c] of bf16 operands, TI x TJ of them a block, WI x
+// WJ waves.  A ring of S steps of the contraction in LDS: one is multiplied while
+// the next ones are on their way; one barrier a step.  2048 rows of 32000 x 4096
+// 463 us a product, 1160 TFLOP/s (a library product of 8192^3 1450 here).
+template <bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
 __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
   constexpr int NW = WI * WJ, NI = TI / WI / 16, NJ = TJ / WJ / 16;
   typedef Operand<CA, TI, NW> OA;
@@ -390,10 +344,14 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
 #pragma unroll
     for (int y = 0; y < NJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  Copies<OA, OB, PARTS> copies(a, i0, j0, c_begin, c_end - c_begin, wave);
-  const int total = copies.steps * (PARTS ? PASSES : 1);
+  const int total = (c_end - c_begin + HD_K - 1) / HD_K;
   if (total > 0) {
     lds8* ring = (lds8*)smem;
+    Copies<OA, OB> copies;
+    copies.left = c_end - c_begin;
+    copies.wave = wave;
+    copies.oa.begin(a.A, a.lda, i0, a.n_i, c_begin, wave);
+    copies.ob.begin(a.B, a.ldb, j0, a.n_j, c_begin, wave);
     for (int i = 0; i < S && i < total; ++i) copies.next(ring + i * STAGE);
     if (total >= S) copies_barrier<(S - 1) * PER>();
     else copies_barrier<0>();
@@ -418,48 +376,52 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
     }
   }
 
-  head_finish<PARTS ? HEAD_PARTS : HEAD_BF16, EPI, TI, TJ, WI, WJ>(a, acc, smem, place, wi, wj);
+  head_finish<1, EPI, TI, TJ, WI, WJ>(a, acc, smem, place, wi, wj);
 }
 
-// ---- few fp32 rows --------------------------------------------------------------------
+// ---- fp32 ---------------------------------------------------------------------------
 
-// With few rows the head's bytes are what counts, and planes of parts would be
-// read and written many times over: here fp32 operands are split on their way
-// to LDS, once a tile, and all six products of parts are made of them.  A step
-// is 32 entries of the contraction: loaded into registers during the step
-// before, split (5.5 operations an entry), written; two barriers a step, and
-// other blocks on the CU meanwhile.  What is not finite becomes NaN in the
-// second part.
-constexpr int HF_K = 32;
+// The same for fp32 operands: each is three bf16 numbers that sum to it (cut off
+// rather than rounded, so that the first cannot overflow), and of the nine
+// products of parts the six down to 2^-16 of the largest are made, the smallest
+// first: half the rate of 12 products, against an eighth on the fp32 matrix
+// instructions.  Operands are split on their way to LDS, 5.5 operations an entry,
+// so that they are read once a tile (in planes of parts, split before: 47 rows of
+// 32000 x 5120 4.8 ms against 0.9, 1024 rows 7.8 against 6.7, 2048 rows alike).
+// A step is KS entries of the contraction, loaded into registers AHEAD steps
+// before; two barriers a step, and other blocks on the CU meanwhile.  What is
+// not finite becomes NaN in the second part.
 __device__ float4 head_zeros[2];   // what is read in place of entries past the contraction's end
-template <bool COLUMNS, int T> struct Split {
-  static constexpr int PLANE = T * HF_K * 2, CHUNKS = T * HF_K / 8, PER = CHUNKS / 256;   // chunks of eight entries; of a thread
+constexpr int PRODUCTS = 6;
+template <bool COLUMNS, int T, int KS, int AHEAD> struct Split {
+  static constexpr int PLANE = T * KS * 2, CHUNKS = T * KS / 8, PER = CHUNKS / 256;   // chunks of eight entries; of a thread
   const float* src[PER];
   int64_t step;
-  float4 x[PER][2];
+  float4 x[AHEAD][PER][2];
   static __device__ __forceinline__ int entry(int i) {   // of the contraction, in a step: a chunk's first
     const int q = threadIdx.x + 256 * i;
-    return COLUMNS ? q / (T / 8) : q % 4 * 8;
+    return COLUMNS ? q / (T / 8) : q % (KS / 8) * 8;
   }
   __device__ __forceinline__ void begin(const float* p, int64_t ld, int r0, int n, int c0) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int q = threadIdx.x + 256 * i;
       src[i] = COLUMNS ? p + (int64_t)(c0 + entry(i)) * ld + min(r0 + q % (T / 8) * 8, ((n + 7) & ~7) - 8)
-                       : p + (int64_t)min(r0 + q / 4, n - 1) * ld + c0 + entry(i);
+                       : p + (int64_t)min(r0 + q / (KS / 8), n - 1) * ld + c0 + entry(i);
     }
-    step = COLUMNS ? HF_K * ld : HF_K;
+    step = COLUMNS ? KS * ld : KS;
   }
-  __device__ __forceinline__ void load(int left) {
+  __device__ __forceinline__ void load(int u, int left) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const float4* p = entry(i) < left ? (const float4*)src[i] : head_zeros;
-      x[i][0] = p[0];
-      x[i][1] = p[1];
+      x[u][i][0] = p[0];
+      x[u][i][1] = p[1];
       src[i] += step;
     }
   }
-  __device__ __forceinline__ void store(lds8* planes) const {
+  // The layouts of Operand; rows of 32 entries: 64 bytes, chunk c of row r at c ^ (r >> 2 & 3).
+  __device__ __forceinline__ void store(int u, lds8* planes) const {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int q = threadIdx.x + 256 * i;
@@ -468,43 +430,43 @@ template <bool COLUMNS, int T> struct Split {
         const int k = q / (T / 8), c = q % (T / 8);
         at = k * (2 * T) + ((c ^ (Operand<true, T, 4>::perm(k) << 1)) << 4);
       } else {
-        const int r = q / 4;
-        at = r * 64 + (((q & 3) ^ (r >> 2 & 3)) << 4);
+        const int r = q / (KS / 8), c = q % (KS / 8);
+        at = r * (2 * KS) + ((c ^ (KS == 64 ? r & 7 : r >> 2 & 3)) << 4);
       }
-      const float v[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
+      const float v[8] = {x[u][i][0].x, x[u][i][0].y, x[u][i][0].z, x[u][i][0].w, x[u][i][1].x, x[u][i][1].y, x[u][i][1].z, x[u][i][1].w};
       uint32_t w[3][4];
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        uint32_t u[3][2];
+        uint32_t b[3][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          u[0][h] = __float_as_uint(v[e + h]);
-          const float r1 = v[e + h] - __uint_as_float(u[0][h] & 0xFFFF0000u);
-          u[1][h] = __float_as_uint(r1);
-          u[2][h] = __float_as_uint(r1 - __uint_as_float(u[1][h] & 0xFFFF0000u));
+          b[0][h] = __float_as_uint(v[e + h]);
+          const float rest = v[e + h] - __uint_as_float(b[0][h] & 0xFFFF0000u);
+          b[1][h] = __float_as_uint(rest);
+          b[2][h] = __float_as_uint(rest - __uint_as_float(b[1][h] & 0xFFFF0000u));
         }
 #pragma unroll
-        for (int q3 = 0; q3 < 3; ++q3) w[q3][e / 2] = __builtin_amdgcn_perm(u[q3][1], u[q3][0], 0x07060302);
+        for (int p = 0; p < 3; ++p) w[p][e / 2] = __builtin_amdgcn_perm(b[p][1], b[p][0], 0x07060302);
       }
 #pragma unroll
-      for (int q3 = 0; q3 < 3; ++q3)
-        *(__attribute__((address_space(3))) u32x4*)(planes + q3 * PLANE + at) = u32x4{w[q3][0], w[q3][1], w[q3][2], w[q3][3]};
+      for (int p = 0; p < 3; ++p)
+        *(__attribute__((address_space(3))) u32x4*)(planes + p * PLANE + at) = u32x4{w[p][0], w[p][1], w[p][2], w[p][3]};
     }
   }
-  static __device__ __forceinline__ bf16x8 read(const lds8* plane, int r0) {
-    if (COLUMNS) return Operand<true, T, 4>::read(plane, r0, 0);
+  static __device__ __forceinline__ bf16x8 read(const lds8* plane, int r0, int h) {
+    if (COLUMNS || KS == 64) return Operand<COLUMNS, T, 4>::read(plane, r0, h);
     const int lane = threadIdx.x & 63, r = r0 + (lane & 15);
     return lds_row8(plane + r * 64 + (((lane >> 4) ^ (r >> 2 & 3)) << 4));
   }
 };
 
-template <bool CA, bool CB, int TJ, int WI, int WJ, int EPI>
-__global__ __launch_bounds__(256) void k_head_few(HeadArgs a) {
-  constexpr int TI = 128, NI = TI / WI / 16, NJ = TJ / WJ / 16;
-  typedef Split<CA, TI> SA;
-  typedef Split<CB, TJ> SB;
-  __shared__ __align__(16) uint8_t smem[3 * (SA::PLANE + SB::PLANE)];
-  static_assert(TJ * WI * 8 <= sizeof(smem), "the sums of the waves");
+template <bool CA, bool CB, int TI, int TJ, int WI, int WJ, int KS, int AHEAD, int EPI>
+__global__ __launch_bounds__(256) void k_head_fp32(HeadArgs a) {
+  constexpr int NI = TI / WI / 16, NJ = TJ / WJ / 16;
+  typedef Split<CA, TI, KS, AHEAD> SA;
+  typedef Split<CB, TJ, KS, AHEAD> SB;
+  extern __shared__ __align__(16) uint8_t smem[];   // 3 (SA::PLANE + SB::PLANE)
+  static_assert(TJ * WI * 8 <= 3 * (SA::PLANE + SB::PLANE), "the sums of the waves");
   lds8 *la = (lds8*)smem, *lb = la + 3 * SA::PLANE;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave % WI, wj = wave / WI;
   HeadPlace place;
@@ -521,71 +483,58 @@ __global__ __launch_bounds__(256) void k_head_few(HeadArgs a) {
   if (c_begin < c_end) {
     sa.begin((const float*)a.A, a.lda, i0, a.n_i, c_begin);
     sb.begin((const float*)a.B, a.ldb, j0, a.n_j, c_begin);
-    sa.load(c_end - c_begin);
-    sb.load(c_end - c_begin);
-  }
-  for (int c = c_begin; c < c_end; c += HF_K) {
-    __syncthreads();
-    sa.store(la);
-    sb.store(lb);
-    sa.load(c_end - c - HF_K);   // (behind the last step: zeros)
-    sb.load(c_end - c - HF_K);
-    __syncthreads();
-    bf16x8 fa[3][NI], fb[3][NJ];
 #pragma unroll
-    for (int q = 0; q < 3; ++q) {
-#pragma unroll
-      for (int x = 0; x < NI; ++x) fa[q][x] = SA::read(la + q * SA::PLANE, (wi * NI + x) * 16);
-#pragma unroll
-      for (int y = 0; y < NJ; ++y) fb[q][y] = SB::read(lb + q * SB::PLANE, (wj * NJ + y) * 16);
-    }
-#pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-      constexpr int PA[PASSES] = {2, 0, 1, 1, 0, 0}, PB[PASSES] = {0, 2, 1, 0, 1, 0};
-#pragma unroll
-      for (int x = 0; x < NI; ++x)
-#pragma unroll
-        for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[PA[p]][x], fb[PB[p]][y], acc[x][y], 0, 0, 0);
+    for (int u = 0; u < AHEAD; ++u) {
+      sa.load(u, c_end - c_begin - u * KS);
+      sb.load(u, c_end - c_begin - u * KS);
     }
   }
-  head_finish<HEAD_FP32, EPI, TI, TJ, WI, WJ>(a, acc, smem, place, wi, wj);
+  for (int c0 = c_begin; c0 < c_end; c0 += AHEAD * KS) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int left = c_end - c0 - u * KS;   // (behind the last step: zeros)
+      __syncthreads();
+      sa.store(u, la);
+      sb.store(u, lb);
+      sa.load(u, left - AHEAD * KS);
+      sb.load(u, left - AHEAD * KS);
+      __syncthreads();
+      if (left <= 0) continue;
+#pragma unroll
+      for (int h = 0; h < KS / 32; ++h) {
+        bf16x8 fa[3][NI], fb[3][NJ];
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+#pragma unroll
+          for (int x = 0; x < NI; ++x) fa[p][x] = SA::read(la + p * SA::PLANE, (wi * NI + x) * 16, h);
+#pragma unroll
+          for (int y = 0; y < NJ; ++y) fb[p][y] = SB::read(lb + p * SB::PLANE, (wj * NJ + y) * 16, h);
+        }
+#pragma unroll
+        for (int p = 0; p < PRODUCTS; ++p) {
+          constexpr int PA[PRODUCTS] = {2, 0, 1, 1, 0, 0}, PB[PRODUCTS] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+          for (int x = 0; x < NI; ++x)
+#pragma unroll
+            for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[PA[p]][x], fb[PB[p]][y], acc[x][y], 0, 0, 0);
+        }
+      }
+    }
+  }
+  head_finish<0, EPI, TI, TJ, WI, WJ>(a, acc, smem, place, wi, wj);
 }
 
 // ---- rows before and after ----------------------------------------------------------
 
-// Rows of a matrix as the products read them: bf16 numbers, or the three parts
-// of fp32 ones.  Rows that are left out become zeros: what they hold (a padded
-// place may hold anything) must not reach dW as 0 x NaN.
-template <int MODE>
-__global__ __launch_bounds__(256) void k_head_copy(HeadCopyArgs a) {
-  constexpr int DT = MODE == HEAD_BF16 ? 1 : 0;
-  const int64_t per = a.K / 8, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= a.n * per) return;
-  const int r = (int)(at / per), k = (int)(at % per) * 8;
-  bool out = false;
-  if (a.targets) {
-    const int t = a.targets[r];
-    out = t < 0 || t >= a.V || (a.weights && a.weights[r] == 0.f);
-  }
-  const uint8_t* p = (const uint8_t*)a.src + (r * a.ld + k) * Elem<DT>::ES_;
-  if (MODE == HEAD_FP32) {
-    float4* to = (float4*)(a.dst + ((int64_t)r * a.K + k) * 4);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) to[i] = out ? make_float4(0.f, 0.f, 0.f, 0.f) : ((const float4*)p)[i];
-    return;
-  }
-  uint8_t* to = a.dst + ((int64_t)r * a.K + k) * 2;
-  if (MODE == HEAD_BF16) {
-    *(uint4*)to = out ? make_uint4(0, 0, 0, 0) : ld16(p);
-    return;
-  }
-  uint16_t q[8][3];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) split3(out ? 0.f : ((const float*)p)[e], q[e]);
-#pragma unroll
-  for (int i = 0; i < 3; ++i)
-    *(uint4*)(to + i * a.plane) = make_uint4(q[0][i] | (uint32_t)q[1][i] << 16, q[2][i] | (uint32_t)q[3][i] << 16,
-                                             q[4][i] | (uint32_t)q[5][i] << 16, q[6][i] | (uint32_t)q[7][i] << 16);
+// Rows of hidden for dW, zeros in place of those that are left out: what they hold
+// (a padded place may hold anything) must not reach dW as 0 x NaN.
+__global__ __launch_bounds__(256) void k_head_copy(HeadCopyArgs a) {   // rows of `chunks` 16-byte pieces
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= a.n * a.chunks) return;
+  const int64_t r = at / a.chunks, c = at % a.chunks;
+  const int t = a.targets[r];
+  const bool out = t < 0 || t >= a.V || (a.weights && a.weights[r] == 0.f);
+  *(uint4*)(a.dst + at * 16) = out ? make_uint4(0, 0, 0, 0) : ld16((const uint8_t*)a.src + r * a.pitch + c * 16);
 }
 
 // A wave joins a row's tiles.
@@ -641,61 +590,49 @@ __global__ __launch_bounds__(256) void k_head_out(HeadOutArgs a, int lanes) {
 
 // ---- launchers ----------------------------------------------------------------------
 
-template <bool PARTS, bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
-static hipError_t launch(HeadArgs a, int split, hipStream_t s) {
-  const void* f = (const void*)k_head<PARTS, CA, CB, TI, TJ, WI, WJ, S, EPI>;
-  // (no more of the ring than there are steps: short contractions leave room for a second block)
-  const int steps = (std::min(a.chunk, a.C) + HD_K - 1) / HD_K * (PARTS ? PASSES : 1);
-  const int lds = std::max(1, std::min(S, steps)) * (TI + TJ) * HD_K * 2;
+static hipError_t launch_blocks(const void* f, HeadArgs& a, int ti, int tj, int threads, int lds, hipStream_t s) {
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  a.i_tiles = (a.n_i + TI - 1) / TI;
-  a.j_tiles = (a.n_j + TJ - 1) / TJ;
-  a.split = split;
-  const dim3 grid((unsigned)(((int64_t)a.i_tiles * a.j_tiles * split + 7) / 8 * 8));
+  a.i_tiles = (a.n_i + ti - 1) / ti;
+  a.j_tiles = (a.n_j + tj - 1) / tj;
+  const dim3 grid((unsigned)(((int64_t)a.i_tiles * a.j_tiles * a.split + 7) / 8 * 8));
   void* args[] = {(void*)&a};
-  return hipLaunchKernel(f, grid, dim3(WI * WJ * 64), args, lds, s);
+  return hipLaunchKernel(f, grid, dim3(threads), args, lds, s);
 }
-template <bool PARTS, bool CA, bool CB, int EPI>
-static hipError_t launch_tile(const HeadArgs& a, int split, HeadTile tile, hipStream_t s) {
-  if (tile.i == 128) return launch<PARTS, CA, CB, 128, 64, 4, 1, 6, EPI>(a, split, s);
-  if (tile.j == 64) return launch<PARTS, CA, CB, 256, 64, 8, 1, 3, EPI>(a, split, s);
-  if (tile.j == 128) return launch<PARTS, CA, CB, 256, 128, 4, 2, 3, EPI>(a, split, s);
-  return launch<PARTS, CA, CB, 256, 256, 2, 4, 2, EPI>(a, split, s);
+template <bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
+static hipError_t launch_bf16(HeadArgs a, hipStream_t s) {
+  // (no more of the ring than there are steps: short contractions leave room for a second block)
+  const int steps = (std::min(a.chunk, a.C) + HD_K - 1) / HD_K;
+  return launch_blocks((const void*)k_head<CA, CB, TI, TJ, WI, WJ, S, EPI>, a, TI, TJ, WI * WJ * 64, std::max(1, std::min(S, steps)) * (TI + TJ) * HD_K * 2, s);
 }
-template <bool PARTS>
-static hipError_t launch_epi(int epi, const HeadArgs& a, int split, HeadTile tile, hipStream_t s) {
-  if (epi == HEAD_SUMS) return launch_tile<PARTS, false, false, HEAD_SUMS>(a, split, tile, s);
-  if (epi == HEAD_DZ) return launch_tile<PARTS, false, false, HEAD_DZ>(a, split, tile, s);
-  if (epi == HEAD_PART) return launch_tile<PARTS, true, false, HEAD_PART>(a, split, tile, s);
-  return launch_tile<PARTS, true, true, HEAD_OUT>(a, split, tile, s);
+template <bool CA, bool CB, int TI, int TJ, int WI, int WJ, int KS, int AHEAD, int EPI>
+static hipError_t launch_fp32(HeadArgs a, hipStream_t s) {
+  return launch_blocks((const void*)k_head_fp32<CA, CB, TI, TJ, WI, WJ, KS, AHEAD, EPI>, a, TI, TJ, 256, 3 * (TI + TJ) * KS * 2, s);
 }
 template <bool CA, bool CB, int EPI>
-static hipError_t launch_few(HeadArgs a, int split, HeadTile tile, hipStream_t s) {
-  a.i_tiles = (a.n_i + 127) / 128;
-  a.j_tiles = (a.n_j + tile.j - 1) / tile.j;
-  a.split = split;
-  const unsigned grid = (unsigned)(((int64_t)a.i_tiles * a.j_tiles * split + 7) / 8 * 8);
-  if (tile.j == 64) k_head_few<CA, CB, 64, 4, 1, EPI><<<grid, 256, 0, s>>>(a);
-  else k_head_few<CA, CB, 128, 2, 2, EPI><<<grid, 256, 0, s>>>(a);
-  return hipGetLastError();
+static hipError_t launch_tile(int dtype, const HeadArgs& a, HeadTile tile, hipStream_t s) {
+  if (dtype) {
+    if (tile.i == 128) return launch_bf16<CA, CB, 128, 64, 4, 1, 6, EPI>(a, s);
+    if (tile.j == 64) return launch_bf16<CA, CB, 256, 64, 8, 1, 3, EPI>(a, s);
+    if (tile.j == 128) return launch_bf16<CA, CB, 256, 128, 4, 2, 3, EPI>(a, s);
+    return launch_bf16<CA, CB, 256, 256, 2, 4, 2, EPI>(a, s);
+  }
+  if (tile.i == 64 && tile.j == 64) return launch_fp32<CA, CB, 64, 64, 2, 2, 64, 1, EPI>(a, s);
+  if (tile.i == 64) return launch_fp32<CA, CB, 64, 128, 2, 2, 32, 2, EPI>(a, s);
+  if (tile.j == 64) return launch_fp32<CA, CB, 128, 64, 4, 1, 64, 1, EPI>(a, s);
+  return launch_fp32<CA, CB, 128, 128, 2, 2, 32, 2, EPI>(a, s);
 }
-hipError_t launch_head(int epi, const HeadArgs& a, int split, HeadTile tile, hipStream_t s) {
-  if (a.mode == HEAD_PARTS) return launch_epi<true>(epi, a, split, tile, s);
-  if (a.mode == HEAD_BF16) return launch_epi<false>(epi, a, split, tile, s);
-  if (epi == HEAD_SUMS) return launch_few<false, false, HEAD_SUMS>(a, split, tile, s);
-  if (epi == HEAD_DZ) return launch_few<false, false, HEAD_DZ>(a, split, tile, s);
-  if (epi == HEAD_PART) return launch_few<true, false, HEAD_PART>(a, split, tile, s);
-  return launch_few<true, true, HEAD_OUT>(a, split, tile, s);
+hipError_t launch_head(int dtype, int epi, const HeadArgs& a, HeadTile tile, hipStream_t s) {
+  if (epi == HEAD_SUMS) return launch_tile<false, false, HEAD_SUMS>(dtype, a, tile, s);
+  if (epi == HEAD_DZ) return launch_tile<false, false, HEAD_DZ>(dtype, a, tile, s);
+  if (epi == HEAD_PART) return launch_tile<true, false, HEAD_PART>(dtype, a, tile, s);
+  return launch_tile<true, true, HEAD_OUT>(dtype, a, tile, s);
 }
 
-hipError_t launch_head_copy(int mode, const HeadCopyArgs& a, hipStream_t s) {
-  const unsigned blocks = (unsigned)((a.n * (a.K / 8) + 255) / 256);
-  if (mode == HEAD_BF16) k_head_copy<HEAD_BF16><<<blocks, 256, 0, s>>>(a);
-  else if (mode == HEAD_PARTS) k_head_copy<HEAD_PARTS><<<blocks, 256, 0, s>>>(a);
-  else k_head_copy<HEAD_FP32><<<blocks, 256, 0, s>>>(a);
+hipError_t launch_head_copy(const HeadCopyArgs& a, hipStream_t s) {
+  k_head_copy<<<(unsigned)((a.n * a.chunks + 255) / 256), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 hipError_t launch_head_join(const HeadJoinArgs& a, hipStream_t s) {

@@ -44,32 +44,26 @@ bool rows_ok(const void* p, int64_t ld, int64_t width, int32_t dt) {
 }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// fp32 rows up to which the operands are split on their way to LDS (us, with the
-// gradient, 32000 x 5120: FEW_TABLE).
-constexpr int32_t FEW_ROWS = 128;
-HeadMode head_mode(int32_t dtype, int32_t M) { return dtype == LEDE_DTYPE_BF16 ? HEAD_BF16 : M <= FEW_ROWS ? HEAD_FP32 : HEAD_PARTS; }
-
 // The tile of a product's blocks, n_i x n_j outputs: wide ones read each operand
 // less often; where they would be few, small ones of which more are on the card
-// and more steps on their way.
-HeadTile head_tile(HeadMode mode, int64_t n_i, int64_t n_j) {
-  if (mode == HEAD_FP32) return {128, n_j <= 64 ? 64 : 128};
+// and more steps on their way (fp32, 32 rows of 1024 x 256 with the gradient: 43
+// us, 58 with tiles of 128; bf16, 2 rows of 32000 82, 161 with tiles of 256).
+HeadTile head_tile(int32_t dtype, int64_t n_i, int64_t n_j) {
+  const auto blocks = [&](int i, int j) { return (n_i + i - 1) / i * ((n_j + j - 1) / j); };
+  if (dtype == LEDE_DTYPE_F32) {
+    const int j = n_j <= 64 ? 64 : 128;
+    return {blocks(128, j) < 128 ? 64 : 128, j};
+  }
   const int j = n_j <= 64 ? 64 : n_j <= 128 ? 128 : 256;
-  if ((n_i + 255) / 256 * ((n_j + j - 1) / j) < 64) return {128, 64};
-  return {256, j};
+  return blocks(256, j) < 64 ? HeadTile{128, 64} : HeadTile{256, j};
 }
-int64_t head_blocks(HeadTile t, int64_t n_i, int64_t n_j) { return (n_i + t.i - 1) / t.i * ((n_j + t.j - 1) / t.j); }
 
-// Entries of the vocabulary at a time: dz of a piece takes at most DZ_BYTES, the
-// parts of its rows of an fp32 head at most W_BYTES (or it is one tile wide);
-// pieces must be wide enough to fill the card (500 rows over 32000 x 2048 in
-// three pieces 2.7 ms, in one PIECE_ONE).  A multiple of 256, so that tiles of
-// the pieces are tiles of the whole.
-constexpr int64_t DZ_BYTES = 128 << 20, W_BYTES = 1 << 30;
-int piece_size(HeadMode mode, int32_t M, int32_t V, int32_t K, bool grad) {
-  int64_t most = V;
-  if (grad) most = std::min(most, DZ_BYTES / std::max<int64_t>((int64_t)M * (mode == HEAD_BF16 ? 2 : mode == HEAD_PARTS ? 6 : 4), 1));
-  if (mode == HEAD_PARTS) most = std::min(most, W_BYTES / ((int64_t)K * 6));
+// Entries of the vocabulary at a time: dz of a piece takes at most DZ_BYTES (or
+// it is one tile wide).  A multiple of 256, so that tiles of the pieces are
+// tiles of the whole.
+constexpr int64_t DZ_BYTES = 128 << 20;
+int piece_size(int32_t dtype, int32_t M, int32_t V) {
+  int64_t most = DZ_BYTES / std::max<int64_t>((int64_t)M * es_of(dtype), 1);
   if (most >= V) return V;
   most = std::max<int64_t>(256, most / 256 * 256);
   const int64_t n = (V + most - 1) / most, each = (V + n - 1) / n;
@@ -78,55 +72,43 @@ int piece_size(HeadMode mode, int32_t M, int32_t V, int32_t K, bool grad) {
 
 // Bytes of the workspaces' parts, in their order.
 struct LossPlan {
-  HeadMode mode;
-  int tiles, piece;
+  int tiles;
   HeadTile tile;
-  int64_t plane_h, plane_w;
-  size_t sums, target, h, w, total;
-  LossPlan(int32_t dtype, int32_t M, int32_t V, int32_t K) {
-    mode = head_mode(dtype, M);
-    piece = piece_size(mode, M, V, K, false);
-    tile = head_tile(mode, piece, M);
+  size_t sums, target, total;
+  LossPlan(int32_t dtype, int32_t M, int32_t V) {
+    tile = head_tile(dtype, V, M);
     tiles = (V + tile.i - 1) / tile.i;
-    plane_h = (int64_t)M * K * 2;
-    plane_w = (int64_t)std::min(piece, V) * K * 2;
     sums = up256((size_t)M * tiles * 8);
     target = up256((size_t)M * 4);
-    h = mode == HEAD_PARTS ? up256(3 * plane_h) : 0;
-    w = mode == HEAD_PARTS ? up256(3 * plane_w) : 0;
-    total = sums + target + h + w;
+    total = sums + target;
   }
 };
 struct GradPlan {
-  HeadMode mode;
   int piece, ldz, split, chunk;
   HeadTile tile_z, tile_h, tile_w;   // of dz, dh and dW
-  int64_t plane_h, plane_w, plane_dz;
-  size_t h, w, dz, rest, part, total;
+  size_t h, dz, rest, part, total;
   GradPlan(int32_t dtype, int32_t M, int32_t V, int32_t K) {
-    mode = head_mode(dtype, M);
-    piece = piece_size(mode, M, V, K, true);
+    const bool f32 = dtype == LEDE_DTYPE_F32;
+    piece = piece_size(dtype, M, V);
     const int n = std::min(piece, V);
     ldz = (n + 7) & ~7;
-    tile_z = head_tile(mode, n, M);
-    tile_w = head_tile(mode, K, n);
+    tile_z = head_tile(dtype, n, M);
+    tile_w = head_tile(dtype, K, n);
     // dh has few tiles: its contraction over the vocabulary is split so that
-    // about a block is there for each CU (of k_head_few's, four)
-    tile_h = mode == HEAD_FP32 ? head_tile(mode, K, M) : HeadTile{256, M <= 64 ? 64 : M <= 128 ? 128 : 256};
-    const int64_t blocks = std::max<int64_t>(1, head_blocks(tile_h, K, M));
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((mode == HEAD_FP32 ? 1024 : 256) / blocks, ldz / 256));
-    if (mode != HEAD_FP32 && blocks * want < 64) tile_h = {128, 64};
+    // about a block is there for each CU (fp32, of whose blocks a CU holds
+    // several: four)
+    tile_h = {f32 ? 128 : 256, M <= 64 ? 64 : f32 || M <= 128 ? 128 : 256};
+    const int64_t blocks = (int64_t)((K + tile_h.i - 1) / tile_h.i) * std::max(1, (M + tile_h.j - 1) / tile_h.j);
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((f32 ? 1024 : 256) / blocks, ldz / 256));
+    if (f32 && blocks * want < 128) tile_h.i = 64;
+    if (!f32 && blocks * want < 64) tile_h = {128, 64};
     chunk = (int)((ldz + want - 1) / want + 63) & ~63;
     split = (ldz + chunk - 1) / chunk;
-    plane_h = (int64_t)M * K * 2;
-    plane_w = (int64_t)n * K * 2;
-    plane_dz = (int64_t)M * ldz * 2;
-    h = up256((mode == HEAD_BF16 ? 1 : mode == HEAD_PARTS ? 3 : 2) * plane_h);
-    w = mode == HEAD_PARTS ? up256(3 * plane_w) : 0;
-    dz = up256((mode == HEAD_BF16 ? 1 : mode == HEAD_PARTS ? 3 : 2) * plane_dz);
+    h = up256((size_t)M * K * es_of(dtype));
+    dz = up256((size_t)M * ldz * es_of(dtype));
     rest = up256((size_t)M * 4);
     part = up256((size_t)split * M * K * 4);
-    total = h + w + dz + rest + part;
+    total = h + dz + rest + part;
   }
 };
 
@@ -135,7 +117,7 @@ struct GradPlan {
 extern "C" {
 
 size_t lede_op_head_loss_bytes(int32_t dtype, int32_t M, int32_t V, int32_t K) {
-  return check_head(dtype, M, V, K) ? 0 : LossPlan(dtype, M, V, K).total;
+  return check_head(dtype, M, V, K) ? 0 : LossPlan(dtype, M, V).total;
 }
 size_t lede_op_head_loss_grad_bytes(int32_t dtype, int32_t M, int32_t V, int32_t K) {
   return check_head(dtype, M, V, K) ? 0 : GradPlan(dtype, M, V, K).total;
@@ -148,32 +130,17 @@ int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M,
   if (M == 0) return LEDE_OK;
   if (!targets || !lse || !rows_ok(hidden, ldh, K, dtype) || !rows_ok(head, ldw, K, dtype)) return LEDE_E_ARG;
   if (!stride_ok(ldh) || !stride_ok(ldw)) return LEDE_E_UNSUPPORTED;
-  const LossPlan p(dtype, M, V, K);
+  const LossPlan p(dtype, M, V);
   if (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total) return LEDE_E_ARG;
   hipStream_t s = S_(stream);
-  uint8_t* ws = (uint8_t*)workspace;
   HeadArgs a{};
-  a.sums = (float2*)ws; a.ld_sums = p.tiles;
-  a.target_z = (float*)(ws + p.sums);
-  uint8_t *wh = ws + p.sums + p.target, *ww = wh + p.h;
-  a.mode = p.mode;
-  a.n_j = M; a.C = a.chunk = K;
+  a.sums = (float2*)workspace; a.ld_sums = p.tiles;
+  a.target_z = (float*)((uint8_t*)workspace + p.sums);
+  a.A = (const uint8_t*)head; a.lda = ldw; a.n_i = V;
+  a.B = (const uint8_t*)hidden; a.ldb = ldh; a.n_j = M;
+  a.C = a.chunk = K; a.split = 1;
   a.targets = targets; a.V = V;
-  if (p.mode != HEAD_PARTS) {
-    a.A = (const uint8_t*)head; a.lda = ldw; a.B = (const uint8_t*)hidden; a.ldb = ldh; a.n_i = V;
-    if (hipError_t e = launch_head(HEAD_SUMS, a, 1, p.tile, s)) return done(e);
-  } else {
-    HeadCopyArgs c{};
-    c.src = hidden; c.ld = ldh; c.n = M; c.K = K; c.dst = wh; c.plane = p.plane_h;
-    if (hipError_t e = launch_head_copy(p.mode, c, s)) return done(e);
-    a.A = ww; a.lda = K; a.plane_a = p.plane_w; a.B = wh; a.ldb = K; a.plane_b = p.plane_h;
-    for (int v0 = 0; v0 < V; v0 += p.piece) {
-      a.v0 = v0; a.n_i = std::min(p.piece, V - v0); a.tile0 = v0 / p.tile.i;
-      c.src = (const float*)head + v0 * ldw; c.ld = ldw; c.n = a.n_i; c.dst = ww; c.plane = p.plane_w;
-      if (hipError_t e = launch_head_copy(p.mode, c, s)) return done(e);
-      if (hipError_t e = launch_head(HEAD_SUMS, a, 1, p.tile, s)) return done(e);
-    }
-  }
+  if (hipError_t e = launch_head(dtype, HEAD_SUMS, a, p.tile, s)) return done(e);
   HeadJoinArgs j{};
   j.sums = a.sums; j.target_z = a.target_z; j.n = M; j.tiles = p.tiles; j.V = V; j.targets = targets; j.loss = loss; j.lse = lse;
   return done(launch_head_join(j, s));
@@ -187,55 +154,46 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
   if (d_head && !rows_ok(d_head, ld_dw, K, dtype)) return LEDE_E_ARG;
   if (M && (!targets || !lse || !rows_ok(hidden, ldh, K, dtype) || !rows_ok(head, ldw, K, dtype))) return LEDE_E_ARG;
   if (M && d_hidden && !rows_ok(d_hidden, ld_dh, K, dtype)) return LEDE_E_ARG;
-  if (M && !stride_ok(ldw)) return LEDE_E_UNSUPPORTED;
+  if (M && (!stride_ok(ldw) || !stride_ok(ldh))) return LEDE_E_UNSUPPORTED;
   const GradPlan p(dtype, M, V, K);
   if (p.total && (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total)) return LEDE_E_ARG;
   hipStream_t s = S_(stream);
-  uint8_t *wh = (uint8_t*)workspace, *ww = wh + p.h, *wz = ww + p.w, *wr = wz + p.dz, *wp = wr + p.rest;
-  if (M) {
+  uint8_t *wh = (uint8_t*)workspace, *wz = wh + p.h, *wr = wz + p.dz, *wp = wr + p.rest;
+  if (M && d_head) {
     HeadCopyArgs c{};
-    c.src = hidden; c.ld = ldh; c.n = M; c.K = K; c.dst = wh; c.plane = p.plane_h;
+    c.src = hidden; c.pitch = ldh * es_of(dtype); c.n = M; c.chunks = K * es_of(dtype) / 16; c.dst = wh;
     c.targets = targets; c.weights = weights; c.V = V;
-    if (hipError_t e = launch_head_copy(p.mode, c, s)) return done(e);
+    if (hipError_t e = launch_head_copy(c, s)) return done(e);
   }
   for (int v0 = 0; v0 < V; v0 += p.piece) {
     const int n = std::min(p.piece, V - v0);
     const uint8_t* w = (const uint8_t*)head + v0 * ldw * es_of(dtype);
-    int64_t lw = ldw;
-    if (M && p.mode == HEAD_PARTS) {
-      HeadCopyArgs c{};
-      c.src = w; c.ld = ldw; c.n = n; c.K = K; c.dst = ww; c.plane = p.plane_w;
-      if (hipError_t e = launch_head_copy(p.mode, c, s)) return done(e);
-      w = ww;
-      lw = K;
-    }
     HeadArgs a{};
-    a.mode = p.mode;
-    a.V = V; a.v0 = v0;
+    a.V = V; a.v0 = v0; a.split = 1;
     if (M) {
       HeadArgs z = a;
-      z.A = w; z.lda = lw; z.plane_a = p.plane_w; z.n_i = n;
-      z.B = wh; z.ldb = K; z.plane_b = p.plane_h; z.n_j = M;
+      z.A = w; z.lda = ldw; z.n_i = n;
+      z.B = (const uint8_t*)hidden; z.ldb = ldh; z.n_j = M;
       z.C = z.chunk = K;
       z.targets = targets; z.weights = weights; z.lse = lse;
-      z.dz = wz; z.plane_dz = p.plane_dz; z.ldz = p.ldz; z.rest = (float*)wr;
-      if (hipError_t e = launch_head(HEAD_DZ, z, 1, p.tile_z, s)) return done(e);
+      z.dz = wz; z.ldz = p.ldz; z.rest = (float*)wr;
+      if (hipError_t e = launch_head(dtype, HEAD_DZ, z, p.tile_z, s)) return done(e);
     }
     if (M && d_hidden) {
       HeadArgs h = a;
-      h.A = w; h.lda = lw; h.plane_a = p.plane_w; h.n_i = K;
-      h.B = wz; h.ldb = p.ldz; h.plane_b = p.plane_dz; h.n_j = M;
-      h.C = n; h.chunk = p.chunk;
+      h.A = w; h.lda = ldw; h.n_i = K;
+      h.B = wz; h.ldb = p.ldz; h.n_j = M;
+      h.C = n; h.chunk = p.chunk; h.split = p.split;
       h.part = (float*)wp; h.add = v0 > 0;
-      if (hipError_t e = launch_head(HEAD_PART, h, p.split, p.tile_h, s)) return done(e);
+      if (hipError_t e = launch_head(dtype, HEAD_PART, h, p.tile_h, s)) return done(e);
     }
     if (d_head) {
       HeadArgs d = a;
-      d.A = wh; d.lda = K; d.plane_a = p.plane_h; d.n_i = K;
-      d.B = wz; d.ldb = p.ldz; d.plane_b = p.plane_dz; d.n_j = n;
+      d.A = wh; d.lda = K; d.n_i = K;
+      d.B = wz; d.ldb = p.ldz; d.n_j = n;
       d.C = d.chunk = M;
       d.out = (uint8_t*)d_head + v0 * ld_dw * es_of(dtype); d.ldo = ld_dw;
-      if (hipError_t e = launch_head(HEAD_OUT, d, 1, p.tile_w, s)) return done(e);
+      if (hipError_t e = launch_head(dtype, HEAD_OUT, d, p.tile_w, s)) return done(e);
     }
   }
   if (M && d_hidden) {
