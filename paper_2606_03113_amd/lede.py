@@ -162,13 +162,10 @@ def load(path: str = LIB_PATH):
     L.lede_dqn_read.argtypes = [vp, i32, fp, sz, P(i32), vp]
     i64, f32 = ctypes.c_int64, ctypes.c_float
     L.lede_op_cache_bytes.argtypes = [i32] * 3
-    i64 = ctypes.c_int64
     L.lede_op_head_loss_bytes.argtypes = L.lede_op_head_loss_grad_bytes.argtypes = [i32, i32, i32, i32]
-    L.lede_op_head_loss_bytes.restype = L.lede_op_head_loss_grad_bytes.restype = sz
     L.lede_op_head_loss.argtypes = [i32, vp, i64, i32, vp, i64, i32, i32, vp, vp, vp, vp, sz, vp]
     L.lede_op_head_loss_grad.argtypes = [i32, vp, i64, i32, vp, i64, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp, sz, vp]
     L.lede_op_quant_bytes.argtypes = [i32, i32, i32]
-    L.lede_op_quant_bytes.restype = sz
     L.lede_op_quantize.argtypes = [i32, vp, i64, i32, i32, i32, vp, vp, vp]
     L.lede_op_quant_pack.argtypes = [vp, vp, i32, i32, i32, vp, vp]
     L.lede_op_quant_linear.argtypes = [i32, vp, i32, i32, i32, vp, i64, i32, i32, vp, i64, vp]
@@ -185,12 +182,13 @@ def load(path: str = LIB_PATH):
                                           vp, i64, vp, sz, vp]
     L.lede_op_logprobs_bytes.argtypes = [i32] * 3
     L.lede_op_logprobs.argtypes = [i32, vp, i64, i32, i32, f32, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
-    for name in ("lede_op_cache_bytes", "lede_op_cache_attention_bytes", "lede_op_logprobs_bytes"):
+    sizes = ("lede_op_cache_bytes", "lede_op_cache_attention_bytes", "lede_op_logprobs_bytes", "lede_op_quant_bytes",
+             "lede_op_head_loss_bytes", "lede_op_head_loss_grad_bytes")
+    for name in sizes:
         getattr(L, name).restype = sz
     for name in EXPORTED:
-        if name not in ("lede_destroy", "lede_last_error", "lede_op_tiled_bytes", "lede_dqn_region_bytes",
-                        "lede_dqn_destroy", "lede_dqn_last_error", "lede_op_cache_bytes",
-                        "lede_op_cache_attention_bytes", "lede_op_logprobs_bytes"):
+        if name not in sizes + ("lede_destroy", "lede_last_error", "lede_op_tiled_bytes", "lede_dqn_region_bytes",
+                                "lede_dqn_destroy", "lede_dqn_last_error"):
             getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L

@@ -51,6 +51,13 @@ def test_bytes_stay_far_below_the_logits(lib, dtype):  # noqa: F811
     assert lib.lede_op_head_loss_bytes(dtype, 1, 1, 8) > 0 and lib.lede_op_head_loss_grad_bytes(dtype, 1, 1, 8) > 0
 
 
+def test_binding_sizes_past_32_bits():
+    L = lede.load()
+    assert L.lede_op_head_loss_bytes(0, 1 << 18, 1 << 20, 8) > 1 << 33
+    assert L.lede_op_head_loss_grad_bytes(0, 1 << 18, 32000, 4096) > 1 << 33
+    assert L.lede_op_quant_bytes(1 << 20, 1 << 14, 32) > 1 << 33
+
+
 def test_binding_refuses_wrong_tensors():
     h, w, t = torch.zeros(4, 64), torch.zeros(100, 64), torch.zeros(4, dtype=torch.int32)
     for call in (lambda: lede.op_head_loss(h, w, t),              # not on the GPU
