@@ -286,11 +286,13 @@ __global__ __launch_bounds__(PG_THREADS) void k_cache_own(CachePagesArgs a) {
         end = block_scan(mine, red, total);
       }
       int take = at.x + end.x - mine.x, move = at.y + end.y - mine.y;
+      // (no more than was counted, also where a page is held and listed as free)
+      const int last = at.x + end.x, last_move = at.y + end.y;
       if (mine.x)
         own_entries(a, s, o, [&](int i, int32_t* c) {
-          if (count_of(c) == INT_MIN + s) return;
+          if (take == last || count_of(c) == INT_MIN + s) return;
           const int fresh = a.free_pages[head + take++];
-          if (i * CACHE_PAGE < o.q.seq) {
+          if (i * CACHE_PAGE < o.q.seq && move < last_move) {
             a.pairs[2 * move] = (int)(c - a.shares);
             a.pairs[2 * move + 1] = fresh;
             ++move;

@@ -326,6 +326,24 @@ def test_entries_outside_the_pool_are_left_alone():
     d.check(pool)
 
 
+def test_own_of_pages_that_are_listed_as_free():
+    """A list that is wrong gives wrong pages, but no more of them than there are, and no pair behind the last."""
+    m = lede()
+    n = 128
+    tables = [[2 * (s // 2), 2 * (s // 2) + 1] for s in range(n)]          # two sequences share two pages
+    for order in (list(range(n)), list(range(n - 1, -1, -1))):
+        pool = Pool([70] * n, [2] * n, tables, order, n // 2, n)
+        d = Device(pool)
+        d.shares.fill_(1)
+        pairs = torch.full((2 * n + 64,), 12345, dtype=torch.int32, device="cuda")
+        out = m.CacheMoves(pairs[:n].view(n // 2, 2), torch.empty(4, dtype=torch.int32, device="cuda"))
+        m.op_cache_own(d.seq, i32([10] * n), d.held, d.free, d.head, d.tables, d.shares, n // 2, out=out)
+        assert out.status.tolist() == [0, n // 2, n, -1]
+        assert bool((pairs[n:] == 12345).all()) and bool((out.pairs < n).all())
+        for name, g in d.guards.items():
+            assert bool((g == 12345).all()), name
+
+
 @pytest.mark.parametrize("kv,hd,n_pages", [(1, 64, 5), (4, 64, 300), (8, 128, 40), (3, 128, 33), (40, 128, 9), (1024, 64, 3)])
 def test_copy(kv, hd, n_pages):
     m = lede()
