@@ -660,9 +660,10 @@ int lede_op_cache_copy(const int32_t* pairs, const int32_t* count, int32_t max_m
 /* Free: each sequence gives back the pages that its seq_lens[s] tokens do not
  * need, the entries from ceil(seq_lens[s] / 64) on of the held[s] (all with
  * seq_lens[s] = 0), and held[s] follows.  Pages without a holder left are put
- * before *free_head in free_pages, in ascending order (pools stay dense).  status [4]: 0 or an
- * error, the number of pages freed, the position in free_pages after the
- * call, the first sequence that failed or -1.  free_head may be status + 2.
+ * before *free_head in free_pages, in ascending order (pools stay dense).
+ * status [4]: 0 or an error, the number of pages freed, the position in
+ * free_pages after the call, the first sequence that failed or -1.  free_head
+ * may be status + 2.
  * LEDE_E_ARG: a negative length, held outside [0, table_ld], free_head outside
  * [0, n_free], fewer than that many entries before it.  Returns
  * LEDE_E_UNSUPPORTED above 2^18 pages. */
@@ -809,7 +810,9 @@ int lede_op_quant_linear(int32_t dtype, const void* packed, int32_t N, int32_t K
  *   loss[m]  lse[m] - z[m][targets[m]]  (fp32; may be null)
  * Products are exact and sums fp32 (fp32 inputs enter as three bf16 numbers
  * each, of whose nine products the six largest count: 2^-22 of the largest).
- * A row whose logits are all -infinity or include a NaN or +infinity has NaN.
+ * A row whose logits are all -infinity or include a NaN or +infinity has NaN;
+ * so has, of fp32 inputs, a row with an entry that is not finite, and every
+ * row where the head has one.
  * LEDE_E_ARG: null pointers, bad dtypes, M < 0, V or K < 1, row strides below
  * K; hidden, head, the gradients, workspace or row strides not multiples of 16
  * bytes; a workspace smaller than lede_op_head_loss_bytes (of the same sizes).

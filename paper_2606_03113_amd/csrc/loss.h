@@ -49,8 +49,8 @@ struct HeadJoinArgs {
 struct HeadOutArgs {
   const float* part;
   int split; int64_t n; int K;
-  const int32_t* targets; const float* rest; int V;   // (bf16)
-  const void* head; int64_t ldw;
+  const int32_t* targets; const float* weights; int V;
+  const float* rest; const void* head; int64_t ldw;   // (bf16)
   void* out; int64_t ldo;
 };
 hipError_t launch_head(int dtype, int epi, const HeadArgs& a, HeadTile tile, hipStream_t s);

@@ -323,7 +323,7 @@ __device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][
 
 // out[j][i] = sum_c A[i][c] B[j][c] of bf16 operands, TI x TJ of them a block, WI x
 // WJ waves.  A ring of S steps of the contraction in LDS: one is multiplied while
-// the next ones are on their way; one barrier a step.  2048 rows of 32000 x 4096
+// the next ones are on their way; one barrier a step.  2048 rows of 32000 x 4096:
 // 463 us a product, 1160 TFLOP/s (a library product of 8192^3 1450 here).
 template <bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
 __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
@@ -576,14 +576,14 @@ __global__ __launch_bounds__(256) void k_head_out(HeadOutArgs a, int lanes) {
   }
   for (int o = 1; o < lanes; o <<= 1) v = make_float4(v.x + __shfl_xor(v.x, o), v.y + __shfl_xor(v.y, o), v.z + __shfl_xor(v.z, o), v.w + __shfl_xor(v.w, o));
   if (!in || lane) return;
-  if (DT == 1) {
-    const int t = a.targets[r];
-    if (t >= 0 && t < a.V) {
-      const float rest = a.rest[r];
-      const uint2 w = *(const uint2*)((const uint16_t*)a.head + t * a.ldw + k);
-      if (rest != 0.f)
-        v = make_float4(fmaf(rest, bf16lo(w.x), v.x), fmaf(rest, bf16hi(w.x), v.y), fmaf(rest, bf16lo(w.y), v.z), fmaf(rest, bf16hi(w.y), v.w));
-    }
+  const int t = a.targets[r];
+  if (t < 0 || t >= a.V || (a.weights && a.weights[r] == 0.f)) {
+    v = make_float4(0.f, 0.f, 0.f, 0.f);   // (the sums are NaN where the head is not finite)
+  } else if (DT == 1) {
+    const float rest = a.rest[r];
+    const uint2 w = *(const uint2*)((const uint16_t*)a.head + t * a.ldw + k);
+    if (rest != 0.f)
+      v = make_float4(fmaf(rest, bf16lo(w.x), v.x), fmaf(rest, bf16hi(w.x), v.y), fmaf(rest, bf16lo(w.y), v.z), fmaf(rest, bf16hi(w.y), v.w));
   }
   store4<DT>((uint8_t*)a.out + r * a.ldo * Elem<DT>::ES_, k, v);
 }

@@ -32,6 +32,7 @@ int check_quant(int32_t N, int32_t K, int32_t group) {
 // ---- the vocabulary head's loss ----
 
 constexpr int32_t MOST_ROWS = 1 << 18, MOST_VOCAB = 1 << 20, MOST_WIDTH = 1 << 15;
+constexpr int32_t LAUNCH_ROWS = 1 << 17;   // with MOST_VOCAB, of whose tiles a launch has fewer than 2^32 threads
 int check_head(int32_t dtype, int32_t M, int32_t V, int32_t K) {
   if (!dtype_ok(dtype) || M < 0 || V < 1 || K < 1) return LEDE_E_ARG;
   return K % 8 || M > MOST_ROWS || V > MOST_VOCAB || K > MOST_WIDTH ? LEDE_E_UNSUPPORTED : LEDE_OK;
@@ -134,15 +135,20 @@ int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M,
   if (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total) return LEDE_E_ARG;
   hipStream_t s = S_(stream);
   HeadArgs a{};
-  a.sums = (float2*)workspace; a.ld_sums = p.tiles;
-  a.target_z = (float*)((uint8_t*)workspace + p.sums);
+  float2* const sums = (float2*)workspace;
+  float* const target_z = (float*)((uint8_t*)workspace + p.sums);
+  a.ld_sums = p.tiles;
   a.A = (const uint8_t*)head; a.lda = ldw; a.n_i = V;
-  a.B = (const uint8_t*)hidden; a.ldb = ldh; a.n_j = M;
+  a.ldb = ldh;
   a.C = a.chunk = K; a.split = 1;
-  a.targets = targets; a.V = V;
-  if (hipError_t e = launch_head(dtype, HEAD_SUMS, a, p.tile, s)) return done(e);
+  a.V = V;
+  for (int m0 = 0; m0 < M; m0 += LAUNCH_ROWS) {
+    a.B = (const uint8_t*)hidden + m0 * ldh * es_of(dtype); a.n_j = std::min(LAUNCH_ROWS, M - m0);
+    a.sums = sums + (int64_t)m0 * p.tiles; a.target_z = target_z + m0; a.targets = targets + m0;
+    if (hipError_t e = launch_head(dtype, HEAD_SUMS, a, p.tile, s)) return done(e);
+  }
   HeadJoinArgs j{};
-  j.sums = a.sums; j.target_z = a.target_z; j.n = M; j.tiles = p.tiles; j.V = V; j.targets = targets; j.loss = loss; j.lse = lse;
+  j.sums = sums; j.target_z = target_z; j.n = M; j.tiles = p.tiles; j.V = V; j.targets = targets; j.loss = loss; j.lse = lse;
   return done(launch_head_join(j, s));
 }
 
@@ -199,7 +205,7 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
   if (M && d_hidden) {
     HeadOutArgs o{};
     o.part = (const float*)wp; o.split = p.split; o.n = M; o.K = K; o.out = d_hidden; o.ldo = ld_dh;
-    o.targets = targets; o.rest = (const float*)wr; o.V = V; o.head = head; o.ldw = ldw;
+    o.targets = targets; o.weights = weights; o.rest = (const float*)wr; o.V = V; o.head = head; o.ldw = ldw;
     return done(launch_head_out(dtype, o, s));
   }
   return LEDE_OK;

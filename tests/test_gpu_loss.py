@@ -95,6 +95,35 @@ def test_rows_left_out_may_hold_anything(M, dtype):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and not bool(got[0][out].any())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_left_out_have_no_gradient_whatever_the_head_holds(dtype):
+    say("head loss, rows left out under a head with a NaN, %s" % dtype)
+    m = lede()
+    hidden, head, targets, weights = inputs(70, 600, 64, DT[dtype], 21)
+    targets[3], targets[69] = -100, 600
+    weights[5] = 0.0
+    lse = m.op_head_loss(hidden, head, targets).lse
+    head[300, 7] = float("nan")
+    dh, _ = m.op_head_loss_grad(hidden, head, targets, lse, weights)
+    out = torch.zeros(70, dtype=torch.bool, device="cuda")
+    out[[3, 5, 69]] = True
+    out |= (targets < 0) | (targets >= 600) | (weights == 0)
+    assert bool((dh[out] == 0).all()) and bool(torch.isnan(dh[~out]).any(1).all())
+
+
+@pytest.mark.parametrize("M,V,dtype", [(131075, 300, "f32"), (131075, 300, "bf16"), (1 << 18, 1 << 20, "f32")])
+def test_rows_past_a_launch(M, V, dtype):
+    say("head loss of many rows M=%d V=%d %s" % (M, V, dtype))
+    hidden, head, targets, _ = inputs(M, V, 8, DT[dtype], 22)
+    r = lede().op_head_loss(hidden, head, targets)
+    rows = torch.tensor([0, 1, 131071, 131072, 131074, M // 2 + 1, M - 1], device="cuda")
+    ref = Reference(hidden[rows], head, targets[rows], None)
+    close(r.lse[rows], ref.lse, ref.lse_tol, "lse")
+    close(r.loss[rows], ref.loss, ref.loss_tol, "loss")
+    del r
+    torch.cuda.empty_cache()
+
+
 def test_everything_left_out_and_no_rows():
     m = lede()
     for dtype in DT.values():
