@@ -17,14 +17,14 @@ enum HeadEpi : int {
 
 // A block's tile of a product: bf16 256 x 64, 128 or 256, or 128 x 64; fp32 64 or
 // 128 x 64 or 128.
-struct HeadTile { int i, j; };
+struct HeadTile { int i, j; bool thin = false; };   // thin: few fp32 rows over a large head
 
 struct HeadArgs {
   const uint8_t *A, *B;
   int64_t lda, ldb;                // elements
   int n_i, n_j, C;                 // rows of A and B, length of the contraction
   int chunk;                       // entries of the contraction that a block takes
-  int i_tiles, j_tiles, split;     // of the grid
+  int i_tiles, j_tiles, split, band;   // of the grid
   const int32_t* targets; const float *weights, *lse;
   int V, v0;                       // the vocabulary, the piece's first entry
   float2* sums; int ld_sums;   // HEAD_SUMS: [row][tile of the vocabulary]

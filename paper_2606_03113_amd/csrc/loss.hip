@@ -186,9 +186,9 @@ __device__ __forceinline__ bool head_place(const HeadArgs& a, HeadPlace& p) {
   const int at = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
   if (at >= per_part * a.split) return false;
   p.part = at / per_part;
-  const int rest = at - p.part * per_part, band = rest / (4 * a.j_tiles);
-  const int in_band = rest - band * 4 * a.j_tiles, rows = min(4, a.i_tiles - 4 * band);
-  p.it = 4 * band + in_band % rows;
+  const int rest = at - p.part * per_part, band = rest / (a.band * a.j_tiles);
+  const int in_band = rest - band * a.band * a.j_tiles, rows = min(a.band, a.i_tiles - a.band * band);
+  p.it = a.band * band + in_band % rows;
   p.jt = in_band / rows;
   return true;
 }
@@ -393,19 +393,47 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
 // not finite becomes NaN in the second part.
 __device__ float4 head_zeros[2];   // what is read in place of entries past the contraction's end
 constexpr int PRODUCTS = 6;
+__device__ __forceinline__ void split8(const float (&v)[8], u32x4 (&w)[3]) {
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    uint32_t b[3][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      b[0][h] = __float_as_uint(v[e + h]);
+      const float rest = v[e + h] - __uint_as_float(b[0][h] & 0xFFFF0000u);
+      b[1][h] = __float_as_uint(rest);
+      b[2][h] = __float_as_uint(rest - __uint_as_float(b[1][h] & 0xFFFF0000u));
+    }
+#pragma unroll
+    for (int p = 0; p < 3; ++p) w[p][e / 2] = __builtin_amdgcn_perm(b[p][1], b[p][0], 0x07060302);
+  }
+}
+// acc += the products of the parts of NI and NJ operands.
+template <int NI, int NJ>
+__device__ __forceinline__ void split_products(const bf16x8 (&fa)[3][NI], const bf16x8 (&fb)[3][NJ], f32x4 (&acc)[NI][NJ]) {
+#pragma unroll
+  for (int p = 0; p < PRODUCTS; ++p) {
+    constexpr int PA[PRODUCTS] = {2, 0, 1, 1, 0, 0}, PB[PRODUCTS] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+    for (int x = 0; x < NI; ++x)
+#pragma unroll
+      for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[PA[p]][x], fb[PB[p]][y], acc[x][y], 0, 0, 0);
+  }
+}
 template <bool COLUMNS, int T, int KS, int AHEAD> struct Split {
-  static constexpr int PLANE = T * KS * 2, CHUNKS = T * KS / 8, PER = CHUNKS / 256;   // chunks of eight entries; of a thread
+  static constexpr int PLANE = T * KS * 2, CHUNKS = T * KS / 8, PER = (CHUNKS + 255) / 256;   // chunks of eight entries; of a thread
   const float* src[PER];
   int64_t step;
   float4 x[AHEAD][PER][2];
+  static __device__ __forceinline__ int chunk(int i) { return (threadIdx.x + 256 * i) % CHUNKS; }
   static __device__ __forceinline__ int entry(int i) {   // of the contraction, in a step: a chunk's first
-    const int q = threadIdx.x + 256 * i;
+    const int q = chunk(i);
     return COLUMNS ? q / (T / 8) : q % (KS / 8) * 8;
   }
   __device__ __forceinline__ void begin(const float* p, int64_t ld, int r0, int n, int c0) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int q = threadIdx.x + 256 * i;
+      const int q = chunk(i);
       src[i] = COLUMNS ? p + (int64_t)(c0 + entry(i)) * ld + min(r0 + q % (T / 8) * 8, ((n + 7) & ~7) - 8)
                        : p + (int64_t)min(r0 + q / (KS / 8), n - 1) * ld + c0 + entry(i);
     }
@@ -424,7 +452,8 @@ template <bool COLUMNS, int T, int KS, int AHEAD> struct Split {
   __device__ __forceinline__ void store(int u, lds8* planes) const {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int q = threadIdx.x + 256 * i;
+      const int q = chunk(i);
+      if (CHUNKS < 256 && threadIdx.x >= CHUNKS) return;
       int at;
       if (COLUMNS) {
         const int k = q / (T / 8), c = q % (T / 8);
@@ -434,23 +463,11 @@ template <bool COLUMNS, int T, int KS, int AHEAD> struct Split {
         at = r * (2 * KS) + ((c ^ (KS == 64 ? r & 7 : r >> 2 & 3)) << 4);
       }
       const float v[8] = {x[u][i][0].x, x[u][i][0].y, x[u][i][0].z, x[u][i][0].w, x[u][i][1].x, x[u][i][1].y, x[u][i][1].z, x[u][i][1].w};
-      uint32_t w[3][4];
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        uint32_t b[3][2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          b[0][h] = __float_as_uint(v[e + h]);
-          const float rest = v[e + h] - __uint_as_float(b[0][h] & 0xFFFF0000u);
-          b[1][h] = __float_as_uint(rest);
-          b[2][h] = __float_as_uint(rest - __uint_as_float(b[1][h] & 0xFFFF0000u));
-        }
-#pragma unroll
-        for (int p = 0; p < 3; ++p) w[p][e / 2] = __builtin_amdgcn_perm(b[p][1], b[p][0], 0x07060302);
-      }
+      u32x4 w[3];
+      split8(v, w);
 #pragma unroll
       for (int p = 0; p < 3; ++p)
-        *(__attribute__((address_space(3))) u32x4*)(planes + p * PLANE + at) = u32x4{w[p][0], w[p][1], w[p][2], w[p][3]};
+        *(__attribute__((address_space(3))) u32x4*)(planes + p * PLANE + at) = w[p];
     }
   }
   static __device__ __forceinline__ bf16x8 read(const lds8* plane, int r0, int h) {
@@ -510,18 +527,118 @@ __global__ __launch_bounds__(256) void k_head_fp32(HeadArgs a) {
 #pragma unroll
           for (int y = 0; y < NJ; ++y) fb[p][y] = SB::read(lb + p * SB::PLANE, (wj * NJ + y) * 16, h);
         }
-#pragma unroll
-        for (int p = 0; p < PRODUCTS; ++p) {
-          constexpr int PA[PRODUCTS] = {2, 0, 1, 1, 0, 0}, PB[PRODUCTS] = {0, 2, 1, 0, 1, 0};
-#pragma unroll
-          for (int x = 0; x < NI; ++x)
-#pragma unroll
-            for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[PA[p]][x], fb[PB[p]][y], acc[x][y], 0, 0, 0);
-        }
+        split_products<NI, NJ>(fa, fb, acc);
       }
     }
   }
   head_finish<0, EPI, TI, TJ, WI, WJ>(a, acc, smem, place, wi, wj);
+}
+
+// Few fp32 rows over a large head, which is read once and bounds it: no two waves
+// share entries of it, so they go straight into registers, two steps ahead; the
+// rows' parts are in LDS, one step's written while the other's are read.
+// Columns: a lane has four neighbouring ones of eight entries of the contraction,
+// one for each of the four tiles, whose row r is column 4 r + x.  THIN_FIG
+template <bool CA, int TJ, int EPI>
+__global__ __launch_bounds__(256, 2) void k_head_thin(HeadArgs a) {
+  constexpr int KS = CA ? 32 : 64, NI = CA ? 4 : 2, NJ = TJ / 16, TI = 64 * NI, H = KS / 32, N4 = H * 8;   // 16-byte loads of a step
+  typedef Split<false, TJ, KS, 2> SB;
+  extern __shared__ __align__(16) uint8_t smem[];   // 6 SB::PLANE
+  lds8* lb = (lds8*)smem;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+  HeadPlace place;
+  if (!head_place(a, place)) return;
+  const int i0 = place.it * TI, j0 = place.jt * TJ;
+  const int c_begin = place.part * a.chunk, c_end = min(c_begin + a.chunk, a.C);
+  f32x4 acc[NI][NJ];
+#pragma unroll
+  for (int x = 0; x < NI; ++x)
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (c_begin < c_end) {
+    SB sb;
+    sb.begin((const float*)a.B, a.ldb, j0, a.n_j, c_begin);
+    const float *src[CA ? 1 : NI], *A = (const float*)a.A;
+    if (CA) {
+      src[0] = A + (int64_t)(c_begin + 8 * lg) * a.lda + min(i0 + wave * 64 + 4 * lr, a.n_i - 4);
+    } else {
+#pragma unroll
+      for (int x = 0; x < NI; ++x) src[x] = A + (int64_t)min(i0 + (wave * NI + x) * 16 + lr, a.n_i - 1) * a.lda + c_begin + 8 * lg;
+    }
+    float4 v[2][N4];
+    auto load = [&](int u, int left) {
+#pragma unroll
+      for (int n = 0; n < N4; ++n) {
+        const int h = CA ? 0 : n / (2 * NI), x = CA ? 0 : n / 2 % NI;   // columns: entry n of the lane's eight
+        const float* p = CA ? src[0] + (int64_t)n * a.lda : src[x] + 32 * h + 4 * (n & 1);
+        v[u][n] = *(const float4*)((CA ? 8 * lg + n : 32 * h + 8 * lg) < left ? p : (const float*)head_zeros);
+      }
+      if (CA) src[0] += KS * a.lda;
+      else
+#pragma unroll
+        for (int x = 0; x < NI; ++x) src[x] += KS;
+    };
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      sb.load(u, c_end - c_begin - u * KS);
+      load(u, c_end - c_begin - u * KS);
+    }
+    for (int c0 = c_begin; c0 < c_end; c0 += 2 * KS) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int left = c_end - c0 - u * KS;   // (behind the last step: zeros)
+        lds8* planes = lb + u * 3 * SB::PLANE;
+        sb.store(u, planes);
+        sb.load(u, left - 2 * KS);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        u32x4 w[H][NI][3];
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int x = 0; x < NI; ++x) {
+            float e[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float4 q = CA ? v[u][k] : v[u][(h * NI + x) * 2 + k / 4];
+              const int at = CA ? x : k % 4;
+              e[k] = at == 0 ? q.x : at == 1 ? q.y : at == 2 ? q.z : q.w;
+            }
+            split8(e, w[h][x]);
+          }
+        load(u, left - 2 * KS);
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          bf16x8 fa[3][NI], fb[3][NJ];
+#pragma unroll
+          for (int p = 0; p < 3; ++p) {
+#pragma unroll
+            for (int x = 0; x < NI; ++x) fa[p][x] = __builtin_bit_cast(bf16x8, w[h][x][p]);
+#pragma unroll
+            for (int y = 0; y < NJ; ++y) fb[p][y] = SB::read(planes + p * SB::PLANE, y * 16, h);
+          }
+          split_products<NI, NJ>(fa, fb, acc);
+        }
+      }
+    }
+  }
+  if (EPI != HEAD_PART) {
+    head_finish<0, EPI, TI, TJ, 4, 1>(a, acc, smem, place, wave, 0);
+    return;
+  }
+#pragma unroll
+  for (int y = 0; y < NJ; ++y)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = j0 + 16 * y + lr, i = i0 + wave * 64 + 4 * (4 * lg + e);
+      if (j >= a.n_j || i >= a.n_i) continue;
+      float4* to = (float4*)(a.part + ((int64_t)place.part * a.n_j + j) * a.n_i + i);
+      float4 s = make_float4(acc[0][y][e], acc[1][y][e], acc[CA ? 2 : 0][y][e], acc[CA ? 3 : 0][y][e]);
+      if (a.add) {
+        const float4 o = *to;
+        s = make_float4(o.x + s.x, o.y + s.y, o.z + s.z, o.w + s.w);
+      }
+      *to = s;
+    }
 }
 
 // ---- rows before and after ----------------------------------------------------------
@@ -597,6 +714,7 @@ static hipError_t launch_blocks(const void* f, HeadArgs& a, int ti, int tj, int 
   }
   a.i_tiles = (a.n_i + ti - 1) / ti;
   a.j_tiles = (a.n_j + tj - 1) / tj;
+  a.band = a.C <= 512 && a.split == 1 ? a.i_tiles : 4;
   const dim3 grid((unsigned)(((int64_t)a.i_tiles * a.j_tiles * a.split + 7) / 8 * 8));
   void* args[] = {(void*)&a};
   return hipLaunchKernel(f, grid, dim3(threads), args, lds, s);
@@ -611,6 +729,10 @@ template <bool CA, bool CB, int TI, int TJ, int WI, int WJ, int KS, int AHEAD, i
 static hipError_t launch_fp32(HeadArgs a, hipStream_t s) {
   return launch_blocks((const void*)k_head_fp32<CA, CB, TI, TJ, WI, WJ, KS, AHEAD, EPI>, a, TI, TJ, 256, 3 * (TI + TJ) * KS * 2, s);
 }
+template <bool CA, int TJ, int EPI>
+static hipError_t launch_thin(HeadArgs a, hipStream_t s) {
+  return launch_blocks((const void*)k_head_thin<CA, TJ, EPI>, a, CA ? 256 : 128, TJ, 256, 6 * TJ * (CA ? 32 : 64) * 2, s);
+}
 template <bool CA, bool CB, int EPI>
 static hipError_t launch_tile(int dtype, const HeadArgs& a, HeadTile tile, hipStream_t s) {
   if (dtype) {
@@ -618,6 +740,11 @@ static hipError_t launch_tile(int dtype, const HeadArgs& a, HeadTile tile, hipSt
     if (tile.j == 64) return launch_bf16<CA, CB, 256, 64, 8, 1, 3, EPI>(a, s);
     if (tile.j == 128) return launch_bf16<CA, CB, 256, 128, 4, 2, 3, EPI>(a, s);
     return launch_bf16<CA, CB, 256, 256, 2, 4, 2, EPI>(a, s);
+  }
+  if constexpr (EPI != HEAD_OUT) {
+    if (tile.thin && tile.j == 16) return launch_thin<CA, 16, EPI>(a, s);
+    if (tile.thin && tile.j == 32) return launch_thin<CA, 32, EPI>(a, s);
+    if (tile.thin) return launch_thin<CA, 64, EPI>(a, s);
   }
   if (tile.i == 64 && tile.j == 64) return launch_fp32<CA, CB, 64, 64, 2, 2, 64, 1, EPI>(a, s);
   if (tile.i == 64) return launch_fp32<CA, CB, 64, 128, 2, 2, 32, 2, EPI>(a, s);

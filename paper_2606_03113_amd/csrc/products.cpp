@@ -49,9 +49,11 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 // less often; where they would be few, small ones of which more are on the card
 // and more steps on their way (fp32, 32 rows of 1024 x 256 with the gradient: 43
 // us, 58 with tiles of 128; bf16, 2 rows of 32000 82, 161 with tiles of 256).
-HeadTile head_tile(int32_t dtype, int64_t n_i, int64_t n_j) {
+HeadTile thin_tile(int i, int64_t n_j) { return {i, n_j <= 16 ? 16 : n_j <= 32 ? 32 : 64, true}; }
+HeadTile head_tile(int32_t dtype, int64_t n_i, int64_t n_j, bool head_rows) {
   const auto blocks = [&](int i, int j) { return (n_i + i - 1) / i * ((n_j + j - 1) / j); };
   if (dtype == LEDE_DTYPE_F32) {
+    if (head_rows && n_j <= 64 && n_i >= 128 * 128) return thin_tile(128, n_j);
     const int j = n_j <= 64 ? 64 : 128;
     return {blocks(128, j) < 128 ? 64 : 128, j};
   }
@@ -77,7 +79,7 @@ struct LossPlan {
   HeadTile tile;
   size_t sums, target, total;
   LossPlan(int32_t dtype, int32_t M, int32_t V) {
-    tile = head_tile(dtype, V, M);
+    tile = head_tile(dtype, V, M, true);
     tiles = (V + tile.i - 1) / tile.i;
     sums = up256((size_t)M * tiles * 8);
     target = up256((size_t)M * 4);
@@ -93,15 +95,18 @@ struct GradPlan {
     piece = piece_size(dtype, M, V);
     const int n = std::min(piece, V);
     ldz = (n + 7) & ~7;
-    tile_z = head_tile(dtype, n, M);
-    tile_w = head_tile(dtype, K, n);
+    tile_z = head_tile(dtype, n, M, true);
+    tile_w = head_tile(dtype, K, n, false);
     // dh has few tiles: its contraction over the vocabulary is split so that
     // about a block is there for each CU (fp32, of whose blocks a CU holds
     // several: four)
     tile_h = {f32 ? 128 : 256, M <= 64 ? 64 : f32 || M <= 128 ? 128 : 256};
     const int64_t blocks = (int64_t)((K + tile_h.i - 1) / tile_h.i) * std::max(1, (M + tile_h.j - 1) / tile_h.j);
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((f32 ? 1024 : 256) / blocks, ldz / 256));
-    if (f32 && blocks * want < 128) tile_h.i = 64;
+    const int64_t thin_blocks = (K + 255) / 256, thin_want = std::min<int64_t>(768 / thin_blocks, ldz / 256);
+    const bool thin = f32 && M <= 64 && thin_blocks * thin_want >= 128;
+    if (thin) tile_h = thin_tile(256, M);
+    const int64_t want = thin ? thin_want : std::max<int64_t>(1, std::min<int64_t>((f32 ? 1024 : 256) / blocks, ldz / 256));
+    if (f32 && !thin && blocks * want < 128) tile_h.i = 64;
     if (!f32 && blocks * want < 64) tile_h = {128, 64};
     chunk = (int)((ldz + want - 1) / want + 63) & ~63;
     split = (ldz + chunk - 1) / chunk;
