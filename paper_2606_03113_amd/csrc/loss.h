@@ -15,8 +15,8 @@ enum HeadEpi : int {
   HEAD_OUT = 3,    // i = k, j = v: dW
 };
 
-// A block's tile of a product: bf16 256 x 64, 128 or 256, or 128 x 64; fp32 64 or
-// 128 x 64 or 128.
+// A block's tile of a product: bf16 256 x 64, 128 or 256, or 128 x 64; fp32 64 x
+// 64, 64 x 128 or 128 x 128, or thin: 128 x 16, 32 or 64, of columns 256 x those.
 struct HeadTile { int i, j; bool thin = false; };   // thin: few fp32 rows over a large head
 
 struct HeadArgs {
@@ -24,7 +24,8 @@ struct HeadArgs {
   int64_t lda, ldb;                // elements
   int n_i, n_j, C;                 // rows of A and B, length of the contraction
   int chunk;                       // entries of the contraction that a block takes
-  int i_tiles, j_tiles, split, band;   // of the grid
+  int i_tiles, j_tiles, split;     // of the grid
+  int band;                        // tiles of i that are taken with all of j
   const int32_t* targets; const float *weights, *lse;
   int V, v0;                       // the vocabulary, the piece's first entry
   float2* sums; int ld_sums;   // HEAD_SUMS: [row][tile of the vocabulary]

@@ -179,7 +179,9 @@ __device__ __forceinline__ void head_step(const lds8* __restrict__ cur, const ld
 // A block's place: blocks b, b + 8, .. run on one XCD, which takes an eighth of
 // the tiles: one part of the contraction after the other, bands of four tiles
 // of i with all tiles of j, so that what runs at a time is about square and
-// shares its operands in the XCD's L2.
+// shares its operands in the XCD's L2.  Of short contractions, bound by what
+// they write, whole rows of the result instead (dW of 35 rows over 128256 x 5120
+// 321 us, 357 in bands).
 struct HeadPlace { int part, it, jt; };
 __device__ __forceinline__ bool head_place(const HeadArgs& a, HeadPlace& p) {
   const int per_part = a.i_tiles * a.j_tiles, per_xcd = (per_part * a.split + 7) / 8;
@@ -251,7 +253,6 @@ __device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][
       const int t = a.targets[jc];
       const float g = a.weights ? a.weights[jc] : 1.f, lse = a.lse[jc];
       const bool out = t < 0 || t >= a.V || g == 0.f;
-      uint8_t* row = a.dz + (int64_t)j * a.ldz * 2;
       auto dz = [&](int x, float (&d)[4]) {
         const int i = i0 + (wi * NI + x) * 16 + 4 * lg, at = t - a.v0 - i;
 #pragma unroll
@@ -263,22 +264,24 @@ __device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][
           if (DT && e == at && j < a.n_j) a.rest[j] = d[e] - Elem<1>::round(d[e]);
         }
       };
+      if constexpr (DT == 0) {
 #pragma unroll
-      for (int x = 0; x < NI; x += 2) {
-        float d[2][4];
-        dz(x, d[0]);
-        dz(x + 1, d[1]);
-        if (DT) {
+        for (int x = 0; x < NI; ++x) {
+          float d[4];
+          dz(x, d);
+          const int i = i0 + (wi * NI + x) * 16 + 4 * lg;
+          if (j < a.n_j && i < a.ldz) *(float4*)((float*)a.dz + (int64_t)j * a.ldz + i) = make_float4(d[0], d[1], d[2], d[3]);
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < NI; x += 2) {
+          float d[2][4];
+          dz(x, d[0]);
+          dz(x + 1, d[1]);
           int i;
           const uint4 u = eight(d[0], d[1], i);
           i += i0 + (wi * NI + x) * 16;
-          if (j < a.n_j && i < a.ldz) *(uint4*)(row + i * 2) = u;
-        } else {
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int i = i0 + (wi * NI + x + b) * 16 + 4 * lg;
-            if (j < a.n_j && i < a.ldz) *(float4*)((float*)a.dz + (int64_t)j * a.ldz + i) = make_float4(d[b][0], d[b][1], d[b][2], d[b][3]);
-          }
+          if (j < a.n_j && i < a.ldz) *(uint4*)(a.dz + ((int64_t)j * a.ldz + i) * 2) = u;
         }
       }
     }
@@ -538,10 +541,11 @@ __global__ __launch_bounds__(256) void k_head_fp32(HeadArgs a) {
 // share entries of it, so they go straight into registers, two steps ahead; the
 // rows' parts are in LDS, one step's written while the other's are read.
 // Columns: a lane has four neighbouring ones of eight entries of the contraction,
-// one for each of the four tiles, whose row r is column 4 r + x.  THIN_FIG
-template <bool CA, int TJ, int EPI>
+// one for each of the four tiles, whose row r is column 4 r + x.  21 rows of 118860
+// x 5120 545 us a pass (4.5 TB/s; 656 in k_head_fp32), dh's 426 (559).
+template <bool CA, int NI, int TJ, int EPI>
 __global__ __launch_bounds__(256, 2) void k_head_thin(HeadArgs a) {
-  constexpr int KS = CA ? 32 : 64, NI = CA ? 4 : 2, NJ = TJ / 16, TI = 64 * NI, H = KS / 32, N4 = H * 8;   // 16-byte loads of a step
+  constexpr int KS = CA ? 32 : 64, NJ = TJ / 16, TI = 64 * NI, H = KS / 32, N4 = H * 8;   // 16-byte loads of a step
   typedef Split<false, TJ, KS, 2> SB;
   extern __shared__ __align__(16) uint8_t smem[];   // 6 SB::PLANE
   lds8* lb = (lds8*)smem;
@@ -632,7 +636,7 @@ __global__ __launch_bounds__(256, 2) void k_head_thin(HeadArgs a) {
       const int j = j0 + 16 * y + lr, i = i0 + wave * 64 + 4 * (4 * lg + e);
       if (j >= a.n_j || i >= a.n_i) continue;
       float4* to = (float4*)(a.part + ((int64_t)place.part * a.n_j + j) * a.n_i + i);
-      float4 s = make_float4(acc[0][y][e], acc[1][y][e], acc[CA ? 2 : 0][y][e], acc[CA ? 3 : 0][y][e]);
+      float4 s = make_float4(acc[0][y][e], acc[CA ? 1 : 0][y][e], acc[CA ? 2 : 0][y][e], acc[CA ? 3 : 0][y][e]);
       if (a.add) {
         const float4 o = *to;
         s = make_float4(o.x + s.x, o.y + s.y, o.z + s.z, o.w + s.w);
@@ -729,9 +733,9 @@ template <bool CA, bool CB, int TI, int TJ, int WI, int WJ, int KS, int AHEAD, i
 static hipError_t launch_fp32(HeadArgs a, hipStream_t s) {
   return launch_blocks((const void*)k_head_fp32<CA, CB, TI, TJ, WI, WJ, KS, AHEAD, EPI>, a, TI, TJ, 256, 3 * (TI + TJ) * KS * 2, s);
 }
-template <bool CA, int TJ, int EPI>
+template <bool CA, int NI, int TJ, int EPI>
 static hipError_t launch_thin(HeadArgs a, hipStream_t s) {
-  return launch_blocks((const void*)k_head_thin<CA, TJ, EPI>, a, CA ? 256 : 128, TJ, 256, 6 * TJ * (CA ? 32 : 64) * 2, s);
+  return launch_blocks((const void*)k_head_thin<CA, NI, TJ, EPI>, a, 64 * NI, TJ, 256, 6 * TJ * (CA ? 32 : 64) * 2, s);
 }
 template <bool CA, bool CB, int EPI>
 static hipError_t launch_tile(int dtype, const HeadArgs& a, HeadTile tile, hipStream_t s) {
@@ -742,13 +746,20 @@ static hipError_t launch_tile(int dtype, const HeadArgs& a, HeadTile tile, hipSt
     return launch_bf16<CA, CB, 256, 256, 2, 4, 2, EPI>(a, s);
   }
   if constexpr (EPI != HEAD_OUT) {
-    if (tile.thin && tile.j == 16) return launch_thin<CA, 16, EPI>(a, s);
-    if (tile.thin && tile.j == 32) return launch_thin<CA, 32, EPI>(a, s);
-    if (tile.thin) return launch_thin<CA, 64, EPI>(a, s);
+    if (tile.thin) {
+      constexpr int NI = CA ? 4 : 2;
+      if constexpr (!CA) {
+        if (tile.i == 64 && tile.j == 16) return launch_thin<CA, 1, 16, EPI>(a, s);
+        if (tile.i == 64 && tile.j == 32) return launch_thin<CA, 1, 32, EPI>(a, s);
+        if (tile.i == 64) return launch_thin<CA, 1, 64, EPI>(a, s);
+      }
+      if (tile.j == 16) return launch_thin<CA, NI, 16, EPI>(a, s);
+      if (tile.j == 32) return launch_thin<CA, NI, 32, EPI>(a, s);
+      return launch_thin<CA, NI, 64, EPI>(a, s);
+    }
   }
   if (tile.i == 64 && tile.j == 64) return launch_fp32<CA, CB, 64, 64, 2, 2, 64, 1, EPI>(a, s);
   if (tile.i == 64) return launch_fp32<CA, CB, 64, 128, 2, 2, 32, 2, EPI>(a, s);
-  if (tile.j == 64) return launch_fp32<CA, CB, 128, 64, 4, 1, 64, 1, EPI>(a, s);
   return launch_fp32<CA, CB, 128, 128, 2, 2, 32, 2, EPI>(a, s);
 }
 hipError_t launch_head(int dtype, int epi, const HeadArgs& a, HeadTile tile, hipStream_t s) {

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <utility>
 
 #include "../../include/lede.h"
 #include "loss.h"
@@ -49,13 +50,16 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 // less often; where they would be few, small ones of which more are on the card
 // and more steps on their way (fp32, 32 rows of 1024 x 256 with the gradient: 43
 // us, 58 with tiles of 128; bf16, 2 rows of 32000 82, 161 with tiles of 256).
+// Few fp32 rows with the head's: thin ones, where the card is full of them; of
+// 64 head rows where there are few of 128 (47 rows of 32000 x 5120 222 us and 233,
+// 21 of 118860 x 5120 566 and 542).
 HeadTile thin_tile(int i, int64_t n_j) { return {i, n_j <= 16 ? 16 : n_j <= 32 ? 32 : 64, true}; }
 HeadTile head_tile(int32_t dtype, int64_t n_i, int64_t n_j, bool head_rows) {
   const auto blocks = [&](int i, int j) { return (n_i + i - 1) / i * ((n_j + j - 1) / j); };
   if (dtype == LEDE_DTYPE_F32) {
-    if (head_rows && n_j <= 64 && n_i >= 128 * 128) return thin_tile(128, n_j);
+    if (head_rows && n_j <= 64 && blocks(64, 64) >= 128) return thin_tile(blocks(128, 64) < 512 ? 64 : 128, n_j);
     const int j = n_j <= 64 ? 64 : 128;
-    return {blocks(128, j) < 128 ? 64 : 128, j};
+    return {j == 64 || blocks(128, j) < 128 ? 64 : 128, j};
   }
   const int j = n_j <= 64 ? 64 : n_j <= 128 ? 128 : 256;
   return blocks(256, j) < 64 ? HeadTile{128, 64} : HeadTile{256, j};
@@ -99,15 +103,21 @@ struct GradPlan {
     tile_w = head_tile(dtype, K, n, false);
     // dh has few tiles: its contraction over the vocabulary is split so that
     // about a block is there for each CU (fp32, of whose blocks a CU holds
-    // several: four)
-    tile_h = {f32 ? 128 : 256, M <= 64 ? 64 : f32 || M <= 128 ? 128 : 256};
-    const int64_t blocks = (int64_t)((K + tile_h.i - 1) / tile_h.i) * std::max(1, (M + tile_h.j - 1) / tile_h.j);
-    const int64_t thin_blocks = (K + 255) / 256, thin_want = std::min<int64_t>(768 / thin_blocks, ldz / 256);
-    const bool thin = f32 && M <= 64 && thin_blocks * thin_want >= 128;
-    if (thin) tile_h = thin_tile(256, M);
-    const int64_t want = thin ? thin_want : std::max<int64_t>(1, std::min<int64_t>((f32 ? 1024 : 256) / blocks, ldz / 256));
-    if (f32 && !thin && blocks * want < 128) tile_h.i = 64;
-    if (!f32 && blocks * want < 64) tile_h = {128, 64};
+    // several: three or four)
+    const auto parts = [&](HeadTile t, int64_t most) {
+      const int64_t blocks = (int64_t)((K + t.i - 1) / t.i) * std::max(1, (M + t.j - 1) / t.j);
+      const int64_t want = std::max<int64_t>(1, std::min<int64_t>(most / blocks, ldz / 256));
+      return std::pair<int64_t, int64_t>{want, blocks * want};
+    };
+    tile_h = f32 ? thin_tile(256, M) : HeadTile{256, M <= 64 ? 64 : M <= 128 ? 128 : 256};
+    auto p = parts(tile_h, f32 ? 768 : 256);
+    if (f32 && (M > 64 || p.second < 128)) {
+      tile_h = {M <= 64 ? 64 : 128, M <= 64 ? 64 : 128};
+      p = parts(tile_h, 1024);
+      if (p.second < 128) tile_h.i = 64;
+    }
+    if (!f32 && p.second < 64) tile_h = {128, 64};
+    const int64_t want = p.first;
     chunk = (int)((ldz + want - 1) / want + 63) & ~63;
     split = (ldz + chunk - 1) / chunk;
     h = up256((size_t)M * K * es_of(dtype));
