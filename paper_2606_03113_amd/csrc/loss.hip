@@ -94,6 +94,8 @@ template <bool COLUMNS, int T, int NW> struct Operand {
   }
 };
 
+// This wave's LDS accesses, then all: loads on their way to registers are not waited for.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_barrier() {   // this wave's copies but the last N, and its LDS reads; then all
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
@@ -513,12 +515,12 @@ __global__ __launch_bounds__(256) void k_head_fp32(HeadArgs a) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const int left = c_end - c0 - u * KS;   // (behind the last step: zeros)
-      __syncthreads();
+      lds_barrier();
       sa.store(u, la);
       sb.store(u, lb);
       sa.load(u, left - AHEAD * KS);
       sb.load(u, left - AHEAD * KS);
-      __syncthreads();
+      lds_barrier();
       if (left <= 0) continue;
 #pragma unroll
       for (int h = 0; h < KS / 32; ++h) {
@@ -594,7 +596,7 @@ __global__ __launch_bounds__(256, 2) void k_head_thin(HeadArgs a) {
         lds8* planes = lb + u * 3 * SB::PLANE;
         sb.store(u, planes);
         sb.load(u, left - 2 * KS);
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        lds_barrier();
         u32x4 w[H][NI][3];
 #pragma unroll
         for (int h = 0; h < H; ++h)
@@ -758,7 +760,8 @@ static hipError_t launch_tile(int dtype, const HeadArgs& a, HeadTile tile, hipSt
       return launch_thin<CA, NI, 64, EPI>(a, s);
     }
   }
-  if (tile.i == 64 && tile.j == 64) return launch_fp32<CA, CB, 64, 64, 2, 2, 64, 1, EPI>(a, s);
+  if constexpr (CA)   // (few rows with the head's: thin)
+    if (tile.i == 64 && tile.j == 64) return launch_fp32<CA, CB, 64, 64, 2, 2, 64, 1, EPI>(a, s);
   if (tile.i == 64) return launch_fp32<CA, CB, 64, 128, 2, 2, 32, 2, EPI>(a, s);
   return launch_fp32<CA, CB, 128, 128, 2, 2, 32, 2, EPI>(a, s);
 }

@@ -48,16 +48,21 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // The tile of a product's blocks, n_i x n_j outputs: wide ones read each operand
 // less often; where they would be few, small ones of which more are on the card
-// and more steps on their way (fp32, 32 rows of 1024 x 256 with the gradient: 43
-// us, 58 with tiles of 128; bf16, 2 rows of 32000 82, 161 with tiles of 256).
-// Few fp32 rows with the head's: thin ones, where the card is full of them; of
-// 64 head rows where there are few of 128 (47 rows of 32000 x 5120 222 us and 233,
-// 21 of 118860 x 5120 566 and 542).
+// and more steps on their way (fp32, 32 rows of 1024 x 256 with the
+// gradient in tiles of 64 43 us, of 128 58; bf16, 2 rows of 32000 82, in tiles of
+// 256 161).
+// Fp32 rows with the head's: thin ones where rows or blocks are few (200 rows of
+// 1024 x 512 8 us, 22 with 64 x 128); of 64 head rows where there are few of 128
+// (47 rows of 32000 x 5120 222 and 233, 21 of 118860 x 5120 566 and 542), and as
+// narrow as lets each block have a CU (60 rows of 1024 x 2048 20, 42 with 64).
 HeadTile thin_tile(int i, int64_t n_j) { return {i, n_j <= 16 ? 16 : n_j <= 32 ? 32 : 64, true}; }
 HeadTile head_tile(int32_t dtype, int64_t n_i, int64_t n_j, bool head_rows) {
   const auto blocks = [&](int i, int j) { return (n_i + i - 1) / i * ((n_j + j - 1) / j); };
   if (dtype == LEDE_DTYPE_F32) {
-    if (head_rows && n_j <= 64 && blocks(64, 64) >= 128) return thin_tile(blocks(128, 64) < 512 ? 64 : 128, n_j);
+    if (head_rows && (n_j <= 64 || blocks(64, 128) < 128)) {
+      if (blocks(128, 64) >= 512) return thin_tile(128, n_j);
+      return thin_tile(64, blocks(64, 16) <= 256 ? 16 : blocks(64, 32) <= 256 ? std::min<int64_t>(n_j, 32) : n_j);
+    }
     const int j = n_j <= 64 ? 64 : 128;
     return {j == 64 || blocks(128, j) < 128 ? 64 : 128, j};
   }
