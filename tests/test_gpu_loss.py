@@ -57,6 +57,15 @@ def test_pieces_of_the_vocabulary(M, V, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,K", [(1, 65409, 8), (3, 70001, 40), (16, 66000, 264), (20, 65537, 72), (33, 65600, 520), (64, 131073, 136), (64, 33000, 256), (65, 33001, 64)])
+def test_few_rows_of_large_heads(M, V, K, dtype):
+    say("head loss, few rows of large heads M=%d V=%d K=%d %s" % (M, V, K, dtype))
+    hidden, head, targets, weights = inputs(M, V, K, DT[dtype], M + V + K)
+    targets[0] = V - 1
+    check(hidden, head, targets, weights)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_one_of_the_two(dtype):
     m = lede()
     hidden, head, targets, weights = inputs(70, 600, 128, DT[dtype], 9)
