@@ -453,7 +453,7 @@ template <bool COLUMNS, int T, int KS, int AHEAD> struct Split {
       src[i] += step;
     }
   }
-  // The layouts of Operand; rows of 32 entries: 64 bytes, chunk c of row r at c ^ (r >> 2 & 3).
+  // The layouts of Operand; rows of 32 entries: 64 bytes, chunk c of row r at c ^ (r >> 1 & 3).
   __device__ __forceinline__ void store(int u, lds8* planes) const {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -465,7 +465,7 @@ template <bool COLUMNS, int T, int KS, int AHEAD> struct Split {
         at = k * (2 * T) + ((c ^ (Operand<true, T, 4>::perm(k) << 1)) << 4);
       } else {
         const int r = q / (KS / 8), c = q % (KS / 8);
-        at = r * (2 * KS) + ((c ^ (KS == 64 ? r & 7 : r >> 2 & 3)) << 4);
+        at = r * (2 * KS) + ((c ^ (KS == 64 ? r & 7 : r >> 1 & 3)) << 4);
       }
       const float v[8] = {x[u][i][0].x, x[u][i][0].y, x[u][i][0].z, x[u][i][0].w, x[u][i][1].x, x[u][i][1].y, x[u][i][1].z, x[u][i][1].w};
       u32x4 w[3];
@@ -478,7 +478,7 @@ template <bool COLUMNS, int T, int KS, int AHEAD> struct Split {
   static __device__ __forceinline__ bf16x8 read(const lds8* plane, int r0, int h) {
     if (COLUMNS || KS == 64) return Operand<COLUMNS, T, 4>::read(plane, r0, h);
     const int lane = threadIdx.x & 63, r = r0 + (lane & 15);
-    return lds_row8(plane + r * 64 + (((lane >> 4) ^ (r >> 2 & 3)) << 4));
+    return lds_row8(plane + r * 64 + (((lane >> 4) ^ (r >> 1 & 3)) << 4));
   }
 };
 
