@@ -12,13 +12,14 @@ enum HeadEpi : int {
   HEAD_SUMS = 0,   // i = v, j = m: each row's maximum and sum of exponentials over the tile, and the target's logit
   HEAD_DZ = 1,     // i = v, j = m: dz, in the operands' type
   HEAD_PART = 2,   // i = k, j = m: fp32 sums of a part of the contraction over v
-  HEAD_OUT = 3,    // i = k, j = v: dW
+  HEAD_OUT = 3,    // i = k, j = v: dW (of few rows: launch_head_outer)
 };
 
 // A block's tile of a product: bf16 256 x 64, 128 or 256, or 128 x 64; fp32 64 x
 // 64, 64 x 128 or 128 x 128, or thin: 128 x 16, 32 or 64, of columns 256 x those.
 struct HeadTile { int i, j; bool thin = false; };   // thin: few fp32 rows over a large head
 
+constexpr int HEAD_OUTER_F32 = 32, HEAD_OUTER_BF16 = 64;   // rows of launch_head_outer, at most
 struct HeadArgs {
   const uint8_t *A, *B;
   int64_t lda, ldb;                // elements
@@ -55,6 +56,7 @@ struct HeadOutArgs {
   void* out; int64_t ldo;
 };
 hipError_t launch_head(int dtype, int epi, const HeadArgs& a, HeadTile tile, hipStream_t s);
+hipError_t launch_head_outer(int dtype, const HeadArgs& a, hipStream_t s);   // dW; of few rows
 hipError_t launch_head_copy(const HeadCopyArgs& a, hipStream_t s);
 hipError_t launch_head_join(const HeadJoinArgs& a, hipStream_t s);
 hipError_t launch_head_out(int dtype, const HeadOutArgs& a, hipStream_t s);

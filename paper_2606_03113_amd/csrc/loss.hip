@@ -12,6 +12,7 @@
 #include "loss.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lede {
 
@@ -183,7 +184,7 @@ __device__ __forceinline__ void head_step(const lds8* __restrict__ cur, const ld
 // of i with all tiles of j, so that what runs at a time is about square and
 // shares its operands in the XCD's L2.  Of short contractions, bound by what
 // they write, whole rows of the result instead (dW of 35 rows over 128256 x 5120
-// 321 us, 357 in bands).
+// 321 us, 357 in bands; for so few there is k_head_outer now).
 struct HeadPlace { int part, it, jt; };
 __device__ __forceinline__ bool head_place(const HeadArgs& a, HeadPlace& p) {
   const int per_part = a.i_tiles * a.j_tiles, per_xcd = (per_part * a.split + 7) / 8;
@@ -647,6 +648,95 @@ __global__ __launch_bounds__(256, 2) void k_head_thin(HeadArgs a) {
     }
 }
 
+// dW of few rows, bound by its stores: a wave keeps its 64 columns of all rows of
+// hidden as operands (the contraction is 32 H rows) and walks over the
+// vocabulary, 64 entries at a time, the next ones' dz on its way.  Neighbouring
+// columns are of four tiles, so that a lane stores four of them and 16 lanes a row's
+// 64; blocks beside each other take the entries in turn, so that the card writes
+// one stretch of dW at a time.  21 fp32 rows over 118860 x 5120 443 us (5.5 TB/s;
+// in k_head_fp32 600), 2 bf16 rows over 128256 x 5120 229 (5.7; in k_head 289), 35
+// of them 299 (321).
+template <int DT, int H>
+__global__ __launch_bounds__(256, 2) void k_head_outer(HeadArgs a) {
+  constexpr int PARTS = DT ? 1 : 3, ES = DT ? 2 : 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+  const int i0 = (blockIdx.x * 4 + wave) * 64;
+  if (i0 >= a.n_i) return;
+  // Four neighbours' eight entries of the contraction, as they lie in memory and as four tiles' operands.
+  typedef typename std::conditional<DT == 1, uint2, float4>::type Four;
+  auto load = [&](Four (&v)[H * 8], const uint8_t* p, int64_t ld, int at) {
+#pragma unroll
+    for (int n = 0; n < H * 8; ++n) {
+      const int c = (n / 8) * 32 + 8 * lg + n % 8;
+      v[n] = *(const Four*)(c < a.C ? p + (c * ld + at) * ES : (const uint8_t*)head_zeros);
+    }
+  };
+  auto operands = [&](const Four (&v)[H * 8], bf16x8 (&f)[H][4][PARTS]) {
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if constexpr (DT == 1) {
+          u32x4 w;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint2 p = v[h * 8 + 2 * k], q = v[h * 8 + 2 * k + 1];
+            w[k] = __builtin_amdgcn_perm(x < 2 ? q.x : q.y, x < 2 ? p.x : p.y, x & 1 ? 0x07060302 : 0x05040100);
+          }
+          f[h][x][0] = __builtin_bit_cast(bf16x8, w);
+        } else {
+          float e[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float4 q = v[h * 8 + k];
+            e[k] = x == 0 ? q.x : x == 1 ? q.y : x == 2 ? q.z : q.w;
+          }
+          u32x4 w[3];
+          split8(e, w);
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) f[h][x][p] = __builtin_bit_cast(bf16x8, w[p]);
+        }
+      }
+  };
+  Four v[H * 8];
+  bf16x8 fh[H][4][PARTS];
+  const int k = i0 + 4 * lr;
+  load(v, a.A, a.lda, min(k, a.n_i - 4));
+  operands(v, fh);
+  const int most = ((a.n_j + 3) & ~3) - 4;
+  auto load_dz = [&](int j0) { load(v, a.B, a.ldb, min(j0 + 4 * lr, most)); };
+  load_dz(blockIdx.y * 64);
+  for (int j0 = blockIdx.y * 64; j0 < a.n_j; j0 += gridDim.y * 64) {
+    bf16x8 fz[H][4][PARTS];
+    operands(v, fz);
+    load_dz(j0 + gridDim.y * 64);
+    f32x4 acc[4][4];   // [y][x]: entry 4 (4 lg + e) + y of the vocabulary, column 4 lr + x
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) acc[y][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int p = 0; p < (DT ? 1 : PRODUCTS); ++p) {
+        constexpr int PA[PRODUCTS] = {2, 0, 1, 1, 0, 0}, PB[PRODUCTS] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            acc[y][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fz[h][y][DT ? 0 : PB[p]], fh[h][x][DT ? 0 : PA[p]], acc[y][x], 0, 0, 0);
+      }
+    if (k >= a.n_i) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int j = j0 + 4 * (4 * lg + e) + y;
+        if (j < a.n_j) store4<DT>((uint8_t*)a.out + (int64_t)j * a.ldo * ES, k, make_float4(acc[y][0][e], acc[y][1][e], acc[y][2][e], acc[y][3][e]));
+      }
+  }
+}
+
 // ---- rows before and after ----------------------------------------------------------
 
 // Rows of hidden for dW, zeros in place of those that are left out: what they hold
@@ -770,6 +860,15 @@ hipError_t launch_head(int dtype, int epi, const HeadArgs& a, HeadTile tile, hip
   if (epi == HEAD_DZ) return launch_tile<false, false, HEAD_DZ>(dtype, a, tile, s);
   if (epi == HEAD_PART) return launch_tile<true, false, HEAD_PART>(dtype, a, tile, s);
   return launch_tile<true, true, HEAD_OUT>(dtype, a, tile, s);
+}
+
+hipError_t launch_head_outer(int dtype, const HeadArgs& a, hipStream_t s) {
+  const int x = (a.n_i + 255) / 256, y = std::max(1, std::min((a.n_j + 63) / 64, 1024 / x));
+  const dim3 grid(x, y);
+  if (dtype && a.C > 32) k_head_outer<1, 2><<<grid, 256, 0, s>>>(a);
+  else if (dtype) k_head_outer<1, 1><<<grid, 256, 0, s>>>(a);
+  else k_head_outer<0, 1><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 hipError_t launch_head_copy(const HeadCopyArgs& a, hipStream_t s) {

@@ -219,7 +219,8 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
       d.B = wz; d.ldb = p.ldz; d.n_j = n;
       d.C = d.chunk = M;
       d.out = (uint8_t*)d_head + v0 * ld_dw * es_of(dtype); d.ldo = ld_dw;
-      if (hipError_t e = launch_head(dtype, HEAD_OUT, d, p.tile_w, s)) return done(e);
+      const bool outer = M <= (dtype == LEDE_DTYPE_F32 ? HEAD_OUTER_F32 : HEAD_OUTER_BF16);
+      if (hipError_t e = outer ? launch_head_outer(dtype, d, s) : launch_head(dtype, HEAD_OUT, d, p.tile_w, s)) return done(e);
     }
   }
   if (M && d_hidden) {
