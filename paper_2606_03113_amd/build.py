@@ -8,7 +8,7 @@ CSRC = os.path.join(HERE, "csrc")
 SO = os.path.join(HERE, "liblede.so")
 SOURCES = ["linear.hip", "wide.hip", "norm.hip", "attention.hip", "accept.hip", "policy.hip", "dqn.hip", "misc.hip", "noalloc.hip",
            "cache.hip", "cache_pages.hip", "cache_attention.hip", "logprobs.hip", "quant.hip", "loss.hip", "runtime.cpp", "dqn.cpp", "cache.cpp",
-           "products.cpp"]
+           "pages.cpp", "products.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,10 +1,12 @@
 // The paged 8-bit K/V cache of a batch of requests: its layout, and the
 // kernels' arguments (cache.hip, cache_attention.hip; entry points in
-// cache.cpp).  Not part of the public C ABI.
+// cache.cpp and pages.cpp).  Not part of the public C ABI.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
+
+#include "../../include/lede.h"
 
 namespace lede {
 
@@ -35,6 +37,17 @@ inline CacheView cache_view(void* region, int n_pages, int nkv, int hd) {
   uint8_t* p = (uint8_t*)region;
   return {p, p + n, (uint32_t*)(p + 2 * n), n_pages, nkv, hd};
 }
+
+// A cache's shape: LEDE_OK, or why it is none.  Page and token counts stay in
+// 32 bits, byte offsets are 64-bit everywhere.
+inline int check_cache(int32_t n_pages, int32_t n_kv, int32_t hd) {
+  if (n_pages < 1 || n_kv < 1) return LEDE_E_ARG;
+  if ((hd != 64 && hd != 128) || n_kv > 1024) return LEDE_E_UNSUPPORTED;
+  return LEDE_OK;
+}
+
+// Of 256 threads: a launch has fewer than 2^32 threads.
+constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;
 
 struct CachePlanArgs {
   const int32_t *seq_lens, *new_lens, *held;  // [n_seqs]
@@ -75,7 +88,7 @@ struct CacheAttnArgs {
   void* out; int64_t ldo;
 };
 
-// The pages' life (cache_pages.hip).  The calls take what they need of these.
+// The pages' life (cache_pages.hip; entry points in pages.cpp).  The calls take what they need of these.
 constexpr int CACHE_MOST_PAGES = 1 << 18;   // of a pool that is freed into or compacted: a bit a page in LDS
 struct CachePagesArgs {
   const int32_t *source, *lens;               // [n_seqs]; lens may be null
