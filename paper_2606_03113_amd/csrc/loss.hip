@@ -198,6 +198,9 @@ __device__ __forceinline__ bool head_place(const HeadArgs& a, HeadPlace& p) {
   return true;
 }
 
+// Whether row r, whose target is t, takes no part in a gradient.
+__device__ __forceinline__ bool left_out(int t, const float* weights, int64_t r, int V) { return t < 0 || t >= V || (weights && weights[r] == 0.f); }
+
 // What becomes of a block's tile of sums.  Lane (lr, lg) of a wave holds, of each
 // of its 16 x 16 tiles, i = 4 lg + 0..3 of j = lr.
 template <int DT, int EPI, int TI, int TJ, int WI, int WJ, int NI, int NJ>
@@ -649,8 +652,8 @@ __global__ __launch_bounds__(256, 2) void k_head_thin(HeadArgs a) {
 }
 
 // dW of few rows, bound by its stores: a wave keeps its 64 columns of all rows of
-// hidden as operands (the contraction is 32 H rows) and walks over the
-// vocabulary, 64 entries at a time, the next ones' dz on its way.  Neighbouring
+// hidden (zeros for those that are left out) as operands (the contraction is 32 H
+// rows) and walks over the vocabulary, 64 entries at a time, the next ones' dz on its way.  Neighbouring
 // columns are of four tiles, so that a lane stores four of them and 16 lanes a row's
 // 64; blocks beside each other take the entries in turn, so that the card writes
 // one stretch of dW at a time.  21 fp32 rows over 118860 x 5120 443 us (5.5 TB/s;
@@ -702,6 +705,10 @@ __global__ __launch_bounds__(256, 2) void k_head_outer(HeadArgs a) {
   bf16x8 fh[H][4][PARTS];
   const int k = i0 + 4 * lr;
   load(v, a.A, a.lda, min(k, a.n_i - 4));
+  const uint64_t kept = __ballot(lane < a.C && !left_out(a.targets[lane], a.weights, lane, a.V));
+#pragma unroll
+  for (int n = 0; n < H * 8; ++n)
+    if (!(kept >> ((n / 8) * 32 + 8 * lg + n % 8) & 1)) v[n] = Four{};
   operands(v, fh);
   const int most = ((a.n_j + 3) & ~3) - 4;
   auto load_dz = [&](int j0) { load(v, a.B, a.ldb, min(j0 + 4 * lr, most)); };
@@ -746,7 +753,7 @@ __global__ __launch_bounds__(256) void k_head_copy(HeadCopyArgs a) {   // rows o
   if (at >= a.n * a.chunks) return;
   const int64_t r = at / a.chunks, c = at % a.chunks;
   const int t = a.targets[r];
-  const bool out = t < 0 || t >= a.V || (a.weights && a.weights[r] == 0.f);
+  const bool out = left_out(t, a.weights, r, a.V);
   *(uint4*)(a.dst + at * 16) = out ? make_uint4(0, 0, 0, 0) : ld16((const uint8_t*)a.src + r * a.pitch + c * 16);
 }
 
@@ -790,7 +797,7 @@ __global__ __launch_bounds__(256) void k_head_out(HeadOutArgs a, int lanes) {
   for (int o = 1; o < lanes; o <<= 1) v = make_float4(v.x + __shfl_xor(v.x, o), v.y + __shfl_xor(v.y, o), v.z + __shfl_xor(v.z, o), v.w + __shfl_xor(v.w, o));
   if (!in || lane) return;
   const int t = a.targets[r];
-  if (t < 0 || t >= a.V || (a.weights && a.weights[r] == 0.f)) {
+  if (left_out(t, a.weights, r, a.V)) {
     v = make_float4(0.f, 0.f, 0.f, 0.f);   // (the sums are NaN where the head is not finite)
   } else if (DT == 1) {
     const float rest = a.rest[r];

@@ -185,7 +185,8 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
   if (p.total && (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total)) return LEDE_E_ARG;
   hipStream_t s = S_(stream);
   uint8_t *wh = (uint8_t*)workspace, *wz = wh + p.h, *wr = wz + p.dz, *wp = wr + p.rest;
-  if (M && d_head) {
+  const bool outer = M <= (dtype == LEDE_DTYPE_F32 ? HEAD_OUTER_F32 : HEAD_OUTER_BF16);
+  if (d_head && !outer) {
     HeadCopyArgs c{};
     c.src = hidden; c.pitch = ldh * es_of(dtype); c.n = M; c.chunks = K * es_of(dtype) / 16; c.dst = wh;
     c.targets = targets; c.weights = weights; c.V = V;
@@ -219,7 +220,10 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
       d.B = wz; d.ldb = p.ldz; d.n_j = n;
       d.C = d.chunk = M;
       d.out = (uint8_t*)d_head + v0 * ld_dw * es_of(dtype); d.ldo = ld_dw;
-      const bool outer = M <= (dtype == LEDE_DTYPE_F32 ? HEAD_OUTER_F32 : HEAD_OUTER_BF16);
+      if (outer) {
+        d.A = (const uint8_t*)hidden; d.lda = ldh;
+        d.targets = targets; d.weights = weights;
+      }
       if (hipError_t e = outer ? launch_head_outer(dtype, d, s) : launch_head(dtype, HEAD_OUT, d, p.tile_w, s)) return done(e);
     }
   }
