@@ -869,6 +869,7 @@ hipError_t launch_head(int dtype, int epi, const HeadArgs& a, HeadTile tile, hip
   return launch_tile<true, true, HEAD_OUT>(dtype, a, tile, s);
 }
 
+// Blocks for two rounds of two a CU (one round: 458 us for 442, the same case).
 hipError_t launch_head_outer(int dtype, const HeadArgs& a, hipStream_t s) {
   const int x = (a.n_i + 255) / 256, y = std::max(1, std::min((a.n_j + 63) / 64, 1024 / x));
   const dim3 grid(x, y);
