@@ -809,7 +809,8 @@ int lede_op_quant_linear(int32_t dtype, const void* packed, int32_t N, int32_t K
  *   lse[m]   log sum_v exp z[m][v]  (fp32; required)
  *   loss[m]  lse[m] - z[m][targets[m]]  (fp32; may be null)
  * Products are exact and sums fp32 (fp32 inputs enter as three bf16 numbers
- * each, of whose nine products the six largest count: 2^-22 of the largest).
+ * each, of whose nine products the six largest count: what is left out is less
+ * than 2^-19 of a product).
  * A row whose logits are all -infinity or include a NaN or +infinity has NaN;
  * so has, of fp32 inputs, a row with an entry that is not finite, and every
  * row where the head has one.

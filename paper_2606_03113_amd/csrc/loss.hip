@@ -392,11 +392,11 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
 
 // The same for fp32 operands: each is three bf16 numbers that sum to it (cut off
 // rather than rounded, so that the first cannot overflow), and of the nine
-// products of parts the six down to 2^-16 of the largest are made, the smallest
-// first: half the rate of 12 products, against an eighth on the fp32 matrix
-// instructions.  Operands are split on their way to LDS, 5.5 operations an entry,
+// products of parts the six down to 2^-14 of the whole are made, the smallest
+// first (the others are below 2^-21, 2^-21 and 2^-28 of it): a sixth of bf16's
+// rate, where the fp32 matrix instructions have a sixteenth.  Operands are split on their way to LDS, 5.5 operations an entry,
 // so that they are read once a tile (in planes of parts, split before: 47 rows of
-// 32000 x 5120 4.8 ms against 0.9, 1024 rows 7.8 against 6.7, 2048 rows alike).
+// 32000 x 5120 4.8 ms against 0.9, 1024 rows 7.0 against 6.7, 2048 rows alike).
 // A step is KS entries of the contraction, loaded into registers AHEAD steps
 // before; two barriers a step, and other blocks on the CU meanwhile.  What is
 // not finite becomes NaN in the second part.

@@ -8,8 +8,9 @@ HALF_STEP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
 
 def chain(n, dtype):
     """Of a product's sum over n terms, relative to the sum of magnitudes: 32 terms meet in a matrix instruction and are
-    added to what is there; fp32 operands enter as six such products of parts, and what the other three would add."""
-    return 2.0 ** -23 * (n / 32 + 33) * (1 if dtype == torch.bfloat16 else 6) + (2.0 ** -22 if dtype == torch.float32 else 0.0)
+    added to what is there; fp32 operands enter as six such products of parts, and what the other three would add (a number cut off at
+    8 bits leaves less than 2^-7 of it: the parts are below 1, 2^-7 and 2^-14 of it)."""
+    return 2.0 ** -23 * (n / 32 + 33) * (1 if dtype == torch.bfloat16 else 6) + (2 * 2.0 ** -21 + 2.0 ** -28 if dtype == torch.float32 else 0.0)
 
 
 class Reference:
