@@ -831,8 +831,9 @@ int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M,
  *   d_head   [V][K]  dz^T hidden
  * of `dtype`, either of them null where it is not asked for.  A row whose
  * weight is 0 is left out, too.  dz enters the two products with bf16's 8 bits
- * where the inputs are bf16 (its rounding and the result's are alike) and
- * with 24 where they are fp32.  d_hidden and d_head overlap nothing else.
+ * where the inputs are bf16 (its rounding and the result's are alike), a row's
+ * dz at its target, usually its largest, with 16, and with 24 where they are
+ * fp32.  d_hidden and d_head overlap nothing else.
  * Sums have a fixed order: the same call gives the same bits.  M = 0 clears
  * d_head.  Errors as above, with lede_op_head_loss_grad_bytes. */
 size_t lede_op_head_loss_grad_bytes(int32_t dtype, int32_t M, int32_t V, int32_t K);

@@ -330,6 +330,90 @@ __device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][
   }
 }
 
+// dW's part of what rounding took from the targets' dz (rest): rest[m] h_m for row
+// t_m of dW, whose largest dz this is.  The block lists the rows whose target lies
+// in its tile, in ascending order, and multiplies 64 of them at a time: their rows
+// of hidden are gathered into A's place in the ring, and an operand of rest in a
+// row's target's place and zeros elsewhere is made in registers (rest in bf16: 2^-16
+// of dz are left).  2048 rows of 32000 x 4096: the error of dW against 64 bits 2.4e-3
+// -> 1.7e-3, bf16's own, for 448 -> 480 us; chains of loads at a block's end, of which
+// targets loaded before the product began save nothing.
+template <int TI, int TJ, int WI, int WJ, int NI, int NJ>
+__device__ __forceinline__ void head_rest(const HeadArgs& a, f32x4 (&acc)[NI][NJ], uint8_t* smem, int i0, int j0, int wi, int wj) {
+  constexpr int NW = WI * WJ, THREADS = NW * 64;
+  typedef Operand<true, TI, NW> OA;
+  static_assert(4 * THREADS * 4 <= TJ * HD_K * 2, "the list has B's place in the ring");
+  __shared__ int found[NW];
+  __shared__ int2 taken[HD_K];   // (place in the tile, rest) of a batch's rows
+  int* const list = (int*)(smem + OA::BYTES);
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t first = a.v0 + j0, cols = min(TJ, a.n_j - j0);
+  for (int r0 = 0; r0 < a.C; r0 += 4 * THREADS) {
+    const int r = r0 + 4 * tid;
+    bool in[4];
+    int at = 0, total = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      in[u] = r + u < a.C && (uint32_t)a.targets[r + u] - first < cols;   // (rows left out for their weight are zeros in A)
+      const uint64_t b = __ballot(in[u]);
+      at += __popcll(b & ((1ull << lane) - 1));
+      total += __popcll(b);
+    }
+    __syncthreads();   // (the ring, and the last rows' list, have been read)
+    if (lane == 0) found[wave] = total;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const int n = found[w];
+      at += w < wave ? n : 0;
+      total += n;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (in[u]) list[at++] = r + u;
+    for (int b0 = 0; b0 < total; b0 += HD_K) {
+      __syncthreads();   // (the list is there; the last batch has been read)
+      const int n = min(HD_K, total - b0);
+      if (tid < HD_K) {
+        const int m = list[b0 + min(tid, n - 1)];
+        taken[tid] = tid < n ? make_int2((int)((uint32_t)a.targets[m] - first), f32_to_bf16(a.rest[m])) : make_int2(-1, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < OA::PER; ++i) {
+        const int k = OA::entry(i, wave), c = (lane % OA::CH) ^ (OA::perm(k) << 1);
+        const int64_t row = list[b0 + min(k, n - 1)];
+        uint4 x = ld16(a.A + (row * a.lda + i0 + min(8 * c, ((a.n_i + 7) & ~7) - 8 - i0)) * 2);
+        if (k >= n) x = make_uint4(0, 0, 0, 0);
+        *(uint4*)(smem + (wave * OA::PER + i) * 1024 + lane * 16) = x;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (32 * h >= n) break;
+        int2 q[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e] = taken[32 * h + 8 * lg + e];
+        bf16x8 fb[NJ];
+#pragma unroll
+        for (int y = 0; y < NJ; ++y) {
+          u32x4 w;
+          const int j = (wj * NJ + y) * 16 + lr;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = (q[2 * e].x == j ? (uint32_t)q[2 * e].y : 0u) | (q[2 * e + 1].x == j ? (uint32_t)q[2 * e + 1].y << 16 : 0u);
+          fb[y] = __builtin_bit_cast(bf16x8, w);
+        }
+#pragma unroll
+        for (int x = 0; x < NI; ++x) {
+          const bf16x8 fa = OA::read((const lds8*)smem, (wi * NI + x) * 16, h);
+#pragma unroll
+          for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa, fb[y], acc[x][y], 0, 0, 0);
+        }
+      }
+    }
+  }
+}
+
 // out[j][i] = sum_c A[i][c] B[j][c] of bf16 operands, TI x TJ of them a block, WI x
 // WJ waves.  A ring of S steps of the contraction in LDS: one is multiplied while
 // the next ones are on their way; one barrier a step.  2048 rows of 32000 x 4096:
@@ -385,6 +469,7 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
     }
   }
 
+  if constexpr (EPI == HEAD_OUT) head_rest<TI, TJ, WI, WJ>(a, acc, smem, i0, j0, wi, wj);
   head_finish<1, EPI, TI, TJ, WI, WJ>(a, acc, smem, place, wi, wj);
 }
 
@@ -710,6 +795,15 @@ __global__ __launch_bounds__(256, 2) void k_head_outer(HeadArgs a) {
   for (int n = 0; n < H * 8; ++n)
     if (!(kept >> ((n / 8) * 32 + 8 * lg + n % 8) & 1)) v[n] = Four{};
   operands(v, fh);
+  // Lane c: row c's target in the piece, and what rounding took from its dz (-1: nothing).
+  int place = -1, rest = 0;
+  if (DT == 1 && (kept >> lane & 1)) {
+    const int t = a.targets[lane] - a.v0;
+    if (t >= 0 && t < a.n_j && a.rest[lane] != 0.f) {
+      place = t;
+      rest = f32_to_bf16(a.rest[lane]);
+    }
+  }
   const int most = ((a.n_j + 3) & ~3) - 4;
   auto load_dz = [&](int j0) { load(v, a.B, a.ldb, min(j0 + 4 * lr, most)); };
   load_dz(blockIdx.y * 64);
@@ -733,6 +827,26 @@ __global__ __launch_bounds__(256, 2) void k_head_outer(HeadArgs a) {
           for (int x = 0; x < 4; ++x)
             acc[y][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fz[h][y][DT ? 0 : PB[p]], fh[h][x][DT ? 0 : PA[p]], acc[y][x], 0, 0, 0);
       }
+    if (DT == 1 && __ballot(place >= j0 && place < j0 + 64)) {   // (as in head_rest)
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        int t[8], r[8];
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+          t[n] = __shfl(place, 32 * h + 8 * lg + n) - j0 - 4 * lr;
+          r[n] = __shfl(rest, 32 * h + 8 * lg + n);
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          u32x4 w;
+#pragma unroll
+          for (int n = 0; n < 4; ++n) w[n] = (t[2 * n] == y ? (uint32_t)r[2 * n] : 0u) | (t[2 * n + 1] == y ? (uint32_t)r[2 * n + 1] << 16 : 0u);
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            acc[y][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), fh[h][x][0], acc[y][x], 0, 0, 0);
+        }
+      }
+    }
     if (k >= a.n_i) continue;
 #pragma unroll
     for (int e = 0; e < 4; ++e)

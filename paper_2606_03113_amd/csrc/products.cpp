@@ -220,9 +220,9 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
       d.B = wz; d.ldb = p.ldz; d.n_j = n;
       d.C = d.chunk = M;
       d.out = (uint8_t*)d_head + v0 * ld_dw * es_of(dtype); d.ldo = ld_dw;
+      d.targets = targets; d.weights = weights; d.rest = (float*)wr;
       if (outer) {
         d.A = (const uint8_t*)hidden; d.lda = ldh;
-        d.targets = targets; d.weights = weights;
       }
       if (hipError_t e = outer ? launch_head_outer(dtype, d, s) : launch_head(dtype, HEAD_OUT, d, p.tile_w, s)) return done(e);
     }
