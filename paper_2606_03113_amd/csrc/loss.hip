@@ -127,54 +127,57 @@ template <class OA, class OB> struct Copies {
   }
 };
 
-// One step of the contraction, in `cur`.  The operands of half a step are read
-// while the other half is multiplied: those of A into the registers that its
-// products have just left, those of B into a second set.  Early in the second
-// half all waves have read all of cur and `next` has arrived: a barrier, and the
-// copies of a later step to cur's place (`to`).  The pointers are said to be
-// apart although `to` is cur: the barrier stands between their uses, and
-// without it the compiler waits for all copies on their way before it reads
-// columns.
-template <class OA, class OB, bool ORDER, bool COPY, int WAIT, int NI, int NJ, class Copies_>
-__device__ __forceinline__ void head_step(const lds8* __restrict__ cur, const lds8* __restrict__ next, lds8* __restrict__ to, Copies_& copies,
-                                          int wi, int wj, bf16x8 (&fa)[NI], bf16x8 (&fb)[2][NJ], f32x4 (&acc)[NI][NJ]) {
+// The products of row x of a wave's tiles.
+template <int NI, int NJ> __device__ __forceinline__ void multiply_row(int x, const bf16x8 (&fa)[NI], const bf16x8 (&fb)[NJ], f32x4 (&acc)[NI][NJ]) {
+#pragma unroll
+  for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[x], fb[y], acc[x][y], 0, 0, 0);
+}
+
+// What stands between two barriers: the copies of a later step to the place `to`
+// that the barrier has set free, all reads of the step in `cur`, which has arrived,
+// and products.  The operands of half a step are read while the other half is
+// multiplied: those of A into the registers that its products have just left,
+// those of B into a second set; the second half's last products are made behind the
+// next barrier, under its first reads (all steps but the FIRST begin with those of the
+// step before).  cur and to are two places of the ring, so that within this
+// function, where no barrier is, neither's accesses touch the other: told so, the
+// compiler reads columns without waiting for copies on their way.  The barriers
+// stand in the caller, where nothing is said of the pointers, and order all of it.
+template <class OA, class OB, bool ORDER, bool FIRST, bool COPY, int EARLY, int NI, int NJ, class Copies_>
+__device__ __forceinline__ void head_step(const lds8* __restrict__ cur, lds8* __restrict__ to, Copies_& copies, int wi, int wj, bf16x8 (&fa)[NI],
+                                          bf16x8 (&fb)[2][NJ], f32x4 (&acc)[NI][NJ]) {
   auto keep_order = []() {
     if (ORDER) __builtin_amdgcn_sched_barrier(0);
   };
-  constexpr int EARLY = NI > 2 ? 2 : 1;   // rows of tiles before the barrier
-  auto read_a = [&](const lds8* t, int h, int x) { fa[x] = OA::read(t, (wi * NI + x) * 16, h); };
-  auto read_b = [&](const lds8* t, int h) {
+  auto read_a = [&](int h, int x) { fa[x] = OA::read(cur, (wi * NI + x) * 16, h); };
+  auto read_b = [&](int h) {
 #pragma unroll
-    for (int y = 0; y < NJ; ++y) fb[h][y] = OB::read(t + OA::BYTES, (wj * NJ + y) * 16, h);
+    for (int y = 0; y < NJ; ++y) fb[h][y] = OB::read(cur + OA::BYTES, (wj * NJ + y) * 16, h);
   };
-  auto multiply = [&](int h, int x) {
+  if (COPY) copies.next(to);
+  read_b(0);
 #pragma unroll
-    for (int y = 0; y < NJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[x], fb[h][y], acc[x][y], 0, 0, 0);
-  };
+  for (int x = 0; x < EARLY; ++x) read_a(0, x);
+#pragma unroll
+  for (int x = EARLY; x < NI; ++x) {
+    if (!FIRST) multiply_row(x, fa, fb[1], acc);
+    read_a(0, x);
+    keep_order();
+  }
+  __builtin_amdgcn_sched_barrier(0);   // (dh's columns, of 2048 rows of 32000 x 4096: 452 us without it, 402 with)
 #pragma unroll
   for (int x = 0; x < NI; ++x) {
-    multiply(0, x);
+    multiply_row(x, fa, fb[0], acc);
     if (x == 0) {   // (not before it: the count of reads on their way ends at 15)
       keep_order();
-      read_b(cur, 1);
+      read_b(1);
     }
-    read_a(cur, 1, x);
+    read_a(1, x);
     keep_order();   // (left alone, reads stand right before what waits for them)
   }
 #pragma unroll
   for (int x = 0; x < EARLY; ++x) {
-    multiply(1, x);
-    keep_order();
-  }
-  copies_barrier<WAIT>();
-  if (COPY) copies.next(to);
-  read_b(next, 0);
-#pragma unroll
-  for (int x = 0; x < EARLY; ++x) read_a(next, 0, x);
-#pragma unroll
-  for (int x = EARLY; x < NI; ++x) {
-    multiply(1, x);
-    read_a(next, 0, x);
+    multiply_row(x, fa, fb[1], acc);
     keep_order();
   }
 }
@@ -448,25 +451,25 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
     for (int i = 0; i < S && i < total; ++i) copies.next(ring + i * STAGE);
     if (total >= S) copies_barrier<(S - 1) * PER>();
     else copies_barrier<0>();
+    constexpr int EARLY = NI > 2 ? 2 : 1;   // rows of tiles of a step's second half before the barrier
     bf16x8 fa[NI], fb[2][NJ];
-#pragma unroll
-    for (int y = 0; y < NJ; ++y) fb[0][y] = OB::read(ring + OA::BYTES, (wj * NJ + y) * 16, 0);
-#pragma unroll
-    for (int x = 0; x < NI; ++x) fa[x] = OA::read(ring, (wi * NI + x) * 16, 0);
+    head_step<OA, OB, !CA, true, false, EARLY>(ring, ring, copies, wi, wj, fa, fb, acc);
     int slot = 0;
     auto after = [&](int x) { return x + 1 == S ? 0 : x + 1; };
-    for (int s = S; s < total; ++s) {
-      lds8* cur = ring + slot * STAGE;
+    for (int s = S; s < total; ++s) {   // (step s is copied to where step s - S was)
+      lds8* left = ring + slot * STAGE;
       slot = after(slot);
-      head_step<OA, OB, !CA, true, (S - 2) * PER>(cur, ring + slot * STAGE, cur, copies, wi, wj, fa, fb, acc);
+      copies_barrier<(S - 2) * PER>();
+      head_step<OA, OB, !CA, false, true, EARLY>(ring + slot * STAGE, left, copies, wi, wj, fa, fb, acc);
     }
 #pragma unroll 1
-    for (int s = max(total - S, 0); s < total; ++s) {
-      lds8* cur = ring + slot * STAGE;
+    for (int s = 1; s < min(S, total); ++s) {
       slot = after(slot);
-      const lds8* next = s + 1 < total ? ring + slot * STAGE : cur;   // (behind the last step: its own once more, which nothing uses)
-      head_step<OA, OB, !CA, false, 0>(cur, next, cur, copies, wi, wj, fa, fb, acc);
+      copies_barrier<0>();
+      head_step<OA, OB, !CA, false, false, EARLY>(ring + slot * STAGE, ring, copies, wi, wj, fa, fb, acc);
     }
+#pragma unroll
+    for (int x = EARLY; x < NI; ++x) multiply_row(x, fa, fb[1], acc);
   }
 
   if constexpr (EPI == HEAD_OUT) head_rest<TI, TJ, WI, WJ>(a, acc, smem, i0, j0, wi, wj);
