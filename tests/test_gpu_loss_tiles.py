@@ -24,9 +24,9 @@ def test_bf16_head_gradient(M, V, K):
     check(*inputs(M, V, K, torch.bfloat16, M + K))
 
 
-# tiles of 128 x 128, 64 x 128, and thin ones of 64 and 128 by 16, 32 and 64; then dW's 128 x 128 and 64 x 128, many rows
+# tiles of 128 x 128, 64 x 128, and thin ones of 64 and 128 by 16, 32 and 64; then dW's 128 x 128, 64 x 128 and 64 x 64, many rows
 @pytest.mark.parametrize("M,V,K", [(200, 8200, 456), (130, 16390, 264), (100, 8200, 456), (60, 33000, 456), (60, 9000, 456), (30, 33000, 328), (30, 9000, 712),
-                                   (12, 33000, 456), (12, 3000, 1032), (60, 1000, 456), (500, 8200, 1032), (700, 300, 520)])
+                                   (12, 33000, 456), (12, 3000, 1032), (60, 1000, 456), (500, 8200, 1032), (700, 300, 520), (300, 60, 1032)])
 def test_fp32(M, V, K):
     say("head loss, many steps M=%d V=%d K=%d f32" % (M, V, K))
     check(*inputs(M, V, K, torch.float32, M + K))
