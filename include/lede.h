@@ -815,11 +815,11 @@ int lede_op_quant_linear(int32_t dtype, const void* packed, int32_t N, int32_t K
  * so has, of fp32 inputs, a row with an entry that is not finite, and every
  * row where the head has one.
  * LEDE_E_ARG: null pointers, bad dtypes, M < 0, V or K < 1, row strides below
- * K; hidden, head, the gradients, workspace or row strides not multiples of 16
- * bytes; a workspace smaller than lede_op_head_loss_bytes (of the same sizes).
+ * K; hidden, head, the gradients, workspace or (of more than one row) row
+ * strides not multiples of 16 bytes; a workspace smaller than lede_op_head_loss_bytes (of the same sizes).
  * LEDE_E_UNSUPPORTED (the sizes are 0): K not a multiple of 8 or above 2^15, M
- * above 2^18, V above 2^20, a row stride of hidden or head of 2^22 elements or
- * more. */
+ * above 2^18, V above 2^20, a row stride of hidden or head (of more than one
+ * row) of 2^22 elements or more. */
 size_t lede_op_head_loss_bytes(int32_t dtype, int32_t M, int32_t V, int32_t K);
 int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M, const void* head, int64_t ldw, int32_t V,
                       int32_t K, const int32_t* targets, float* loss, float* lse, void* workspace, size_t workspace_bytes,

@@ -40,9 +40,12 @@ int check_head(int32_t dtype, int32_t M, int32_t V, int32_t K) {
 }
 // Row strides: a tile's rows are addressed with 32 bits.
 bool stride_ok(int64_t ld) { return ld < 1 << 22; }
-// Rows that the kernels read or write in 16-byte pieces.
-bool rows_ok(const void* p, int64_t ld, int64_t width, int32_t dt) {
-  return p && aligned(p, 16) && ld >= width && ld * es_of(dt) % 16 == 0;
+// Rows that the kernels read or write in 16-byte pieces.  The stride of a single
+// one has nothing to meet but to hold it, and becomes `width`.
+bool rows_ok(const void* p, int64_t& ld, int64_t rows, int64_t width, int32_t dt) {
+  if (!p || !aligned(p, 16) || ld < width) return false;
+  if (rows == 1) ld = width;
+  return ld * es_of(dt) % 16 == 0;
 }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
@@ -149,7 +152,7 @@ int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M,
                       void* stream) {
   if (int rc = check_head(dtype, M, V, K)) return rc;
   if (M == 0) return LEDE_OK;
-  if (!targets || !lse || !rows_ok(hidden, ldh, K, dtype) || !rows_ok(head, ldw, K, dtype)) return LEDE_E_ARG;
+  if (!targets || !lse || !rows_ok(hidden, ldh, M, K, dtype) || !rows_ok(head, ldw, V, K, dtype)) return LEDE_E_ARG;
   if (!stride_ok(ldh) || !stride_ok(ldw)) return LEDE_E_UNSUPPORTED;
   const LossPlan p(dtype, M, V);
   if (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total) return LEDE_E_ARG;
@@ -177,9 +180,9 @@ int lede_op_head_loss_grad(int32_t dtype, const void* hidden, int64_t ldh, int32
                            void* d_head, int64_t ld_dw, void* workspace, size_t workspace_bytes, void* stream) {
   if (int rc = check_head(dtype, M, V, K)) return rc;
   if (!d_head && (!d_hidden || M == 0)) return LEDE_OK;
-  if (d_head && !rows_ok(d_head, ld_dw, K, dtype)) return LEDE_E_ARG;
-  if (M && (!targets || !lse || !rows_ok(hidden, ldh, K, dtype) || !rows_ok(head, ldw, K, dtype))) return LEDE_E_ARG;
-  if (M && d_hidden && !rows_ok(d_hidden, ld_dh, K, dtype)) return LEDE_E_ARG;
+  if (d_head && !rows_ok(d_head, ld_dw, V, K, dtype)) return LEDE_E_ARG;
+  if (M && (!targets || !lse || !rows_ok(hidden, ldh, M, K, dtype) || !rows_ok(head, ldw, V, K, dtype))) return LEDE_E_ARG;
+  if (M && d_hidden && !rows_ok(d_hidden, ld_dh, M, K, dtype)) return LEDE_E_ARG;
   if (M && (!stride_ok(ldw) || !stride_ok(ldh))) return LEDE_E_UNSUPPORTED;
   const GradPlan p(dtype, M, V, K);
   if (p.total && (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total)) return LEDE_E_ARG;
