@@ -257,7 +257,7 @@ __global__ __launch_bounds__(PG_THREADS) void k_cache_own(CachePagesArgs a) {
         own_entries(a, s, o, [&](int i, const int32_t* c) {
           if (count_of(c) == INT_MIN + s) return;
           ++mine.x;
-          mine.y += i * CACHE_PAGE < o.q.seq;
+          mine.y += i < pages_of(o.q.seq);
         });
       return mine;
     };
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(PG_THREADS) void k_cache_own(CachePagesArgs a) {
         own_entries(a, s, o, [&](int i, int32_t* c) {
           if (take == last || count_of(c) == INT_MIN + s) return;
           const int fresh = a.free_pages[head + take++];
-          if (i * CACHE_PAGE < o.q.seq && move < last_move) {
+          if (i < pages_of(o.q.seq) && move < last_move) {
             a.pairs[2 * move] = (int)(c - a.shares);
             a.pairs[2 * move + 1] = fresh;
             ++move;
