@@ -706,6 +706,12 @@ def op_cache_plan(seq_lens, new_lens, held, free_pages, free_head, tables, max_r
     return out
 
 
+def _int32(sizes: int, what: str):
+    """sizes: the bits of all that a call takes as 32-bit numbers (ctypes cuts larger ones off without a word)."""
+    if sizes >> 31:
+        raise LedeError(LEDE_E_UNSUPPORTED, what + ": sizes of 2^31 or more")
+
+
 def _status(torch, status, n: int, device, what: str):
     if status is None:
         return torch.empty(n, dtype=torch.int32, device=device)
@@ -724,6 +730,7 @@ def op_cache_fork(source, seq_lens, held, tables, shares, lens=None, status=None
     _need(_dense(dev, torch.int32, source, seq_lens, held, tables, shares) and tables.dim() == 2 and source.numel() == n
           and held.numel() == n and tables.shape[0] == n
           and (lens is None or (_dense(dev, torch.int32, lens) and lens.numel() == n)), "op_cache_fork")
+    _int32(n | tables.shape[1] | shares.numel(), "op_cache_fork")
     status = _status(torch, status, 3, dev, "op_cache_fork")
     _call(dev, "op_cache_fork", load().lede_op_cache_fork, source.data_ptr(), None if lens is None else lens.data_ptr(),
           seq_lens.data_ptr(), held.data_ptr(), n, tables.data_ptr(), tables.shape[1], shares.data_ptr(), shares.numel(),
@@ -756,6 +763,7 @@ def op_cache_own(seq_lens, new_lens, held, free_pages, free_head, tables, shares
     _need(_dense(dev, torch.int32, seq_lens, new_lens, held, free_pages, free_head, tables, shares) and tables.dim() == 2
           and new_lens.numel() == n and held.numel() == n and tables.shape[0] == n and free_head.numel() == 1 and max_moves >= 0,
           "op_cache_own")
+    _int32(n | free_pages.numel() | tables.shape[1] | shares.numel() | max_moves, "op_cache_own")
     out = _moves(torch, out, max_moves, dev, "op_cache_own")
     _call(dev, "op_cache_own", load().lede_op_cache_own, seq_lens.data_ptr(), new_lens.data_ptr(), held.data_ptr(), n,
           free_pages.data_ptr(), free_pages.numel(), free_head.data_ptr(), tables.data_ptr(), tables.shape[1], shares.data_ptr(),
@@ -770,6 +778,7 @@ def op_cache_copy(cache: Cache, pairs, count):
     import torch
     dev = cache.device
     _need(_dense(dev, torch.int32, pairs, count) and pairs.dim() == 2 and pairs.shape[1] == 2 and count.numel() == 1, "op_cache_copy")
+    _int32(pairs.shape[0], "op_cache_copy")
     _call(dev, "op_cache_copy", load().lede_op_cache_copy, pairs.data_ptr(), count.data_ptr(), pairs.shape[0], cache.region.data_ptr(),
           cache.n_pages, cache.n_kv, cache.head_dim)
 
@@ -783,6 +792,7 @@ def op_cache_free(seq_lens, held, free_pages, free_head, tables, shares, status=
     dev, n = seq_lens.device, seq_lens.numel()
     _need(_dense(dev, torch.int32, seq_lens, held, free_pages, free_head, tables, shares) and tables.dim() == 2 and held.numel() == n
           and tables.shape[0] == n and free_head.numel() == 1, "op_cache_free")
+    _int32(n | free_pages.numel() | tables.shape[1] | shares.numel(), "op_cache_free")
     status = _status(torch, status, 4, dev, "op_cache_free")
     _call(dev, "op_cache_free", load().lede_op_cache_free, seq_lens.data_ptr(), held.data_ptr(), n, free_pages.data_ptr(),
           free_pages.numel(), free_head.data_ptr(), tables.data_ptr(), tables.shape[1], shares.data_ptr(), shares.numel(),
@@ -798,6 +808,7 @@ def op_cache_compact(held, free_pages, free_head, tables, shares, max_moves: int
     dev, n, max_moves = held.device, held.numel(), int(max_moves)
     _need(_dense(dev, torch.int32, held, free_pages, free_head, tables, shares) and tables.dim() == 2 and tables.shape[0] == n
           and free_head.numel() == 1 and max_moves >= 0, "op_cache_compact")
+    _int32(n | free_pages.numel() | tables.shape[1] | shares.numel() | max_moves, "op_cache_compact")
     out = _moves(torch, out, max_moves, dev, "op_cache_compact")
     _call(dev, "op_cache_compact", load().lede_op_cache_compact, held.data_ptr(), n, free_pages.data_ptr(), free_pages.numel(),
           free_head.data_ptr(), tables.data_ptr(), tables.shape[1], shares.data_ptr(), shares.numel(), out.pairs.data_ptr(), max_moves,
@@ -928,6 +939,7 @@ def op_quantize(w, group: int = 64):
     _need(w.dim() == 2, "op_quantize")
     (N, K), dev = w.shape, w.device
     ld = _matrix_stride(w, "op_quantize")
+    _int32(N | K | group, "op_quantize")
     if load().lede_op_quant_bytes(N, K, group) == 0:
         raise LedeError(LEDE_E_UNSUPPORTED, "op_quantize: %d x %d, group %d" % (N, K, group))
     codes = torch.empty(N, (K + 1) // 2, dtype=torch.uint8, device=dev)
@@ -944,6 +956,7 @@ class QuantMatrix:
     def __init__(self, codes, scales, K: int, group: int):
         import torch
         N, dev = codes.shape[0], codes.device
+        _int32(N | K | group, "QuantMatrix")
         nbytes = load().lede_op_quant_bytes(N, K, group)
         if nbytes == 0:
             raise LedeError(LEDE_E_UNSUPPORTED, "4-bit matrix of %d x %d, group %d" % (N, K, group))
@@ -962,6 +975,7 @@ def op_quant_linear(matrix: QuantMatrix, x, dtype=None, out=None):
     dev, N, K = matrix.device, matrix.N, matrix.K
     _need(x.dim() == 2 and x.shape[1] == K and x.device == dev, "op_quant_linear")
     M, ldx = x.shape[0], _matrix_stride(x, "op_quant_linear: x")
+    _int32(M, "op_quant_linear")
     if out is None:
         out = torch.empty(M, N, dtype=dtype or x.dtype, device=dev)
         ldy = N
@@ -985,6 +999,7 @@ def _head_inputs(torch, hidden, head, targets, what: str):
     dev = hidden.device
     _need(hidden.dim() == 2 and head.dim() == 2 and hidden.shape[1] == head.shape[1] and head.device == dev and head.dtype == hidden.dtype
           and _dense(dev, torch.int32, targets) and targets.numel() == hidden.shape[0], what)
+    _int32(hidden.shape[0] | hidden.shape[1] | head.shape[0], what)
     return (_dtype_code(torch, hidden.dtype), hidden.shape[0], head.shape[0], hidden.shape[1], _matrix_stride(hidden, what),
             _matrix_stride(head, what))
 
