@@ -811,9 +811,10 @@ int lede_op_quant_linear(int32_t dtype, const void* packed, int32_t N, int32_t K
  * Products are exact and sums fp32 (fp32 inputs enter as three bf16 numbers
  * each, of whose nine products the six largest count: what is left out is less
  * than 2^-19 of a product).
- * A row whose logits are all -infinity or include a NaN or +infinity has NaN;
- * so has, of fp32 inputs, a row with an entry that is not finite, and every
- * row where the head has one.
+ * A row whose logits are all -infinity or include a NaN or +infinity has NaN
+ * (and so has every row of hidden with an entry that is not finite).  Logits of
+ * -infinity, of infinite entries of the head, count as none (fp32 forms the
+ * logits beside them once more, which takes its time).
  * LEDE_E_ARG: null pointers, bad dtypes, M < 0, V or K < 1, row strides below
  * K; hidden, head, the gradients, workspace or (of more than one row) row
  * strides not multiples of 16 bytes; a workspace smaller than lede_op_head_loss_bytes (of the same sizes).
@@ -833,7 +834,8 @@ int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M,
  * weight is 0 is left out, too.  dz enters the two products with bf16's 8 bits
  * where the inputs are bf16 (its rounding and the result's are alike), a row's
  * dz at its target, usually its largest, with 16, and with 24 where they are
- * fp32.  d_hidden and d_head overlap nothing else.
+ * fp32.  An infinite entry of the head makes its column of d_hidden NaN where
+ * dz is 0, as the product has it.  d_hidden and d_head overlap nothing else.
  * Sums have a fixed order: the same call gives the same bits.  M = 0 clears
  * d_head.  Errors as above, with lede_op_head_loss_grad_bytes. */
 size_t lede_op_head_loss_grad_bytes(int32_t dtype, int32_t M, int32_t V, int32_t K);

@@ -44,9 +44,12 @@ struct HeadCopyArgs {
 };
 struct HeadJoinArgs {
   const float2* sums; const float* target_z;
-  int n, tiles, V;
+  int n, tiles, tile, V;           // (tile: entries of the vocabulary)
   const int32_t* targets;
   float *loss, *lse;
+  const float *hidden, *head;      // (fp32; else null)
+  int64_t ldh, ldw;
+  int K;
 };
 struct HeadOutArgs {
   const float* part;

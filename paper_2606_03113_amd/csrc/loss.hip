@@ -266,7 +266,9 @@ __device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][
         const int i = i0 + (wi * NI + x) * 16 + 4 * lg, at = t - a.v0 - i;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float q = acc[x][y][e] - lse;
+          float q = acc[x][y][e] - lse;
+          // (fp32's parts make NaN of a logit of -infinity; with a finite lse there is no other that is not finite)
+          if (DT == 0 && !(q == q) && fabsf(lse) < INFINITY) q = -INFINITY;
           d[e] = DT ? __expf(q) : expf(q);
           if (e == at) d[e] = expm1f(q);   // (p - 1 keeps its bits where p is near 1)
           d[e] = out || i + e >= a.n_i ? 0.f : d[e] * g;
@@ -487,7 +489,8 @@ __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
 // 32000 x 5120 4.8 ms against 0.9, 1024 rows 7.0 against 6.7, 2048 rows alike).
 // A step is KS entries of the contraction, loaded into registers AHEAD steps
 // before; two barriers a step, and other blocks on the CU meanwhile.  What is
-// not finite becomes NaN in the second part.
+// not finite becomes NaN in the second part, and so do the logits it meets, which
+// are formed again (head_join_again).
 __device__ float4 head_zeros[2];   // what is read in place of entries past the contraction's end
 constexpr int PRODUCTS = 6;
 __device__ __forceinline__ void split8(const float (&v)[8], u32x4 (&w)[3]) {
@@ -874,6 +877,54 @@ __global__ __launch_bounds__(256) void k_head_copy(HeadCopyArgs a) {   // rows o
   *(uint4*)(a.dst + at * 16) = out ? make_uint4(0, 0, 0, 0) : ld16((const uint8_t*)a.src + r * a.pitch + c * 16);
 }
 
+// A row's maximum m and sum s of fp32 logits of which some tiles' are NaN: these are
+// formed again, in 64 bits and without parts, so that an infinite entry of the head
+// does what it does to a product (a vocabulary masked by logits of -infinity keeps
+// its others), and so is the target's logit zt among them.  A row of hidden with an
+// entry that is not finite has no sum, whatever the head is.  A wave's loads are of 64
+// rows of the head: 1024 rows of 32000 x 5120, whose last 40 entries are masked,
+// 1.65 -> 2.0 ms, the last 2000 8.0 (a row of the head at a time over the lanes 15).
+__device__ __forceinline__ void head_join_again(const HeadJoinArgs& a, int j, const float2* p, float& m, float& s, float& zt) {
+  const int lane = threadIdx.x & 63;
+  const float* h = a.hidden + j * a.ldh;
+  bool finite = true;
+  for (int k = lane; k < a.K; k += 64) finite = finite && fabsf(h[k]) < INFINITY;
+  if (__ballot(!finite)) return;
+  m = -INFINITY;
+  s = 0.f;
+  auto add = [&](float z, float n) {   // n e^z
+    const float most = fmaxf(m, z), base = most == -INFINITY ? 0.f : most;
+    s = s * __expf(m - base) + n * __expf(z - base);
+    m = most;
+  };
+  for (int t0 = 0; t0 < a.tiles; t0 += 64) {
+    const float2 q = t0 + lane < a.tiles ? p[t0 + lane] : make_float2(-INFINITY, 0.f);
+    const bool nan = !(q.y == q.y);
+    if (!nan) add(q.x, q.y);
+    for (uint64_t left = __ballot(nan); left; left &= left - 1) {
+      const int first = (t0 + __ffsll((unsigned long long)left) - 1) * a.tile, end = min(first + a.tile, a.V);
+      for (int v0 = first; v0 < end; v0 += 64) {
+        const int v = v0 + lane;
+        double z = 0.0;
+        if (v < end) {
+          const float* w = a.head + v * a.ldw;
+#pragma unroll 8
+          for (int k = 0; k < a.K; k += 4) {
+            const float4 x = *(const float4*)(h + k), y = *(const float4*)(w + k);
+            z = fma((double)x.x, (double)y.x, fma((double)x.y, (double)y.y, fma((double)x.z, (double)y.z, fma((double)x.w, (double)y.w, z))));
+          }
+          add((float)z, z == z ? 1.f : (float)z);
+        }
+        const uint64_t target = __ballot(v < end && v == a.targets[j]);
+        if (target) zt = __shfl((float)z, __ffsll((unsigned long long)target) - 1);
+      }
+    }
+  }
+  const float most = wave_max(m);
+  s = wave_sum(s * __expf(m - (most == -INFINITY ? 0.f : most)));
+  m = most;
+}
+
 // A wave joins a row's tiles.
 __global__ __launch_bounds__(256) void k_head_join(HeadJoinArgs a) {
   const int lane = threadIdx.x & 63, j = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -886,11 +937,13 @@ __global__ __launch_bounds__(256) void k_head_join(HeadJoinArgs a) {
   float s = 0.f;
   for (int i = lane; i < a.tiles; i += 64) s += p[i].y * __expf(p[i].x - base);
   s = wave_sum(s);
-  if (lane) return;
-  const double lse = m == -INFINITY ? (double)__builtin_nanf("") : (double)m + log((double)s);
   const int t = a.targets[j];
   const bool in = t >= 0 && t < a.V;
-  if (a.loss) a.loss[j] = in ? (float)(lse - (double)a.target_z[j]) : 0.f;
+  float zt = in ? a.target_z[j] : 0.f;
+  if (a.hidden && !(s == s)) head_join_again(a, j, p, m, s, zt);
+  if (lane) return;
+  const double lse = m == -INFINITY ? (double)__builtin_nanf("") : (double)m + log((double)s);
+  if (a.loss) a.loss[j] = in ? (float)(lse - (double)zt) : 0.f;
   a.lse[j] = (float)lse;
 }
 

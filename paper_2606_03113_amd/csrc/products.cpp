@@ -171,7 +171,10 @@ int lede_op_head_loss(int32_t dtype, const void* hidden, int64_t ldh, int32_t M,
     if (hipError_t e = launch_head(dtype, HEAD_SUMS, a, p.tile, s)) return done(e);
   }
   HeadJoinArgs j{};
-  j.sums = sums; j.target_z = target_z; j.n = M; j.tiles = p.tiles; j.V = V; j.targets = targets; j.loss = loss; j.lse = lse;
+  j.sums = sums; j.target_z = target_z; j.n = M; j.tiles = p.tiles; j.tile = p.tile.i; j.V = V; j.targets = targets; j.loss = loss; j.lse = lse;
+  if (dtype == LEDE_DTYPE_F32) {
+    j.hidden = (const float*)hidden; j.ldh = ldh; j.head = (const float*)head; j.ldw = ldw; j.K = K;
+  }
   return done(launch_head_join(j, s));
 }
 
