@@ -16,7 +16,8 @@ enum HeadEpi : int {
 };
 
 // A block's tile of a product: bf16 256 x 64, 128 or 256, or 128 x 64; fp32 64 x
-// 64, 64 x 128 or 128 x 128, or thin: 128 x 16, 32 or 64, of columns 256 x those.
+// 64, 64 x 128 or 128 x 128, or thin: 64 or 128 x 16, 32 or 64, of columns 256 x
+// those.
 struct HeadTile { int i, j; bool thin = false; };   // thin: few fp32 rows over a large head
 
 constexpr int HEAD_OUTER_F32 = 32, HEAD_OUTER_BF16 = 64;   // rows of launch_head_outer, at most
