@@ -222,7 +222,7 @@ template <class Each> __device__ __forceinline__ void own_entries(const CachePag
 // (INT_MIN + s stands for that).  The others take pages from the free list in
 // sequence order, then in table order; of a page with tokens before the new
 // ones the content has to follow (a pair for the copy).  A chain of loads,
-// atomics and their loads: 4 sequences 6.3 us, 256 7.5.
+// atomics and their loads: 4 sequences 6.0 us, 256 7.3.
 __global__ __launch_bounds__(PG_THREADS) void k_cache_own(CachePagesArgs a) {
   __shared__ Two red[PG_WAVES];
   __shared__ int bad_seq, bad_code;
@@ -395,8 +395,8 @@ __global__ __launch_bounds__(256) void k_cache_leave(CachePagesArgs a) {
 
 // The pages without a holder go to the list in ascending order, which does not
 // depend on who came last.  MARKED: k_cache_leave has found them.  Bound by
-// chains of loads: 71 entries of 64 sequences 5.6 us in one launch,
-// 12400 of 1001 16 in two (in one 36).
+// chains of loads: 71 entries of 64 sequences 6.4 us in one launch,
+// 12400 of 1001 17 in two (in one 36).
 template <bool MARKED>
 __global__ __launch_bounds__(PG_THREADS) void k_cache_free(CachePagesArgs a) {
   __shared__ uint32_t words[CACHE_MOST_PAGES / 32];
@@ -479,7 +479,7 @@ __global__ __launch_bounds__(PG_THREADS) void k_cache_free(CachePagesArgs a) {
 // With L live pages, the k-th of those from page L on (in ascending order)
 // moves to the k-th hole before it: as many as there are holes, and no page is
 // both read and written.  Bound by the chains of loads: 3500 entries of 150
-// sequences in a pool of 5000 14.4 us, 120 of 9 7.3.
+// sequences in a pool of 5000 14.1 us, 120 of 9 6.8.
 __global__ __launch_bounds__(PG_THREADS) void k_cache_compact(CachePagesArgs a) {
   __shared__ uint32_t words[CACHE_MOST_PAGES / 32];
   __shared__ int before[PG_THREADS];

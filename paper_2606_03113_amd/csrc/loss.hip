@@ -344,8 +344,8 @@ __device__ __forceinline__ void head_finish(const HeadArgs& a, f32x4 (&acc)[NI][
 // of hidden are gathered into A's place in the ring, and an operand of rest in a
 // row's target's place and zeros elsewhere is made in registers (rest in bf16: 2^-16
 // of dz are left).  2048 rows of 32000 x 4096: the error of dW against 64 bits 2.4e-3
-// -> 1.7e-3, bf16's own, for 448 -> 480 us; chains of loads at a block's end, of which
-// targets loaded before the product began save nothing.
+// -> 1.7e-3, bf16's own, for about 30 us of 476; chains of loads at a block's end, of
+// which targets loaded before the product began save nothing.
 template <int TI, int TJ, int WI, int WJ, int NI, int NJ>
 __device__ __forceinline__ void head_rest(const HeadArgs& a, f32x4 (&acc)[NI][NJ], uint8_t* smem, int i0, int j0, int wi, int wj) {
   constexpr int NW = WI * WJ, THREADS = NW * 64;
@@ -425,7 +425,7 @@ __device__ __forceinline__ void head_rest(const HeadArgs& a, f32x4 (&acc)[NI][NJ
 // out[j][i] = sum_c A[i][c] B[j][c] of bf16 operands, TI x TJ of them a block, WI x
 // WJ waves.  A ring of S steps of the contraction in LDS: one is multiplied while
 // the next ones are on their way; one barrier a step.  2048 rows of 32000 x 4096:
-// 463 us a product, 1160 TFLOP/s (a library product of 8192^3 1450 here).
+// 406 to 476 us a product, 1130 to 1320 TFLOP/s (a library product of 8192^3 1450 here).
 template <bool CA, bool CB, int TI, int TJ, int WI, int WJ, int S, int EPI>
 __global__ __launch_bounds__(WI * WJ * 64) void k_head(HeadArgs a) {
   constexpr int NW = WI * WJ, NI = TI / WI / 16, NJ = TJ / WJ / 16;
@@ -642,7 +642,7 @@ __global__ __launch_bounds__(256) void k_head_fp32(HeadArgs a) {
 // rows' parts are in LDS, one step's written while the other's are read.
 // Columns: a lane has four neighbouring ones of eight entries of the contraction,
 // one for each of the four tiles, whose row r is column 4 r + x.  21 rows of 118860
-// x 5120 545 us a pass (4.5 TB/s; 656 in k_head_fp32), dh's 426 (559).
+// x 5120 524 us a pass (4.6 TB/s; 656 in k_head_fp32), dh's 403 (559).
 template <bool CA, int NI, int TJ, int EPI>
 __global__ __launch_bounds__(256, 2) void k_head_thin(HeadArgs a) {
   constexpr int KS = CA ? 32 : 64, NJ = TJ / 16, TI = 64 * NI, H = KS / 32, N4 = H * 8;   // 16-byte loads of a step
@@ -750,7 +750,7 @@ __global__ __launch_bounds__(256, 2) void k_head_thin(HeadArgs a) {
 // rows) and walks over the vocabulary, 64 entries at a time, the next ones' dz on its way.  Neighbouring
 // columns are of four tiles, so that a lane stores four of them and 16 lanes a row's
 // 64; blocks beside each other take the entries in turn, so that the card writes
-// one stretch of dW at a time.  21 fp32 rows over 118860 x 5120 443 us (5.5 TB/s;
+// one stretch of dW at a time.  21 fp32 rows over 118860 x 5120 434 us (5.6 TB/s;
 // in k_head_fp32 600), 2 bf16 rows over 128256 x 5120 229 (5.7; in k_head 289), 35
 // of them 299 (321).
 template <int DT, int H>
